@@ -472,8 +472,175 @@ int odsgd_set_launch_config(odsgd_ctx* ctx, int block_threads, int ctas_per_sm);
 /* How many kernels this context has launched since create. */
 int odsgd_get_launch_count(odsgd_ctx* ctx, uint64_t* launches);
 
+/* ------------------------------------------------------------------------------------------
+ * Language-model operators around the update.
+ *
+ * What a worker runs on either side of its model when the parameter set is a language model's:
+ * token rows out of the weight arena (odsgd_embed_lookup) and their gradient into the gradient
+ * arena (odsgd_embed_grad), the score of a taken token (odsgd_token_logprob), the clipped policy
+ * loss with its gradient (odsgd_policy_loss), and the norm, clipping and lay-out of a list of
+ * gradient tensors into the arena the server reads (odsgd_grad_set_*).
+ *
+ * These calls take no context.  They run on the current CUDA device, on `stream`, and allocate
+ * nothing (odsgd_grad_set_create alone allocates a table); outputs and workspaces are the
+ * caller's.  A failed call has written nothing; odsgd_last_error(NULL) has its text for the
+ * calling thread.  Inputs are read and outputs written in stream order: memory that belongs to
+ * another stream has to be ordered by the caller.
+ *
+ * Rows are addressed in two levels, [n_outer][n_inner], with strides counted in elements, so
+ * that a shifted view (all positions but the last of each sequence), a transposed batch or a
+ * value broadcast along a level (stride 0, inputs only) needs no copy.  The last axis (a
+ * table's or activation's `dim`, the vocabulary) is contiguous.  Strides are >= 0; rows that are
+ * written must not overlap.  Pointers need the alignment of their element type only; 16-byte
+ * aligned rows run fastest.  Sums and softmax statistics are held in 32 bits or more; results are
+ * rounded once to the type they are stored in.  The order of every sum is fixed by the sizes of
+ * the call: equal inputs give equal bits.
+ */
+#define ODSGD_F32 0
+#define ODSGD_BF16 1
+#define ODSGD_F16 2
+#define ODSGD_I32 3
+#define ODSGD_I64 4
+
+/*
+ * Token embedding.  `table` has `vocab` rows of `dim` elements, table_stride elements apart: a
+ * tensor inside a weight arena (lookup) or inside a gradient arena (gradient).  `act` holds one
+ * row of `dim` elements per token.
+ */
+typedef struct odsgd_embed_desc {
+    const void* tokens;           /* device, [n_outer][n_inner] of token_type */
+    void* act;                    /* device, [n_outer][n_inner][dim] of act_type: written by the lookup, read by the gradient */
+    void* table;                  /* device, [vocab][dim] of table_type: read by the lookup, written by the gradient */
+    int token_type;               /* ODSGD_I32 or ODSGD_I64 */
+    int act_type;                 /* ODSGD_F32, ODSGD_BF16 or ODSGD_F16 */
+    int table_type;               /* the same; the gradient's table is ODSGD_F32 */
+    int accumulate;               /* gradient: 0 writes the whole table (zeros in rows no token names), 1 adds to it */
+    int64_t n_outer, n_inner;     /* either may be 0; the product at most ODSGD_MAX_TOKENS */
+    int64_t token_stride_outer, token_stride_inner;
+    int64_t act_stride_outer, act_stride_inner;
+    int64_t vocab, dim;           /* >= 1; vocab below 2^31 - 1, dim at most 2^20 */
+    int64_t table_stride;         /* >= dim */
+    int64_t padding_token;        /* gradient: this token's row gets no gradient; negative: none */
+    float scale;                  /* lookup: act = scale * row; gradient: row = scale * sum */
+} odsgd_embed_desc;
+#define ODSGD_MAX_TOKENS (1 << 24)
+
+/*
+ * act[t] = scale * table[tokens[t]], the product in 32 bits.  A token outside [0, vocab) (the
+ * padding of a ragged batch) gives a row of zeros.
+ * Errors: ERR_ARG, ERR_ALIGN (a pointer below its type's alignment), ERR_OVERLAP (act overlaps
+ * the table or the tokens, or its rows one another), ERR_UNSUPPORTED (sizes beyond the limits),
+ * ERR_CUDA.
+ */
+int odsgd_embed_lookup(const odsgd_embed_desc* desc, void* stream);
+
+/*
+ * table[v] (+)= scale * sum of act[t] over the tokens t equal to v, in ascending order of t.
+ * The tokens are sorted (stably) on the device, so that each row is one ordered sum whatever the
+ * token frequencies; nothing is added atomically.  Tokens outside [0, vocab) and the padding
+ * token contribute nothing.  `workspace`: device memory of at least the size that
+ * odsgd_embed_grad_workspace() reports for the same sizes and types, 16-byte aligned, free again
+ * when the call's work is done.
+ */
+int odsgd_embed_grad_workspace(const odsgd_embed_desc* desc, size_t* bytes);
+int odsgd_embed_grad(const odsgd_embed_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Token scores and the clipped policy loss over rows of logits z, with c = inv_temp:
+ *     logp = c z[y] - log sum_j exp(c z[j])
+ *     r    = exp(logp - old)          pg = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)
+ *     d    = ref - logp               kl = exp(d) - d - 1
+ *     loss = sum over the rows of w (pg + kl_coef kl)
+ *     dlogits[j] = grad_scale c k ([j == y] - softmax(c z)[j])
+ *         k = w ((r A <= clip(r) A ? -A r : 0) + kl_coef (1 - exp(d)))
+ * w is the row's weight (mask and normalisation in one: 1 / tokens, say).  Rows with w == 0 or a
+ * label outside [0, vocab) are not read: logp 0, no part in the sums, a gradient row of zeros,
+ * whatever their logits hold.  A vocabulary entry of -inf has probability 0 and gradient 0; a
+ * row with nothing but -inf, or with NaN or +inf, gives NaN, as the formula does.
+ */
+typedef struct odsgd_policy_desc {
+    const void* logits;           /* device, [n_outer][n_inner][vocab] of type */
+    const void* labels;           /* device, [n_outer][n_inner] of label_type */
+    const float* old_logp;        /* device, the same, as are the next three: log-probability under the acting policy */
+    const float* ref_logp;        /* under the reference policy; NULL only with kl_coef == 0 (the KL sum is then 0) */
+    const float* advantages;
+    const float* weights;
+    void* dlogits;                /* device, as logits and of its type; may be the logits themselves (same pointer and strides) */
+    float* logp;                  /* device, out, n_outer * n_inner floats */
+    float* lse;                   /* token_logprob: out, the same size: log sum_j exp(c z[j]); may be NULL */
+    float* stats;                 /* policy_loss: out, 4 floats: loss, sum w pg, sum w kl, sum of w where the ratio was clipped */
+    int type;                     /* ODSGD_F32, ODSGD_BF16 or ODSGD_F16 */
+    int label_type;               /* ODSGD_I32 or ODSGD_I64 */
+    int64_t n_outer, n_inner;     /* either may be 0; the product below 2^27 */
+    int64_t vocab;                /* 1 .. 2^30 */
+    int64_t logits_stride_outer, logits_stride_inner;
+    int64_t label_stride_outer, label_stride_inner;
+    int64_t old_stride_outer, old_stride_inner;
+    int64_t ref_stride_outer, ref_stride_inner;
+    int64_t adv_stride_outer, adv_stride_inner;
+    int64_t weight_stride_outer, weight_stride_inner;
+    int64_t dlogits_stride_outer, dlogits_stride_inner;
+    float inv_temp;               /* > 0 */
+    float clip_low, clip_high;    /* >= 0 */
+    float kl_coef;
+    float grad_scale;             /* factor on dlogits (loss scale, 1 / accumulation steps); the sums do not carry it */
+} odsgd_policy_desc;
+
+/*
+ * The score alone (old policy, reference policy, evaluation): reads logits, labels, inv_temp;
+ * writes logp and lse (0 in rows whose label is outside [0, vocab)).  Ignores the other fields.
+ */
+int odsgd_token_logprob(const odsgd_policy_desc* desc, void* stream);
+
+/*
+ * The loss and its gradient in one pass: each row of logits is read once, kept on the chip while
+ * its softmax statistics are joined, and its gradient written (rows of more than
+ * ODSGD_RESIDENT_BYTES bytes are read twice).  `workspace` as for odsgd_embed_grad.
+ * Errors of both calls: ERR_ARG, ERR_ALIGN, ERR_OVERLAP (an output overlaps an input or another
+ * output), ERR_UNSUPPORTED, ERR_CUDA.
+ */
+#define ODSGD_RESIDENT_BYTES (1 << 19)
+int odsgd_policy_loss_workspace(const odsgd_policy_desc* desc, size_t* bytes);
+int odsgd_policy_loss(const odsgd_policy_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Norm and clipping of many gradient tensors.  A set is a list of tensors, each belonging to one
+ * of n_groups groups (the workers): per group g
+ *     norm[g] = sqrt(sum over its tensors and their elements of x^2)
+ *     k[g]    = norm[g] > max_norm ? max_norm / norm[g] : 1
+ * and every x becomes k[g] x, in its own place and type (arenas NULL) or in the group's fp32
+ * arena at the tensor's offset (elements of the arena that no tensor covers, such as the padding
+ * between tensors, are not written).  The sum of squares and the norm are held in 64 bits, so
+ * that neither tiny nor huge elements are lost; norms[g] is rounded to 32.  A norm that is NaN
+ * clips nothing (it is there for the caller to see); an infinite one makes k = 0.
+ *
+ * Like a bound gradient table, a set is checked once and used every iteration; its tensors have
+ * to stay where they are.  create() allocates one device table (24 bytes a tensor and 12 bytes per
+ * few thousand elements) with cudaMalloc and fills it on `stream`: not while that stream is
+ * capturing (ERR_STATE), and calls on other streams have to be ordered behind it.  The table also
+ * holds the partial sums of a call, so the calls of one set must not overlap on the GPU.
+ *   norms  device, n_groups floats, out; NULL if not wanted (clip only)
+ * Errors: ERR_ARG (NULL, bad type or group, a tensor beyond its arena, max_norm negative or NaN),
+ * ERR_ALIGN, ERR_OVERLAP (tensors in place, or places in an arena, that overlap; an arena that
+ * overlaps a tensor), ERR_STATE (capture; another current device than the set's), ERR_CUDA.
+ */
+typedef struct odsgd_grad_tensor {
+    void* data;                   /* device; NULL only with numel == 0 */
+    size_t numel;
+    size_t offset;                /* first element in the group's arena; ignored without arenas */
+    int type;                     /* ODSGD_F32, ODSGD_BF16 or ODSGD_F16 */
+    int group;                    /* 0 .. n_groups - 1 */
+} odsgd_grad_tensor;
+typedef struct odsgd_grad_set odsgd_grad_set;
+
+int odsgd_grad_set_create(odsgd_grad_set** out, const odsgd_grad_tensor* tensors, size_t n_tensors, int n_groups,
+                          float* const* arenas, size_t arena_len, void* stream);
+int odsgd_grad_set_norm(odsgd_grad_set* set, float* norms, void* stream);
+int odsgd_grad_set_clip(odsgd_grad_set* set, float max_norm, float* norms, void* stream);
+int odsgd_grad_set_destroy(odsgd_grad_set* set);
+
 /* Text describing the last failure on `ctx` (or, for ctx == NULL, of the last failed
- * odsgd_create on this thread).  Never NULL. */
+ * odsgd_create or context-free call on this thread).  Never NULL. */
 const char* odsgd_last_error(odsgd_ctx* ctx);
 
 #ifdef __cplusplus

@@ -40,7 +40,9 @@ EXPORTS = (
     "odsgd_lr_poly_decay", "odsgd_fused_update_mult_static", "odsgd_get_iteration", "odsgd_set_iteration",
     "odsgd_bind_grads", "odsgd_unbind_grads", "odsgd_global_update_bound", "odsgd_fused_update_bound",
     "odsgd_ssgd_step_bound", "odsgd_step_bound", "odsgd_worker_local_update", "odsgd_shard_range",
-    "odsgd_set_weight_mirrors",
+    "odsgd_set_weight_mirrors", "odsgd_embed_lookup", "odsgd_embed_grad_workspace", "odsgd_embed_grad",
+    "odsgd_token_logprob", "odsgd_policy_loss_workspace", "odsgd_policy_loss", "odsgd_grad_set_create",
+    "odsgd_grad_set_norm", "odsgd_grad_set_clip", "odsgd_grad_set_destroy",
 )
 
 
@@ -121,6 +123,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "odsgd_shard_range": ([ctypes.c_size_t, ci, ci, ctypes.POINTER(ctypes.c_size_t),
                                ctypes.POINTER(ctypes.c_size_t)], ci),
         "odsgd_set_weight_mirrors": ([vp, pvp, pvp, ci], ci),
+        "odsgd_embed_lookup": ([vp, vp], ci),
+        "odsgd_embed_grad_workspace": ([vp, ctypes.POINTER(ctypes.c_size_t)], ci),
+        "odsgd_embed_grad": ([vp, vp, ctypes.c_size_t, vp], ci),
+        "odsgd_token_logprob": ([vp, vp], ci),
+        "odsgd_policy_loss_workspace": ([vp, ctypes.POINTER(ctypes.c_size_t)], ci),
+        "odsgd_policy_loss": ([vp, vp, ctypes.c_size_t, vp], ci),
+        "odsgd_grad_set_create": ([ctypes.POINTER(vp), vp, ctypes.c_size_t, ci, pvp, ctypes.c_size_t, vp], ci),
+        "odsgd_grad_set_norm": ([vp, vp, vp], ci),
+        "odsgd_grad_set_clip": ([vp, cf, vp, vp], ci),
+        "odsgd_grad_set_destroy": ([vp], ci),
     }
     for name, (argtypes, restype) in sig.items():
         fn = getattr(lib, name)  # AttributeError if the library lacks a declared symbol

@@ -12,8 +12,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libodsgd.so")
-SOURCES = [os.path.join(CSRC, "odsgd.cu")]
-HEADERS = [os.path.join(CSRC, "odsgd_kernels.cuh"), os.path.join(INCLUDE, "odsgd.h")]
+SOURCES = [os.path.join(CSRC, "odsgd.cu"), os.path.join(CSRC, "odsgd_lm.cu")]
+HEADERS = [os.path.join(CSRC, "odsgd_kernels.cuh"), os.path.join(CSRC, "odsgd_lm_kernels.cuh"), os.path.join(INCLUDE, "odsgd.h")]
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",

@@ -75,7 +75,7 @@ struct odsgd_ctx {
 
 namespace {
 
-thread_local std::string g_create_err;
+thread_local std::string g_create_err;  // of the last failed odsgd_create or context-free call
 
 int fail(odsgd_ctx* ctx, int code, const std::string& msg) {
     if (ctx) ctx->err = msg; else g_create_err = msg;
@@ -589,6 +589,11 @@ int scheduled_step(odsgd_ctx* c, F call) {
 }
 
 }  // namespace
+
+namespace odsgd {
+// For the context-free calls of odsgd_lm.cu.
+void set_thread_error(const std::string& msg) { g_create_err = msg; }
+}  // namespace odsgd
 
 extern "C" {
 

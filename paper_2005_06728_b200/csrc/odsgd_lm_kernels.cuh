@@ -1,0 +1,1010 @@
+// Device code of the language-model operators around the update (sm_100a): token embedding and
+// its gradient, token scores, the clipped policy loss with its gradient, gradient norm and clip.
+//
+// All of them are bound by memory traffic; each kernel's comment says how it keeps to one read of
+// what it reads and one write of what it writes.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math_constants.h>
+#include <stdint.h>
+
+#include "odsgd.h"
+
+namespace odsgd_lm {
+
+using bf16 = __nv_bfloat16;
+using f16 = __half;
+
+// Scheduled early, run in order: see the update kernels.
+__device__ __forceinline__ void dependent_launch_prologue() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// ------------------------------------------------------------------ elements and 16-byte vectors
+template <typename T>
+__device__ __forceinline__ float to_f32(T x);
+template <>
+__device__ __forceinline__ float to_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float to_f32<bf16>(bf16 x) { return __bfloat162float(x); }
+template <>
+__device__ __forceinline__ float to_f32<f16>(f16 x) { return __half2float(x); }
+
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ bf16 from_f32<bf16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ f16 from_f32<f16>(float x) { return __float2half_rn(x); }
+
+// Elements of T in 16 bytes.
+template <typename T>
+constexpr int kLanes = 16 / (int)sizeof(T);
+
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& q, float (&x)[kLanes<T>]);
+template <>
+__device__ __forceinline__ void unpack<float>(const uint4& q, float (&x)[4]) {
+    x[0] = __uint_as_float(q.x);
+    x[1] = __uint_as_float(q.y);
+    x[2] = __uint_as_float(q.z);
+    x[3] = __uint_as_float(q.w);
+}
+template <>
+__device__ __forceinline__ void unpack<bf16>(const uint4& q, float (&x)[8]) {
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+template <>
+__device__ __forceinline__ void unpack<f16>(const uint4& q, float (&x)[8]) {
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float (&x)[kLanes<T>]);
+template <>
+__device__ __forceinline__ uint4 pack<float>(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+template <>
+__device__ __forceinline__ uint4 pack<bf16>(const float (&x)[8]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        u[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+template <>
+__device__ __forceinline__ uint4 pack<f16>(const float (&x)[8]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+        u[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+// Negative infinity in every lane.
+template <typename T>
+__device__ __forceinline__ uint4 neg_inf_vector() {
+    constexpr uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0u;
+    if constexpr (sizeof(T) == 4) return make_uint4(w, w, w, w);
+    const T h = from_f32<T>(-CUDART_INF_F);
+    const uint32_t u = *reinterpret_cast<const uint16_t*>(&h) * 0x10001u;
+    return make_uint4(u, u, u, u);
+}
+
+__device__ __forceinline__ long long load_token(const void* p, bool wide, long long i) {
+    return wide ? static_cast<const long long*>(p)[i] : (long long)static_cast<const int*>(p)[i];
+}
+
+// ------------------------------------------------------------------ clusters
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    cluster_arrive();
+    cluster_wait();
+}
+// The address of a variable of this CTA's shared memory in the CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t cluster_address(const void* smem, unsigned rank) {
+    uint32_t out;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(out) : "r"((uint32_t)__cvta_generic_to_shared(smem)), "r"(rank));
+    return out;
+}
+__device__ __forceinline__ void cluster_store(uint32_t addr, float x) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(x) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_load(uint32_t addr) {
+    uint32_t x;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
+    return x;
+}
+
+// ------------------------------------------------------------------ rows of logits
+// One cluster of `cluster` CTAs takes one row; the row's 16-byte vectors are split evenly over it.
+constexpr int kRowVectors = 8;    // vectors a thread holds at a time
+constexpr int kRowThreads = 512;  // most threads of a CTA: 64 KB of a row in registers
+constexpr int kRowCluster = 8;    // most CTAs of a row (the portable limit)
+
+enum RowMode : int {
+    kRowScore = 0,     // logp and lse only
+    kRowResident = 1,  // loss and gradient, the row held in registers between its read and its write
+    kRowStream = 2,    // loss and gradient of a row too long for that: read twice
+};
+
+struct VecView {
+    const float* p;
+    long long so, si;
+};
+
+struct RowArgs {
+    const void* z;
+    const void* labels;
+    VecView old_logp, ref_logp, adv, weight;
+    void* dz;
+    float* logp;
+    float* lse;
+    float* terms;  // [3][rows]: w pg, w kl, w of clipped rows
+    long long z_so, z_si, l_so, l_si, d_so, d_si;
+    long long vocab;
+    unsigned rows, n_inner;
+    int wide_labels;
+    int cluster;
+    float inv_temp, clip_low, clip_high, kl_coef, grad_scale;
+};
+
+// Maximum m of a set of z and sum of exp(c (z - m)); m = -inf, s = 0 for the empty set.
+struct MaxSum {
+    float m, s;
+};
+
+// exp(c (z - m)) in the precision the row's type deserves: 16-bit logits through the base-2
+// exponential of the special-function unit (2^-22 relative, far below the 2^-8 or 2^-11 that the
+// gradient is rounded to); 32-bit logits through expf.  The difference comes first: c m alone
+// overflows where a mask holds the type's lowest value.
+template <typename T>
+struct RowExp {
+    float c, m;
+    __device__ __forceinline__ RowExp(float inv_temp, float m_) : c(sizeof(T) == 4 ? inv_temp : inv_temp * 1.4426950408889634f), m(m_) {}
+    __device__ __forceinline__ float operator()(float z) const {
+        if constexpr (sizeof(T) == 4) {
+            return expf((z - m) * c);
+        } else {
+            float r;
+            const float t = (z - m) * c;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+            return r;
+        }
+    }
+};
+
+// Factor that moves a sum held against maximum `from` to maximum `to`.  The empty set (-inf) has
+// s = 0, or a NaN that has to stay.
+__device__ __forceinline__ float rebase(float from, float to, float c) {
+    return from == -CUDART_INF_F ? 1.0f : expf((from - to) * c);
+}
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    return MaxSum{m, a.s * rebase(a.m, m, c) + b.s * rebase(b.m, m, c)};
+}
+// Over the lanes of a warp; every lane gets the same bits (each step adds the same two numbers on
+// both sides).
+__device__ __forceinline__ MaxSum warp_join(MaxSum x, float c) {
+    float m = x.m;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    float s = x.s * rebase(x.m, m, c);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    return MaxSum{m, s};
+}
+
+// A row as 16-byte vectors: vector v covers elements [v L - head, (v + 1) L - head), `head` being
+// how far the row starts behind a 16-byte boundary; what lies outside the row is left alone.
+template <typename T>
+struct RowVectors {
+    static constexpr int L = kLanes<T>;
+    const T* row;
+    long long vocab;
+    int head;
+    __device__ __forceinline__ RowVectors(const T* r, long long v)
+        : row(r), vocab(v), head((int)((reinterpret_cast<uintptr_t>(r) & 15) / sizeof(T))) {}
+    __device__ __forceinline__ long long count() const { return (head + vocab + L - 1) / L; }
+    __device__ __forceinline__ bool whole(long long v) const { return v * L >= head && (v + 1) * L <= head + vocab; }
+    __device__ __forceinline__ uint4 load(long long v) const {
+        if (whole(v)) return __ldcs(reinterpret_cast<const uint4*>(row - head) + v);
+        uint4 q = neg_inf_vector<T>();
+        T* e = reinterpret_cast<T*>(&q);
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+            const long long j = v * L + i - head;
+            if (j >= 0 && j < vocab) e[i] = row[j];
+        }
+        return q;
+    }
+};
+
+// Vector v of the gradient row; `same` says that the row starts as far behind a 16-byte boundary
+// as the logits' does.
+template <typename T>
+__device__ __forceinline__ void store_row_vector(T* drow, const RowVectors<T>& rv, long long v, const uint4& q, bool same) {
+    constexpr int L = kLanes<T>;
+    if (same && rv.whole(v)) {
+        __stcs(reinterpret_cast<uint4*>(drow - rv.head) + v, q);
+        return;
+    }
+    const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const long long j = v * L + i - rv.head;
+        if (j >= 0 && j < rv.vocab) drow[j] = e[i];
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ MaxSum vectors_max_sum(const uint4 (&q)[kRowVectors], float inv_temp) {
+    constexpr int L = kLanes<T>;
+    float m = -CUDART_INF_F;
+#pragma unroll
+    for (int k = 0; k < kRowVectors; ++k) {
+        float x[L];
+        unpack<T>(q[k], x);
+#pragma unroll
+        for (int i = 0; i < L; ++i) m = fmaxf(m, x[i]);
+    }
+    const RowExp<T> e(inv_temp, m == -CUDART_INF_F ? 0.0f : m);
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kRowVectors; ++k) {
+        float x[L];
+        unpack<T>(q[k], x);
+        float p = 0.0f;
+#pragma unroll
+        for (int i = 0; i < L; ++i) p += e(x[i]);
+        s += p;
+    }
+    return MaxSum{m, s};
+}
+
+// What a row's statistics make of its loss, and the factor k of its gradient.
+struct RowLoss {
+    float k, pg, kl, clipped;
+};
+__device__ __forceinline__ RowLoss row_loss(const RowArgs& a, float logp, float w, long long o, long long i) {
+    const float old = a.old_logp.p[o * a.old_logp.so + i * a.old_logp.si];
+    const float A = a.adv.p[o * a.adv.so + i * a.adv.si];
+    const float r = expf(logp - old);
+    const float bounded = fminf(fmaxf(r, 1.0f - a.clip_low), 1.0f + a.clip_high) * A;
+    const float free_term = r * A;
+    const bool cut = free_term > bounded;
+    RowLoss out;
+    // NaN stays: a comparison with it is false, and r itself is NaN
+    out.pg = -w * (cut ? bounded : free_term);
+    out.clipped = cut ? w : 0.0f;
+    float g = cut ? 0.0f : -free_term;
+    out.kl = 0.0f;
+    if (a.ref_logp.p != nullptr) {
+        const float d = a.ref_logp.p[o * a.ref_logp.so + i * a.ref_logp.si] - logp;
+        const float em = expm1f(d);  // exp(d) - 1 without its cancellation near d = 0
+        out.kl = w * (em - d);
+        g -= a.kl_coef * em;
+    }
+    out.k = w * g * a.inv_temp * a.grad_scale;
+    return out;
+}
+
+template <typename T, int MODE>
+__global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant__ RowArgs a) {
+    constexpr int L = kLanes<T>;
+    __shared__ MaxSum warp_part[kRowThreads / 32];
+    __shared__ MaxSum cta_part[kRowCluster];
+    dependent_launch_prologue();
+    const unsigned cs = (unsigned)a.cluster;
+    const unsigned row = blockIdx.x / cs, rank = blockIdx.x % cs;
+    const long long o = row / a.n_inner, i = row % a.n_inner;
+    const RowVectors<T> rv(static_cast<const T*>(a.z) + o * a.z_so + i * a.z_si, a.vocab);
+    const long long y = load_token(a.labels, a.wide_labels != 0, o * a.l_so + i * a.l_si);
+    const float w = MODE == kRowScore ? 1.0f : a.weight.p[o * a.weight.so + i * a.weight.si];
+    T* drow = MODE == kRowScore ? nullptr : static_cast<T*>(a.dz) + o * a.d_so + i * a.d_si;
+    const bool same = MODE != kRowScore && ((reinterpret_cast<uintptr_t>(drow) ^ reinterpret_cast<uintptr_t>(rv.row)) & 15) == 0;
+    const long long total = rv.count();
+    const long long per = (total + cs - 1) / cs;
+    const long long v0 = rank * per, v1 = v0 + per < total ? v0 + per : total;
+    const bool first = rank == 0 && threadIdx.x == 0;
+
+    if (w == 0.0f || y < 0 || y >= a.vocab) {  // the whole cluster leaves here together
+        if (first) {
+            a.logp[row] = 0.0f;
+            if (MODE == kRowScore) {
+                if (a.lse != nullptr) a.lse[row] = 0.0f;
+            } else {
+                a.terms[row] = a.terms[a.rows + row] = a.terms[2 * (size_t)a.rows + row] = 0.0f;
+            }
+        }
+        if (MODE != kRowScore) {
+            const uint4 zero = make_uint4(0, 0, 0, 0);
+            for (long long v = v0 + threadIdx.x; v < v1; v += blockDim.x) store_row_vector(drow, rv, v, zero, same);
+        }
+        return;
+    }
+    if (cs > 1) cluster_arrive();  // this CTA runs: its shared memory may be written (waited for below)
+    const float zy = to_f32(rv.row[y]);
+
+    uint4 q[kRowVectors];
+    MaxSum x{-CUDART_INF_F, 0.0f};
+    const long long step = (long long)blockDim.x * kRowVectors;
+    auto load = [&](long long b) {
+#pragma unroll
+        for (int k = 0; k < kRowVectors; ++k) {
+            const long long v = b + (long long)k * blockDim.x + threadIdx.x;
+            q[k] = v < v1 ? rv.load(v) : neg_inf_vector<T>();
+        }
+        return vectors_max_sum<T>(q, a.inv_temp);
+    };
+    if (MODE == kRowResident) {
+        x = load(v0);  // the host made sure that one round covers the CTA's part
+    } else {
+        for (long long b = v0; b < v1; b += step) x = join(x, load(b), a.inv_temp);
+    }
+    x = warp_join(x, a.inv_temp);
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    if (warps > 1) {
+        if (lane == 0) warp_part[threadIdx.x >> 5] = x;
+        __syncthreads();
+        x = lane < warps ? warp_part[lane] : MaxSum{-CUDART_INF_F, 0.0f};
+        x = warp_join(x, a.inv_temp);
+    }
+    if (cs > 1) {
+        cluster_wait();
+        if (threadIdx.x < cs) {
+            const uint32_t at = cluster_address(&cta_part[rank], threadIdx.x);
+            cluster_store(at, x.m);
+            cluster_store(at + 4, x.s);
+        }
+        // also orders every CTA's reads of the row ahead of every CTA's writes, for dz == z
+        cluster_sync();
+        x = lane < (int)cs ? cta_part[lane] : MaxSum{-CUDART_INF_F, 0.0f};
+        x = warp_join(x, a.inv_temp);
+    } else if (MODE != kRowScore) {
+        __syncthreads();  // every thread has read z[y] before one of them may write there
+    }
+    const float log_s = logf(x.s);
+    const float logp = (zy - x.m) * a.inv_temp - log_s;
+    if (MODE == kRowScore) {
+        if (first) {
+            a.logp[row] = logp;
+            if (a.lse != nullptr) a.lse[row] = x.m * a.inv_temp + log_s;
+        }
+        return;
+    }
+    const RowLoss loss = row_loss(a, logp, w, o, i);
+    if (first) {
+        a.logp[row] = logp;
+        a.terms[row] = loss.pg;
+        a.terms[a.rows + row] = loss.kl;
+        a.terms[2 * (size_t)a.rows + row] = loss.clipped;
+    }
+    // dz_j = k ([j == y] - exp(c (z_j - m)) / s)
+    const RowExp<T> e(a.inv_temp, x.m);
+    const float neg = -loss.k / x.s;
+    const long long vy = (rv.head + y) / L;
+    const int ly = (int)((rv.head + y) % L);
+    for (long long b = v0; b < v1; b += step) {  // one round when resident
+#pragma unroll
+        for (int k = 0; k < kRowVectors; ++k) {
+            const long long v = b + (long long)k * blockDim.x + threadIdx.x;
+            if (v >= v1) continue;
+            if (MODE == kRowStream) q[k] = rv.load(v);
+            float p[L];
+            unpack<T>(q[k], p);
+#pragma unroll
+            for (int l = 0; l < L; ++l) p[l] = neg * e(p[l]);
+            if (v == vy) {
+#pragma unroll
+                for (int l = 0; l < L; ++l) p[l] += l == ly ? loss.k : 0.0f;
+            }
+            store_row_vector(drow, rv, v, pack<T>(p), same);
+        }
+    }
+}
+
+// Sums the rows' terms in a fixed order, in 64 bits: one CTA.
+struct StatsArgs {
+    const float* terms;
+    float* stats;
+    unsigned rows;
+    float kl_coef;
+};
+constexpr int kStatsThreads = 1024;
+
+template <int N, int THREADS>
+__device__ __forceinline__ void block_sum(double (&x)[N], double* smem) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) x[n] += __shfl_down_sync(0xffffffffu, x[n], d);
+        if (lane == 0) smem[n * (THREADS / 32) + warp] = x[n];
+    }
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            x[n] = lane < THREADS / 32 ? smem[n * (THREADS / 32) + lane] : 0.0;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) x[n] += __shfl_down_sync(0xffffffffu, x[n], d);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kStatsThreads) stats_kernel(const __grid_constant__ StatsArgs a) {
+    __shared__ double part[3 * kStatsThreads / 32];
+    dependent_launch_prologue();
+    double x[3] = {0.0, 0.0, 0.0};
+    for (unsigned r = threadIdx.x; r < a.rows; r += kStatsThreads) {
+#pragma unroll
+        for (int n = 0; n < 3; ++n) x[n] += a.terms[(size_t)n * a.rows + r];
+    }
+    block_sum<3, kStatsThreads>(x, part);
+    if (threadIdx.x == 0) {
+        a.stats[0] = (float)(x[0] + (double)a.kl_coef * x[1]);
+        a.stats[1] = (float)x[0];
+        a.stats[2] = (float)x[1];
+        a.stats[3] = (float)x[2];
+    }
+}
+
+// ------------------------------------------------------------------ embedding lookup
+struct LookupArgs {
+    const void* tokens;
+    const void* table;
+    void* act;
+    long long t_so, t_si, a_so, a_si, stride, vocab, dim;
+    unsigned rows, n_inner;
+    int wide_tokens;
+    float scale;
+};
+constexpr int kLookupRows = 4;  // rows a thread has in flight
+constexpr int kLookupThreads = 256;
+
+// VEC: a thread takes as many columns as 16 bytes of the wider type hold... of the activation's
+// type; otherwise one column.  blockDim = (columns, rows).
+template <typename TT, typename TA, bool VEC>
+__global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_constant__ LookupArgs a) {
+    constexpr int W = VEC ? (kLanes<TT> > kLanes<TA> ? kLanes<TT> : kLanes<TA>) : 1;
+    dependent_launch_prologue();
+    const long long col = ((long long)blockIdx.y * blockDim.x + threadIdx.x) * W;
+    if (col >= a.dim) return;
+    const unsigned r0 = (blockIdx.x * blockDim.y + threadIdx.y) * kLookupRows;
+    const TT* src[kLookupRows];
+#pragma unroll
+    for (int k = 0; k < kLookupRows; ++k) {
+        src[k] = nullptr;
+        if (r0 + k < a.rows) {
+            const long long o = (r0 + k) / a.n_inner, i = (r0 + k) % a.n_inner;
+            const long long t = load_token(a.tokens, a.wide_tokens != 0, o * a.t_so + i * a.t_si);
+            if (t >= 0 && t < a.vocab) src[k] = static_cast<const TT*>(a.table) + t * a.stride + col;
+        }
+    }
+    float x[kLookupRows][W];
+#pragma unroll
+    for (int k = 0; k < kLookupRows; ++k) {
+#pragma unroll
+        for (int l = 0; l < W; ++l) x[k][l] = 0.0f;
+        if (src[k] == nullptr) continue;
+        if constexpr (VEC) {
+#pragma unroll
+            for (int v = 0; v < W / kLanes<TT>; ++v) {
+                float y[kLanes<TT>];
+                unpack<TT>(__ldg(reinterpret_cast<const uint4*>(src[k]) + v), y);
+#pragma unroll
+                for (int l = 0; l < kLanes<TT>; ++l) x[k][v * kLanes<TT> + l] = y[l];
+            }
+        } else {
+            x[k][0] = to_f32(*src[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kLookupRows; ++k) {
+        if (r0 + k >= a.rows) break;
+        const long long o = (r0 + k) / a.n_inner, i = (r0 + k) % a.n_inner;
+        TA* dst = static_cast<TA*>(a.act) + o * a.a_so + i * a.a_si + col;
+#pragma unroll
+        for (int l = 0; l < W; ++l) x[k][l] = src[k] == nullptr ? 0.0f : x[k][l] * a.scale;
+        if constexpr (VEC) {
+#pragma unroll
+            for (int v = 0; v < W / kLanes<TA>; ++v) {
+                float y[kLanes<TA>];
+#pragma unroll
+                for (int l = 0; l < kLanes<TA>; ++l) y[l] = x[k][v * kLanes<TA> + l];
+                reinterpret_cast<uint4*>(dst)[v] = pack<TA>(y);
+            }
+        } else {
+            *dst = from_f32<TA>(x[k][0]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ embedding gradient
+// Three launches.
+//   sort_kernel  One cluster sorts the tokens' positions by token, stably (least significant digit
+//                first, up to 9 bits a pass), and lists the tokens whose run crosses a block boundary.  The
+//                other clusters of the grid meanwhile write zeros to the rows that no token names
+//                (they need the tokens, not their order), which hides the sort.
+//   sum_kernel   A CTA takes `block` consecutive sorted positions and a slab of columns, and adds
+//                runs of equal tokens in 32 bits.  A run inside the block is written to the table,
+//                the part of one that crosses a boundary to the workspace.  Work is split by
+//                position, so a token that fills half the batch costs no more than rare ones.
+//   join_kernel  Adds the parts of the runs that cross boundaries, in order.
+// The order of every sum depends on sizes and tokens alone.
+constexpr int kSortCluster = 8;
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortBits = 9;
+constexpr int kSortRadix = 1 << kSortBits;
+constexpr int kSortSmem = (kSortWarps * kSortRadix + 2 * kSortRadix + kSortWarps) * 4;
+constexpr int kFillClusters = 17;   // with the sorting one, 144 CTAs: one for each of 148 SMs
+constexpr int kFillRows = 1 << 17;  // rows a CTA marks at a time: 16 KB of bits
+
+struct SpanRun {
+    unsigned token, first, last;  // blocks [first, last]
+};
+
+struct EmbedGradArgs {
+    const void* tokens;
+    const void* act;
+    float* table;
+    long long t_so, t_si, a_so, a_si, stride, vocab, dim, padding;
+    unsigned n, n_inner;
+    int wide_tokens, accumulate;
+    float scale;
+    // workspace
+    unsigned* key[2];
+    unsigned* pos[2];
+    unsigned* counts;  // [0] valid tokens, [1] spanning runs
+    SpanRun* runs;
+    float* head;  // [blocks][pitch]: part of the run that began in an earlier block
+    float* tail;  // [blocks][pitch]: first part of a run that goes on in the next block
+    long long pitch;
+    unsigned block;  // positions of a block
+    int passes, bits;
+};
+
+__device__ __forceinline__ unsigned token_key(const EmbedGradArgs& a, unsigned t) {
+    const long long o = t / a.n_inner, i = t % a.n_inner;
+    const long long x = load_token(a.tokens, a.wide_tokens != 0, o * a.t_so + i * a.t_si);
+    return x >= 0 && x < a.vocab && x != a.padding ? (unsigned)x : (unsigned)a.vocab;
+}
+
+__device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* smem) {
+    unsigned* cnt = smem;                           // [warps][radix]
+    unsigned* tot = cnt + kSortWarps * kSortRadix;  // [radix], read by the other CTAs
+    unsigned* base = tot + kSortRadix;              // [radix]
+    unsigned* wsum = base + kSortRadix;             // [warps]
+    const unsigned rank = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned radix = 1u << a.bits;
+    // each warp of the cluster owns a contiguous range, so that warp order is position order
+    unsigned per = (a.n + kSortCluster * kSortWarps - 1) / (kSortCluster * kSortWarps);
+    per = (per + 31) / 32 * 32;
+    const unsigned lo = min(a.n, (rank * kSortWarps + warp) * per), hi = min(a.n, lo + per);
+    if (rank == 0 && tid == 0) {
+        a.counts[0] = a.n;
+        a.counts[1] = 0;
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const unsigned* kin = a.key[pass & 1];
+        const unsigned* pin = a.pos[pass & 1];
+        unsigned* kout = a.key[(pass & 1) ^ 1];
+        unsigned* pout = a.pos[(pass & 1) ^ 1];
+        const int shift = pass * a.bits;
+        for (unsigned d = tid; d < kSortWarps * radix; d += kSortThreads) cnt[d] = 0;
+        __syncthreads();
+        unsigned* mine = cnt + warp * radix;
+        for (unsigned t = lo + lane; t < hi; t += 32) {
+            const unsigned key = pass == 0 ? token_key(a, t) : __ldcg(kin + t);
+            atomicAdd(mine + ((key >> shift) & (radix - 1)), 1u);
+        }
+        __syncthreads();
+        if (tid < radix) {  // exclusive scan over the warps, digit by digit
+            unsigned run = 0;
+            for (int v = 0; v < kSortWarps; ++v) {
+                const unsigned c = cnt[v * radix + tid];
+                cnt[v * radix + tid] = run;
+                run += c;
+            }
+            tot[tid] = run;
+        }
+        cluster_sync();
+        // place of each digit: all smaller digits, then this digit in the CTAs before this one
+        unsigned all = 0, before = 0;
+        if (tid < radix) {
+            for (unsigned c = 0; c < kSortCluster; ++c) {
+                const unsigned x = cluster_load(cluster_address(tot + tid, c));
+                before += c < rank ? x : 0;
+                all += x;
+            }
+        }
+        unsigned scan = all;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const unsigned y = __shfl_up_sync(0xffffffffu, scan, d);
+            if (lane >= (unsigned)d) scan += y;
+        }
+        if (lane == 31) wsum[warp] = scan;
+        __syncthreads();
+        if (tid < radix) {
+            unsigned below = 0;
+            for (unsigned v = 0; v < warp; ++v) below += wsum[v];
+            base[tid] = below + scan - all + before;
+        }
+        __syncthreads();
+        for (unsigned t0 = lo; t0 < hi; t0 += 32) {
+            const unsigned t = t0 + lane;
+            const bool in = t < hi;
+            const unsigned act = __ballot_sync(0xffffffffu, in);
+            if (in) {
+                const unsigned key = pass == 0 ? token_key(a, t) : __ldcg(kin + t);
+                const unsigned d = (key >> shift) & (radix - 1);
+                const unsigned peers = __match_any_sync(act, d);
+                const unsigned at = base[d] + mine[d] + __popc(peers & ((1u << lane) - 1));
+                __syncwarp(act);
+                if ((peers >> lane) == 1) mine[d] += __popc(peers);  // the last of the equal lanes
+                kout[at] = key;
+                pout[at] = pass == 0 ? t : __ldcg(pin + t);
+            }
+            __syncwarp();
+        }
+        cluster_sync();  // the pass is complete, in memory, for all CTAs of the cluster
+    }
+    const unsigned* key = a.key[a.passes & 1];
+    for (unsigned t = rank * kSortThreads + tid; t < a.n; t += kSortCluster * kSortThreads) {
+        const unsigned k = __ldcg(key + t);
+        if (k == (unsigned)a.vocab && (t == 0 || __ldcg(key + t - 1) != k)) a.counts[0] = t;
+        // the first boundary inside a run lists it, with the block its last position lies in
+        if (t > 0 && t % a.block == 0 && k != (unsigned)a.vocab && __ldcg(key + t - 1) == k &&
+            (t == a.block || __ldcg(key + t - a.block - 1) != k)) {
+            unsigned last = t / a.block, up = (a.n - 1) / a.block;  // key[last * block] == k
+            while (last < up) {
+                const unsigned mid = last + (up - last + 1) / 2;
+                if (__ldcg(key + mid * (size_t)a.block) == k) last = mid; else up = mid - 1;
+            }
+            a.runs[atomicAdd(a.counts + 1, 1u)] = SpanRun{k, t / a.block - 1, last};
+        }
+    }
+}
+
+// Zeros in the rows of [r0, r1) that no token names.
+__device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, unsigned* bits, long long r0, long long r1) {
+    const unsigned rows = (unsigned)(r1 - r0);
+    for (unsigned i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) bits[i] = 0;
+    __syncthreads();
+    for (unsigned t = threadIdx.x; t < a.n; t += blockDim.x) {
+        const unsigned k = token_key(a, t);
+        if (k >= r0 && k < r1) atomicOr(bits + ((unsigned)(k - r0) >> 5), 1u << ((unsigned)(k - r0) & 31));
+    }
+    __syncthreads();
+    const bool vec = (reinterpret_cast<uintptr_t>(a.table) & 15) == 0 && a.stride % 4 == 0;
+    const unsigned lane = threadIdx.x & 31;
+    for (unsigned r = threadIdx.x >> 5; r < rows; r += blockDim.x >> 5) {
+        if ((bits[r >> 5] >> (r & 31)) & 1) continue;
+        float* row = a.table + (r0 + r) * a.stride;
+        const long long n4 = vec ? a.dim / 4 : 0;
+        for (long long j = lane; j < n4; j += 32) __stcs(reinterpret_cast<float4*>(row) + j, make_float4(0, 0, 0, 0));
+        for (long long j = n4 * 4 + lane; j < a.dim; j += 32) __stcs(row + j, 0.0f);
+    }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kSortCluster, 1, 1)
+    sort_kernel(const __grid_constant__ EmbedGradArgs a) {
+    extern __shared__ unsigned smem[];
+    dependent_launch_prologue();
+    if (blockIdx.x < kSortCluster) {
+        sort_tokens(a, smem);
+        return;
+    }
+    const long long ctas = gridDim.x - kSortCluster, me = blockIdx.x - kSortCluster;
+    const long long per = (a.vocab + ctas - 1) / ctas;
+    const long long lo = me * per, hi = lo + per < a.vocab ? lo + per : a.vocab;
+    for (long long r = lo; r < hi; r += kFillRows) fill_rows(a, smem, r, r + kFillRows < hi ? r + kFillRows : hi);
+}
+
+constexpr int kSumThreads = 128;
+constexpr int kSumBatch = 8;       // rows in flight
+constexpr int kSumMaxBlock = 128;  // most positions of a block
+
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant__ EmbedGradArgs a) {
+    constexpr int W = VEC ? kLanes<T> : 1;
+    __shared__ unsigned key[kSumMaxBlock + 2];
+    __shared__ unsigned pos[kSumMaxBlock];
+    dependent_launch_prologue();
+    const unsigned valid = a.counts[0];
+    const unsigned i0 = blockIdx.x * a.block;
+    if (i0 >= valid) return;
+    const unsigned n = min(a.block, valid - i0);
+    const unsigned* skey = a.key[a.passes & 1];
+    const unsigned* spos = a.pos[a.passes & 1];
+    const unsigned none = (unsigned)a.vocab;
+    for (unsigned i = threadIdx.x; i < n + 2; i += blockDim.x) {
+        const long long t = (long long)i0 + i - 1;
+        key[i] = t >= 0 && t < valid ? skey[t] : none;
+        if (i < n) pos[i] = spos[i0 + i];
+    }
+    __syncthreads();
+    const long long col = ((long long)blockIdx.y * blockDim.x + threadIdx.x) * W;
+    if (col >= a.dim) return;
+    const T* src = static_cast<const T*>(a.act) + col;
+    float acc[W];
+#pragma unroll
+    for (int l = 0; l < W; ++l) acc[l] = 0.0f;
+    bool crossed = key[0] == key[1];  // the run began in an earlier block
+    for (unsigned b = 0; b < n; b += kSumBatch) {
+        float x[kSumBatch][W];
+#pragma unroll
+        for (int k = 0; k < kSumBatch; ++k) {
+            if (b + k >= n) continue;
+            const unsigned p = pos[b + k];
+            const T* row = src + (p / a.n_inner) * a.a_so + (p % a.n_inner) * a.a_si;
+            if constexpr (VEC) unpack<T>(__ldg(reinterpret_cast<const uint4*>(row)), x[k]); else x[k][0] = to_f32(*row);
+        }
+#pragma unroll
+        for (int k = 0; k < kSumBatch; ++k) {
+            if (b + k >= n) continue;
+#pragma unroll
+            for (int l = 0; l < W; ++l) acc[l] += x[k][l];
+            const unsigned here = key[b + k + 1], next = key[b + k + 2];
+            const bool last = b + k + 1 == n;
+            if (next == here && !last) continue;
+            // the run ends, or the block does
+            float* dst;
+            if (crossed) {
+                dst = a.head + blockIdx.x * a.pitch + col;
+            } else if (next == here) {
+                dst = a.tail + blockIdx.x * a.pitch + col;
+            } else {
+                dst = a.table + here * a.stride + col;
+#pragma unroll
+                for (int l = 0; l < W; ++l) acc[l] *= a.scale;
+                if (a.accumulate) {
+#pragma unroll
+                    for (int l = 0; l < W; ++l) acc[l] += dst[l];
+                }
+            }
+            if constexpr (VEC) {
+#pragma unroll
+                for (int l = 0; l < W; l += 4)
+                    *reinterpret_cast<float4*>(dst + l) = make_float4(acc[l], acc[l + 1], acc[l + 2], acc[l + 3]);
+            } else {
+                *dst = acc[0];
+            }
+#pragma unroll
+            for (int l = 0; l < W; ++l) acc[l] = 0.0f;
+            crossed = false;
+        }
+    }
+}
+
+// Eight warps share a run's parts, a column a lane; the warps' sums are added in warp order.
+constexpr int kJoinWarps = 8;
+constexpr int kJoinGrid = 64;
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_constant__ EmbedGradArgs a) {
+    __shared__ float part[kJoinWarps][32];
+    dependent_launch_prologue();
+    const unsigned runs = a.counts[1];
+    const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long col = (long long)blockIdx.y * 32 + lane;
+    for (unsigned r = blockIdx.x; r < runs; r += gridDim.x) {
+        const SpanRun run = a.runs[r];
+        float s = 0.0f;
+        if (col < a.dim) {
+#pragma unroll 8
+            for (unsigned b = run.first + warp; b <= run.last; b += kJoinWarps)
+                s += (b == run.first ? a.tail : a.head)[b * a.pitch + col];
+        }
+        part[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0 && col < a.dim) {
+            s = part[0][lane];
+#pragma unroll
+            for (int v = 1; v < kJoinWarps; ++v) s += part[v][lane];
+            float* dst = a.table + run.token * a.stride + col;
+            s *= a.scale;
+            *dst = a.accumulate ? *dst + s : s;
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ gradient norm and clip
+// Two launches.  norm_kernel sums the squares of one chunk per CTA in 64 bits (a product of two
+// 32-bit numbers is exact there) and leaves one partial per chunk; the CTA that finishes a group
+// adds the group's partials in chunk order and stores norm and factor.  clip_kernel walks the
+// chunks backwards: the ones read last are still in the L2.
+constexpr int kClipThreads = 256;
+
+struct GradEntry {
+    const void* src;
+    float* dst;  // place in the arena, or nullptr: in place
+    unsigned long long numel;
+    unsigned first_chunk;
+    int type_group;  // type | group << 8 | (16-byte aligned) << 16
+};
+struct GradGroup {
+    unsigned first_chunk, n_chunks;
+    unsigned arrived;
+    float factor;
+};
+struct GradArgs {
+    const GradEntry* entries;
+    const unsigned* chunk_entry;
+    double* partial;
+    GradGroup* groups;
+    float* norms;
+    unsigned n_chunks, chunk;
+    int n_groups;
+    float max_norm;
+};
+
+__device__ __forceinline__ float clip_factor(double norm, float max_norm) {
+    return norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.0f;
+}
+
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const T* p, unsigned n, bool vec) {
+    constexpr int L = kLanes<T>;
+    constexpr int U = 4;
+    double s[U] = {0.0, 0.0, 0.0, 0.0};
+    unsigned done = 0;
+    if (vec) {
+        const unsigned nv = n / L;
+        for (unsigned b = 0; b < nv; b += U * kClipThreads) {
+            uint4 q[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const unsigned v = b + k * kClipThreads + threadIdx.x;
+                q[k] = v < nv ? __ldg(reinterpret_cast<const uint4*>(p) + v) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                float x[L];
+                unpack<T>(q[k], x);
+#pragma unroll
+                for (int l = 0; l < L; ++l) s[k] = fma((double)x[l], (double)x[l], s[k]);
+            }
+        }
+        done = nv * L;
+    }
+    for (unsigned j = done + threadIdx.x; j < n; j += kClipThreads) {
+        const double x = to_f32(p[j]);
+        s[0] = fma(x, x, s[0]);
+    }
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+__global__ void __launch_bounds__(kClipThreads) norm_kernel(const __grid_constant__ GradArgs a) {
+    __shared__ double part[kClipThreads / 32];
+    __shared__ bool last;
+    dependent_launch_prologue();
+    if (blockIdx.x == 0 && threadIdx.x < a.n_groups && a.groups[threadIdx.x].n_chunks == 0) {
+        a.groups[threadIdx.x].factor = 1.0f;
+        if (a.norms != nullptr) a.norms[threadIdx.x] = 0.0f;
+    }
+    if (blockIdx.x >= a.n_chunks) return;
+    const GradEntry e = a.entries[a.chunk_entry[blockIdx.x]];
+    const unsigned long long at = (unsigned long long)(blockIdx.x - e.first_chunk) * a.chunk;
+    const unsigned n = (unsigned)(e.numel - at < a.chunk ? e.numel - at : a.chunk);
+    const int type = e.type_group & 0xff, group = (e.type_group >> 8) & 0xff;
+    const bool vec = (e.type_group >> 16) != 0;
+    double s[1];
+    if (type == ODSGD_F32) s[0] = chunk_squares(static_cast<const float*>(e.src) + at, n, vec);
+    else if (type == ODSGD_BF16) s[0] = chunk_squares(static_cast<const bf16*>(e.src) + at, n, vec);
+    else s[0] = chunk_squares(static_cast<const f16*>(e.src) + at, n, vec);
+    block_sum<1, kClipThreads>(s, part);
+    GradGroup* g = a.groups + group;
+    if (threadIdx.x == 0) {
+        a.partial[blockIdx.x] = s[0];
+        __threadfence();
+        last = atomicAdd(&g->arrived, 1u) == g->n_chunks - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double t[1] = {0.0};
+    for (unsigned c = threadIdx.x; c < g->n_chunks; c += kClipThreads) t[0] += __ldcg(a.partial + g->first_chunk + c);
+    block_sum<1, kClipThreads>(t, part);
+    if (threadIdx.x == 0) {
+        const double norm = sqrt(t[0]);
+        g->factor = clip_factor(norm, a.max_norm);
+        g->arrived = 0;  // for the next call
+        if (a.norms != nullptr) a.norms[group] = (float)norm;
+    }
+}
+
+// dst of the arena (float) or the tensor itself (T).
+template <typename T, typename D>
+__device__ __forceinline__ void chunk_scale(const T* p, D* d, unsigned n, float f, bool vec) {
+    constexpr int L = kLanes<T>;
+    constexpr int U = 4;
+    unsigned done = 0;
+    if (vec) {
+        const unsigned nv = n / L;
+        for (unsigned b = 0; b < nv; b += U * kClipThreads) {
+            uint4 q[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const unsigned v = b + k * kClipThreads + threadIdx.x;
+                if (v < nv) q[k] = __ldcs(reinterpret_cast<const uint4*>(p) + v);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const unsigned v = b + k * kClipThreads + threadIdx.x;
+                if (v >= nv) continue;
+                float x[L];
+                unpack<T>(q[k], x);
+#pragma unroll
+                for (int l = 0; l < L; ++l) x[l] *= f;
+                if constexpr (sizeof(T) == sizeof(D)) {
+                    __stcs(reinterpret_cast<uint4*>(d) + v, pack<T>(x));
+                } else {
+#pragma unroll
+                    for (int l = 0; l < L; l += 4)
+                        __stcs(reinterpret_cast<float4*>(d + (size_t)v * L + l), make_float4(x[l], x[l + 1], x[l + 2], x[l + 3]));
+                }
+            }
+        }
+        done = nv * L;
+    }
+    for (unsigned j = done + threadIdx.x; j < n; j += kClipThreads) d[j] = from_f32<D>(to_f32(p[j]) * f);
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_entry(const GradEntry& e, unsigned long long at, unsigned n, float f, bool vec) {
+    const T* p = static_cast<const T*>(e.src) + at;
+    if (e.dst != nullptr) {
+        chunk_scale<T, float>(p, e.dst + at, n, f, vec);
+    } else if (f != 1.0f) {  // in place, a factor of one leaves every bit as it is
+        chunk_scale<T, T>(p, const_cast<T*>(p), n, f, vec);
+    }
+}
+
+__global__ void __launch_bounds__(kClipThreads) clip_kernel(const __grid_constant__ GradArgs a) {
+    dependent_launch_prologue();
+    const unsigned c = a.n_chunks - 1 - blockIdx.x;
+    const GradEntry e = a.entries[a.chunk_entry[c]];
+    const unsigned long long at = (unsigned long long)(c - e.first_chunk) * a.chunk;
+    const unsigned n = (unsigned)(e.numel - at < a.chunk ? e.numel - at : a.chunk);
+    const int type = e.type_group & 0xff;
+    const float f = a.groups[(e.type_group >> 8) & 0xff].factor;
+    const bool vec = (e.type_group >> 16) != 0;
+    if (type == ODSGD_F32) scale_entry<float>(e, at, n, f, vec);
+    else if (type == ODSGD_BF16) scale_entry<bf16>(e, at, n, f, vec);
+    else scale_entry<f16>(e, at, n, f, vec);
+}
+
+}  // namespace odsgd_lm
