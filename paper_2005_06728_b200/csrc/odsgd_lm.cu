@@ -334,9 +334,9 @@ struct RowShape {
 
 // CTAs and threads of a row.  The row is cut so that a CTA's part fits its registers (64 KB at 512
 // threads), and further, down to 4 KB a CTA, while the grid has fewer CTAs than the GPU has SMs.
-RowShape row_shape(int64_t rows, int64_t vocab, int elem, int64_t slack, bool loss, int sms) {
+RowShape row_shape(int64_t rows, int64_t vocab, int elem, bool loss, int sms) {
     RowShape s;
-    const int64_t vectors = ceil_div(vocab + slack, 16 / elem);
+    const int64_t vectors = std::max<int64_t>(1, vocab / (16 / elem));
     const int64_t hold = (int64_t)kRowThreads * kRowVectors;
     s.cluster = 1;
     if (loss)
@@ -393,9 +393,7 @@ int launch_rows(const odsgd_policy_desc* d, bool loss, float* terms, void* strea
     } else {
         a.lse = d->lse;
     }
-    const int es = size_of(d->type);
-    const bool whole = rows_aligned16(d->logits, es, a.z_so, a.z_si, d->n_outer, d->n_inner);
-    const RowShape s = row_shape(a.rows, a.vocab, es, whole ? 0 : 16 / es - 1, loss, sms);
+    const RowShape s = row_shape(a.rows, a.vocab, size_of(d->type), loss, sms);
     a.cluster = s.cluster;
     switch (d->type) {
         case ODSGD_F32: return launch_rows_t<float>(a, s, stream);

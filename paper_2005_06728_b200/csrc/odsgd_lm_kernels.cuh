@@ -103,6 +103,27 @@ __device__ __forceinline__ uint4 pack<f16>(const float (&x)[8]) {
     return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
+// Two floats in one register pair, added and multiplied by one instruction each.
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 f2(float x, float y) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void split(F2 a, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v)); }
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+
 // Negative infinity in every lane.
 template <typename T>
 __device__ __forceinline__ uint4 neg_inf_vector() {
@@ -191,17 +212,48 @@ template <typename T>
 struct RowExp {
     float c, m;
     __device__ __forceinline__ RowExp(float inv_temp, float m_) : c(sizeof(T) == 4 ? inv_temp : inv_temp * 1.4426950408889634f), m(m_) {}
-    __device__ __forceinline__ float operator()(float z) const {
-        if constexpr (sizeof(T) == 4) {
-            return expf((z - m) * c);
-        } else {
-            float r;
-            const float t = (z - m) * c;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
-            return r;
-        }
+    __device__ __forceinline__ F2 operator()(float z0, float z1) const {
+        float t0, t1;
+        split((f2(z0, z1) + f2(-m, -m)) * f2(c, c), t0, t1);
+        if constexpr (sizeof(T) == 4) return f2(expf(t0), expf(t1));
+        float r0, r1;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(t0));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(t1));
+        return f2(r0, r1);
     }
 };
+
+// Largest element of a vector (NaN is passed over; it comes back through the sum).
+template <typename T>
+__device__ __forceinline__ float vectors_max(const uint4 (&q)[kRowVectors]);
+template <>
+__device__ __forceinline__ float vectors_max<float>(const uint4 (&q)[kRowVectors]) {
+    float m = -CUDART_INF_F;
+#pragma unroll
+    for (int k = 0; k < kRowVectors; ++k)
+        m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(q[k].x), __uint_as_float(q[k].y)), fmaxf(__uint_as_float(q[k].z), __uint_as_float(q[k].w))));
+    return m;
+}
+template <typename H2>
+__device__ __forceinline__ H2 pairs_max(const uint4 (&q)[kRowVectors]) {
+    const auto as = [](const uint32_t& u) { return *reinterpret_cast<const H2*>(&u); };
+    H2 m = as(q[0].x);
+#pragma unroll
+    for (int k = 0; k < kRowVectors; ++k) m = __hmax2(m, __hmax2(__hmax2(as(q[k].x), as(q[k].y)), __hmax2(as(q[k].z), as(q[k].w))));
+    return m;
+}
+// The half instructions return NaN where both operands are.
+__device__ __forceinline__ float pair_max(float x, float y) { return fmaxf(-CUDART_INF_F, fmaxf(x, y)); }
+template <>
+__device__ __forceinline__ float vectors_max<bf16>(const uint4 (&q)[kRowVectors]) {
+    const __nv_bfloat162 m = pairs_max<__nv_bfloat162>(q);
+    return pair_max(__low2float(m), __high2float(m));
+}
+template <>
+__device__ __forceinline__ float vectors_max<f16>(const uint4 (&q)[kRowVectors]) {
+    const __half2 m = pairs_max<__half2>(q);
+    return pair_max(__low2float(m), __high2float(m));
+}
 
 // Factor that moves a sum held against maximum `from` to maximum `to`.  The empty set (-inf) has
 // s = 0, or a NaN that has to stay.
@@ -224,71 +276,63 @@ __device__ __forceinline__ MaxSum warp_join(MaxSum x, float c) {
     return MaxSum{m, s};
 }
 
-// A row as 16-byte vectors: vector v covers elements [v L - head, (v + 1) L - head), `head` being
-// how far the row starts behind a 16-byte boundary; what lies outside the row is left alone.
+// A row as `vectors` whole 16-byte vectors behind `head` elements, and what is left behind those.
+// The edges, fewer than 2 L elements, are held one a thread by the first warp of the row.
 template <typename T>
-struct RowVectors {
+struct RowParts {
     static constexpr int L = kLanes<T>;
-    const T* row;
-    long long vocab;
-    int head;
-    __device__ __forceinline__ RowVectors(const T* r, long long v)
-        : row(r), vocab(v), head((int)((reinterpret_cast<uintptr_t>(r) & 15) / sizeof(T))) {}
-    __device__ __forceinline__ long long count() const { return (head + vocab + L - 1) / L; }
-    __device__ __forceinline__ bool whole(long long v) const { return v * L >= head && (v + 1) * L <= head + vocab; }
-    __device__ __forceinline__ uint4 load(long long v) const {
-        if (whole(v)) return __ldcs(reinterpret_cast<const uint4*>(row - head) + v);
-        uint4 q = neg_inf_vector<T>();
-        T* e = reinterpret_cast<T*>(&q);
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-            const long long j = v * L + i - head;
-            if (j >= 0 && j < vocab) e[i] = row[j];
-        }
-        return q;
+    int head, vectors, tail;
+    __device__ __forceinline__ RowParts(const T* row, int vocab) {
+        head = min(vocab, (int)(((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / sizeof(T)));
+        vectors = (vocab - head) / L;
+        tail = vocab - head - vectors * L;
+    }
+    // Element that thread t of the row holds besides its vectors; -1: none.
+    __device__ __forceinline__ int edge(int t) const {
+        if (t < head) return t;
+        if (t >= 16 && t < 16 + tail) return head + vectors * L + t - 16;
+        return -1;
     }
 };
 
-// Vector v of the gradient row; `same` says that the row starts as far behind a 16-byte boundary
-// as the logits' does.
+__device__ __forceinline__ void store_elements(float* p, const uint4& q) {
+    p[0] = __uint_as_float(q.x);
+    p[1] = __uint_as_float(q.y);
+    p[2] = __uint_as_float(q.z);
+    p[3] = __uint_as_float(q.w);
+}
 template <typename T>
-__device__ __forceinline__ void store_row_vector(T* drow, const RowVectors<T>& rv, long long v, const uint4& q, bool same) {
-    constexpr int L = kLanes<T>;
-    if (same && rv.whole(v)) {
-        __stcs(reinterpret_cast<uint4*>(drow - rv.head) + v, q);
-        return;
-    }
-    const T* e = reinterpret_cast<const T*>(&q);
+__device__ __forceinline__ void store_elements(T* p, const uint4& q) {
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+    unsigned short* h = reinterpret_cast<unsigned short*>(p);
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-        const long long j = v * L + i - rv.head;
-        if (j >= 0 && j < rv.vocab) drow[j] = e[i];
-    }
+    for (int i = 0; i < 8; ++i) h[i] = (unsigned short)(u[i / 2] >> (i % 2 * 16));
+}
+// `aligned`: the gradient's row starts as far behind a 16-byte boundary as the logits' does.
+template <typename T>
+__device__ __forceinline__ void store_vector(T* p, const uint4& q, bool aligned) {
+    if (aligned) __stcs(reinterpret_cast<uint4*>(p), q);
+    else store_elements(p, q);
 }
 
 template <typename T>
 __device__ __forceinline__ MaxSum vectors_max_sum(const uint4 (&q)[kRowVectors], float inv_temp) {
     constexpr int L = kLanes<T>;
-    float m = -CUDART_INF_F;
-#pragma unroll
-    for (int k = 0; k < kRowVectors; ++k) {
-        float x[L];
-        unpack<T>(q[k], x);
-#pragma unroll
-        for (int i = 0; i < L; ++i) m = fmaxf(m, x[i]);
-    }
+    const float m = vectors_max<T>(q);
     const RowExp<T> e(inv_temp, m == -CUDART_INF_F ? 0.0f : m);
-    float s = 0.0f;
+    F2 s = f2(0.0f, 0.0f);
 #pragma unroll
     for (int k = 0; k < kRowVectors; ++k) {
         float x[L];
         unpack<T>(q[k], x);
-        float p = 0.0f;
+        F2 p = e(x[0], x[1]);
 #pragma unroll
-        for (int i = 0; i < L; ++i) p += e(x[i]);
-        s += p;
+        for (int i = 2; i < L; i += 2) p = p + e(x[i], x[i + 1]);
+        s = s + p;
     }
-    return MaxSum{m, s};
+    float s0, s1;
+    split(s, s0, s1);
+    return MaxSum{m, s0 + s1};
 }
 
 // What a row's statistics make of its loss, and the factor k of its gradient.
@@ -319,23 +363,25 @@ __device__ __forceinline__ RowLoss row_loss(const RowArgs& a, float logp, float 
 }
 
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__(kRowThreads, 2) row_kernel(const __grid_constant__ RowArgs a) {
     constexpr int L = kLanes<T>;
     __shared__ MaxSum warp_part[kRowThreads / 32];
     __shared__ MaxSum cta_part[kRowCluster];
     dependent_launch_prologue();
     const unsigned cs = (unsigned)a.cluster;
     const unsigned row = blockIdx.x / cs, rank = blockIdx.x % cs;
+    const int tid = (int)threadIdx.x, threads = (int)blockDim.x;
     const long long o = row / a.n_inner, i = row % a.n_inner;
-    const RowVectors<T> rv(static_cast<const T*>(a.z) + o * a.z_so + i * a.z_si, a.vocab);
+    const T* zrow = static_cast<const T*>(a.z) + o * a.z_so + i * a.z_si;
+    T* drow = MODE == kRowScore ? nullptr : static_cast<T*>(a.dz) + o * a.d_so + i * a.d_si;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(drow) ^ reinterpret_cast<uintptr_t>(zrow)) & 15) == 0;
     const long long y = load_token(a.labels, a.wide_labels != 0, o * a.l_so + i * a.l_si);
     const float w = MODE == kRowScore ? 1.0f : a.weight.p[o * a.weight.so + i * a.weight.si];
-    T* drow = MODE == kRowScore ? nullptr : static_cast<T*>(a.dz) + o * a.d_so + i * a.d_si;
-    const bool same = MODE != kRowScore && ((reinterpret_cast<uintptr_t>(drow) ^ reinterpret_cast<uintptr_t>(rv.row)) & 15) == 0;
-    const long long total = rv.count();
-    const long long per = (total + cs - 1) / cs;
-    const long long v0 = rank * per, v1 = v0 + per < total ? v0 + per : total;
-    const bool first = rank == 0 && threadIdx.x == 0;
+    const RowParts<T> parts(zrow, (int)a.vocab);
+    const int per = (parts.vectors + (int)cs - 1) / (int)cs;
+    const int v0 = min((int)rank * per, parts.vectors), v1 = min(v0 + per, parts.vectors);
+    const int edge = rank == 0 ? parts.edge(tid) : -1;
+    const bool first = rank == 0 && tid == 0;
 
     if (w == 0.0f || y < 0 || y >= a.vocab) {  // the whole cluster leaves here together
         if (first) {
@@ -347,34 +393,36 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
             }
         }
         if (MODE != kRowScore) {
-            const uint4 zero = make_uint4(0, 0, 0, 0);
-            for (long long v = v0 + threadIdx.x; v < v1; v += blockDim.x) store_row_vector(drow, rv, v, zero, same);
+            for (int v = v0 + tid; v < v1; v += threads) store_vector(drow + parts.head + v * L, make_uint4(0, 0, 0, 0), aligned);
+            if (edge >= 0) drow[edge] = from_f32<T>(0.0f);
         }
         return;
     }
     if (cs > 1) cluster_arrive();  // this CTA runs: its shared memory may be written (waited for below)
-    const float zy = to_f32(rv.row[y]);
+    const float zy = to_f32(zrow[y]);
+    const float ze = edge >= 0 ? to_f32(zrow[edge]) : -CUDART_INF_F;
 
     uint4 q[kRowVectors];
-    MaxSum x{-CUDART_INF_F, 0.0f};
-    const long long step = (long long)blockDim.x * kRowVectors;
-    auto load = [&](long long b) {
+    const uint4* zv = reinterpret_cast<const uint4*>(zrow + parts.head);
+    const int step = threads * kRowVectors;
+    auto load = [&](int b) {
 #pragma unroll
         for (int k = 0; k < kRowVectors; ++k) {
-            const long long v = b + (long long)k * blockDim.x + threadIdx.x;
-            q[k] = v < v1 ? rv.load(v) : neg_inf_vector<T>();
+            const int v = b + k * threads + tid;
+            q[k] = v < v1 ? __ldcs(zv + v) : neg_inf_vector<T>();
         }
         return vectors_max_sum<T>(q, a.inv_temp);
     };
+    MaxSum x{ze, ze == -CUDART_INF_F ? 0.0f : ze - ze + 1.0f};  // NaN and +inf leave NaN
     if (MODE == kRowResident) {
-        x = load(v0);  // the host made sure that one round covers the CTA's part
+        x = join(x, load(v0), a.inv_temp);  // the host made sure that one round covers the CTA's part
     } else {
-        for (long long b = v0; b < v1; b += step) x = join(x, load(b), a.inv_temp);
+        for (int b = v0; b < v1; b += step) x = join(x, load(b), a.inv_temp);
     }
     x = warp_join(x, a.inv_temp);
-    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int lane = tid & 31, warps = threads >> 5;
     if (warps > 1) {
-        if (lane == 0) warp_part[threadIdx.x >> 5] = x;
+        if (lane == 0) warp_part[tid >> 5] = x;
         __syncthreads();
         x = lane < warps ? warp_part[lane] : MaxSum{-CUDART_INF_F, 0.0f};
         x = warp_join(x, a.inv_temp);
@@ -409,27 +457,41 @@ __global__ void __launch_bounds__(kRowThreads) row_kernel(const __grid_constant_
         a.terms[a.rows + row] = loss.kl;
         a.terms[2 * (size_t)a.rows + row] = loss.clipped;
     }
+    // The packed vectors alone live across the join: without this the compiler keeps the unpacked
+    // ones as well, and spills.
+#pragma unroll
+    for (int k = 0; k < kRowVectors; ++k) asm volatile("" : "+r"(q[k].x), "+r"(q[k].y), "+r"(q[k].z), "+r"(q[k].w));
     // dz_j = k ([j == y] - exp(c (z_j - m)) / s)
     const RowExp<T> e(a.inv_temp, x.m);
     const float neg = -loss.k / x.s;
-    const long long vy = (rv.head + y) / L;
-    const int ly = (int)((rv.head + y) % L);
-    for (long long b = v0; b < v1; b += step) {  // one round when resident
+    const int in_body = (int)y - parts.head;  // place of the label among the vectors' elements
+    const int vy = in_body >= 0 ? in_body / L : -1, ly = in_body % L;
+    auto store = [&](int b) {
 #pragma unroll
         for (int k = 0; k < kRowVectors; ++k) {
-            const long long v = b + (long long)k * blockDim.x + threadIdx.x;
+            const int v = b + k * threads + tid;
             if (v >= v1) continue;
-            if (MODE == kRowStream) q[k] = rv.load(v);
+            if (MODE == kRowStream) q[k] = __ldcs(zv + v);
             float p[L];
             unpack<T>(q[k], p);
 #pragma unroll
-            for (int l = 0; l < L; ++l) p[l] = neg * e(p[l]);
+            for (int l = 0; l < L; l += 2) split(e(p[l], p[l + 1]) * f2(neg, neg), p[l], p[l + 1]);
             if (v == vy) {
 #pragma unroll
                 for (int l = 0; l < L; ++l) p[l] += l == ly ? loss.k : 0.0f;
             }
-            store_row_vector(drow, rv, v, pack<T>(p), same);
+            store_vector(drow + parts.head + v * L, pack<T>(p), aligned);
         }
+    };
+    if (MODE == kRowResident) {
+        store(v0);
+    } else {
+        for (int b = v0; b < v1; b += step) store(b);
+    }
+    if (edge >= 0) {
+        float p0, p1;
+        split(e(ze, ze) * f2(neg, neg), p0, p1);
+        drow[edge] = from_f32<T>(p0 + (edge == (int)y ? loss.k : 0.0f));
     }
 }
 
