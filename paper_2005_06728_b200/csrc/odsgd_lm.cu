@@ -329,35 +329,26 @@ int check_policy(const odsgd_policy_desc* d, bool loss) {
 }
 
 struct RowShape {
-    int mode, cluster, threads;
+    int cluster, threads;
 };
 
-// CTAs and threads of a row.  The row is cut so that a CTA's part fits its registers (64 KB at 512
-// threads), and further, down to 4 KB a CTA, while the grid has fewer CTAs than the GPU has SMs.
 RowShape row_shape(int64_t rows, int64_t vocab, int elem, bool loss, int sms) {
     RowShape s;
     const int64_t vectors = std::max<int64_t>(1, vocab / (16 / elem));
-    const int64_t hold = (int64_t)kRowThreads * kRowVectors;
     s.cluster = 1;
-    if (loss)
-        while (s.cluster < kRowCluster && ceil_div(vectors, s.cluster) > hold) s.cluster *= 2;
     while (s.cluster < kRowCluster && rows * s.cluster < sms && vectors > (int64_t)s.cluster * 256) s.cluster *= 2;
     const int64_t part = ceil_div(vectors, s.cluster);
-    s.mode = !loss ? kRowScore : part <= hold ? kRowResident : kRowStream;
-    // eight vectors a thread when there are rows enough to fill the GPU, one when there are not
+    // a batch of vectors a thread when there are rows enough to fill the GPU, one vector when there are not
     const int64_t each = rows * s.cluster >= 2 * (int64_t)sms ? kRowVectors : 1;
     s.threads = (int)std::min<int64_t>(kRowThreads, std::max<int64_t>(32, ceil_div(ceil_div(part, each), 32) * 32));
     return s;
 }
 
 template <typename T>
-int launch_rows_t(const RowArgs& a, const RowShape& s, void* stream) {
+int launch_rows_t(const RowArgs& a, const RowShape& s, bool loss, void* stream) {
     const dim3 grid(a.rows * (unsigned)s.cluster), block((unsigned)s.threads);
-    switch (s.mode) {
-        case kRowScore: return launch("score kernel", row_kernel<T, kRowScore>, grid, block, 0, s.cluster, stream, a);
-        case kRowResident: return launch("policy loss kernel", row_kernel<T, kRowResident>, grid, block, 0, s.cluster, stream, a);
-        default: return launch("policy loss kernel", row_kernel<T, kRowStream>, grid, block, 0, s.cluster, stream, a);
-    }
+    return loss ? launch("policy loss kernel", row_kernel<T, true>, grid, block, 0, s.cluster, stream, a)
+                : launch("score kernel", row_kernel<T, false>, grid, block, 0, s.cluster, stream, a);
 }
 
 int launch_rows(const odsgd_policy_desc* d, bool loss, float* terms, void* stream) {
@@ -396,9 +387,9 @@ int launch_rows(const odsgd_policy_desc* d, bool loss, float* terms, void* strea
     const RowShape s = row_shape(a.rows, a.vocab, size_of(d->type), loss, sms);
     a.cluster = s.cluster;
     switch (d->type) {
-        case ODSGD_F32: return launch_rows_t<float>(a, s, stream);
-        case ODSGD_BF16: return launch_rows_t<bf16>(a, s, stream);
-        default: return launch_rows_t<f16>(a, s, stream);
+        case ODSGD_F32: return launch_rows_t<float>(a, s, loss, stream);
+        case ODSGD_BF16: return launch_rows_t<bf16>(a, s, loss, stream);
+        default: return launch_rows_t<f16>(a, s, loss, stream);
     }
 }
 

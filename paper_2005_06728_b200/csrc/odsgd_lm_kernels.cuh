@@ -123,6 +123,11 @@ __device__ __forceinline__ F2 operator*(F2 a, F2 b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
     return r;
 }
+__device__ __forceinline__ F2 multiply_add(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
 
 // Negative infinity in every lane.
 template <typename T>
@@ -167,16 +172,10 @@ __device__ __forceinline__ uint32_t cluster_load(uint32_t addr) {
 }
 
 // ------------------------------------------------------------------ rows of logits
-// One cluster of `cluster` CTAs takes one row; the row's 16-byte vectors are split evenly over it.
-constexpr int kRowVectors = 8;    // vectors a thread holds at a time
-constexpr int kRowThreads = 512;  // most threads of a CTA: 64 KB of a row in registers
+// A cluster of `cluster` CTAs takes a row; the row's 16-byte vectors are split evenly over it.
+constexpr int kRowVectors = 4;    // vectors a thread has in flight
+constexpr int kRowThreads = 512;  // most threads of a CTA
 constexpr int kRowCluster = 8;    // most CTAs of a row (the portable limit)
-
-enum RowMode : int {
-    kRowScore = 0,     // logp and lse only
-    kRowResident = 1,  // loss and gradient, the row held in registers between its read and its write
-    kRowStream = 2,    // loss and gradient of a row too long for that: read twice
-};
 
 struct VecView {
     const float* p;
@@ -204,22 +203,35 @@ struct MaxSum {
     float m, s;
 };
 
-// exp(c (z - m)) in the precision the row's type deserves: 16-bit logits through the base-2
-// exponential of the special-function unit (2^-22 relative, far below the 2^-8 or 2^-11 that the
-// gradient is rounded to); 32-bit logits through expf.  The difference comes first: c m alone
-// overflows where a mask holds the type's lowest value.
+// exp(c (z - m)) in the precision the row's type deserves.
+//   32-bit logits: expf.
+//   16-bit logits: the base-2 exponential of the special-function unit (2^-22 relative, far below the
+//   2^-8 or 2^-11 that the gradient is rounded to) of one multiply-add, c2 z - c2 m with
+//   c2 = c / ln 2.  The rounding of c2 m is common to all elements: `fix` takes it back out of
+//   their sum or factor.  Where c2 m would overflow (a mask of the type's lowest value), z that differ
+//   are so far apart that any c gives 0, and 2^-64 makes both products exact and small.
 template <typename T>
 struct RowExp {
-    float c, m;
-    __device__ __forceinline__ RowExp(float inv_temp, float m_) : c(sizeof(T) == 4 ? inv_temp : inv_temp * 1.4426950408889634f), m(m_) {}
+    float c, m, fix;
+    __device__ __forceinline__ RowExp(float inv_temp, float m_) : c(inv_temp), m(m_), fix(1.0f) {
+        if constexpr (sizeof(T) == 2) {
+            c = inv_temp * 1.4426950408889634f;
+            if (fabsf(m_ * c) > 1e37f) c = 5.421010862427522e-20f;
+            m = m_ * c;
+            fix = fmaf(fmaf(m_, c, -m), -0.6931471805599453f, 1.0f);
+        }
+    }
     __device__ __forceinline__ F2 operator()(float z0, float z1) const {
         float t0, t1;
-        split((f2(z0, z1) + f2(-m, -m)) * f2(c, c), t0, t1);
-        if constexpr (sizeof(T) == 4) return f2(expf(t0), expf(t1));
-        float r0, r1;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(t0));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(t1));
-        return f2(r0, r1);
+        if constexpr (sizeof(T) == 4) {
+            return f2(expf((z0 - m) * c), expf((z1 - m) * c));
+        } else {
+            split(multiply_add(f2(z0, z1), f2(c, c), f2(-m, -m)), t0, t1);
+            float r0, r1;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(t0));
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(t1));
+            return f2(r0, r1);
+        }
     }
 };
 
@@ -315,54 +327,98 @@ __device__ __forceinline__ void store_vector(T* p, const uint4& q, bool aligned)
     else store_elements(p, q);
 }
 
+// x joined with the elements of some vectors.
 template <typename T>
-__device__ __forceinline__ MaxSum vectors_max_sum(const uint4 (&q)[kRowVectors], float inv_temp) {
+__device__ __forceinline__ MaxSum add_vectors(MaxSum x, const uint4 (&q)[kRowVectors], float inv_temp) {
     constexpr int L = kLanes<T>;
-    const float m = vectors_max<T>(q);
+    const float m = fmaxf(x.m, vectors_max<T>(q));
     const RowExp<T> e(inv_temp, m == -CUDART_INF_F ? 0.0f : m);
-    F2 s = f2(0.0f, 0.0f);
+    F2 sum = f2(0.0f, 0.0f);
 #pragma unroll
     for (int k = 0; k < kRowVectors; ++k) {
-        float x[L];
-        unpack<T>(q[k], x);
-        F2 p = e(x[0], x[1]);
+        float z[L];
+        unpack<T>(q[k], z);
+        F2 part = e(z[0], z[1]);
 #pragma unroll
-        for (int i = 2; i < L; i += 2) p = p + e(x[i], x[i + 1]);
-        s = s + p;
+        for (int i = 2; i < L; i += 2) part = part + e(z[i], z[i + 1]);
+        sum = sum + part;
     }
     float s0, s1;
-    split(s, s0, s1);
-    return MaxSum{m, s0 + s1};
+    split(sum, s0, s1);
+    return MaxSum{m, fmaf(x.s, rebase(x.m, m, inv_temp), (s0 + s1) * e.fix)};
 }
 
+// A row's inputs besides its logits.
+struct RowInputs {
+    float old_logp = 0.0f, ref_logp = 0.0f, adv = 0.0f;
+    __device__ __forceinline__ void load(const RowArgs& a, long long o, long long i) {
+        old_logp = a.old_logp.p[o * a.old_logp.so + i * a.old_logp.si];
+        if (a.ref_logp.p != nullptr) ref_logp = a.ref_logp.p[o * a.ref_logp.so + i * a.ref_logp.si];
+        adv = a.adv.p[o * a.adv.so + i * a.adv.si];
+    }
+};
 // What a row's statistics make of its loss, and the factor k of its gradient.
 struct RowLoss {
     float k, pg, kl, clipped;
-};
-__device__ __forceinline__ RowLoss row_loss(const RowArgs& a, float logp, float w, long long o, long long i) {
-    const float old = a.old_logp.p[o * a.old_logp.so + i * a.old_logp.si];
-    const float A = a.adv.p[o * a.adv.so + i * a.adv.si];
-    const float r = expf(logp - old);
-    const float bounded = fminf(fmaxf(r, 1.0f - a.clip_low), 1.0f + a.clip_high) * A;
-    const float free_term = r * A;
-    const bool cut = free_term > bounded;
-    RowLoss out;
-    // NaN stays: a comparison with it is false, and r itself is NaN
-    out.pg = -w * (cut ? bounded : free_term);
-    out.clipped = cut ? w : 0.0f;
-    float g = cut ? 0.0f : -free_term;
-    out.kl = 0.0f;
-    if (a.ref_logp.p != nullptr) {
-        const float d = a.ref_logp.p[o * a.ref_logp.so + i * a.ref_logp.si] - logp;
-        const float em = expm1f(d);  // exp(d) - 1 without its cancellation near d = 0
-        out.kl = w * (em - d);
-        g -= a.kl_coef * em;
+    __device__ __forceinline__ RowLoss(const RowArgs& a, const RowInputs& in, float logp, float w) {
+        const float r = expf(logp - in.old_logp);
+        const float bounded = fminf(fmaxf(r, 1.0f - a.clip_low), 1.0f + a.clip_high) * in.adv;
+        const float free_term = r * in.adv;
+        const bool cut = free_term > bounded;
+        // NaN stays: a comparison with it is false, and r itself is NaN
+        pg = -w * (cut ? bounded : free_term);
+        clipped = cut ? w : 0.0f;
+        float g = cut ? 0.0f : -free_term;
+        kl = 0.0f;
+        if (a.ref_logp.p != nullptr) {
+            const float d = in.ref_logp - logp;
+            const float em = expm1f(d);  // exp(d) - 1 without its cancellation near d = 0
+            kl = w * (em - d);
+            g -= a.kl_coef * em;
+        }
+        k = w * g * a.inv_temp * a.grad_scale;
     }
-    out.k = w * g * a.inv_temp * a.grad_scale;
-    return out;
-}
+    __device__ __forceinline__ void store(const RowArgs& a, unsigned row, float logp) const {
+        a.logp[row] = logp;
+        a.terms[row] = pg;
+        a.terms[a.rows + row] = kl;
+        a.terms[2 * (size_t)a.rows + row] = clipped;
+    }
+};
 
-template <typename T, int MODE>
+// dz_j = k ([j == y] - exp(c (z_j - m)) / s): of a vector's elements as if none were the label, and
+// of one element.
+template <typename T>
+struct RowGradient {
+    RowExp<T> e;
+    float neg;  // -k / s
+    __device__ __forceinline__ RowGradient(float inv_temp, float m, float neg_) : e(inv_temp, m), neg(neg_ * e.fix) {}
+    __device__ __forceinline__ uint4 operator()(const uint4& q) const {
+        constexpr int L = kLanes<T>;
+        float p[L];
+        unpack<T>(q, p);
+#pragma unroll
+        for (int l = 0; l < L; l += 2) split(e(p[l], p[l + 1]) * f2(neg, neg), p[l], p[l + 1]);
+        return pack<T>(p);
+    }
+    __device__ __forceinline__ T element(float z, float k) const {
+        float p0, p1;
+        split(e(z, z) * f2(neg, neg), p0, p1);
+        return from_f32<T>(p0 + k);
+    }
+};
+
+// One element as a set: NaN and +inf leave NaN.
+__device__ __forceinline__ MaxSum single(float z) { return MaxSum{z, z == -CUDART_INF_F ? 0.0f : z - z + 1.0f}; }
+
+// Scores, and the loss with its gradient.  One CTA takes a row (a cluster shares it where rows are
+// few, or so long that the rows in flight would not stay in the L2) and goes over it twice: maximum
+// and sum, then the gradient.  The second reading finds the row in the L2, its last vectors still
+// in registers; DRAM sees one read and one write.  What bounds it is the overlap of the two passes of
+// the CTAs of an SM; holding rows in registers or shared memory across a cluster instead was
+// measured slower in five forms (DRAM waits for the cluster's sums, and clusters of eight leave
+// SMs empty).
+template <typename T, bool LOSS>
 __global__ void __launch_bounds__(kRowThreads, 2) row_kernel(const __grid_constant__ RowArgs a) {
     constexpr int L = kLanes<T>;
     __shared__ MaxSum warp_part[kRowThreads / 32];
@@ -373,27 +429,26 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_kernel(const __grid_consta
     const int tid = (int)threadIdx.x, threads = (int)blockDim.x;
     const long long o = row / a.n_inner, i = row % a.n_inner;
     const T* zrow = static_cast<const T*>(a.z) + o * a.z_so + i * a.z_si;
-    T* drow = MODE == kRowScore ? nullptr : static_cast<T*>(a.dz) + o * a.d_so + i * a.d_si;
+    T* drow = LOSS ? static_cast<T*>(a.dz) + o * a.d_so + i * a.d_si : nullptr;
     const bool aligned = ((reinterpret_cast<uintptr_t>(drow) ^ reinterpret_cast<uintptr_t>(zrow)) & 15) == 0;
     const long long y = load_token(a.labels, a.wide_labels != 0, o * a.l_so + i * a.l_si);
-    const float w = MODE == kRowScore ? 1.0f : a.weight.p[o * a.weight.so + i * a.weight.si];
+    const float w = LOSS ? a.weight.p[o * a.weight.so + i * a.weight.si] : 1.0f;
     const RowParts<T> parts(zrow, (int)a.vocab);
     const int per = (parts.vectors + (int)cs - 1) / (int)cs;
-    const int v0 = min((int)rank * per, parts.vectors), v1 = min(v0 + per, parts.vectors);
+    const int v0 = min((int)rank * per, parts.vectors), n = min(per, parts.vectors - v0);
+    const uint4* zv = reinterpret_cast<const uint4*>(zrow + parts.head) + v0;  // the CTA's n vectors
+    T* dv = drow + parts.head + v0 * L;
     const int edge = rank == 0 ? parts.edge(tid) : -1;
     const bool first = rank == 0 && tid == 0;
 
     if (w == 0.0f || y < 0 || y >= a.vocab) {  // the whole cluster leaves here together
         if (first) {
             a.logp[row] = 0.0f;
-            if (MODE == kRowScore) {
-                if (a.lse != nullptr) a.lse[row] = 0.0f;
-            } else {
-                a.terms[row] = a.terms[a.rows + row] = a.terms[2 * (size_t)a.rows + row] = 0.0f;
-            }
+            if (LOSS) a.terms[row] = a.terms[a.rows + row] = a.terms[2 * (size_t)a.rows + row] = 0.0f;
+            else if (a.lse != nullptr) a.lse[row] = 0.0f;
         }
-        if (MODE != kRowScore) {
-            for (int v = v0 + tid; v < v1; v += threads) store_vector(drow + parts.head + v * L, make_uint4(0, 0, 0, 0), aligned);
+        if (LOSS) {
+            for (int v = tid; v < n; v += threads) store_vector(dv + v * L, make_uint4(0, 0, 0, 0), aligned);
             if (edge >= 0) drow[edge] = from_f32<T>(0.0f);
         }
         return;
@@ -401,23 +456,24 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_kernel(const __grid_consta
     if (cs > 1) cluster_arrive();  // this CTA runs: its shared memory may be written (waited for below)
     const float zy = to_f32(zrow[y]);
     const float ze = edge >= 0 ? to_f32(zrow[edge]) : -CUDART_INF_F;
+    RowInputs in;
+    if (LOSS) in.load(a, o, i);
 
-    uint4 q[kRowVectors];
-    const uint4* zv = reinterpret_cast<const uint4*>(zrow + parts.head);
+    MaxSum x = single(ze);
     const int step = threads * kRowVectors;
-    auto load = [&](int b) {
+    uint4 q[kRowVectors];
+    int b = 0;
+    for (; b + step <= n; b += step) {
 #pragma unroll
-        for (int k = 0; k < kRowVectors; ++k) {
-            const int v = b + k * threads + tid;
-            q[k] = v < v1 ? __ldcs(zv + v) : neg_inf_vector<T>();
-        }
-        return vectors_max_sum<T>(q, a.inv_temp);
-    };
-    MaxSum x{ze, ze == -CUDART_INF_F ? 0.0f : ze - ze + 1.0f};  // NaN and +inf leave NaN
-    if (MODE == kRowResident) {
-        x = join(x, load(v0), a.inv_temp);  // the host made sure that one round covers the CTA's part
+        for (int k = 0; k < kRowVectors; ++k) q[k] = LOSS ? zv[b + k * threads + tid] : __ldcs(zv + b + k * threads + tid);
+        x = add_vectors<T>(x, q, a.inv_temp);
+    }
+    if (b < n) {
+#pragma unroll
+        for (int k = 0; k < kRowVectors; ++k) q[k] = b + k * threads + tid < n ? __ldcs(zv + b + k * threads + tid) : neg_inf_vector<T>();
+        x = add_vectors<T>(x, q, a.inv_temp);
     } else {
-        for (int b = v0; b < v1; b += step) x = join(x, load(b), a.inv_temp);
+        b -= step;  // the batch that q holds
     }
     x = warp_join(x, a.inv_temp);
     const int lane = tid & 31, warps = threads >> 5;
@@ -434,65 +490,45 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_kernel(const __grid_consta
             cluster_store(at, x.m);
             cluster_store(at + 4, x.s);
         }
-        // also orders every CTA's reads of the row ahead of every CTA's writes, for dz == z
+        // also orders every CTA's reads of z[y] ahead of every CTA's writes, for dz == z
         cluster_sync();
         x = lane < (int)cs ? cta_part[lane] : MaxSum{-CUDART_INF_F, 0.0f};
         x = warp_join(x, a.inv_temp);
-    } else if (MODE != kRowScore) {
+    } else if (LOSS) {
         __syncthreads();  // every thread has read z[y] before one of them may write there
     }
     const float log_s = logf(x.s);
     const float logp = (zy - x.m) * a.inv_temp - log_s;
-    if (MODE == kRowScore) {
+    if (!LOSS) {
         if (first) {
             a.logp[row] = logp;
             if (a.lse != nullptr) a.lse[row] = x.m * a.inv_temp + log_s;
         }
         return;
     }
-    const RowLoss loss = row_loss(a, logp, w, o, i);
-    if (first) {
-        a.logp[row] = logp;
-        a.terms[row] = loss.pg;
-        a.terms[a.rows + row] = loss.kl;
-        a.terms[2 * (size_t)a.rows + row] = loss.clipped;
-    }
-    // The packed vectors alone live across the join: without this the compiler keeps the unpacked
-    // ones as well, and spills.
-#pragma unroll
-    for (int k = 0; k < kRowVectors; ++k) asm volatile("" : "+r"(q[k].x), "+r"(q[k].y), "+r"(q[k].z), "+r"(q[k].w));
-    // dz_j = k ([j == y] - exp(c (z_j - m)) / s)
-    const RowExp<T> e(a.inv_temp, x.m);
-    const float neg = -loss.k / x.s;
-    const int in_body = (int)y - parts.head;  // place of the label among the vectors' elements
-    const int vy = in_body >= 0 ? in_body / L : -1, ly = in_body % L;
-    auto store = [&](int b) {
+    const RowLoss loss(a, in, logp, w);
+    if (first) loss.store(a, row, logp);
+    const RowGradient<T> grad(a.inv_temp, x.m, -loss.k / x.s);
+    if (aligned) {
+        uint4* to = reinterpret_cast<uint4*>(dv);
 #pragma unroll
         for (int k = 0; k < kRowVectors; ++k) {
             const int v = b + k * threads + tid;
-            if (v >= v1) continue;
-            if (MODE == kRowStream) q[k] = __ldcs(zv + v);
-            float p[L];
-            unpack<T>(q[k], p);
-#pragma unroll
-            for (int l = 0; l < L; l += 2) split(e(p[l], p[l + 1]) * f2(neg, neg), p[l], p[l + 1]);
-            if (v == vy) {
-#pragma unroll
-                for (int l = 0; l < L; ++l) p[l] += l == ly ? loss.k : 0.0f;
-            }
-            store_vector(drow + parts.head + v * L, pack<T>(p), aligned);
+            if (v >= 0 && v < n) __stcs(to + v, grad(q[k]));
         }
-    };
-    if (MODE == kRowResident) {
-        store(v0);
+        for (b -= step; b >= 0; b -= step) {
+#pragma unroll
+            for (int k = 0; k < kRowVectors; ++k) q[k] = __ldcs(zv + b + k * threads + tid);
+#pragma unroll
+            for (int k = 0; k < kRowVectors; ++k) __stcs(to + b + k * threads + tid, grad(q[k]));
+        }
     } else {
-        for (int b = v0; b < v1; b += step) store(b);
+        for (int v = tid; v < n; v += threads) store_elements(dv + v * L, grad(zv[v]));
     }
-    if (edge >= 0) {
-        float p0, p1;
-        split(e(ze, ze) * f2(neg, neg), p0, p1);
-        drow[edge] = from_f32<T>(p0 + (edge == (int)y ? loss.k : 0.0f));
-    }
+    // the label's element again, by the thread that has written its vector
+    const int at = (int)y - parts.head - v0 * L;
+    if (at >= 0 && at / L < n && at / L % threads == tid) dv[at] = grad.element(zy, loss.k);
+    if (edge >= 0) drow[edge] = grad.element(ze, edge == (int)y ? loss.k : 0.0f);
 }
 
 // Sums the rows' terms in a fixed order, in 64 bits: one CTA.
