@@ -328,27 +328,40 @@ int check_policy(const odsgd_policy_desc* d, bool loss) {
     return ODSGD_OK;
 }
 
+// How a call cuts its rows: CTAs of a row, threads of a CTA, and which build of the kernel.
 struct RowShape {
     int cluster, threads;
+    bool wide;  // loss: 512-thread CTAs, two an SM, instead of 256-thread ones, five an SM
 };
+
+constexpr int kScoreThreads = 128, kScoreCtas = 12;
+constexpr int kNarrowThreads = 256, kNarrowCtas = 5;
+constexpr int kWideThreads = 512, kWideCtas = 2;
+// Rows in flight are read again from the L2 (126 MB) while their gradients pass through it.
+constexpr int64_t kRowsInFlightBytes = 80 << 20;
 
 RowShape row_shape(int64_t rows, int64_t vocab, int elem, bool loss, int sms) {
     RowShape s;
     const int64_t vectors = std::max<int64_t>(1, vocab / (16 / elem));
+    s.wide = loss && vectors * 16 * kNarrowCtas * sms > kRowsInFlightBytes;
     s.cluster = 1;
+    if (loss)
+        while (s.cluster < kRowCluster && vectors * 16 * kWideCtas * sms > kRowsInFlightBytes * s.cluster) s.cluster *= 2;
     while (s.cluster < kRowCluster && rows * s.cluster < sms && vectors > (int64_t)s.cluster * 256) s.cluster *= 2;
     const int64_t part = ceil_div(vectors, s.cluster);
     // a batch of vectors a thread when there are rows enough to fill the GPU, one vector when there are not
     const int64_t each = rows * s.cluster >= 2 * (int64_t)sms ? kRowVectors : 1;
-    s.threads = (int)std::min<int64_t>(kRowThreads, std::max<int64_t>(32, ceil_div(ceil_div(part, each), 32) * 32));
+    const int64_t most = !loss ? kScoreThreads : s.wide ? kWideThreads : kNarrowThreads;
+    s.threads = (int)std::min(most, std::max<int64_t>(32, ceil_div(ceil_div(part, each), 32) * 32));
     return s;
 }
 
 template <typename T>
 int launch_rows_t(const RowArgs& a, const RowShape& s, bool loss, void* stream) {
     const dim3 grid(a.rows * (unsigned)s.cluster), block((unsigned)s.threads);
-    return loss ? launch("policy loss kernel", row_kernel<T, true>, grid, block, 0, s.cluster, stream, a)
-                : launch("score kernel", row_kernel<T, false>, grid, block, 0, s.cluster, stream, a);
+    if (!loss) return launch("score kernel", row_kernel<T, false, kScoreThreads, kScoreCtas>, grid, block, 0, s.cluster, stream, a);
+    return s.wide ? launch("policy loss kernel", row_kernel<T, true, kWideThreads, kWideCtas>, grid, block, 0, s.cluster, stream, a)
+                  : launch("policy loss kernel", row_kernel<T, true, kNarrowThreads, kNarrowCtas>, grid, block, 0, s.cluster, stream, a);
 }
 
 int launch_rows(const odsgd_policy_desc* d, bool loss, float* terms, void* stream) {

@@ -418,10 +418,10 @@ __device__ __forceinline__ MaxSum single(float z) { return MaxSum{z, z == -CUDAR
 // the CTAs of an SM; holding rows in registers or shared memory across a cluster instead was
 // measured slower in five forms (DRAM waits for the cluster's sums, and clusters of eight leave
 // SMs empty).
-template <typename T, bool LOSS>
-__global__ void __launch_bounds__(kRowThreads, 2) row_kernel(const __grid_constant__ RowArgs a) {
+template <typename T, bool LOSS, int THREADS, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) row_kernel(const __grid_constant__ RowArgs a) {
     constexpr int L = kLanes<T>;
-    __shared__ MaxSum warp_part[kRowThreads / 32];
+    __shared__ MaxSum warp_part[THREADS / 32];
     __shared__ MaxSum cta_part[kRowCluster];
     dependent_launch_prologue();
     const unsigned cs = (unsigned)a.cluster;
@@ -456,8 +456,6 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_kernel(const __grid_consta
     if (cs > 1) cluster_arrive();  // this CTA runs: its shared memory may be written (waited for below)
     const float zy = to_f32(zrow[y]);
     const float ze = edge >= 0 ? to_f32(zrow[edge]) : -CUDART_INF_F;
-    RowInputs in;
-    if (LOSS) in.load(a, o, i);
 
     MaxSum x = single(ze);
     const int step = threads * kRowVectors;
@@ -475,6 +473,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) row_kernel(const __grid_consta
     } else {
         b -= step;  // the batch that q holds
     }
+    RowInputs in;
+    if (LOSS) in.load(a, o, i);
     x = warp_join(x, a.inv_temp);
     const int lane = tid & 31, warps = threads >> 5;
     if (warps > 1) {
