@@ -241,7 +241,7 @@ GradShape grad_shape(const odsgd_embed_desc* d) {
     // positions of a block: enough CTAs to fill the machine several times over before blocks grow
     const int64_t slabs = ceil_div(d->dim, (int64_t)kSumThreads * (16 / size_of(d->act_type)));
     s.block = 16;
-    while (s.block < (unsigned)kSumMaxBlock && (int64_t)(s.n / s.block) * slabs > 148 * 16) s.block *= 2;
+    while (2 * s.block <= (unsigned)kSumMaxBlock && (int64_t)(s.n / s.block) * slabs > 148 * 16) s.block *= 2;
     s.blocks = (unsigned)ceil_div(s.n, s.block);
     s.pitch = ceil_div(d->dim, 4) * 4;
     size_t at = 0;
@@ -622,6 +622,7 @@ int odsgd_embed_grad(const odsgd_embed_desc* d, void* workspace, size_t workspac
         a.n = s.n;
         a.n_inner = (unsigned)std::max<int64_t>(1, d->n_inner);
         a.wide_tokens = d->token_type == ODSGD_I64;
+        a.flat = d->n_outer == 1 || a.t_so == d->n_inner * a.t_si;
         a.accumulate = d->accumulate != 0;
         a.scale = d->scale;
         for (int i = 0; i < 2; ++i) {
@@ -647,7 +648,7 @@ int odsgd_embed_grad(const odsgd_embed_desc* d, void* workspace, size_t workspac
             default: rc = launch_sum<f16>(a, s, vec, stream); break;
         }
         if (rc != ODSGD_OK || s.blocks < 2) return rc;
-        const dim3 grid(std::min<unsigned>(s.blocks - 1, kJoinGrid), (unsigned)ceil_div(a.dim, 32));
+        const dim3 grid(std::min<unsigned>(s.blocks - 1, kJoinGrid), (unsigned)ceil_div(a.dim, kJoinColumns));
         return launch("embedding gradient join kernel", join_kernel, grid, dim3(32 * kJoinWarps), 0, 1, stream, a);
     });
 }

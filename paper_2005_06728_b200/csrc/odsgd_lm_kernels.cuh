@@ -680,11 +680,12 @@ struct EmbedGradArgs {
     long long t_so, t_si, a_so, a_si, stride, vocab, dim, padding;
     unsigned n, n_inner;
     int wide_tokens, accumulate;
+    int flat;  // token t lies at t * t_si
     float scale;
     // workspace
     unsigned* key[2];
     unsigned* pos[2];
-    unsigned* counts;  // [0] valid tokens, [1] spanning runs
+    unsigned* counts;  // [0] spanning runs
     SpanRun* runs;
     float* head;  // [blocks][pitch]: part of the run that began in an earlier block
     float* tail;  // [blocks][pitch]: first part of a run that goes on in the next block
@@ -693,10 +694,18 @@ struct EmbedGradArgs {
     int passes, bits;
 };
 
-__device__ __forceinline__ unsigned token_key(const EmbedGradArgs& a, unsigned t) {
-    const long long o = t / a.n_inner, i = t % a.n_inner;
-    const long long x = load_token(a.tokens, a.wide_tokens != 0, o * a.t_so + i * a.t_si);
-    return x >= 0 && x < a.vocab && x != a.padding ? (unsigned)x : (unsigned)a.vocab;
+// Tokens t, t + step, ... as sort keys; those that do not count, and places beyond n, as `vocab`.
+constexpr int kKeyBatch = 4;
+__device__ __forceinline__ void token_keys(const EmbedGradArgs& a, unsigned t, unsigned step, unsigned (&key)[kKeyBatch]) {
+    long long x[kKeyBatch];
+#pragma unroll
+    for (int k = 0; k < kKeyBatch; ++k) {
+        const unsigned j = t + k * step;
+        x[k] = -1;
+        if (j < a.n) x[k] = load_token(a.tokens, a.wide_tokens != 0, a.flat ? j * a.t_si : j / a.n_inner * a.t_so + j % a.n_inner * a.t_si);
+    }
+#pragma unroll
+    for (int k = 0; k < kKeyBatch; ++k) key[k] = x[k] >= 0 && x[k] < a.vocab && x[k] != a.padding ? (unsigned)x[k] : (unsigned)a.vocab;
 }
 
 __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* smem) {
@@ -710,10 +719,7 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
     unsigned per = (a.n + kSortCluster * kSortWarps - 1) / (kSortCluster * kSortWarps);
     per = (per + 31) / 32 * 32;
     const unsigned lo = min(a.n, (rank * kSortWarps + warp) * per), hi = min(a.n, lo + per);
-    if (rank == 0 && tid == 0) {
-        a.counts[0] = a.n;
-        a.counts[1] = 0;
-    }
+    if (rank == 0 && tid == 0) a.counts[0] = 0;
     for (int pass = 0; pass < a.passes; ++pass) {
         const unsigned* kin = a.key[pass & 1];
         const unsigned* pin = a.pos[pass & 1];
@@ -723,9 +729,20 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
         for (unsigned d = tid; d < kSortWarps * radix; d += kSortThreads) cnt[d] = 0;
         __syncthreads();
         unsigned* mine = cnt + warp * radix;
-        for (unsigned t = lo + lane; t < hi; t += 32) {
-            const unsigned key = pass == 0 ? token_key(a, t) : __ldcg(kin + t);
-            atomicAdd(mine + ((key >> shift) & (radix - 1)), 1u);
+        unsigned key[kKeyBatch], pos[kKeyBatch];
+        const auto load = [&](unsigned t) {
+            if (pass == 0) {
+                token_keys(a, t, 32, key);
+            } else {
+#pragma unroll
+                for (int k = 0; k < kKeyBatch; ++k) key[k] = t + 32 * k < hi ? __ldcg(kin + t + 32 * k) : 0;
+            }
+        };
+        for (unsigned t = lo + lane; t < hi; t += 32 * kKeyBatch) {
+            load(t);
+#pragma unroll
+            for (int k = 0; k < kKeyBatch; ++k)
+                if (t + 32 * k < hi) atomicAdd(mine + ((key[k] >> shift) & (radix - 1)), 1u);
         }
         __syncthreads();
         if (tid < radix) {  // exclusive scan over the warps, digit by digit
@@ -761,37 +778,43 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
             base[tid] = below + scan - all + before;
         }
         __syncthreads();
-        for (unsigned t0 = lo; t0 < hi; t0 += 32) {
-            const unsigned t = t0 + lane;
-            const bool in = t < hi;
-            const unsigned act = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const unsigned key = pass == 0 ? token_key(a, t) : __ldcg(kin + t);
-                const unsigned d = (key >> shift) & (radix - 1);
-                const unsigned peers = __match_any_sync(act, d);
-                const unsigned at = base[d] + mine[d] + __popc(peers & ((1u << lane) - 1));
-                __syncwarp(act);
-                if ((peers >> lane) == 1) mine[d] += __popc(peers);  // the last of the equal lanes
-                kout[at] = key;
-                pout[at] = pass == 0 ? t : __ldcg(pin + t);
+        for (unsigned t0 = lo; t0 < hi; t0 += 32 * kKeyBatch) {
+            load(t0 + lane);
+#pragma unroll
+            for (int k = 0; k < kKeyBatch; ++k) {
+                const unsigned t = t0 + 32 * k + lane;
+                pos[k] = pass == 0 || t >= hi ? t : __ldcg(pin + t);
             }
-            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < kKeyBatch; ++k) {
+                const bool in = t0 + 32 * k + lane < hi;
+                const unsigned act = __ballot_sync(0xffffffffu, in);
+                if (in) {
+                    const unsigned d = (key[k] >> shift) & (radix - 1);
+                    const unsigned peers = __match_any_sync(act, d);
+                    const unsigned at = base[d] + mine[d] + __popc(peers & ((1u << lane) - 1));
+                    __syncwarp(act);
+                    if ((peers >> lane) == 1) mine[d] += __popc(peers);  // the last of the equal lanes
+                    kout[at] = key[k];
+                    pout[at] = pos[k];
+                }
+                __syncwarp();
+            }
         }
         cluster_sync();  // the pass is complete, in memory, for all CTAs of the cluster
     }
     const unsigned* key = a.key[a.passes & 1];
-    for (unsigned t = rank * kSortThreads + tid; t < a.n; t += kSortCluster * kSortThreads) {
+    for (unsigned t = (rank * kSortThreads + tid + 1) * a.block; t < a.n; t += kSortCluster * kSortThreads * a.block) {
         const unsigned k = __ldcg(key + t);
-        if (k == (unsigned)a.vocab && (t == 0 || __ldcg(key + t - 1) != k)) a.counts[0] = t;
         // the first boundary inside a run lists it, with the block its last position lies in
-        if (t > 0 && t % a.block == 0 && k != (unsigned)a.vocab && __ldcg(key + t - 1) == k &&
+        if (k != (unsigned)a.vocab && __ldcg(key + t - 1) == k &&
             (t == a.block || __ldcg(key + t - a.block - 1) != k)) {
             unsigned last = t / a.block, up = (a.n - 1) / a.block;  // key[last * block] == k
             while (last < up) {
                 const unsigned mid = last + (up - last + 1) / 2;
                 if (__ldcg(key + mid * (size_t)a.block) == k) last = mid; else up = mid - 1;
             }
-            a.runs[atomicAdd(a.counts + 1, 1u)] = SpanRun{k, t / a.block - 1, last};
+            a.runs[atomicAdd(a.counts, 1u)] = SpanRun{k, t / a.block - 1, last};
         }
     }
 }
@@ -801,9 +824,14 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, unsigned* bits
     const unsigned rows = (unsigned)(r1 - r0);
     for (unsigned i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) bits[i] = 0;
     __syncthreads();
-    for (unsigned t = threadIdx.x; t < a.n; t += blockDim.x) {
-        const unsigned k = token_key(a, t);
-        if (k >= r0 && k < r1) atomicOr(bits + ((unsigned)(k - r0) >> 5), 1u << ((unsigned)(k - r0) & 31));
+    for (unsigned t = threadIdx.x; t < a.n; t += kKeyBatch * blockDim.x) {
+        unsigned key[kKeyBatch];
+        token_keys(a, t, blockDim.x, key);
+#pragma unroll
+        for (int k = 0; k < kKeyBatch; ++k) {
+            const unsigned r = key[k] - (unsigned)r0;
+            if (r < rows) atomicOr(bits + (r >> 5), 1u << (r & 31));  // (`vocab` lies behind r1)
+        }
     }
     __syncthreads();
     const bool vec = (reinterpret_cast<uintptr_t>(a.table) & 15) == 0 && a.stride % 4 == 0;
@@ -833,50 +861,67 @@ __global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kSortCluster, 1
 }
 
 constexpr int kSumThreads = 128;
-constexpr int kSumBatch = 8;       // rows in flight
-constexpr int kSumMaxBlock = 128;  // most positions of a block
+constexpr int kSumCtas = 8;
+constexpr int kSumBatch = 8;       // rows a thread has in flight
+constexpr int kSumMaxBlock = 126;  // most positions of a block
+
+// A vector of T, or one T.
+template <typename T, bool VEC>
+struct Piece;
+template <typename T>
+struct Piece<T, true> {
+    static constexpr int W = kLanes<T>;
+    uint4 q;
+    __device__ __forceinline__ void load(const T* p) { q = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void add_to(float (&acc)[W]) const {
+        float x[W];
+        unpack<T>(q, x);
+#pragma unroll
+        for (int l = 0; l < W; ++l) acc[l] += x[l];
+    }
+};
+template <typename T>
+struct Piece<T, false> {
+    static constexpr int W = 1;
+    T x;
+    __device__ __forceinline__ void load(const T* p) { x = *p; }
+    __device__ __forceinline__ void add_to(float (&acc)[1]) const { acc[0] += to_f32(x); }
+};
 
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant__ EmbedGradArgs a) {
-    constexpr int W = VEC ? kLanes<T> : 1;
-    __shared__ unsigned key[kSumMaxBlock + 2];
-    __shared__ unsigned pos[kSumMaxBlock];
+__global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid_constant__ EmbedGradArgs a) {
+    constexpr int W = Piece<T, VEC>::W;
+    __shared__ unsigned key[kSumMaxBlock + 2];   // of the positions, and one on either side
+    __shared__ const T* row[kSumMaxBlock];
     dependent_launch_prologue();
-    const unsigned valid = a.counts[0];
-    const unsigned i0 = blockIdx.x * a.block;
-    if (i0 >= valid) return;
-    const unsigned n = min(a.block, valid - i0);
-    const unsigned* skey = a.key[a.passes & 1];
-    const unsigned* spos = a.pos[a.passes & 1];
+    const unsigned i0 = blockIdx.x * a.block, n = min(a.block, a.n - i0);
     const unsigned none = (unsigned)a.vocab;
     for (unsigned i = threadIdx.x; i < n + 2; i += blockDim.x) {
-        const long long t = (long long)i0 + i - 1;
-        key[i] = t >= 0 && t < valid ? skey[t] : none;
-        if (i < n) pos[i] = spos[i0 + i];
+        const unsigned t = i0 + i - 1;  // wraps to a large number before the first
+        key[i] = t < a.n ? a.key[a.passes & 1][t] : none;
+        if (i >= 1 && i <= n) {
+            const unsigned p = a.pos[a.passes & 1][t];
+            row[i - 1] = static_cast<const T*>(a.act) + p / a.n_inner * a.a_so + p % a.n_inner * a.a_si;
+        }
     }
     __syncthreads();
     const long long col = ((long long)blockIdx.y * blockDim.x + threadIdx.x) * W;
     if (col >= a.dim) return;
-    const T* src = static_cast<const T*>(a.act) + col;
     float acc[W];
 #pragma unroll
     for (int l = 0; l < W; ++l) acc[l] = 0.0f;
     bool crossed = key[0] == key[1];  // the run began in an earlier block
-    for (unsigned b = 0; b < n; b += kSumBatch) {
-        float x[kSumBatch][W];
+    for (unsigned b = 0; b < n && key[b + 1] != none; b += kSumBatch) {
+        Piece<T, VEC> x[kSumBatch];
+#pragma unroll
+        for (int k = 0; k < kSumBatch; ++k)
+            if (b + k < n && key[b + k + 1] != none) x[k].load(row[b + k] + col);
 #pragma unroll
         for (int k = 0; k < kSumBatch; ++k) {
             if (b + k >= n) continue;
-            const unsigned p = pos[b + k];
-            const T* row = src + (p / a.n_inner) * a.a_so + (p % a.n_inner) * a.a_si;
-            if constexpr (VEC) unpack<T>(__ldg(reinterpret_cast<const uint4*>(row)), x[k]); else x[k][0] = to_f32(*row);
-        }
-#pragma unroll
-        for (int k = 0; k < kSumBatch; ++k) {
-            if (b + k >= n) continue;
-#pragma unroll
-            for (int l = 0; l < W; ++l) acc[l] += x[k][l];
             const unsigned here = key[b + k + 1], next = key[b + k + 2];
+            if (here == none) continue;
+            x[k].add_to(acc);
             const bool last = b + k + 1 == n;
             if (next == here && !last) continue;
             // the run ends, or the block does
@@ -908,32 +953,43 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const __grid_constant_
     }
 }
 
-// Eight warps share a run's parts, a column a lane; the warps' sums are added in warp order.
+// A CTA takes a run and a slab of columns; eight warps share its parts, and the warps' sums are
+// added in warp order.
 constexpr int kJoinWarps = 8;
-constexpr int kJoinGrid = 64;
+constexpr int kJoinGrid = 148;
+constexpr int kJoinColumns = 128;  // four a lane
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_constant__ EmbedGradArgs a) {
-    __shared__ float part[kJoinWarps][32];
+    __shared__ float4 part[kJoinWarps][32];
     dependent_launch_prologue();
-    const unsigned runs = a.counts[1];
+    const unsigned runs = a.counts[0];
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long col = (long long)blockIdx.y * 32 + lane;
+    const long long col = (long long)blockIdx.y * kJoinColumns + 4 * lane;  // the parts' pitch is a multiple of four
     for (unsigned r = blockIdx.x; r < runs; r += gridDim.x) {
         const SpanRun run = a.runs[r];
-        float s = 0.0f;
+        float4 s = make_float4(0, 0, 0, 0);
         if (col < a.dim) {
-#pragma unroll 8
-            for (unsigned b = run.first + warp; b <= run.last; b += kJoinWarps)
-                s += (b == run.first ? a.tail : a.head)[b * a.pitch + col];
+#pragma unroll 4
+            for (unsigned b = run.first + warp; b <= run.last; b += kJoinWarps) {
+                const float4 x = *reinterpret_cast<const float4*>((b == run.first ? a.tail : a.head) + b * a.pitch + col);
+                s.x += x.x;
+                s.y += x.y;
+                s.z += x.z;
+                s.w += x.w;
+            }
         }
         part[warp][lane] = s;
         __syncthreads();
-        if (warp == 0 && col < a.dim) {
-            s = part[0][lane];
+        if (warp < 4) {  // a column a thread
+            const long long c = (long long)blockIdx.y * kJoinColumns + threadIdx.x;
+            const float* p = reinterpret_cast<const float*>(part);
+            float t = p[threadIdx.x];
 #pragma unroll
-            for (int v = 1; v < kJoinWarps; ++v) s += part[v][lane];
-            float* dst = a.table + run.token * a.stride + col;
-            s *= a.scale;
-            *dst = a.accumulate ? *dst + s : s;
+            for (int v = 1; v < kJoinWarps; ++v) t += p[v * kJoinColumns + threadIdx.x];
+            t *= a.scale;
+            if (c < a.dim) {
+                float* dst = a.table + run.token * a.stride + c;
+                *dst = a.accumulate ? *dst + t : t;
+            }
         }
         __syncthreads();
     }
