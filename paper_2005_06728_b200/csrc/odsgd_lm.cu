@@ -637,7 +637,8 @@ int odsgd_embed_grad(const odsgd_embed_desc* d, void* workspace, size_t workspac
         a.block = s.block;
         a.passes = s.passes;
         a.bits = s.bits;
-        const unsigned clusters = 1 + (a.accumulate ? 0 : kFillClusters);
+        const unsigned fill = (unsigned)std::min<int64_t>(kFillClusters, ceil_div(a.vocab * a.dim * 4, kFillBytes));
+        const unsigned clusters = 1 + (a.accumulate ? 0 : fill);
         rc = launch("token sort kernel", sort_kernel, dim3(clusters * kSortCluster), dim3(kSortThreads), kSortSmem, 1, stream, a);
         if (rc != ODSGD_OK || s.n == 0) return rc;
         const bool vec = aligned16(a.table) && a.stride % 4 == 0 &&

@@ -666,7 +666,8 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortBits = 9;
 constexpr int kSortRadix = 1 << kSortBits;
 constexpr int kSortSmem = (kSortWarps * kSortRadix + 2 * kSortRadix + kSortWarps) * 4;
-constexpr int kFillClusters = 17;   // with the sorting one, 144 CTAs: one for each of 148 SMs
+constexpr int kFillClusters = 70;   // most clusters that write zeros, ...
+constexpr int kFillBytes = 1 << 20;  // ... each at least so many of the table
 constexpr int kFillRows = 1 << 17;  // rows a CTA marks at a time: 16 KB of bits
 
 struct SpanRun {
@@ -708,6 +709,23 @@ __device__ __forceinline__ void token_keys(const EmbedGradArgs& a, unsigned t, u
     for (int k = 0; k < kKeyBatch; ++k) key[k] = x[k] >= 0 && x[k] < a.vocab && x[k] != a.padding ? (unsigned)x[k] : (unsigned)a.vocab;
 }
 
+// Of the sorted tokens, those whose run crosses a block boundary: the first boundary inside the run
+// lists it, with the block its last position lies in.
+__device__ __forceinline__ void list_runs(const EmbedGradArgs& a, unsigned thread, unsigned threads) {
+    const unsigned* key = a.key[a.passes & 1];
+    for (unsigned t = (thread + 1) * a.block; t < a.n; t += threads * a.block) {
+        const unsigned k = __ldcg(key + t);
+        if (k != (unsigned)a.vocab && __ldcg(key + t - 1) == k && (t == a.block || __ldcg(key + t - a.block - 1) != k)) {
+            unsigned last = t / a.block, up = (a.n - 1) / a.block;  // key[last * block] == k
+            while (last < up) {
+                const unsigned mid = last + (up - last + 1) / 2;
+                if (__ldcg(key + mid * (size_t)a.block) == k) last = mid; else up = mid - 1;
+            }
+            a.runs[atomicAdd(a.counts, 1u)] = SpanRun{k, t / a.block - 1, last};
+        }
+    }
+}
+
 __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* smem) {
     unsigned* cnt = smem;                           // [warps][radix]
     unsigned* tot = cnt + kSortWarps * kSortRadix;  // [radix], read by the other CTAs
@@ -747,10 +765,15 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
         __syncthreads();
         if (tid < radix) {  // exclusive scan over the warps, digit by digit
             unsigned run = 0;
-            for (int v = 0; v < kSortWarps; ++v) {
-                const unsigned c = cnt[v * radix + tid];
-                cnt[v * radix + tid] = run;
-                run += c;
+            for (int v0 = 0; v0 < kSortWarps; v0 += 8) {
+                unsigned c[8];
+#pragma unroll
+                for (int v = 0; v < 8; ++v) c[v] = cnt[(v0 + v) * radix + tid];
+#pragma unroll
+                for (int v = 0; v < 8; ++v) {
+                    cnt[(v0 + v) * radix + tid] = run;
+                    run += c[v];
+                }
             }
             tot[tid] = run;
         }
@@ -803,20 +826,40 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
         }
         cluster_sync();  // the pass is complete, in memory, for all CTAs of the cluster
     }
-    const unsigned* key = a.key[a.passes & 1];
-    for (unsigned t = (rank * kSortThreads + tid + 1) * a.block; t < a.n; t += kSortCluster * kSortThreads * a.block) {
-        const unsigned k = __ldcg(key + t);
-        // the first boundary inside a run lists it, with the block its last position lies in
-        if (k != (unsigned)a.vocab && __ldcg(key + t - 1) == k &&
-            (t == a.block || __ldcg(key + t - a.block - 1) != k)) {
-            unsigned last = t / a.block, up = (a.n - 1) / a.block;  // key[last * block] == k
-            while (last < up) {
-                const unsigned mid = last + (up - last + 1) / 2;
-                if (__ldcg(key + mid * (size_t)a.block) == k) last = mid; else up = mid - 1;
+    list_runs(a, rank * kSortThreads + tid, kSortCluster * kSortThreads);
+}
+
+// At most one position a thread: token and position in one number, sorted by a bitonic network, the
+// exchanges inside a warp by shuffles (2 us where the digit passes and their barriers take 10).
+__device__ __forceinline__ void sort_few_tokens(const EmbedGradArgs& a, unsigned long long* smem) {
+    const unsigned tid = threadIdx.x;
+    unsigned key[kKeyBatch];
+    token_keys(a, tid, a.n, key);  // the first of the batch; the others lie beyond n
+    if (tid == 0) a.counts[0] = 0;
+    unsigned long long x = (unsigned long long)key[0] << 32 | tid;
+    for (unsigned size = 2; size <= kSortThreads; size *= 2) {
+        if (size > 32 && size / 2 >= a.n) break;  // what lies beyond n is in its place already
+        const bool up = (tid & size) == 0;
+        for (unsigned d = size / 2; d > 0; d /= 2) {
+            unsigned long long y;
+            if (d >= 32) {
+                __syncthreads();
+                smem[tid] = x;
+                __syncthreads();
+                y = smem[tid ^ d];
+            } else {
+                y = __shfl_xor_sync(0xffffffffu, x, d);
             }
-            a.runs[atomicAdd(a.counts, 1u)] = SpanRun{k, t / a.block - 1, last};
+            const bool lower = (tid & d) == 0;
+            x = (lower == up) == (x < y) ? x : y;
         }
     }
+    if (tid < a.n) {
+        a.key[a.passes & 1][tid] = (unsigned)(x >> 32);
+        a.pos[a.passes & 1][tid] = (unsigned)x;
+    }
+    __syncthreads();
+    list_runs(a, tid, kSortThreads);
 }
 
 // Zeros in the rows of [r0, r1) that no token names.
@@ -848,10 +891,11 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, unsigned* bits
 
 __global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kSortCluster, 1, 1)
     sort_kernel(const __grid_constant__ EmbedGradArgs a) {
-    extern __shared__ unsigned smem[];
+    extern __shared__ __align__(8) unsigned smem[];
     dependent_launch_prologue();
     if (blockIdx.x < kSortCluster) {
-        sort_tokens(a, smem);
+        if (a.n > kSortThreads) sort_tokens(a, smem);
+        else if (blockIdx.x == 0) sort_few_tokens(a, reinterpret_cast<unsigned long long*>(smem));
         return;
     }
     const long long ctas = gridDim.x - kSortCluster, me = blockIdx.x - kSortCluster;
@@ -953,9 +997,9 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
     }
 }
 
-// A CTA takes a run and a slab of columns; eight warps share its parts, and the warps' sums are
+// A CTA takes a run and a slab of columns; four warps share its parts, and the warps' sums are
 // added in warp order.
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 4;
 constexpr int kJoinGrid = 148;
 constexpr int kJoinColumns = 128;  // four a lane
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_constant__ EmbedGradArgs a) {
@@ -979,7 +1023,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_cons
         }
         part[warp][lane] = s;
         __syncthreads();
-        if (warp < 4) {  // a column a thread
+        {  // a column a thread
             const long long c = (long long)blockIdx.y * kJoinColumns + threadIdx.x;
             const float* p = reinterpret_cast<const float*>(part);
             float t = p[threadIdx.x];
