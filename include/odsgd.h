@@ -610,13 +610,14 @@ int odsgd_policy_loss(const odsgd_policy_desc* desc, void* workspace, size_t wor
  *     k[g]    = norm[g] > max_norm ? max_norm / norm[g] : 1
  * and every x becomes k[g] x, in its own place and type (arenas NULL) or in the group's fp32
  * arena at the tensor's offset (elements of the arena that no tensor covers, such as the padding
- * between tensors, are not written).  The sum of squares and the norm are held in 64 bits, so
- * that neither tiny nor huge elements are lost; norms[g] is rounded to 32.  A norm that is NaN
+ * between tensors, are not written).  Neither tiny nor huge elements are lost: the squares of
+ * 16 bytes of elements are added in 32 bits where those hold them and in 64 where not, all
+ * further sums and the norm are held in 64; norms[g] is rounded to 32.  A norm that is NaN
  * clips nothing (it is there for the caller to see); an infinite one makes k = 0.
  *
  * Like a bound gradient table, a set is checked once and used every iteration; its tensors have
- * to stay where they are.  create() allocates one device table (24 bytes a tensor and 12 bytes per
- * few thousand elements) with cudaMalloc and fills it on `stream`: not while that stream is
+ * to stay where they are.  create() allocates one device table (32 bytes per 4096 or
+ * 16384 elements) with cudaMalloc and fills it on `stream`: not while that stream is
  * capturing (ERR_STATE), and calls on other streams have to be ordered behind it.  The table also
  * holds the partial sums of a call, so the calls of one set must not overlap on the GPU.
  *   norms  device, n_groups floats, out; NULL if not wanted (clip only)

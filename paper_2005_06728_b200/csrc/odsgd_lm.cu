@@ -420,11 +420,10 @@ int check_workspace(const void* ws, size_t have, size_t need) {
 struct odsgd_grad_set {
     int device = 0;
     int n_groups = 0;
-    unsigned n_chunks = 0, chunk = 0;
+    unsigned n_chunks = 0;
     void* table = nullptr;
     std::vector<unsigned char> host;  // what the table was filled from
-    const GradEntry* entries = nullptr;
-    const unsigned* chunk_entry = nullptr;
+    const GradChunk* chunks = nullptr;
     double* partial = nullptr;
     GradGroup* groups = nullptr;
     ~odsgd_grad_set() {
@@ -476,34 +475,35 @@ int make_set(odsgd_grad_set* s, const odsgd_grad_tensor* t, size_t n, int n_grou
     }
     std::stable_sort(order.begin(), order.end(), [&](size_t a, size_t b) { return t[a].group < t[b].group; });
     // chunks of 16384 elements; of 4096 where those would leave SMs without work
-    s->chunk = total / 16384 < 148 * 4 ? 4096 : 16384;
-    std::vector<GradEntry> entries;
-    std::vector<unsigned> chunk_entry;
+    const size_t most = total / 16384 < 148 * 4 ? 4096 : 16384;
+    std::vector<GradChunk> chunks;
     std::vector<GradGroup> groups((size_t)n_groups, GradGroup{0, 0, 0, 1.0f});
     for (size_t k : order) {
-        const size_t chunks = (t[k].numel + s->chunk - 1) / s->chunk;
-        if (chunk_entry.size() + chunks >= (size_t)INT32_MAX) return fail(ODSGD_ERR_UNSUPPORTED, "too many elements in one gradient set");
-        GradEntry e = {};
-        e.src = t[k].data;
-        e.dst = arenas ? arenas[t[k].group] + t[k].offset : nullptr;
-        e.numel = t[k].numel;
-        e.first_chunk = (unsigned)chunk_entry.size();
-        const bool vec = aligned16(e.src) && aligned16(e.dst);
-        e.type_group = t[k].type | t[k].group << 8 | (vec ? 1 << 16 : 0);
+        const size_t es = (size_t)size_of(t[k].type);
+        const size_t count = (t[k].numel + most - 1) / most;
+        if (chunks.size() + count >= (size_t)INT32_MAX / 4) return fail(ODSGD_ERR_UNSUPPORTED, "too many elements in one gradient set");
+        float* dst = arenas ? arenas[t[k].group] + t[k].offset : nullptr;
+        const bool vec = aligned16(t[k].data) && aligned16(dst);
         GradGroup& g = groups[(size_t)t[k].group];
-        if (g.n_chunks == 0) g.first_chunk = e.first_chunk;
-        g.n_chunks += (unsigned)chunks;
-        chunk_entry.insert(chunk_entry.end(), chunks, (unsigned)entries.size());
-        entries.push_back(e);
+        if (g.n_chunks == 0) g.first_chunk = (unsigned)chunks.size();
+        g.n_chunks += (unsigned)count;
+        for (size_t at = 0; at < t[k].numel; at += most) {
+            GradChunk c = {};
+            c.src = static_cast<const char*>(t[k].data) + at * es;
+            c.dst = dst ? dst + at : nullptr;
+            c.n = (unsigned)std::min(most, t[k].numel - at);
+            c.type_vec = (unsigned short)(t[k].type | (vec ? 1 << 8 : 0));
+            c.group = (unsigned short)t[k].group;
+            chunks.push_back(c);
+        }
     }
-    s->n_chunks = (unsigned)chunk_entry.size();
+    s->n_chunks = (unsigned)chunks.size();
     s->n_groups = n_groups;
-    const size_t at_groups = entries.size() * sizeof(GradEntry), at_chunks = at_groups + groups.size() * sizeof(GradGroup);
-    const size_t filled = (at_chunks + chunk_entry.size() * 4 + 15) / 16 * 16;
+    const size_t at_groups = chunks.size() * sizeof(GradChunk);
+    const size_t filled = (at_groups + groups.size() * sizeof(GradGroup) + 15) / 16 * 16;
     s->host.resize(filled);
-    if (!entries.empty()) memcpy(s->host.data(), entries.data(), at_groups);
-    memcpy(s->host.data() + at_groups, groups.data(), at_chunks - at_groups);
-    if (!chunk_entry.empty()) memcpy(s->host.data() + at_chunks, chunk_entry.data(), chunk_entry.size() * 4);
+    if (!chunks.empty()) memcpy(s->host.data(), chunks.data(), at_groups);
+    memcpy(s->host.data() + at_groups, groups.data(), groups.size() * sizeof(GradGroup));
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     cudaError_t e = cudaStreamIsCapturing(stream, &cap);
     if (e != cudaSuccess) return cuda_fail("cudaStreamIsCapturing", e);
@@ -516,9 +516,8 @@ int make_set(odsgd_grad_set* s, const odsgd_grad_tensor* t, size_t n, int n_grou
         return cuda_fail("gradient set table allocation", e);
     }
     unsigned char* base = static_cast<unsigned char*>(s->table);
-    s->entries = reinterpret_cast<const GradEntry*>(base);
+    s->chunks = reinterpret_cast<const GradChunk*>(base);
     s->groups = reinterpret_cast<GradGroup*>(base + at_groups);
-    s->chunk_entry = reinterpret_cast<const unsigned*>(base + at_chunks);
     s->partial = reinterpret_cast<double*>(base + filled);
     e = cudaMemcpyAsync(s->table, s->host.data(), filled, cudaMemcpyHostToDevice, stream);
     if (e != cudaSuccess) return cuda_fail("gradient set table upload", e);
@@ -535,13 +534,11 @@ int run_set(odsgd_grad_set* s, bool clip, float max_norm, float* norms, void* st
     if (rc != ODSGD_OK) return rc;
     if (dev != s->device) return fail(ODSGD_ERR_STATE, "the gradient set belongs to another device than the current one");
     GradArgs a = {};
-    a.entries = s->entries;
-    a.chunk_entry = s->chunk_entry;
+    a.chunks = s->chunks;
     a.partial = s->partial;
     a.groups = s->groups;
     a.norms = norms;
     a.n_chunks = s->n_chunks;
-    a.chunk = s->chunk;
     a.n_groups = s->n_groups;
     a.max_norm = max_norm;
     rc = launch("gradient norm kernel", norm_kernel, dim3(std::max(1u, s->n_chunks)), dim3(kClipThreads), 0, 1, stream, a);
