@@ -477,7 +477,7 @@ int make_set(odsgd_grad_set* s, const odsgd_grad_tensor* t, size_t n, int n_grou
     // chunks of 16384 elements; of 4096 where those would leave SMs without work
     const size_t most = total / 16384 < 148 * 4 ? 4096 : 16384;
     std::vector<GradChunk> chunks;
-    std::vector<GradGroup> groups((size_t)n_groups, GradGroup{0, 0, 0, 1.0f});
+    std::vector<GradGroup> groups((size_t)n_groups, GradGroup{0, 0, 1.0f});
     for (size_t k : order) {
         const size_t es = (size_t)size_of(t[k].type);
         const size_t count = (t[k].numel + most - 1) / most;
@@ -541,7 +541,8 @@ int run_set(odsgd_grad_set* s, bool clip, float max_norm, float* norms, void* st
     a.n_chunks = s->n_chunks;
     a.n_groups = s->n_groups;
     a.max_norm = max_norm;
-    rc = launch("gradient norm kernel", norm_kernel, dim3(std::max(1u, s->n_chunks)), dim3(kClipThreads), 0, 1, stream, a);
+    if (s->n_chunks > 0) rc = launch("gradient norm kernel", norm_kernel, dim3(s->n_chunks), dim3(kClipThreads), 0, 1, stream, a);
+    if (rc == ODSGD_OK) rc = launch("gradient norm sum kernel", finish_kernel, dim3((unsigned)s->n_groups), dim3(kFinishThreads), 0, 1, stream, a);
     if (rc != ODSGD_OK || !clip || s->n_chunks == 0) return rc;
     return launch("gradient clip kernel", clip_kernel, dim3(s->n_chunks), dim3(kClipThreads), 0, 1, stream, a);
 }
