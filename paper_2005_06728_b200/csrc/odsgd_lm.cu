@@ -194,21 +194,24 @@ int check_embed(const odsgd_embed_desc* d, bool lookup) {
     return ODSGD_OK;
 }
 
-// Whether all rows of a strided buffer start on 16 bytes.
-bool rows_aligned16(const void* p, int elem, int64_t so, int64_t si, int64_t n_outer, int64_t n_inner) {
-    return aligned16(p) && (n_outer <= 1 || so * elem % 16 == 0) && (n_inner <= 1 || si * elem % 16 == 0);
+// Whether all rows of a strided buffer start on `bytes` bytes (a power of two).
+bool rows_aligned(const void* p, int elem, int64_t so, int64_t si, int64_t n_outer, int64_t n_inner, int bytes = 16) {
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (n_outer <= 1 || so * elem % bytes == 0) && (n_inner <= 1 || si * elem % bytes == 0);
 }
 
 template <typename TT, typename TA>
-int launch_lookup(const LookupArgs& a, bool vec_ok, void* stream) {
-    constexpr int W = kLanes<TT> > kLanes<TA> ? kLanes<TT> : kLanes<TA>;
+int launch_lookup(LookupArgs a, bool vec_ok, void* stream) {
+    constexpr int W = kLanes<TT> < kLanes<TA> ? kLanes<TT> : kLanes<TA>;
     const bool vec = vec_ok && a.dim % W == 0;
     const int64_t cols = vec ? a.dim / W : a.dim;
-    // as many threads along the row as it has vectors, the rest along the rows
+    // as many threads along the row as it has pieces, the rest along the rows
     const int slabs = (int)ceil_div(cols, kLookupThreads);
     const int bx = (int)ceil_div(ceil_div(cols, slabs), 32) * 32;
     const int by = std::max(1, kLookupThreads / bx);
-    const dim3 grid((unsigned)ceil_div(a.rows, (int64_t)by * kLookupRows), (unsigned)slabs);
+    // eight rows a thread where that still gives every SM several CTAs, down to one where it does not
+    a.per = 8;
+    while (a.per > 1 && ceil_div(a.rows, (int64_t)by * a.per) * slabs < 148 * 8) a.per /= 2;
+    const dim3 grid((unsigned)ceil_div(a.rows, (int64_t)by * a.per), (unsigned)slabs);
     const dim3 block((unsigned)bx, (unsigned)by);
     return vec ? launch("lookup kernel", lookup_kernel<TT, TA, true>, grid, block, 0, 1, stream, a)
                : launch("lookup kernel", lookup_kernel<TT, TA, false>, grid, block, 0, 1, stream, a);
@@ -243,7 +246,7 @@ GradShape grad_shape(const odsgd_embed_desc* d) {
     s.block = 16;
     while (2 * s.block <= (unsigned)kSumMaxBlock && (int64_t)(s.n / s.block) * slabs > 148 * 16) s.block *= 2;
     s.blocks = (unsigned)ceil_div(s.n, s.block);
-    s.pitch = ceil_div(d->dim, 4) * 4;
+    s.pitch = ceil_div(d->dim, 8) * 8;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -571,8 +574,8 @@ int odsgd_embed_lookup(const odsgd_embed_desc* d, void* stream) {
         a.n_inner = (unsigned)d->n_inner;
         a.wide_tokens = d->token_type == ODSGD_I64;
         a.scale = d->scale;
-        const bool vec = rows_aligned16(d->table, size_of(d->table_type), 0, a.stride, 1, a.vocab) &&
-                         rows_aligned16(d->act, size_of(d->act_type), a.a_so, a.a_si, d->n_outer, d->n_inner);
+        const bool vec = rows_aligned(d->table, size_of(d->table_type), 0, a.stride, 1, a.vocab) &&
+                         rows_aligned(d->act, size_of(d->act_type), a.a_so, a.a_si, d->n_outer, d->n_inner);
         switch (d->table_type) {
             case ODSGD_F32: return launch_lookup_t<float>(a, d->act_type, vec, stream);
             case ODSGD_BF16: return launch_lookup_t<bf16>(a, d->act_type, vec, stream);
@@ -639,8 +642,9 @@ int odsgd_embed_grad(const odsgd_embed_desc* d, void* workspace, size_t workspac
         const unsigned clusters = 1 + (a.accumulate ? 0 : fill);
         rc = launch("token sort kernel", sort_kernel, dim3(clusters * kSortCluster), dim3(kSortThreads), kSortSmem, 1, stream, a);
         if (rc != ODSGD_OK || s.n == 0) return rc;
+        a.wide = rows_aligned(a.table, 4, 0, a.stride, 1, a.vocab, 32);
         const bool vec = aligned16(a.table) && a.stride % 4 == 0 &&
-                         rows_aligned16(d->act, size_of(d->act_type), a.a_so, a.a_si, d->n_outer, d->n_inner);
+                         rows_aligned(d->act, size_of(d->act_type), a.a_so, a.a_si, d->n_outer, d->n_inner);
         switch (d->act_type) {
             case ODSGD_F32: rc = launch_sum<float>(a, s, vec, stream); break;
             case ODSGD_BF16: rc = launch_sum<bf16>(a, s, vec, stream); break;

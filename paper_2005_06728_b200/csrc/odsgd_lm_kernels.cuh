@@ -103,6 +103,13 @@ __device__ __forceinline__ uint4 pack<f16>(const float (&x)[8]) {
     return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
+// Eight floats in one store, 32-byte aligned (two of 16 bytes leave every sector half written at a time).
+__device__ __forceinline__ void store_eight(float* p, const float* x) {
+    asm volatile("st.global.cs.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]),
+                 "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
+}
+__device__ __forceinline__ bool aligned32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
+
 // Two floats in one register pair, added and multiplied by one instruction each.
 struct F2 {
     unsigned long long v;
@@ -585,65 +592,78 @@ struct LookupArgs {
     long long t_so, t_si, a_so, a_si, stride, vocab, dim;
     unsigned rows, n_inner;
     int wide_tokens;
+    int per;  // rows of a thread
     float scale;
 };
-constexpr int kLookupRows = 4;  // rows a thread has in flight
 constexpr int kLookupThreads = 256;
+constexpr int kLookupRows = 64;  // most rows of a CTA
 
-// VEC: a thread takes as many columns as 16 bytes of the wider type hold... of the activation's
-// type; otherwise one column.  blockDim = (columns, rows).
+// One column of T or, with VEC, as many as 16 bytes of the wider type hold: that side moves 16 bytes
+// a thread, the other 8 or 16, and both without gaps between the threads.
+template <typename T, int W>
+__device__ __forceinline__ void load_columns(const T* p, float (&x)[W]) {
+    if constexpr (W == 1) {
+        x[0] = to_f32(*p);
+    } else if constexpr (W == kLanes<T>) {
+        unpack<T>(__ldg(reinterpret_cast<const uint4*>(p)), x);
+    } else {
+        float y[8];
+        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
+        unpack<T>(make_uint4(q.x, q.y, 0, 0), y);
+#pragma unroll
+        for (int l = 0; l < W; ++l) x[l] = y[l];
+    }
+}
+template <typename T, int W>
+__device__ __forceinline__ void store_columns(T* p, const float (&x)[W]) {
+    if constexpr (W == 1) {
+        *p = from_f32<T>(x[0]);
+    } else if constexpr (W == kLanes<T>) {
+        *reinterpret_cast<uint4*>(p) = pack<T>(x);
+    } else {
+        const float y[8] = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+        const uint4 q = pack<T>(y);
+        *reinterpret_cast<uint2*>(p) = make_uint2(q.x, q.y);
+    }
+}
+
+// blockDim = (columns, rows); the CTA's rows, a.per for each of its thread rows, are looked up once, by as many
+// threads.  Four rows a thread are in flight.
 template <typename TT, typename TA, bool VEC>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_constant__ LookupArgs a) {
-    constexpr int W = VEC ? (kLanes<TT> > kLanes<TA> ? kLanes<TT> : kLanes<TA>) : 1;
+    constexpr int W = VEC ? (kLanes<TT> < kLanes<TA> ? kLanes<TT> : kLanes<TA>) : 1;
+    constexpr int B = 4;
+    __shared__ const TT* from[kLookupRows];
+    __shared__ TA* to[kLookupRows];
     dependent_launch_prologue();
+    const unsigned rows = blockDim.y * a.per, r0 = blockIdx.x * rows, n = min(rows, a.rows - r0);
+    for (unsigned r = threadIdx.y * blockDim.x + threadIdx.x; r < n; r += blockDim.x * blockDim.y) {
+        const unsigned o = (r0 + r) / a.n_inner, i = (r0 + r) % a.n_inner;
+        const long long t = load_token(a.tokens, a.wide_tokens != 0, o * a.t_so + i * a.t_si);
+        from[r] = t >= 0 && t < a.vocab ? static_cast<const TT*>(a.table) + t * a.stride : nullptr;
+        to[r] = static_cast<TA*>(a.act) + o * a.a_so + i * a.a_si;
+    }
+    __syncthreads();
     const long long col = ((long long)blockIdx.y * blockDim.x + threadIdx.x) * W;
     if (col >= a.dim) return;
-    const unsigned r0 = (blockIdx.x * blockDim.y + threadIdx.y) * kLookupRows;
-    const TT* src[kLookupRows];
+    for (unsigned r = threadIdx.y; r < n; r += B * blockDim.y) {
+        float x[B][W];
 #pragma unroll
-    for (int k = 0; k < kLookupRows; ++k) {
-        src[k] = nullptr;
-        if (r0 + k < a.rows) {
-            const long long o = (r0 + k) / a.n_inner, i = (r0 + k) % a.n_inner;
-            const long long t = load_token(a.tokens, a.wide_tokens != 0, o * a.t_so + i * a.t_si);
-            if (t >= 0 && t < a.vocab) src[k] = static_cast<const TT*>(a.table) + t * a.stride + col;
+        for (int k = 0; k < B; ++k) {
+#pragma unroll
+            for (int l = 0; l < W; ++l) x[k][l] = 0.0f;
+            const unsigned j = r + k * blockDim.y;
+            if (j < n && from[j] != nullptr) load_columns<TT, W>(from[j] + col, x[k]);
         }
-    }
-    float x[kLookupRows][W];
 #pragma unroll
-    for (int k = 0; k < kLookupRows; ++k) {
+        for (int k = 0; k < B; ++k) {
+            const unsigned j = r + k * blockDim.y;
+            if (j >= n) break;
+            if (from[j] != nullptr) {  // (zeros stay zeros whatever the scale)
 #pragma unroll
-        for (int l = 0; l < W; ++l) x[k][l] = 0.0f;
-        if (src[k] == nullptr) continue;
-        if constexpr (VEC) {
-#pragma unroll
-            for (int v = 0; v < W / kLanes<TT>; ++v) {
-                float y[kLanes<TT>];
-                unpack<TT>(__ldg(reinterpret_cast<const uint4*>(src[k]) + v), y);
-#pragma unroll
-                for (int l = 0; l < kLanes<TT>; ++l) x[k][v * kLanes<TT> + l] = y[l];
+                for (int l = 0; l < W; ++l) x[k][l] *= a.scale;
             }
-        } else {
-            x[k][0] = to_f32(*src[k]);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < kLookupRows; ++k) {
-        if (r0 + k >= a.rows) break;
-        const long long o = (r0 + k) / a.n_inner, i = (r0 + k) % a.n_inner;
-        TA* dst = static_cast<TA*>(a.act) + o * a.a_so + i * a.a_si + col;
-#pragma unroll
-        for (int l = 0; l < W; ++l) x[k][l] = src[k] == nullptr ? 0.0f : x[k][l] * a.scale;
-        if constexpr (VEC) {
-#pragma unroll
-            for (int v = 0; v < W / kLanes<TA>; ++v) {
-                float y[kLanes<TA>];
-#pragma unroll
-                for (int l = 0; l < kLanes<TA>; ++l) y[l] = x[k][v * kLanes<TA> + l];
-                reinterpret_cast<uint4*>(dst)[v] = pack<TA>(y);
-            }
-        } else {
-            *dst = from_f32<TA>(x[k][0]);
+            store_columns<TA, W>(to[j] + col, x[k]);
         }
     }
 }
@@ -682,6 +702,7 @@ struct EmbedGradArgs {
     unsigned n, n_inner;
     int wide_tokens, accumulate;
     int flat;  // token t lies at t * t_si
+    int wide;  // the table's rows start on 32 bytes
     float scale;
     // workspace
     unsigned* key[2];
@@ -984,8 +1005,11 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
                 }
             }
             if constexpr (VEC) {
+                if constexpr (W == 8) {
+                    if (a.wide) store_eight(dst, acc);
+                }
 #pragma unroll
-                for (int l = 0; l < W; l += 4)
+                for (int l = 0; l < W && !(W == 8 && a.wide); l += 4)
                     *reinterpret_cast<float4*>(dst + l) = make_float4(acc[l], acc[l + 1], acc[l + 2], acc[l + 3]);
             } else {
                 *dst = acc[0];
@@ -1153,6 +1177,7 @@ template <typename T, typename D>
 __device__ __forceinline__ void chunk_scale(const GradChunk& c, D* d, float f) {
     constexpr int L = kLanes<T>;
     const T* p = static_cast<const T*>(c.src);
+    const bool wide = aligned32(d);
     unsigned done = 0;
     if (chunk_vec(c)) {
         const unsigned nv = c.n / L;
@@ -1173,6 +1198,8 @@ __device__ __forceinline__ void chunk_scale(const GradChunk& c, D* d, float f) {
                 for (int l = 0; l < L; ++l) x[l] *= f;
                 if constexpr (sizeof(T) == sizeof(D)) {
                     __stcs(reinterpret_cast<uint4*>(d) + v, pack<T>(x));
+                } else if (wide) {
+                    store_eight(d + (size_t)v * L, x);
                 } else {
 #pragma unroll
                     for (int l = 0; l < L; l += 4)
