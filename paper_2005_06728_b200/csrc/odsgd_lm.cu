@@ -201,9 +201,8 @@ bool rows_aligned(const void* p, int elem, int64_t so, int64_t si, int64_t n_out
 
 template <typename TT, typename TA>
 int launch_lookup(LookupArgs a, bool vec_ok, void* stream) {
-    constexpr int W = kLanes<TT> < kLanes<TA> ? kLanes<TT> : kLanes<TA>;
-    const bool vec = vec_ok && a.dim % W == 0;
-    const int64_t cols = vec ? a.dim / W : a.dim;
+    const bool vec = vec_ok && a.dim % kLookupColumns<TT, TA, true> == 0;
+    const int64_t cols = ceil_div(a.dim, vec ? kLookupColumns<TT, TA, true> : kLookupColumns<TT, TA, false>);
     // as many threads along the row as it has pieces, the rest along the rows
     const int slabs = (int)ceil_div(cols, kLookupThreads);
     const int bx = (int)ceil_div(ceil_div(cols, slabs), 32) * 32;
@@ -268,7 +267,7 @@ GradShape grad_shape(const odsgd_embed_desc* d) {
 template <typename T>
 int launch_sum(const EmbedGradArgs& a, const GradShape& s, bool vec_ok, void* stream) {
     const bool vec = vec_ok && a.dim % kLanes<T> == 0;
-    const int64_t cols = vec ? a.dim / kLanes<T> : a.dim;
+    const int64_t cols = ceil_div(a.dim, vec ? Piece<T, true>::W : Piece<T, false>::W);
     const int64_t slabs = ceil_div(cols, kSumThreads);
     const unsigned threads = (unsigned)(ceil_div(ceil_div(cols, slabs), 32) * 32);
     const dim3 grid(s.blocks, (unsigned)slabs);

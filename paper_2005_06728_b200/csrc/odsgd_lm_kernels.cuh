@@ -597,13 +597,19 @@ struct LookupArgs {
 };
 constexpr int kLookupThreads = 256;
 constexpr int kLookupRows = 64;  // most rows of a CTA
+template <typename TT, typename TA, bool VEC>
+constexpr int kLookupColumns = VEC ? (kLanes<TT> < kLanes<TA> ? kLanes<TT> : kLanes<TA>) : 4;  // of a thread
 
-// One column of T or, with VEC, as many as 16 bytes of the wider type hold: that side moves 16 bytes
-// a thread, the other 8 or 16, and both without gaps between the threads.
-template <typename T, int W>
-__device__ __forceinline__ void load_columns(const T* p, float (&x)[W]) {
-    if constexpr (W == 1) {
-        x[0] = to_f32(*p);
+// A thread's W columns of a row, from column `col` on.  VEC: next to one another, as many as 16 bytes of
+// the wider type hold: that side moves 16 bytes a thread, the other 8 or 16, and both without
+// gaps between the threads.  Otherwise (rows that are not aligned): blockDim.x apart, up to dim.
+template <typename T, bool VEC, int W>
+__device__ __forceinline__ void load_columns(const T* row, long long col, long long dim, float (&x)[W]) {
+    const T* p = row + col;
+    if constexpr (!VEC) {
+#pragma unroll
+        for (int l = 0; l < W; ++l)
+            if (col + l * (int)blockDim.x < dim) x[l] = to_f32(p[l * (int)blockDim.x]);
     } else if constexpr (W == kLanes<T>) {
         unpack<T>(__ldg(reinterpret_cast<const uint4*>(p)), x);
     } else {
@@ -614,10 +620,13 @@ __device__ __forceinline__ void load_columns(const T* p, float (&x)[W]) {
         for (int l = 0; l < W; ++l) x[l] = y[l];
     }
 }
-template <typename T, int W>
-__device__ __forceinline__ void store_columns(T* p, const float (&x)[W]) {
-    if constexpr (W == 1) {
-        *p = from_f32<T>(x[0]);
+template <typename T, bool VEC, int W>
+__device__ __forceinline__ void store_columns(T* row, long long col, long long dim, const float (&x)[W]) {
+    T* p = row + col;
+    if constexpr (!VEC) {
+#pragma unroll
+        for (int l = 0; l < W; ++l)
+            if (col + l * (int)blockDim.x < dim) p[l * (int)blockDim.x] = from_f32<T>(x[l]);
     } else if constexpr (W == kLanes<T>) {
         *reinterpret_cast<uint4*>(p) = pack<T>(x);
     } else {
@@ -631,7 +640,7 @@ __device__ __forceinline__ void store_columns(T* p, const float (&x)[W]) {
 // threads.  Four rows a thread are in flight.
 template <typename TT, typename TA, bool VEC>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_constant__ LookupArgs a) {
-    constexpr int W = VEC ? (kLanes<TT> < kLanes<TA> ? kLanes<TT> : kLanes<TA>) : 1;
+    constexpr int W = kLookupColumns<TT, TA, VEC>;
     constexpr int B = 4;
     __shared__ const TT* from[kLookupRows];
     __shared__ TA* to[kLookupRows];
@@ -644,7 +653,7 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
         to[r] = static_cast<TA*>(a.act) + o * a.a_so + i * a.a_si;
     }
     __syncthreads();
-    const long long col = ((long long)blockIdx.y * blockDim.x + threadIdx.x) * W;
+    const long long col = (long long)blockIdx.y * blockDim.x * W + threadIdx.x * (VEC ? W : 1);
     if (col >= a.dim) return;
     for (unsigned r = threadIdx.y; r < n; r += B * blockDim.y) {
         float x[B][W];
@@ -653,7 +662,7 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
 #pragma unroll
             for (int l = 0; l < W; ++l) x[k][l] = 0.0f;
             const unsigned j = r + k * blockDim.y;
-            if (j < n && from[j] != nullptr) load_columns<TT, W>(from[j] + col, x[k]);
+            if (j < n && from[j] != nullptr) load_columns<TT, VEC>(from[j], col, a.dim, x[k]);
         }
 #pragma unroll
         for (int k = 0; k < B; ++k) {
@@ -663,7 +672,7 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
 #pragma unroll
                 for (int l = 0; l < W; ++l) x[k][l] *= a.scale;
             }
-            store_columns<TA, W>(to[j] + col, x[k]);
+            store_columns<TA, VEC>(to[j], col, a.dim, x[k]);
         }
     }
 }
@@ -930,14 +939,15 @@ constexpr int kSumCtas = 8;
 constexpr int kSumBatch = 8;       // rows a thread has in flight
 constexpr int kSumMaxBlock = 126;  // most positions of a block
 
-// A vector of T, or one T.
+// A thread's columns of a row: a vector of T, or (rows that are not aligned) T's blockDim.x apart, of
+// which `left` columns remain.
 template <typename T, bool VEC>
 struct Piece;
 template <typename T>
 struct Piece<T, true> {
     static constexpr int W = kLanes<T>;
     uint4 q;
-    __device__ __forceinline__ void load(const T* p) { q = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void load(const T* p, long long) { q = __ldcs(reinterpret_cast<const uint4*>(p)); }
     __device__ __forceinline__ void add_to(float (&acc)[W]) const {
         float x[W];
         unpack<T>(q, x);
@@ -947,10 +957,16 @@ struct Piece<T, true> {
 };
 template <typename T>
 struct Piece<T, false> {
-    static constexpr int W = 1;
-    T x;
-    __device__ __forceinline__ void load(const T* p) { x = *p; }
-    __device__ __forceinline__ void add_to(float (&acc)[1]) const { acc[0] += to_f32(x); }
+    static constexpr int W = 4;
+    T x[W];
+    __device__ __forceinline__ void load(const T* p, long long left) {
+#pragma unroll
+        for (int l = 0; l < W; ++l) x[l] = l * (int)blockDim.x < left ? p[l * (int)blockDim.x] : from_f32<T>(0.0f);
+    }
+    __device__ __forceinline__ void add_to(float (&acc)[W]) const {
+#pragma unroll
+        for (int l = 0; l < W; ++l) acc[l] += to_f32(x[l]);
+    }
 };
 
 template <typename T, bool VEC>
@@ -970,8 +986,8 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
         }
     }
     __syncthreads();
-    const long long col = ((long long)blockIdx.y * blockDim.x + threadIdx.x) * W;
-    if (col >= a.dim) return;
+    const long long col = (long long)blockIdx.y * blockDim.x * W + threadIdx.x * (VEC ? W : 1), left = a.dim - col;
+    if (left <= 0) return;
     float acc[W];
 #pragma unroll
     for (int l = 0; l < W; ++l) acc[l] = 0.0f;
@@ -980,7 +996,7 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
         Piece<T, VEC> x[kSumBatch];
 #pragma unroll
         for (int k = 0; k < kSumBatch; ++k)
-            if (b + k < n && key[b + k + 1] != none) x[k].load(row[b + k] + col);
+            if (b + k < n && key[b + k + 1] != none) x[k].load(row[b + k] + col, left);
 #pragma unroll
         for (int k = 0; k < kSumBatch; ++k) {
             if (b + k >= n) continue;
@@ -1001,7 +1017,10 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
                 for (int l = 0; l < W; ++l) acc[l] *= a.scale;
                 if (a.accumulate) {
 #pragma unroll
-                    for (int l = 0; l < W; ++l) acc[l] += dst[l];
+                    for (int l = 0; l < W; ++l) {
+                        const int j = VEC ? l : l * (int)blockDim.x;
+                        if (VEC || j < left) acc[l] += dst[j];
+                    }
                 }
             }
             if constexpr (VEC) {
@@ -1012,7 +1031,9 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
                 for (int l = 0; l < W && !(W == 8 && a.wide); l += 4)
                     *reinterpret_cast<float4*>(dst + l) = make_float4(acc[l], acc[l + 1], acc[l + 2], acc[l + 3]);
             } else {
-                *dst = acc[0];
+#pragma unroll
+                for (int l = 0; l < W; ++l)
+                    if (l * (int)blockDim.x < left) dst[l * (int)blockDim.x] = acc[l];
             }
 #pragma unroll
             for (int l = 0; l < W; ++l) acc[l] = 0.0f;
