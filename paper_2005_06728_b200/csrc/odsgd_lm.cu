@@ -351,8 +351,9 @@ RowShape row_shape(int64_t rows, int64_t vocab, int elem, bool loss, int sms) {
         while (s.cluster < kRowCluster && vectors * 16 * kWideCtas * sms > kRowsInFlightBytes * s.cluster) s.cluster *= 2;
     while (s.cluster < kRowCluster && rows * s.cluster < sms && vectors > (int64_t)s.cluster * 256) s.cluster *= 2;
     const int64_t part = ceil_div(vectors, s.cluster);
-    // a batch of vectors a thread when there are rows enough to fill the GPU, one vector when there are not
-    const int64_t each = rows * s.cluster >= 2 * (int64_t)sms ? kRowVectors : 1;
+    // four batches of vectors a thread when there are rows enough to fill the GPU (4096 rows of 4000
+    // 32-bit logits: 26 us where one batch takes 36), one vector when there are not
+    const int64_t each = rows * s.cluster >= 2 * (int64_t)sms ? 4 * kRowVectors : 1;
     const int64_t most = !loss ? kScoreThreads : s.wide ? kWideThreads : kNarrowThreads;
     s.threads = (int)std::min(most, std::max<int64_t>(32, ceil_div(ceil_div(part, each), 32) * 32));
     return s;
@@ -422,7 +423,7 @@ int check_workspace(const void* ws, size_t have, size_t need) {
 struct odsgd_grad_set {
     int device = 0;
     int n_groups = 0;
-    unsigned n_chunks = 0;
+    unsigned n_chunks = 0, most_chunks = 0;  // in all, and of a group
     void* table = nullptr;
     std::vector<unsigned char> host;  // what the table was filled from
     const GradChunk* chunks = nullptr;
@@ -501,6 +502,7 @@ int make_set(odsgd_grad_set* s, const odsgd_grad_tensor* t, size_t n, int n_grou
     }
     s->n_chunks = (unsigned)chunks.size();
     s->n_groups = n_groups;
+    for (const GradGroup& g : groups) s->most_chunks = std::max(s->most_chunks, g.n_chunks);
     const size_t at_groups = chunks.size() * sizeof(GradChunk);
     const size_t filled = (at_groups + groups.size() * sizeof(GradGroup) + 15) / 16 * 16;
     s->host.resize(filled);
@@ -543,10 +545,14 @@ int run_set(odsgd_grad_set* s, bool clip, float max_norm, float* norms, void* st
     a.n_chunks = s->n_chunks;
     a.n_groups = s->n_groups;
     a.max_norm = max_norm;
-    if (s->n_chunks > 0) rc = launch("gradient norm kernel", norm_kernel, dim3(s->n_chunks), dim3(kClipThreads), 0, 1, stream, a);
-    if (rc == ODSGD_OK) rc = launch("gradient norm sum kernel", finish_kernel, dim3((unsigned)s->n_groups), dim3(kFinishThreads), 0, 1, stream, a);
+    const dim3 chunks(s->n_chunks), block(kClipThreads);
+    if (s->n_chunks > 0) rc = launch("gradient norm kernel", norm_kernel, chunks, block, 0, 1, stream, a);
+    if (rc != ODSGD_OK) return rc;
+    if (clip && s->n_chunks > 0 && s->most_chunks <= kJoinChunks)
+        return launch("gradient clip kernel", clip_kernel<true>, chunks, block, 0, 1, stream, a);
+    rc = launch("gradient norm sum kernel", finish_kernel, dim3((unsigned)s->n_groups), dim3(kFinishThreads), 0, 1, stream, a);
     if (rc != ODSGD_OK || !clip || s->n_chunks == 0) return rc;
-    return launch("gradient clip kernel", clip_kernel, dim3(s->n_chunks), dim3(kClipThreads), 0, 1, stream, a);
+    return launch("gradient clip kernel", clip_kernel<false>, chunks, block, 0, 1, stream, a);
 }
 
 }  // namespace

@@ -1176,18 +1176,24 @@ __global__ void __launch_bounds__(kClipThreads) norm_kernel(const __grid_constan
     if (threadIdx.x == 0) a.partial[blockIdx.x] = s[0];
 }
 
+// The norm of a group from its chunks' partials, by thread 0 of a CTA.
+template <int THREADS>
+__device__ __forceinline__ double group_norm(const GradArgs& a, const GradGroup& g, double* smem) {
+    double t[1] = {0.0};
+#pragma unroll 4
+    for (unsigned j = threadIdx.x; j < g.n_chunks; j += THREADS) t[0] += a.partial[g.first_chunk + j];
+    block_sum<1, THREADS>(t, smem);
+    return sqrt(t[0]);
+}
+
 // A CTA a group.
 constexpr int kFinishThreads = 512;
 __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ GradArgs a) {
     __shared__ double part[kFinishThreads / 32];
     dependent_launch_prologue();
     GradGroup* g = a.groups + blockIdx.x;
-    double t[1] = {0.0};
-#pragma unroll 4
-    for (unsigned j = threadIdx.x; j < g->n_chunks; j += kFinishThreads) t[0] += a.partial[g->first_chunk + j];
-    block_sum<1, kFinishThreads>(t, part);
+    const double norm = group_norm<kFinishThreads>(a, *g, part);
     if (threadIdx.x == 0) {
-        const double norm = sqrt(t[0]);
         g->factor = clip_factor(norm, a.max_norm);
         if (a.norms != nullptr) a.norms[blockIdx.x] = (float)norm;
     }
@@ -1239,10 +1245,30 @@ __device__ __forceinline__ void scale_chunk(const GradChunk& c, float f) {
     else if (f != 1.0f) chunk_scale<T, T>(c, static_cast<T*>(const_cast<void*>(c.src)), f);  // else every bit stays
 }
 
+// JOIN: each CTA adds its group's partials itself, which saves a launch where they are few.
+constexpr unsigned kJoinChunks = 1024;
+template <bool JOIN>
 __global__ void __launch_bounds__(kClipThreads) clip_kernel(const __grid_constant__ GradArgs a) {
+    __shared__ double part[kClipThreads / 32];
+    __shared__ float factor;
     dependent_launch_prologue();
-    const GradChunk c = a.chunks[a.n_chunks - 1 - blockIdx.x];
-    const float f = a.groups[c.group].factor;
+    const unsigned i = a.n_chunks - 1 - blockIdx.x;
+    const GradChunk c = a.chunks[i];
+    float f;
+    if (JOIN) {
+        const GradGroup g = a.groups[c.group];
+        const double norm = group_norm<kClipThreads>(a, g, part);
+        if (threadIdx.x == 0) {
+            factor = clip_factor(norm, a.max_norm);
+            if (i == g.first_chunk && a.norms != nullptr) a.norms[c.group] = (float)norm;
+        }
+        if (blockIdx.x == 0 && threadIdx.x < a.n_groups && a.groups[threadIdx.x].n_chunks == 0 && a.norms != nullptr)
+            a.norms[threadIdx.x] = 0.0f;
+        __syncthreads();
+        f = factor;
+    } else {
+        f = a.groups[c.group].factor;
+    }
     const int type = c.type_vec & 0xff;
     if (type == ODSGD_F32) scale_chunk<float>(c, f);
     else if (type == ODSGD_BF16) scale_chunk<bf16>(c, f);

@@ -19,7 +19,8 @@ levels.  There is no CPU fallback and no autograd: the gradient calls are the ba
 from __future__ import annotations
 
 import ctypes
-from typing import List, NamedTuple, Optional, Sequence, Tuple
+import struct
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -33,40 +34,11 @@ _TYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int
 _FLOATS = (torch.float32, torch.bfloat16, torch.float16)
 _INTS = (torch.int32, torch.int64)
 
-_vp, _ci, _i64, _cf = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
-
-
-class _EmbedDesc(ctypes.Structure):
-    _fields_ = [
-        ("tokens", _vp), ("act", _vp), ("table", _vp),
-        ("token_type", _ci), ("act_type", _ci), ("table_type", _ci), ("accumulate", _ci),
-        ("n_outer", _i64), ("n_inner", _i64),
-        ("token_stride_outer", _i64), ("token_stride_inner", _i64),
-        ("act_stride_outer", _i64), ("act_stride_inner", _i64),
-        ("vocab", _i64), ("dim", _i64), ("table_stride", _i64), ("padding_token", _i64),
-        ("scale", _cf),
-    ]
-
-
-class _PolicyDesc(ctypes.Structure):
-    _fields_ = [
-        ("logits", _vp), ("labels", _vp), ("old_logp", _vp), ("ref_logp", _vp), ("advantages", _vp), ("weights", _vp),
-        ("dlogits", _vp), ("logp", _vp), ("lse", _vp), ("stats", _vp),
-        ("type", _ci), ("label_type", _ci),
-        ("n_outer", _i64), ("n_inner", _i64), ("vocab", _i64),
-        ("logits_stride_outer", _i64), ("logits_stride_inner", _i64),
-        ("label_stride_outer", _i64), ("label_stride_inner", _i64),
-        ("old_stride_outer", _i64), ("old_stride_inner", _i64),
-        ("ref_stride_outer", _i64), ("ref_stride_inner", _i64),
-        ("adv_stride_outer", _i64), ("adv_stride_inner", _i64),
-        ("weight_stride_outer", _i64), ("weight_stride_inner", _i64),
-        ("dlogits_stride_outer", _i64), ("dlogits_stride_inner", _i64),
-        ("inv_temp", _cf), ("clip_low", _cf), ("clip_high", _cf), ("kl_coef", _cf), ("grad_scale", _cf),
-    ]
-
-
-class _GradTensor(ctypes.Structure):
-    _fields_ = [("data", _vp), ("numel", ctypes.c_size_t), ("offset", ctypes.c_size_t), ("type", _ci), ("group", _ci)]
+# odsgd_embed_desc, odsgd_policy_desc and odsgd_grad_tensor of include/odsgd.h, packed by struct: a call is
+# a few microseconds, and filling a ctypes structure would be one of them.
+_EMBED = struct.Struct("3P4i10qf4x")
+_POLICY = struct.Struct("10P2i17q5f4x")
+_GRAD_TENSOR = struct.Struct("PNN2i")
 
 
 class TokenLogprob(NamedTuple):
@@ -91,16 +63,18 @@ def _check(rc: int) -> None:
         raise OdsgdError(rc, binding.load_library().odsgd_last_error(None).decode())
 
 
-def _need(t: torch.Tensor, name: str, dtypes) -> None:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes:
+def _need(t: torch.Tensor, name: str, dtypes, dev: int) -> int:
+    """The type code of a tensor of one of `dtypes` on the current device, `dev`."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or not t.is_cuda:
         raise TypeError(f"{name}: need a CUDA tensor of {' / '.join(str(d) for d in dtypes)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+    return _TYPE[t.dtype]
 
 
-def _on_device(*tensors: Optional[torch.Tensor]) -> None:
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+def _shape(t: torch.Tensor, shape, name: str) -> None:
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 def _levels(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int, int, int]:
@@ -125,30 +99,39 @@ def _levels(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int, int, int]:
     return outer, shape[-1], step, stride[-1]
 
 
-def _last_contiguous(t: torch.Tensor, name: str) -> None:
+def _rows(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int, int, int]:
+    """The same of a tensor with one more axis, which has to be contiguous."""
     if t.dim() == 0 or (t.stride(-1) != 1 and t.shape[-1] != 1):
         raise ValueError(f"{name}: the last axis must be contiguous")
+    return _levels(t, lead, name)
 
 
-def _same_shape(t: torch.Tensor, shape, name: str) -> None:
-    if t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-
-
-def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+def _new(like: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
     """Memory of the stream that the work runs on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+
+
+# The current stream's handle without the Stream object around it (a third of a small call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _handle(stream: Optional[torch.cuda.Stream], dev: int) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return binding._stream_handle(stream)
 
 
 def _table(table: torch.Tensor, name: str) -> Tuple[int, int, int]:
     if table.dim() != 2:
         raise ValueError(f"{name}: need [vocab, dim]")
-    _last_contiguous(table, name)
     vocab, dim = table.shape
-    return vocab, dim, table.stride(0) if vocab > 1 else max(dim, table.stride(0))
+    stride, last = table.stride()
+    if last != 1 and dim != 1:
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    return vocab, dim, stride if vocab > 1 else max(dim, stride)
 
 
 # --------------------------------------------------------------------------- embedding
@@ -157,23 +140,21 @@ def embed_lookup(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.
                  out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """scale * table[tokens], rounded once to `dtype` (default: the table's).  A token outside
     [0, vocab), such as the -1 that pads a ragged batch, gives a row of zeros."""
-    _need(tokens, "tokens", _INTS)
-    _need(table, "table", _FLOATS)
+    dev = torch.cuda.current_device()
+    token_type = _need(tokens, "tokens", _INTS, dev)
+    table_type = _need(table, "table", _FLOATS, dev)
     vocab, dim, stride = _table(table, "table")
-    lead = tokens.dim()
+    shape = (*tokens.shape, dim)
     if out is None:
-        out = _empty((*tokens.shape, dim), table.dtype if dtype is None else dtype, tokens.device, stream)
+        out = _new(table, shape, table.dtype if dtype is None else dtype, stream)
     elif dtype is not None and out.dtype != dtype:
         raise ValueError("out and dtype disagree")
-    _need(out, "out", _FLOATS)
-    _same_shape(out, torch.Size((*tokens.shape, dim)), "out")
-    _last_contiguous(out, "out")
-    _on_device(tokens, table, out)
-    no, ni, tso, tsi = _levels(tokens, lead, "tokens")
-    _, _, aso, asi = _levels(out, lead, "out")
-    d = _EmbedDesc(tokens.data_ptr(), out.data_ptr(), table.data_ptr(), _TYPE[tokens.dtype], _TYPE[out.dtype],
-                   _TYPE[table.dtype], 0, no, ni, tso, tsi, aso, asi, vocab, dim, stride, -1, scale)
-    _check(binding.load_library().odsgd_embed_lookup(ctypes.addressof(d), binding._stream_handle(stream)))
+    out_type = _need(out, "out", _FLOATS, dev)
+    _shape(out, shape, "out")
+    lead = tokens.dim()
+    d = _EMBED.pack(tokens.data_ptr(), out.data_ptr(), table.data_ptr(), token_type, out_type, table_type, 0,
+                    *_levels(tokens, lead, "tokens"), *_rows(out, lead, "out")[2:], vocab, dim, stride, -1, scale)
+    _check(binding.load_library().odsgd_embed_lookup(d, _handle(stream, dev)))
     return out
 
 
@@ -183,36 +164,34 @@ def embed_grad(tokens: torch.Tensor, grad: torch.Tensor, dtable: torch.Tensor, *
     """dtable[v] = scale * sum of grad over the positions of token v, zeros where there is none
     (accumulate: added to what is there).  `dtable` is float32, normally a view of the worker's
     gradient arena.  Tokens outside [0, vocab) and `padding_token` contribute nothing."""
-    _need(tokens, "tokens", _INTS)
-    _need(grad, "grad", _FLOATS)
-    _need(dtable, "dtable", (torch.float32,))
+    dev = torch.cuda.current_device()
+    token_type = _need(tokens, "tokens", _INTS, dev)
+    grad_type = _need(grad, "grad", _FLOATS, dev)
+    _need(dtable, "dtable", (torch.float32,), dev)
     vocab, dim, stride = _table(dtable, "dtable")
-    _same_shape(grad, torch.Size((*tokens.shape, dim)), "grad")
-    _last_contiguous(grad, "grad")
-    _on_device(tokens, grad, dtable, workspace)
+    _shape(grad, (*tokens.shape, dim), "grad")
     lead = tokens.dim()
-    no, ni, tso, tsi = _levels(tokens, lead, "tokens")
-    _, _, aso, asi = _levels(grad, lead, "grad")
-    d = _EmbedDesc(tokens.data_ptr(), grad.data_ptr(), dtable.data_ptr(), _TYPE[tokens.dtype], _TYPE[grad.dtype], F32,
-                   1 if accumulate else 0, no, ni, tso, tsi, aso, asi, vocab, dim, stride,
-                   -1 if padding_token is None else padding_token, scale)
+    d = _EMBED.pack(tokens.data_ptr(), grad.data_ptr(), dtable.data_ptr(), token_type, grad_type, F32, 1 if accumulate else 0,
+                    *_levels(tokens, lead, "tokens"), *_rows(grad, lead, "grad")[2:], vocab, dim, stride,
+                    -1 if padding_token is None else padding_token, scale)
     lib = binding.load_library()
     if workspace is None:
         need = ctypes.c_size_t()
-        _check(lib.odsgd_embed_grad_workspace(ctypes.addressof(d), ctypes.byref(need)))
-        workspace = _empty((max(16, need.value),), torch.uint8, tokens.device, stream)
-    _check(lib.odsgd_embed_grad(ctypes.addressof(d), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                binding._stream_handle(stream)))
+        _check(lib.odsgd_embed_grad_workspace(d, ctypes.byref(need)))
+        workspace = _new(grad, max(16, need.value), torch.uint8, stream)
+    elif not workspace.is_contiguous() or workspace.get_device() != dev:
+        raise ValueError("workspace: need a contiguous tensor on the current device")
+    _check(lib.odsgd_embed_grad(d, workspace.data_ptr(), workspace.nbytes, _handle(stream, dev)))
     return dtable
 
 
 def embed_grad_workspace(tokens: torch.Tensor, grad: torch.Tensor, dtable: torch.Tensor) -> int:
     """Bytes of workspace that embed_grad needs for tensors of these shapes and types."""
     no, ni, _, _ = _levels(tokens, tokens.dim(), "tokens")
-    d = _EmbedDesc(None, None, None, _TYPE[tokens.dtype], _TYPE[grad.dtype], F32, 0, no, ni, 0, 0, 0, 0,
-                   dtable.shape[0], dtable.shape[1], dtable.shape[1], -1, 1.0)
+    d = _EMBED.pack(0, 0, 0, _TYPE[tokens.dtype], _TYPE[grad.dtype], F32, 0, no, ni, 0, 0, 0, 0,
+                    dtable.shape[0], dtable.shape[1], dtable.shape[1], -1, 1.0)
     need = ctypes.c_size_t()
-    _check(binding.load_library().odsgd_embed_grad_workspace(ctypes.addressof(d), ctypes.byref(need)))
+    _check(binding.load_library().odsgd_embed_grad_workspace(d, ctypes.byref(need)))
     return need.value
 
 
@@ -222,20 +201,18 @@ def token_logprob(logits: torch.Tensor, labels: torch.Tensor, *, inv_temp: float
                   stream: Optional[torch.cuda.Stream] = None) -> TokenLogprob:
     """log softmax(inv_temp * logits)[label] and the row's log of summed exponentials, in float32;
     zeros where the label is outside [0, vocab)."""
-    _need(logits, "logits", _FLOATS)
-    _need(labels, "labels", _INTS)
-    _last_contiguous(logits, "logits")
-    _same_shape(labels, logits.shape[:-1], "labels")
-    _on_device(logits, labels)
+    dev = torch.cuda.current_device()
+    kind = _need(logits, "logits", _FLOATS, dev)
+    label_type = _need(labels, "labels", _INTS, dev)
     lead = labels.dim()
-    no, ni, zso, zsi = _levels(logits, lead, "logits")
+    no, ni, zso, zsi = _rows(logits, lead, "logits")
+    shape = labels.shape
+    _shape(logits, (*shape, logits.shape[-1]), "logits")
     _, _, lso, lsi = _levels(labels, lead, "labels")
-    both = _empty((2, *labels.shape), torch.float32, logits.device, stream)
-    logp, lse = both.unbind(0)
-    d = _PolicyDesc(logits.data_ptr(), labels.data_ptr(), None, None, None, None, None, logp.data_ptr(), lse.data_ptr(),
-                    None, _TYPE[logits.dtype], _TYPE[labels.dtype], no, ni, logits.shape[-1], zso, zsi, lso, lsi)
-    d.inv_temp = inv_temp
-    _check(binding.load_library().odsgd_token_logprob(ctypes.addressof(d), binding._stream_handle(stream)))
+    logp, lse = _new(logits, shape, torch.float32, stream), _new(logits, shape, torch.float32, stream)
+    d = _POLICY.pack(logits.data_ptr(), labels.data_ptr(), 0, 0, 0, 0, 0, logp.data_ptr(), lse.data_ptr(), 0, kind, label_type,
+                     no, ni, logits.shape[-1], zso, zsi, lso, lsi, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, inv_temp, 0.0, 0.0, 0.0, 0.0)
+    _check(binding.load_library().odsgd_token_logprob(d, _handle(stream, dev)))
     return TokenLogprob(logp, lse)
 
 
@@ -248,44 +225,39 @@ def policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tens
     `old_logp`, `ref_logp`, `advantages` and `weights` are float32 of the labels' shape (expanded
     views welcome); a weight is mask and normalisation in one.  `dlogits` may be `logits` itself.
     """
-    _need(logits, "logits", _FLOATS)
-    _need(labels, "labels", _INTS)
-    _last_contiguous(logits, "logits")
-    shape = logits.shape[:-1]
-    _same_shape(labels, shape, "labels")
+    dev = torch.cuda.current_device()
+    kind = _need(logits, "logits", _FLOATS, dev)
+    label_type = _need(labels, "labels", _INTS, dev)
+    shape, whole = labels.shape, logits.shape
     lead = len(shape)
-    vectors = (old_logp, ref_logp, advantages, weights)
-    strides: List[int] = []
-    for t, name in zip(vectors, ("old_logp", "ref_logp", "advantages", "weights")):
-        if t is None:
-            strides += (0, 0)
-            continue
-        _need(t, name, (torch.float32,))
-        _same_shape(t, shape, name)
-        strides += _levels(t, lead, name)[2:]
+    if whole[:-1] != shape or len(whole) == 0:
+        raise ValueError(f"labels: shape {tuple(shape)}, expected {tuple(whole[:-1])}")
+    no, ni, zso, zsi = _rows(logits, lead, "logits")
+
+    def vector(t, name):
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.get_device() != dev or t.shape != shape:
+            _need(t, name, (torch.float32,), dev)
+            _shape(t, shape, name)
+        return t.stride() if lead == 2 else _levels(t, lead, name)[2:]
+
+    strides = (*_levels(labels, lead, "labels")[2:], *vector(old_logp, "old_logp"),
+               *((0, 0) if ref_logp is None else vector(ref_logp, "ref_logp")),
+               *vector(advantages, "advantages"), *vector(weights, "weights"))
     if dlogits is None:
-        dlogits = _empty(logits.shape, logits.dtype, logits.device, stream)
+        dlogits = _new(logits, whole, logits.dtype, stream)
     else:
-        _need(dlogits, "dlogits", (logits.dtype,))
-        _same_shape(dlogits, logits.shape, "dlogits")
-        _last_contiguous(dlogits, "dlogits")
-    _on_device(logits, labels, *vectors, dlogits)
-    no, ni, zso, zsi = _levels(logits, lead, "logits")
-    _, _, lso, lsi = _levels(labels, lead, "labels")
-    _, _, dso, dsi = _levels(dlogits, lead, "dlogits")
-    # one allocation: the four sums, then the rows' scores; and the workspace (12 bytes a row)
+        _need(dlogits, "dlogits", (logits.dtype,), dev)
+        _shape(dlogits, whole, "dlogits")
     n = no * ni
-    out = _empty((4 + n,), torch.float32, logits.device, stream)
-    stats, logp = out[:4], out[4:].view(shape)
-    work = _empty((max(4, 3 * n),), torch.float32, logits.device, stream)
-    d = _PolicyDesc(logits.data_ptr(), labels.data_ptr(), old_logp.data_ptr(),
-                    None if ref_logp is None else ref_logp.data_ptr(), advantages.data_ptr(), weights.data_ptr(),
-                    dlogits.data_ptr(), logp.data_ptr(), None, stats.data_ptr(), _TYPE[logits.dtype],
-                    _TYPE[labels.dtype], no, ni, logits.shape[-1], zso, zsi, lso, lsi, *strides, dso, dsi,
-                    inv_temp, clip_low, clip_high, kl_coef, grad_scale)
-    _check(binding.load_library().odsgd_policy_loss(ctypes.addressof(d), work.data_ptr(), 4 * work.numel(),
-                                                    binding._stream_handle(stream)))
-    return PolicyLoss(stats, logp, dlogits)
+    head = _new(logits, 4 + max(4, 3 * n), torch.float32, stream)  # the four sums, and the workspace (12 bytes a row)
+    logp = _new(logits, shape, torch.float32, stream)
+    at = head.data_ptr()
+    d = _POLICY.pack(logits.data_ptr(), labels.data_ptr(), old_logp.data_ptr(), 0 if ref_logp is None else ref_logp.data_ptr(),
+                     advantages.data_ptr(), weights.data_ptr(), dlogits.data_ptr(), logp.data_ptr(), 0, at, kind, label_type,
+                     no, ni, whole[-1], zso, zsi, *strides, *_rows(dlogits, lead, "dlogits")[2:],
+                     inv_temp, clip_low, clip_high, kl_coef, grad_scale)
+    _check(binding.load_library().odsgd_policy_loss(d, at + 16, 4 * head.numel() - 16, _handle(stream, dev)))
+    return PolicyLoss(head[:4], logp, dlogits)
 
 
 # --------------------------------------------------------------------------- gradient norm and clip
@@ -319,6 +291,7 @@ class GradSet:
             if len({a.numel() for a in arenas}) != 1:
                 raise ValueError("the arenas differ in length")
         self._keep = ([list(g) for g in groups], list(arenas) if arenas is not None else None)
+        self._dev = dev = torch.cuda.current_device()
         per_group = offsets is not None and len(offsets) > 0 and isinstance(offsets[0], (list, tuple))
         rows = []
         for g, tensors in enumerate(groups):
@@ -327,36 +300,37 @@ class GradSet:
                 offs = offsets[g] if per_group else offsets
                 if len(offs) < len(tensors):
                     raise ValueError(f"group {g}: {len(tensors)} tensors, {len(offs)} offsets")
+                if any(o < 0 for o in offs):
+                    raise ValueError("negative offset")
             for k, t in enumerate(tensors):
-                _need(t, f"groups[{g}][{k}]", _FLOATS)
+                kind = _need(t, f"groups[{g}][{k}]", _FLOATS, dev)
                 if not t.is_contiguous():
                     raise ValueError(f"groups[{g}][{k}]: need a contiguous tensor")
-                _on_device(t)
-                rows.append((t.data_ptr(), t.numel(), int(offs[k]) if offs is not None else 0, _TYPE[t.dtype], g))
-        if any(r[2] < 0 for r in rows):
-            raise ValueError("negative offset")
-        tab = (_GradTensor * max(1, len(rows)))(*[_GradTensor(*r) for r in rows])
+                rows.append(_GRAD_TENSOR.pack(t.data_ptr(), t.numel(), int(offs[k]) if offs is not None else 0, kind, g))
         atab, alen = None, 0
         if arenas is not None:
+            for i, a in enumerate(arenas):
+                _need(a, f"arenas[{i}]", (torch.float32,), dev)
             atab = binding._ptr_table([binding._dev_ptr(a, f"arenas[{i}]") for i, a in enumerate(arenas)])
-            _on_device(*arenas)
             alen = arenas[0].numel()
-        self._device = torch.device("cuda", torch.cuda.current_device())
-        _check(self._lib.odsgd_grad_set_create(ctypes.byref(self._h), ctypes.addressof(tab), len(rows), self.n_groups, atab, alen,
-                                               binding._stream_handle(stream)))
+        _check(self._lib.odsgd_grad_set_create(ctypes.byref(self._h), b"".join(rows), len(rows), self.n_groups, atab, alen,
+                                               _handle(stream, dev)))
 
     def _out(self, out: Optional[torch.Tensor], stream) -> torch.Tensor:
         if not self._h:
             raise ValueError("the gradient set is closed")
         if out is None:
-            return _empty((self.n_groups,), torch.float32, self._device, stream)
-        binding._dev_ptr(out, "out", self.n_groups)
+            with torch.cuda.stream(stream):
+                return torch.empty(self.n_groups, dtype=torch.float32, device=torch.device("cuda", self._dev))
+        _need(out, "out", (torch.float32,), self._dev)
+        if out.numel() != self.n_groups or not out.is_contiguous():
+            raise ValueError(f"out: need {self.n_groups} contiguous elements")
         return out
 
     def norm(self, *, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The 2-norm of each group over all its tensors (float32); nothing else is written."""
         out = self._out(out, stream)
-        _check(self._lib.odsgd_grad_set_norm(self._h, out.data_ptr(), binding._stream_handle(stream)))
+        _check(self._lib.odsgd_grad_set_norm(self._h, out.data_ptr(), _handle(stream, self._dev)))
         return out
 
     def clip(self, max_norm: float, *, out: Optional[torch.Tensor] = None,
@@ -364,7 +338,7 @@ class GradSet:
         """Scales each group by min(1, max_norm / norm), into its arena or in place; returns the
         norms of before."""
         out = self._out(out, stream)
-        _check(self._lib.odsgd_grad_set_clip(self._h, max_norm, out.data_ptr(), binding._stream_handle(stream)))
+        _check(self._lib.odsgd_grad_set_clip(self._h, max_norm, out.data_ptr(), _handle(stream, self._dev)))
         return out
 
     def close(self) -> None:
