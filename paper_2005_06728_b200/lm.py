@@ -30,9 +30,9 @@ from .binding import OK, OdsgdError
 F32, BF16, F16, I32, I64 = 0, 1, 2, 3, 4
 MAX_TOKENS = 1 << 24
 
-_TYPE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.int32: I32, torch.int64: I64}
-_FLOATS = (torch.float32, torch.bfloat16, torch.float16)
-_INTS = (torch.int32, torch.int64)
+_FLOATS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_FLOAT32 = {torch.float32: F32}
+_INTS = {torch.int32: I32, torch.int64: I64}
 
 # odsgd_embed_desc, odsgd_policy_desc and odsgd_grad_tensor of include/odsgd.h, packed by struct: a call is
 # a few microseconds, and filling a ctypes structure would be one of them.
@@ -63,13 +63,16 @@ def _check(rc: int) -> None:
         raise OdsgdError(rc, binding.load_library().odsgd_last_error(None).decode())
 
 
-def _need(t: torch.Tensor, name: str, dtypes, dev: int) -> int:
-    """The type code of a tensor of one of `dtypes` on the current device, `dev`."""
-    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or not t.is_cuda:
-        raise TypeError(f"{name}: need a CUDA tensor of {' / '.join(str(d) for d in dtypes)}")
-    if t.get_device() != dev:
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
-    return _TYPE[t.dtype]
+def _need(t: torch.Tensor, name: str, codes: dict, dev: int) -> int:
+    """The code of a tensor of one of the types of `codes` on the current device, `dev`."""
+    if isinstance(t, torch.Tensor):
+        code = codes.get(t.dtype)
+        if code is not None:
+            if t.get_device() == dev:
+                return code
+            if t.is_cuda:
+                raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
+    raise TypeError(f"{name}: need a CUDA tensor of {' / '.join(str(d) for d in codes)}")
 
 
 def _shape(t: torch.Tensor, shape, name: str) -> None:
@@ -77,18 +80,27 @@ def _shape(t: torch.Tensor, shape, name: str) -> None:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
-def _levels(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int, int, int]:
-    """(n_outer, n_inner, stride_outer, stride_inner) of the first `lead` axes."""
+# Tensors are passed to the library as [outer][inner], or [outer][inner][last], with two strides.
+
+def _sizes(shape) -> Tuple[int, int]:
+    """(outer, inner) of leading axes."""
+    if len(shape) == 2:
+        return shape
+    outer = 1
+    for n in shape[:-1]:
+        outer *= n
+    return outer, shape[-1] if len(shape) else 1
+
+
+def _levels(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int]:
+    """Strides of the two levels that the first `lead` axes make."""
+    stride = t.stride()
     if lead == 2:
-        s, st = t.shape, t.stride()
-        return s[0], s[1], st[0], st[1]
-    if lead == 1:
-        return 1, t.shape[0], 0, t.stride(0)
-    if lead == 0:
-        return 1, 1, 0, 0
-    shape, stride = list(t.shape[:lead]), list(t.stride()[:lead])
+        return stride[:2]
+    if lead < 2:
+        return (0, stride[0]) if lead else (0, 0)
     outer, step = 1, 0  # all but the last leading axis fold into one level
-    for n, s in reversed(list(zip(shape[:-1], stride[:-1]))):
+    for n, s in reversed(list(zip(t.shape[:lead - 1], stride[:lead - 1]))):
         if n == 1:
             continue
         if outer == 1:
@@ -96,22 +108,24 @@ def _levels(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int, int, int]:
         elif s != outer * step:
             raise ValueError(f"{name}: its leading axes do not fold into two strided levels (make it contiguous)")
         outer *= n
-    return outer, shape[-1], step, stride[-1]
+    return step, stride[lead - 1]
 
 
-def _rows(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int, int, int]:
+def _rows(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int]:
     """The same of a tensor with one more axis, which has to be contiguous."""
-    if t.dim() == 0 or (t.stride(-1) != 1 and t.shape[-1] != 1):
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
         raise ValueError(f"{name}: the last axis must be contiguous")
     return _levels(t, lead, name)
 
 
 def _new(like: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """Memory of the stream that the work runs on."""
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(stream):
-        return like.new_empty(shape, dtype=dtype)
+    """Contiguous memory of the stream that the work runs on; `shape` None: like's."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _new(like, shape, dtype, None)
+    if shape is None:
+        return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
+    return like.new_empty(shape, dtype=dtype)
 
 
 # The current stream's handle without the Stream object around it (a third of a small call).
@@ -153,7 +167,7 @@ def embed_lookup(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.
     _shape(out, shape, "out")
     lead = tokens.dim()
     d = _EMBED.pack(tokens.data_ptr(), out.data_ptr(), table.data_ptr(), token_type, out_type, table_type, 0,
-                    *_levels(tokens, lead, "tokens"), *_rows(out, lead, "out")[2:], vocab, dim, stride, -1, scale)
+                    *_sizes(tokens.shape), *_levels(tokens, lead, "tokens"), *_rows(out, lead, "out"), vocab, dim, stride, -1, scale)
     _check(binding.load_library().odsgd_embed_lookup(d, _handle(stream, dev)))
     return out
 
@@ -167,12 +181,12 @@ def embed_grad(tokens: torch.Tensor, grad: torch.Tensor, dtable: torch.Tensor, *
     dev = torch.cuda.current_device()
     token_type = _need(tokens, "tokens", _INTS, dev)
     grad_type = _need(grad, "grad", _FLOATS, dev)
-    _need(dtable, "dtable", (torch.float32,), dev)
+    _need(dtable, "dtable", _FLOAT32, dev)
     vocab, dim, stride = _table(dtable, "dtable")
     _shape(grad, (*tokens.shape, dim), "grad")
     lead = tokens.dim()
     d = _EMBED.pack(tokens.data_ptr(), grad.data_ptr(), dtable.data_ptr(), token_type, grad_type, F32, 1 if accumulate else 0,
-                    *_levels(tokens, lead, "tokens"), *_rows(grad, lead, "grad")[2:], vocab, dim, stride,
+                    *_sizes(tokens.shape), *_levels(tokens, lead, "tokens"), *_rows(grad, lead, "grad"), vocab, dim, stride,
                     -1 if padding_token is None else padding_token, scale)
     lib = binding.load_library()
     if workspace is None:
@@ -187,8 +201,7 @@ def embed_grad(tokens: torch.Tensor, grad: torch.Tensor, dtable: torch.Tensor, *
 
 def embed_grad_workspace(tokens: torch.Tensor, grad: torch.Tensor, dtable: torch.Tensor) -> int:
     """Bytes of workspace that embed_grad needs for tensors of these shapes and types."""
-    no, ni, _, _ = _levels(tokens, tokens.dim(), "tokens")
-    d = _EMBED.pack(0, 0, 0, _TYPE[tokens.dtype], _TYPE[grad.dtype], F32, 0, no, ni, 0, 0, 0, 0,
+    d = _EMBED.pack(0, 0, 0, _INTS[tokens.dtype], _FLOATS[grad.dtype], F32, 0, *_sizes(tokens.shape), 0, 0, 0, 0,
                     dtable.shape[0], dtable.shape[1], dtable.shape[1], -1, 1.0)
     need = ctypes.c_size_t()
     _check(binding.load_library().odsgd_embed_grad_workspace(d, ctypes.byref(need)))
@@ -204,14 +217,14 @@ def token_logprob(logits: torch.Tensor, labels: torch.Tensor, *, inv_temp: float
     dev = torch.cuda.current_device()
     kind = _need(logits, "logits", _FLOATS, dev)
     label_type = _need(labels, "labels", _INTS, dev)
-    lead = labels.dim()
-    no, ni, zso, zsi = _rows(logits, lead, "logits")
-    shape = labels.shape
-    _shape(logits, (*shape, logits.shape[-1]), "logits")
-    _, _, lso, lsi = _levels(labels, lead, "labels")
-    logp, lse = _new(logits, shape, torch.float32, stream), _new(logits, shape, torch.float32, stream)
+    shape, whole = labels.shape, logits.shape
+    lead = len(shape)
+    if len(whole) != lead + 1 or whole[:-1] != shape:
+        raise ValueError(f"labels: shape {tuple(shape)}, expected {tuple(whole[:-1])}")
+    strides = (*_rows(logits, lead, "logits"), *_levels(labels, lead, "labels"))
+    logp, lse = _new(labels, None, torch.float32, stream), _new(labels, None, torch.float32, stream)
     d = _POLICY.pack(logits.data_ptr(), labels.data_ptr(), 0, 0, 0, 0, 0, logp.data_ptr(), lse.data_ptr(), 0, kind, label_type,
-                     no, ni, logits.shape[-1], zso, zsi, lso, lsi, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, inv_temp, 0.0, 0.0, 0.0, 0.0)
+                     *_sizes(shape), whole[-1], *strides, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, inv_temp, 0.0, 0.0, 0.0, 0.0)
     _check(binding.load_library().odsgd_token_logprob(d, _handle(stream, dev)))
     return TokenLogprob(logp, lse)
 
@@ -230,33 +243,33 @@ def policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tens
     label_type = _need(labels, "labels", _INTS, dev)
     shape, whole = labels.shape, logits.shape
     lead = len(shape)
-    if whole[:-1] != shape or len(whole) == 0:
+    if len(whole) != lead + 1 or whole[:-1] != shape:
         raise ValueError(f"labels: shape {tuple(shape)}, expected {tuple(whole[:-1])}")
-    no, ni, zso, zsi = _rows(logits, lead, "logits")
 
     def vector(t, name):
-        if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.get_device() != dev or t.shape != shape:
-            _need(t, name, (torch.float32,), dev)
+        _need(t, name, _FLOAT32, dev)
+        if t.shape != shape:
             _shape(t, shape, name)
-        return t.stride() if lead == 2 else _levels(t, lead, name)[2:]
+        return t.stride() if lead == 2 else _levels(t, lead, name)
 
-    strides = (*_levels(labels, lead, "labels")[2:], *vector(old_logp, "old_logp"),
+    strides = (*_rows(logits, lead, "logits"), *_levels(labels, lead, "labels"), *vector(old_logp, "old_logp"),
                *((0, 0) if ref_logp is None else vector(ref_logp, "ref_logp")),
                *vector(advantages, "advantages"), *vector(weights, "weights"))
     if dlogits is None:
-        dlogits = _new(logits, whole, logits.dtype, stream)
+        dlogits = _new(logits, None, None, stream)
     else:
-        _need(dlogits, "dlogits", (logits.dtype,), dev)
+        _need(dlogits, "dlogits", {logits.dtype: kind}, dev)
         _shape(dlogits, whole, "dlogits")
-    n = no * ni
+    outer, inner = _sizes(shape)
+    n = outer * inner
     head = _new(logits, 4 + max(4, 3 * n), torch.float32, stream)  # the four sums, and the workspace (12 bytes a row)
-    logp = _new(logits, shape, torch.float32, stream)
+    logp = _new(labels, None, torch.float32, stream)
     at = head.data_ptr()
     d = _POLICY.pack(logits.data_ptr(), labels.data_ptr(), old_logp.data_ptr(), 0 if ref_logp is None else ref_logp.data_ptr(),
                      advantages.data_ptr(), weights.data_ptr(), dlogits.data_ptr(), logp.data_ptr(), 0, at, kind, label_type,
-                     no, ni, whole[-1], zso, zsi, *strides, *_rows(dlogits, lead, "dlogits")[2:],
+                     outer, inner, whole[-1], *strides, *_rows(dlogits, lead, "dlogits"),
                      inv_temp, clip_low, clip_high, kl_coef, grad_scale)
-    _check(binding.load_library().odsgd_policy_loss(d, at + 16, 4 * head.numel() - 16, _handle(stream, dev)))
+    _check(binding.load_library().odsgd_policy_loss(d, at + 16, 12 * n if n > 1 else 16, _handle(stream, dev)))
     return PolicyLoss(head[:4], logp, dlogits)
 
 
@@ -310,7 +323,7 @@ class GradSet:
         atab, alen = None, 0
         if arenas is not None:
             for i, a in enumerate(arenas):
-                _need(a, f"arenas[{i}]", (torch.float32,), dev)
+                _need(a, f"arenas[{i}]", _FLOAT32, dev)
             atab = binding._ptr_table([binding._dev_ptr(a, f"arenas[{i}]") for i, a in enumerate(arenas)])
             alen = arenas[0].numel()
         _check(self._lib.odsgd_grad_set_create(ctypes.byref(self._h), b"".join(rows), len(rows), self.n_groups, atab, alen,
@@ -322,7 +335,7 @@ class GradSet:
         if out is None:
             with torch.cuda.stream(stream):
                 return torch.empty(self.n_groups, dtype=torch.float32, device=torch.device("cuda", self._dev))
-        _need(out, "out", (torch.float32,), self._dev)
+        _need(out, "out", _FLOAT32, self._dev)
         if out.numel() != self.n_groups or not out.is_contiguous():
             raise ValueError(f"out: need {self.n_groups} contiguous elements")
         return out
