@@ -603,3 +603,46 @@ def test_refusals():
         st.norm()
     lm.GradSet([[g, g[50:]]], offsets=[0, 100], arenas=[flat])  # sources may share memory
     torch.cuda.synchronize()
+
+
+# --------------------------------------------------------------------------- the calls together
+
+def test_policy_example_learns_and_repeats():
+    """The example's workers find most of the right answers (chance is 1 in 61), and a second run has
+    the same bits."""
+    from paper_2005_06728_b200 import policy_example
+
+    a = policy_example.train(steps=120)
+    assert sum(a.rewards[:10]) / 10 < 0.1 and sum(a.rewards[-10:]) / 10 > 0.5
+    assert max(max(n) for n in a.norms) > 0.5, "some gradients were clipped"
+    b = policy_example.train(steps=120)
+    assert torch.equal(a.weights, b.weights) and a.losses == b.losses and a.norms == b.norms
+
+
+def test_chain_against_autograd():
+    """Lookup, two products, loss and both gradients against torch's derivative of the 64-bit loss.
+    The longest sums have 400 terms and there are four of them one after another: 4 * 400 u = 1e-4
+    of the sums of magnitudes, which here stay within a few times the results' norm."""
+    V, D, B, S = 53, 24, 5, 80
+    tok, y = tokens_of((B, S), V, 110), tokens_of((B, S), V, 111, bad=False)
+    E, H = randn(V, D, seed=112, sigma=0.5), randn(V, D, seed=113, sigma=0.4)
+    x = lm.embed_lookup(tok, E, scale=2.0)
+    z = x @ H.t()
+    old, adv, w, ref = policy_inputs(z, y, 114, 1.25)
+    r = lm.policy_loss(z, y, old, adv, w, ref_logp=ref, clip_low=0.2, clip_high=0.28, kl_coef=0.07, inv_temp=1.25)
+    dz = r.dlogits.view(-1, V)
+    dH = dz.t() @ x.view(-1, D)
+    dE = lm.embed_grad(tok, (dz @ H).view(B, S, D), torch.empty_like(E), scale=2.0)
+    e64, h64 = E.double().cpu().requires_grad_(), H.double().cpu().requires_grad_()
+    t = tok.cpu()
+    ok = (t >= 0) & (t < V)
+    x64 = e64[t.clamp(0, V - 1)] * 2.0 * ok[..., None]
+    lp = torch.log_softmax(x64 @ h64.t() * 1.25, -1).gather(-1, y.cpu()[..., None])[..., 0]
+    rt = torch.exp(lp - R.host(old))
+    pg = -torch.minimum(rt * R.host(adv), rt.clamp(0.8, 1.28) * R.host(adv))
+    d = R.host(ref) - lp
+    loss = (R.host(w) * (pg + 0.07 * (torch.expm1(d) - d))).sum()
+    loss.backward()
+    assert abs(float(r.loss) - float(loss.detach())) <= 1e-4 * float((R.host(w) * R.host(adv).abs()).sum())
+    for got, want in ((dE, e64.grad), (dH, h64.grad)):
+        assert float((R.host(got) - want).norm()) <= 1e-4 * float(want.norm())
