@@ -130,11 +130,6 @@ __device__ __forceinline__ F2 operator*(F2 a, F2 b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
     return r;
 }
-__device__ __forceinline__ F2 multiply_add(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
 
 // Negative infinity in every lane.
 template <typename T>
@@ -210,35 +205,23 @@ struct MaxSum {
     float m, s;
 };
 
-// exp(c (z - m)) in the precision the row's type deserves.
-//   32-bit logits: expf.
-//   16-bit logits: the base-2 exponential of the special-function unit (2^-22 relative, far below the
-//   2^-8 or 2^-11 that the gradient is rounded to) of one multiply-add, c2 z - c2 m with
-//   c2 = c / ln 2.  The rounding of c2 m is common to all elements: `fix` takes it back out of
-//   their sum or factor.  Where c2 m would overflow (a mask of the type's lowest value), z that differ
-//   are so far apart that any c gives 0, and 2^-64 makes both products exact and small.
+// exp(c (z - m)) in the precision the row's type deserves: 32-bit logits through expf; 16-bit ones
+// through the base-2 exponential of the special-function unit (2^-22 relative, far below the 2^-8 or
+// 2^-11 that the gradient is rounded to).  The difference comes first: the largest element has
+// exactly 1, and c m alone would overflow where a mask holds the type's lowest value.
 template <typename T>
 struct RowExp {
-    float c, m, fix;
-    __device__ __forceinline__ RowExp(float inv_temp, float m_) : c(inv_temp), m(m_), fix(1.0f) {
-        if constexpr (sizeof(T) == 2) {
-            c = inv_temp * 1.4426950408889634f;
-            if (fabsf(m_ * c) > 1e37f) c = 5.421010862427522e-20f;
-            m = m_ * c;
-            fix = fmaf(fmaf(m_, c, -m), -0.6931471805599453f, 1.0f);
-        }
-    }
+    float c, m;
+    __device__ __forceinline__ RowExp(float inv_temp, float m_) : c(sizeof(T) == 4 ? inv_temp : inv_temp * 1.4426950408889634f), m(m_) {}
+    __device__ __forceinline__ F2 exponent(float z0, float z1) const { return (f2(z0, z1) + f2(-m, -m)) * f2(c, c); }
     __device__ __forceinline__ F2 operator()(float z0, float z1) const {
         float t0, t1;
-        if constexpr (sizeof(T) == 4) {
-            return f2(expf((z0 - m) * c), expf((z1 - m) * c));
-        } else {
-            split(multiply_add(f2(z0, z1), f2(c, c), f2(-m, -m)), t0, t1);
-            float r0, r1;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(t0));
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(t1));
-            return f2(r0, r1);
-        }
+        split(exponent(z0, z1), t0, t1);
+        if constexpr (sizeof(T) == 4) return f2(expf(t0), expf(t1));
+        float r0, r1;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(t0));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(t1));
+        return f2(r0, r1);
     }
 };
 
@@ -352,7 +335,7 @@ __device__ __forceinline__ MaxSum add_vectors(MaxSum x, const uint4 (&q)[kRowVec
     }
     float s0, s1;
     split(sum, s0, s1);
-    return MaxSum{m, fmaf(x.s, rebase(x.m, m, inv_temp), (s0 + s1) * e.fix)};
+    return MaxSum{m, fmaf(x.s, rebase(x.m, m, inv_temp), s0 + s1)};
 }
 
 // A row's inputs besides its logits.
@@ -399,7 +382,7 @@ template <typename T>
 struct RowGradient {
     RowExp<T> e;
     float neg;  // -k / s
-    __device__ __forceinline__ RowGradient(float inv_temp, float m, float neg_) : e(inv_temp, m), neg(neg_ * e.fix) {}
+    __device__ __forceinline__ RowGradient(float inv_temp, float m, float neg_) : e(inv_temp, m), neg(neg_) {}
     __device__ __forceinline__ uint4 operator()(const uint4& q) const {
         constexpr int L = kLanes<T>;
         float p[L];
