@@ -230,7 +230,7 @@ struct GradShape {
     unsigned n, blocks, block;
     int64_t pitch;
     int bits, passes;
-    size_t at_key[2], at_pos[2], at_counts, at_runs, at_head, at_tail, bytes;
+    size_t at_key[2], at_pos[2], at_counts, at_named, at_runs, at_head, at_tail, bytes;
 };
 
 GradShape grad_shape(const odsgd_embed_desc* d) {
@@ -257,6 +257,7 @@ GradShape grad_shape(const odsgd_embed_desc* d) {
         s.at_pos[i] = take(4 * (size_t)s.n);
     }
     s.at_counts = take(8);
+    s.at_named = take((size_t)ceil_div(d->vocab, 32) * 4);
     s.at_runs = take(sizeof(SpanRun) * (size_t)s.blocks);
     s.at_head = take(4 * (size_t)s.blocks * s.pitch);
     s.at_tail = take(4 * (size_t)s.blocks * s.pitch);
@@ -270,7 +271,7 @@ int launch_sum(const EmbedGradArgs& a, const GradShape& s, bool vec_ok, void* st
     const int64_t cols = ceil_div(a.dim, vec ? Piece<T, true>::W : Piece<T, false>::W);
     const int64_t slabs = ceil_div(cols, kSumThreads);
     const unsigned threads = (unsigned)(ceil_div(ceil_div(cols, slabs), 32) * 32);
-    const dim3 grid(s.blocks, (unsigned)slabs);
+    const dim3 grid(s.blocks + a.fills, (unsigned)slabs);
     return vec ? launch("embedding gradient kernel", sum_kernel<T, true>, grid, dim3(threads), 0, 1, stream, a)
                : launch("embedding gradient kernel", sum_kernel<T, false>, grid, dim3(threads), 0, 1, stream, a);
 }
@@ -643,9 +644,20 @@ int odsgd_embed_grad(const odsgd_embed_desc* d, void* workspace, size_t workspac
         a.block = s.block;
         a.passes = s.passes;
         a.bits = s.bits;
-        const unsigned fill = (unsigned)std::min<int64_t>(kFillClusters, ceil_div(a.vocab * a.dim * 4, kFillBytes));
-        const unsigned clusters = 1 + (a.accumulate ? 0 : fill);
-        rc = launch("token sort kernel", sort_kernel, dim3(clusters * kSortCluster), dim3(kSortThreads), kSortSmem, 1, stream, a);
+        // Zeros beside the sort: for few tokens 128 MB (all of 65 MB beside 500 tokens: 21 us, 24 MB of it
+        // 27), else as many as the digit passes take time for, some 10 us and 0.8 us per thousand tokens
+        // (131072 tokens, 537 MB: 199 us at 4000 bytes a token, 216 at 2000).
+        int64_t early = 0;
+        if (!a.accumulate) {
+            const int64_t bytes = s.n <= (unsigned)kSortThreads ? 128 << 20 : (50 << 20) + (int64_t)s.n * 4000;
+            early = std::min<int64_t>(a.vocab, ceil_div(bytes / (a.dim * 4), kFillRows) * kFillRows);
+            if (s.n == 0) early = a.vocab;
+            a.fills = (unsigned)ceil_div(a.vocab - early, kFillRows);
+        }
+        a.early = (unsigned)early;
+        a.named = reinterpret_cast<unsigned*>(ws + s.at_named);
+        const unsigned fill = (unsigned)std::min<int64_t>(kFillClusters, ceil_div(early * a.dim * 4, kFillBytes));
+        rc = launch("token sort kernel", sort_kernel, dim3((1 + fill) * kSortCluster), dim3(kSortThreads), kSortSmem, 1, stream, a);
         if (rc != ODSGD_OK || s.n == 0) return rc;
         a.wide = rows_aligned(a.table, 4, 0, a.stride, 1, a.vocab, 32);
         const bool vec = aligned16(a.table) && a.stride % 4 == 0 &&

@@ -663,13 +663,14 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
 // ------------------------------------------------------------------ embedding gradient
 // Three launches.
 //   sort_kernel  One cluster sorts the tokens' positions by token, stably (least significant digit
-//                first, up to 9 bits a pass), and lists the tokens whose run crosses a block boundary.  The
-//                other clusters of the grid meanwhile write zeros to the rows that no token names
-//                (they need the tokens, not their order), which hides the sort.
+//                first, up to 9 bits a pass), marks the tokens that occur, and lists those whose run crosses a
+//                block boundary.  The other CTAs of the grid meanwhile write zeros to the first
+//                `early` rows of the table, as many as the sort takes time for, named or not.
 //   sum_kernel   A CTA takes `block` consecutive sorted positions and a slab of columns, and adds
 //                runs of equal tokens in 32 bits.  A run inside the block is written to the table,
 //                the part of one that crosses a boundary to the workspace.  Work is split by
 //                position, so a token that fills half the batch costs no more than rare ones.
+//                Further CTAs, spread among these, write zeros to the other rows that no token names.
 //   join_kernel  Adds the parts of the runs that cross boundaries, in order.
 // The order of every sum depends on sizes and tokens alone.
 constexpr int kSortCluster = 8;
@@ -678,9 +679,9 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortBits = 9;
 constexpr int kSortRadix = 1 << kSortBits;
 constexpr int kSortSmem = (kSortWarps * kSortRadix + 2 * kSortRadix + kSortWarps) * 4;
-constexpr int kFillClusters = 70;   // most clusters that write zeros, ...
-constexpr int kFillBytes = 1 << 20;  // ... each at least so many of the table
-constexpr int kFillRows = 1 << 17;  // rows a CTA marks at a time: 16 KB of bits
+constexpr int kFillClusters = 1000;  // most clusters that write zeros beside the sort, ...
+constexpr int kFillBytes = 1 << 18;  // ... each at least so many of the table
+constexpr int kFillRows = 32;        // rows of a CTA that writes zeros beside the sums: one word of marks
 
 struct SpanRun {
     unsigned token, first, last;  // blocks [first, last]
@@ -700,6 +701,9 @@ struct EmbedGradArgs {
     unsigned* key[2];
     unsigned* pos[2];
     unsigned* counts;  // [0] spanning runs
+    unsigned* named;   // a bit for each row from `early` on: some token names it
+    unsigned early;    // a multiple of kFillRows, or vocab
+    unsigned fills;    // CTAs of sum_kernel that write zeros
     SpanRun* runs;
     float* head;  // [blocks][pitch]: part of the run that began in an earlier block
     float* tail;  // [blocks][pitch]: first part of a run that goes on in the next block
@@ -722,10 +726,23 @@ __device__ __forceinline__ void token_keys(const EmbedGradArgs& a, unsigned t, u
     for (int k = 0; k < kKeyBatch; ++k) key[k] = x[k] >= 0 && x[k] < a.vocab && x[k] != a.padding ? (unsigned)x[k] : (unsigned)a.vocab;
 }
 
-// Of the sorted tokens, those whose run crosses a block boundary: the first boundary inside the run
-// lists it, with the block its last position lies in.
+__device__ __forceinline__ void clear_marks(const EmbedGradArgs& a, unsigned thread, unsigned threads) {
+    if (a.fills == 0) return;
+    const unsigned words = ((unsigned)a.vocab - a.early + 31) / 32;
+    for (unsigned i = thread; i < words; i += threads) a.named[i] = 0;
+}
+
+// Of the sorted tokens: marks the rows that are named, and lists the runs that cross a block
+// boundary (the first boundary inside the run does, with the block its last position lies in).
 __device__ __forceinline__ void list_runs(const EmbedGradArgs& a, unsigned thread, unsigned threads) {
     const unsigned* key = a.key[a.passes & 1];
+    if (a.fills > 0) {
+#pragma unroll 4
+        for (unsigned t = thread; t < a.n; t += threads) {
+            const unsigned k = __ldcg(key + t), row = k - a.early;
+            if (k >= a.early && k < (unsigned)a.vocab && (t == 0 || __ldcg(key + t - 1) != k)) atomicOr(a.named + row / 32, 1u << row % 32);
+        }
+    }
     for (unsigned t = (thread + 1) * a.block; t < a.n; t += threads * a.block) {
         const unsigned k = __ldcg(key + t);
         if (k != (unsigned)a.vocab && __ldcg(key + t - 1) == k && (t == a.block || __ldcg(key + t - a.block - 1) != k)) {
@@ -751,6 +768,7 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
     per = (per + 31) / 32 * 32;
     const unsigned lo = min(a.n, (rank * kSortWarps + warp) * per), hi = min(a.n, lo + per);
     if (rank == 0 && tid == 0) a.counts[0] = 0;
+    clear_marks(a, rank * kSortThreads + tid, kSortCluster * kSortThreads);
     for (int pass = 0; pass < a.passes; ++pass) {
         const unsigned* kin = a.key[pass & 1];
         const unsigned* pin = a.pos[pass & 1];
@@ -849,6 +867,7 @@ __device__ __forceinline__ void sort_few_tokens(const EmbedGradArgs& a, unsigned
     unsigned key[kKeyBatch];
     token_keys(a, tid, a.n, key);  // the first of the batch; the others lie beyond n
     if (tid == 0) a.counts[0] = 0;
+    clear_marks(a, tid, kSortThreads);
     unsigned long long x = (unsigned long long)key[0] << 32 | tid;
     for (unsigned size = 2; size <= kSortThreads; size *= 2) {
         if (size > 32 && size / 2 >= a.n) break;  // what lies beyond n is in its place already
@@ -875,33 +894,6 @@ __device__ __forceinline__ void sort_few_tokens(const EmbedGradArgs& a, unsigned
     list_runs(a, tid, kSortThreads);
 }
 
-// Zeros in the rows of [r0, r1) that no token names.
-__device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, unsigned* bits, long long r0, long long r1) {
-    const unsigned rows = (unsigned)(r1 - r0);
-    for (unsigned i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) bits[i] = 0;
-    __syncthreads();
-    for (unsigned t = threadIdx.x; t < a.n; t += kKeyBatch * blockDim.x) {
-        unsigned key[kKeyBatch];
-        token_keys(a, t, blockDim.x, key);
-#pragma unroll
-        for (int k = 0; k < kKeyBatch; ++k) {
-            const unsigned r = key[k] - (unsigned)r0;
-            if (r < rows) atomicOr(bits + (r >> 5), 1u << (r & 31));  // (`vocab` lies behind r1)
-        }
-    }
-    __syncthreads();
-    const bool vec = (reinterpret_cast<uintptr_t>(a.table) & 15) == 0 && a.stride % 4 == 0;
-    const unsigned lane = threadIdx.x & 31;
-    for (unsigned r = threadIdx.x >> 5; r < rows; r += blockDim.x >> 5) {
-        if ((bits[r >> 5] >> (r & 31)) & 1) continue;
-        float* row = a.table + (r0 + r) * a.stride;
-        const long long n4 = vec ? a.dim / 4 : 0;
-        for (long long j = lane; j < n4; j += 32) __stcs(reinterpret_cast<float4*>(row) + j, make_float4(0, 0, 0, 0));
-        for (long long j = n4 * 4 + lane; j < a.dim; j += 32) __stcs(row + j, 0.0f);
-    }
-    __syncthreads();
-}
-
 __global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kSortCluster, 1, 1)
     sort_kernel(const __grid_constant__ EmbedGradArgs a) {
     extern __shared__ __align__(8) unsigned smem[];
@@ -911,10 +903,23 @@ __global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kSortCluster, 1
         else if (blockIdx.x == 0) sort_few_tokens(a, reinterpret_cast<unsigned long long*>(smem));
         return;
     }
-    const long long ctas = gridDim.x - kSortCluster, me = blockIdx.x - kSortCluster;
-    const long long per = (a.vocab + ctas - 1) / ctas;
-    const long long lo = me * per, hi = lo + per < a.vocab ? lo + per : a.vocab;
-    for (long long r = lo; r < hi; r += kFillRows) fill_rows(a, smem, r, r + kFillRows < hi ? r + kFillRows : hi);
+    const unsigned ctas = gridDim.x - kSortCluster, me = blockIdx.x - kSortCluster;
+    const unsigned per = (a.early + ctas - 1) / ctas, lo = min(a.early, me * per), hi = min(a.early, lo + per);
+    const bool vec = (reinterpret_cast<uintptr_t>(a.table) & 15) == 0 && a.stride % 4 == 0;
+    if (vec && a.stride == a.dim) {  // one piece of memory
+        float4* p = reinterpret_cast<float4*>(a.table + lo * a.dim);
+        const long long n4 = (long long)(hi - lo) * a.dim / 4;
+#pragma unroll 4
+        for (long long j = threadIdx.x; j < n4; j += kSortThreads) __stcs(p + j, make_float4(0, 0, 0, 0));
+        return;
+    }
+    const unsigned lane = threadIdx.x & 31;
+    for (unsigned r = lo + (threadIdx.x >> 5); r < hi; r += kSortWarps) {
+        float* row = a.table + r * a.stride;
+        const long long n4 = vec ? a.dim / 4 : 0;
+        for (long long j = lane; j < n4; j += 32) __stcs(reinterpret_cast<float4*>(row) + j, make_float4(0, 0, 0, 0));
+        for (long long j = n4 * 4 + lane; j < a.dim; j += 32) __stcs(row + j, 0.0f);
+    }
 }
 
 constexpr int kSumThreads = 128;
@@ -958,7 +963,33 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
     __shared__ unsigned key[kSumMaxBlock + 2];   // of the positions, and one on either side
     __shared__ const T* row[kSumMaxBlock];
     dependent_launch_prologue();
-    const unsigned i0 = blockIdx.x * a.block, n = min(a.block, a.n - i0);
+    const long long col = (long long)blockIdx.y * blockDim.x * W + threadIdx.x * (VEC ? W : 1), left = a.dim - col;
+    // CTA x writes zeros if the number of those before it grows behind it: they are spread evenly
+    const unsigned fill = (unsigned)((unsigned long long)blockIdx.x * a.fills / gridDim.x);
+    if ((unsigned)((blockIdx.x + 1ull) * a.fills / gridDim.x) != fill) {
+        if (left <= 0) return;
+        const unsigned r0 = a.early + fill * kFillRows, rows = min((unsigned)a.vocab - r0, (unsigned)kFillRows);
+        const unsigned named = a.named[fill];
+        for (unsigned r = 0; r < rows; ++r) {
+            if ((named >> r) & 1) continue;
+            float* p = a.table + (r0 + r) * a.stride + col;
+            const float zero[8] = {};
+            if constexpr (VEC) {
+                if (W == 8 && a.wide) {
+                    store_eight(p, zero);
+                } else {
+#pragma unroll
+                    for (int l = 0; l < W; l += 4) __stcs(reinterpret_cast<float4*>(p + l), make_float4(0, 0, 0, 0));
+                }
+            } else {
+#pragma unroll
+                for (int l = 0; l < W; ++l)
+                    if (l * (int)blockDim.x < left) p[l * (int)blockDim.x] = 0.0f;
+            }
+        }
+        return;
+    }
+    const unsigned me = blockIdx.x - fill, i0 = me * a.block, n = min(a.block, a.n - i0);
     const unsigned none = (unsigned)a.vocab;
     for (unsigned i = threadIdx.x; i < n + 2; i += blockDim.x) {
         const unsigned t = i0 + i - 1;  // wraps to a large number before the first
@@ -969,7 +1000,6 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
         }
     }
     __syncthreads();
-    const long long col = (long long)blockIdx.y * blockDim.x * W + threadIdx.x * (VEC ? W : 1), left = a.dim - col;
     if (left <= 0) return;
     float acc[W];
 #pragma unroll
@@ -991,9 +1021,9 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
             // the run ends, or the block does
             float* dst;
             if (crossed) {
-                dst = a.head + blockIdx.x * a.pitch + col;
+                dst = a.head + me * a.pitch + col;
             } else if (next == here) {
-                dst = a.tail + blockIdx.x * a.pitch + col;
+                dst = a.tail + me * a.pitch + col;
             } else {
                 dst = a.table + here * a.stride + col;
 #pragma unroll
