@@ -593,13 +593,12 @@ typedef struct odsgd_policy_desc {
 int odsgd_token_logprob(const odsgd_policy_desc* desc, void* stream);
 
 /*
- * The loss and its gradient in one pass: each row of logits is read once, kept on the chip while
- * its softmax statistics are joined, and its gradient written (rows of more than
- * ODSGD_RESIDENT_BYTES bytes are read twice).  `workspace` as for odsgd_embed_grad.
+ * The loss and its gradient in one call.  Each row is gone over twice, for its softmax statistics
+ * and for its gradient, by the same CTA, the second time out of the L2: DRAM sees one read of the
+ * logits and one write of their gradient.  `workspace` as for odsgd_embed_grad (12 bytes a row).
  * Errors of both calls: ERR_ARG, ERR_ALIGN, ERR_OVERLAP (an output overlaps an input or another
  * output), ERR_UNSUPPORTED, ERR_CUDA.
  */
-#define ODSGD_RESIDENT_BYTES (1 << 19)
 int odsgd_policy_loss_workspace(const odsgd_policy_desc* desc, size_t* bytes);
 int odsgd_policy_loss(const odsgd_policy_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
 
