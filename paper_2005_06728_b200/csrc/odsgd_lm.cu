@@ -106,6 +106,25 @@ int check_buffers(const Buf* bufs, int n, int64_t n_outer, int64_t n_inner, int 
     return ODSGD_OK;
 }
 
+// A written buffer of `bytes` bytes without rows (sums, workspace) against the others of a call.
+int check_outside(const char* name, const void* p, size_t bytes, const Buf* bufs, int n, int64_t n_outer, int64_t n_inner) {
+    if (n_outer == 0 || n_inner == 0) return ODSGD_OK;
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+    for (int i = 0; i < n; ++i) {
+        Range r;
+        if (range_of(bufs[i], n_outer, n_inner, &r) && lo < r.hi && r.lo < lo + bytes)
+            return fail(ODSGD_ERR_OVERLAP, std::string(name) + " overlaps " + bufs[i].name);
+    }
+    return ODSGD_OK;
+}
+
+int check_workspace(const void* ws, size_t have, size_t need) {
+    if (!ws) return fail(ODSGD_ERR_ARG, "workspace is NULL");
+    if (!aligned16(ws)) return fail(ODSGD_ERR_ALIGN, "workspace is not 16-byte aligned");
+    if (have < need) return fail(ODSGD_ERR_ARG, "workspace has " + std::to_string(have) + " bytes, " + std::to_string(need) + " are needed");
+    return ODSGD_OK;
+}
+
 int cuda_fail(const char* what, cudaError_t e) {
     cudaGetLastError();
     return fail(ODSGD_ERR_CUDA, std::string(what) + ": " + cudaGetErrorString(e));
@@ -160,7 +179,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t kMaxDim = 1 << 20;  // column slabs of every kernel stay below the grid's limit in y
 
 // The lookup writes act, the gradient writes the table.
-int check_embed(const odsgd_embed_desc* d, bool lookup) {
+int check_embed(const odsgd_embed_desc* d, bool lookup, const void* ws = nullptr, size_t ws_bytes = 0) {
     if (!d) return fail(ODSGD_ERR_ARG, "desc is NULL");
     if (!is_token_type(d->token_type)) return fail(ODSGD_ERR_ARG, "token_type must be ODSGD_I32 or ODSGD_I64");
     if (!is_float_type(d->act_type)) return fail(ODSGD_ERR_ARG, "act_type must be ODSGD_F32, ODSGD_BF16 or ODSGD_F16");
@@ -185,6 +204,11 @@ int check_embed(const odsgd_embed_desc* d, bool lookup) {
     const Buf table = {"table", d->table, size_of(d->table_type), 0, d->table_stride, d->dim, !lookup};
     Range t, r;
     if (!range_of(table, 1, d->vocab, &t)) return fail(ODSGD_ERR_UNSUPPORTED, "table is beyond the address range");
+    if (ws) {
+        int rc_ws = check_outside("workspace", ws, ws_bytes, &table, 1, 1, d->vocab);
+        if (rc_ws == ODSGD_OK) rc_ws = check_outside("workspace", ws, ws_bytes, bufs, 2, d->n_outer, d->n_inner);
+        if (rc_ws != ODSGD_OK) return rc_ws;
+    }
     if (d->n_outer == 0 || d->n_inner == 0) return ODSGD_OK;
     for (int i = 0; i < 2; ++i) {
         if (lookup && i == 1) continue;  // two inputs
@@ -289,7 +313,7 @@ int allow_sort_smem() {
 }
 
 // ------------------------------------------------------------------ rows of logits
-int check_policy(const odsgd_policy_desc* d, bool loss) {
+int check_policy(const odsgd_policy_desc* d, bool loss, const void* ws = nullptr, size_t ws_bytes = 0) {
     if (!d) return fail(ODSGD_ERR_ARG, "desc is NULL");
     if (!is_float_type(d->type)) return fail(ODSGD_ERR_ARG, "type must be ODSGD_F32, ODSGD_BF16 or ODSGD_F16");
     if (!is_token_type(d->label_type)) return fail(ODSGD_ERR_ARG, "label_type must be ODSGD_I32 or ODSGD_I64");
@@ -320,15 +344,12 @@ int check_policy(const odsgd_policy_desc* d, bool loss) {
     bufs[n++] = {"weights", d->weights, 4, d->weight_stride_outer, d->weight_stride_inner, 1, false};
     same_ok = n;
     bufs[n++] = {"dlogits", d->dlogits, es, d->dlogits_stride_outer, d->dlogits_stride_inner, d->vocab, true};
-    const int rc = check_buffers(bufs, n, d->n_outer, ni, same_ok);
-    if (rc != ODSGD_OK || d->n_outer == 0 || ni == 0) return rc;
-    const uintptr_t s0 = reinterpret_cast<uintptr_t>(d->stats);
-    for (int i = 0; i < n; ++i) {
-        Range r;
-        range_of(bufs[i], d->n_outer, ni, &r);
-        if (s0 < r.hi && r.lo < s0 + 16) return fail(ODSGD_ERR_OVERLAP, std::string("stats overlaps ") + bufs[i].name);
-    }
-    return ODSGD_OK;
+    int rc = check_buffers(bufs, n, d->n_outer, ni, same_ok);
+    if (rc == ODSGD_OK) rc = check_outside("stats", d->stats, 16, bufs, n, d->n_outer, ni);
+    if (rc != ODSGD_OK || !ws) return rc;
+    const uintptr_t w = reinterpret_cast<uintptr_t>(ws), st = reinterpret_cast<uintptr_t>(d->stats);
+    if (w < st + 16 && st < w + ws_bytes) return fail(ODSGD_ERR_OVERLAP, "workspace overlaps stats");
+    return check_outside("workspace", ws, ws_bytes, bufs, n, d->n_outer, ni);
 }
 
 // How a call cuts its rows: CTAs of a row, threads of a CTA, and which build of the kernel.
@@ -412,16 +433,18 @@ int launch_rows(const odsgd_policy_desc* d, bool loss, float* terms, void* strea
 
 size_t policy_bytes(const odsgd_policy_desc* d) { return std::max<size_t>(16, (size_t)(d->n_outer * d->n_inner) * 12); }
 
-int check_workspace(const void* ws, size_t have, size_t need) {
-    if (!ws) return fail(ODSGD_ERR_ARG, "workspace is NULL");
-    if (!aligned16(ws)) return fail(ODSGD_ERR_ALIGN, "workspace is not 16-byte aligned");
-    if (have < need) return fail(ODSGD_ERR_ARG, "workspace has " + std::to_string(have) + " bytes, " + std::to_string(need) + " are needed");
-    return ODSGD_OK;
-}
+}  // namespace
 
+namespace {
+// Memory that a gradient set reads (kind 0) or writes (1).
+struct Span {
+    uintptr_t lo, hi;
+    int kind;
+};
 }  // namespace
 
 struct odsgd_grad_set {
+    std::vector<Span> spans;  // in ascending order; `norms` may lie in none of them
     int device = 0;
     int n_groups = 0;
     unsigned n_chunks = 0, most_chunks = 0;  // in all, and of a group
@@ -436,11 +459,6 @@ struct odsgd_grad_set {
 };
 
 namespace {
-
-struct Span {
-    uintptr_t lo, hi;
-    int kind;  // 0 read, 1 written
-};
 
 int make_set(odsgd_grad_set* s, const odsgd_grad_tensor* t, size_t n, int n_groups, float* const* arenas, size_t arena_len,
              cudaStream_t stream) {
@@ -477,6 +495,9 @@ int make_set(odsgd_grad_set* s, const odsgd_grad_tensor* t, size_t n, int n_grou
         end_any = std::max(end_any, p.hi);
         if (p.kind == 1) end_written = std::max(end_written, p.hi);
     }
+    // for the check of `norms`: where spans nest, the end of those so far
+    for (size_t i = 1; i < spans.size(); ++i) spans[i].hi = std::max(spans[i].hi, spans[i - 1].hi);
+    s->spans = spans;
     std::stable_sort(order.begin(), order.end(), [&](size_t a, size_t b) { return t[a].group < t[b].group; });
     // chunks of 16384 elements; of 4096 where those would leave SMs without work
     const size_t most = total / 16384 < 148 * 4 ? 4096 : 16384;
@@ -534,6 +555,12 @@ int run_set(odsgd_grad_set* s, bool clip, float max_norm, float* norms, void* st
     if (!clip && !norms) return fail(ODSGD_ERR_ARG, "norms is NULL");
     if (clip && !(max_norm >= 0.0f)) return fail(ODSGD_ERR_ARG, "max_norm is negative or NaN");
     if (reinterpret_cast<uintptr_t>(norms) % 4 != 0) return fail(ODSGD_ERR_ALIGN, "norms is not 4-byte aligned");
+    if (norms) {
+        // of the spans that begin below the end of norms, does one reach into it?
+        const uintptr_t lo = reinterpret_cast<uintptr_t>(norms), hi = lo + 4 * (size_t)s->n_groups;
+        const auto it = std::lower_bound(s->spans.begin(), s->spans.end(), hi, [](const Span& a, uintptr_t x) { return a.lo < x; });
+        if (it != s->spans.begin() && (it - 1)->hi > lo) return fail(ODSGD_ERR_OVERLAP, "norms overlaps a gradient tensor or its place in an arena");
+    }
     int dev = 0;
     int rc = current_device(&dev);
     if (rc != ODSGD_OK) return rc;
@@ -609,6 +636,7 @@ int odsgd_embed_grad(const odsgd_embed_desc* d, void* workspace, size_t workspac
         if (rc != ODSGD_OK) return rc;
         const GradShape s = grad_shape(d);
         rc = check_workspace(workspace, workspace_bytes, s.bytes);
+        if (rc == ODSGD_OK) rc = check_embed(d, false, workspace, s.bytes);
         if (rc != ODSGD_OK) return rc;
         rc = allow_sort_smem();
         if (rc != ODSGD_OK) return rc;
@@ -697,6 +725,7 @@ int odsgd_policy_loss(const odsgd_policy_desc* d, void* workspace, size_t worksp
         int rc = check_policy(d, true);
         if (rc != ODSGD_OK) return rc;
         rc = check_workspace(workspace, workspace_bytes, policy_bytes(d));
+        if (rc == ODSGD_OK) rc = check_policy(d, true, workspace, policy_bytes(d));
         if (rc != ODSGD_OK) return rc;
         StatsArgs st = {};
         st.terms = static_cast<const float*>(workspace);

@@ -92,6 +92,18 @@ def test_lookup_beyond_32_bit_offsets():
 
 # --------------------------------------------------------------------------- embedding gradient
 
+def test_embed_grad_beyond_32_bit_offsets():
+    dt = torch.full((70000, 65536), POISON, device=DEV)  # 4.6e9 elements
+    tok = torch.tensor([69999, 5, 69999, 66001, -1], device=DEV)
+    g = randn(5, 65536, seed=119, dtype=BF16)
+    lm.embed_grad(tok, g, dt, scale=2.0)
+    assert torch.equal(dt[69999], 2 * (g[0].float() + g[2].float())) and torch.equal(dt[66001], 2 * g[3].float())
+    assert torch.equal(dt[5], 2 * g[1].float())
+    for row in (0, 4, 6, 32767, 65535, 65536, 66000, 66002, 69998):
+        assert not bool(dt[row].any()), "rows that no token names are zero"
+    assert float(dt[::7].double().abs().sum()) == float(dt[[r for r in (5, 66001, 69999) if r % 7 == 0]].double().abs().sum())
+
+
 def check_grad(tok, grad, vocab, scale=1.0, padding=None, accumulate=False, offset=0, pad=0):
     dim = grad.shape[-1]
     dt, check = in_poison((vocab, dim), F32, offset, pad)
@@ -321,6 +333,42 @@ def test_policy_loss_masks(dtype, vocab):
     assert bool(torch.isnan(got.stats[0]))
     sc = lm.token_logprob(z, y)
     assert torch.isnan(sc.logp).cpu().tolist() == bad.tolist()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_rows_of_the_lowest_value(dtype):
+    """Nothing but the type's lowest value: every entry equally likely, at any temperature."""
+    vocab = 3001
+    z = torch.full((2, vocab), torch.finfo(dtype).min, dtype=dtype, device=DEV)
+    z[1] = torch.finfo(dtype).max
+    y = torch.tensor([7, 3000], device=DEV)
+    for c in (0.5, 1.0, 2.0):
+        got = lm.token_logprob(z, y, inv_temp=c)
+        assert bool(((got.logp + math.log(vocab)).abs() < 1e-5).all())
+        one = torch.ones(2, device=DEV)
+        p = lm.policy_loss(z, y, got.logp, one, one, inv_temp=c)
+        want = torch.full((2, vocab), c / vocab, dtype=torch.float64)
+        want[0, 7] -= c
+        want[1, 3000] -= c
+        R.within(p.dlogits, want, want.abs() * (R.UNIT[dtype] + 1e-5) + R.TINY[dtype], "dlogits")
+
+
+def test_policy_loss_beyond_32_bit_offsets():
+    rows, vocab = 34000, 131072  # 4.5e9 logits, in place
+    z = torch.empty(rows, vocab, dtype=BF16, device=DEV)
+    for a in range(0, rows, 2000):
+        z[a:a + 2000] = torch.randn(2000, vocab, generator=gen(120 + a), device=DEV, dtype=BF16)
+    pick = torch.tensor([0, 16383, 16384, 32767, 32768, 33999], device=DEV)
+    few = z[pick].clone()
+    y = torch.randint(0, vocab, (rows,), generator=gen(121), device=DEV)
+    adv, w = randn(rows, seed=122), torch.full((rows,), 1.0, device=DEV)
+    old = torch.full((rows,), -12.0, device=DEV)
+    want = lm.policy_loss(few, y[pick], old[pick], adv[pick], w[pick])
+    got = lm.policy_loss(z, y, old, adv, w, dlogits=z)
+    # fewer rows are cut differently: the same sums in another order
+    R.within(got.logp[pick], R.host(want.logp), 2 * R.score_bound(few, 1.0, R.host(want.logp)), "logp")
+    g = R.host(want.dlogits)
+    R.within(z[pick], g, g.abs() * (2 * R.UNIT[BF16] + 1e-4) + R.TINY[BF16], "dlogits")
 
 
 def test_policy_loss_label_of_probability_zero():
@@ -594,6 +642,7 @@ def test_refusals():
     refused(binding.ERR_ARG, lm.GradSet, [[g]], offsets=[301], arenas=[flat])
     refused(binding.ERR_ARG, lm.GradSet, [[g]] * 65)
     st = lm.GradSet([[g]])
+    refused(binding.ERR_OVERLAP, st.clip, 1.0, out=g[99:])
     refused(binding.ERR_ARG, st.clip, -1.0)
     refused(binding.ERR_ARG, st.clip, float("nan"))
     with pytest.raises(ValueError):

@@ -122,6 +122,8 @@ def test_embed_overlaps_and_workspace(lib):
     assert lib.odsgd_embed_grad(embed(), None, 1 << 30, None) == binding.ERR_ARG and "workspace" in err(lib)
     assert lib.odsgd_embed_grad(embed(), ctypes.c_void_p(0x4000008), 1 << 30, None) == binding.ERR_ALIGN
     assert lib.odsgd_embed_grad(embed(), ws, need.value - 1, None) == binding.ERR_ARG and str(need.value) in err(lib)
+    for at in (0x2000000 - 16, 0x3000000 + 4 * 1596, 0x1000000):
+        assert lib.odsgd_embed_grad(embed(), ctypes.c_void_p(at), need.value, None) == binding.ERR_OVERLAP and "workspace" in err(lib)
     big = ctypes.c_size_t()
     assert lib.odsgd_embed_grad_workspace(embed(n_outer=1 << 12, n_inner=1 << 12, dim=4096), ctypes.byref(big)) == binding.OK
     assert big.value > 4 * 4 * (1 << 24), "sizes beyond 32 bits"
@@ -201,6 +203,8 @@ def test_loss_workspace_and_empty_calls(lib):
     assert lib.odsgd_policy_loss(policy(), None, 1 << 20, None) == binding.ERR_ARG
     assert lib.odsgd_policy_loss(policy(), ctypes.c_void_p(0x5000004), 1 << 20, None) == binding.ERR_ALIGN
     assert lib.odsgd_policy_loss(policy(), ctypes.c_void_p(0x5000000), need.value - 1, None) == binding.ERR_ARG
+    for at in (0x1000000, 0x3000000 + 32, 0x4000000, 0x4200000, 0x2000000):
+        assert lib.odsgd_policy_loss(policy(), ctypes.c_void_p(at), need.value, None) == binding.ERR_OVERLAP and "workspace" in err(lib)
     assert lib.odsgd_token_logprob(None, None) == binding.ERR_ARG and lib.odsgd_policy_loss(None, None, 0, None) == binding.ERR_ARG
     assert lib.odsgd_token_logprob(policy(n_inner=0, logits=0, labels=0, logp=0), None) == binding.OK
     # the transposed batch: rows interleave, and do not overlap
