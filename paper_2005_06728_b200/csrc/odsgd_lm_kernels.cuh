@@ -796,9 +796,14 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
         const auto load = [&](unsigned t) {
             if (pass == 0) {
                 token_keys(a, t, 32, key);
+#pragma unroll
+                for (int k = 0; k < kKeyBatch; ++k) pos[k] = t + 32 * k;
             } else {
 #pragma unroll
-                for (int k = 0; k < kKeyBatch; ++k) key[k] = t + 32 * k < hi ? __ldcg(kin + t + 32 * k) : 0;
+                for (int k = 0; k < kKeyBatch; ++k) {
+                    key[k] = t + 32 * k < hi ? __ldcg(kin + t + 32 * k) : 0;
+                    pos[k] = t + 32 * k < hi ? __ldcg(pin + t + 32 * k) : 0;
+                }
             }
         };
         for (unsigned t = lo + lane; t < hi; t += 32 * kKeyBatch) {
@@ -840,19 +845,13 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
         }
         if (lane == 31) wsum[warp] = scan;
         __syncthreads();
-        if (tid < radix) {
-            unsigned below = 0;
-            for (unsigned v = 0; v < warp; ++v) below += wsum[v];
-            base[tid] = below + scan - all + before;
-        }
+        unsigned below = lane < warp ? wsum[lane] : 0;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) below += __shfl_xor_sync(0xffffffffu, below, d);
+        if (tid < radix) base[tid] = below + scan - all + before;
         __syncthreads();
         for (unsigned t0 = lo; t0 < hi; t0 += 32 * kKeyBatch) {
-            load(t0 + lane);
-#pragma unroll
-            for (int k = 0; k < kKeyBatch; ++k) {
-                const unsigned t = t0 + 32 * k + lane;
-                pos[k] = pass == 0 || t >= hi ? t : __ldcg(pin + t);
-            }
+            if (per > 32 * kKeyBatch) load(t0 + lane);  // else all are in registers still
 #pragma unroll
             for (int k = 0; k < kKeyBatch; ++k) {
                 const bool in = t0 + 32 * k + lane < hi;

@@ -161,6 +161,13 @@ def test_embed_grad_token_frequencies(dtype, kind):
     check_grad(tok, grad, vocab, 1.0, padding, accumulate=True)
 
 
+@pytest.mark.parametrize("vocab", [1, 2, 30, 255, 256, 511, 512, 513, 131071, 262144])
+@pytest.mark.parametrize("n", [1024, 1025, 3000, 33000])
+def test_embed_grad_digits(vocab, n):
+    """One to three digit passes of every width, and the two sorts on either side of their border."""
+    check_grad(tokens_of((n,), vocab, 17), randn(n, 4, seed=18), vocab)
+
+
 @pytest.mark.parametrize("n,dim", [(70001, 32), (300000, 8), (4096, 2056)])
 def test_embed_grad_many_tokens(n, dim):
     vocab = 5000
