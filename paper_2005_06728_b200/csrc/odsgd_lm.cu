@@ -381,12 +381,34 @@ RowShape row_shape(int64_t rows, int64_t vocab, int elem, bool loss, int sms) {
     return s;
 }
 
+constexpr int kHoldNarrow = 40 << 10, kHoldWide = 108 << 10;  // shared memory of a CTA: what an SM has, over its CTAs
+
+template <typename T, int THREADS, int CTAS>
+int launch_loss(RowArgs a, const RowShape& s, int hold_bytes, void* stream) {
+    static std::atomic<bool> done[kMaxDevices] = {};
+    int dev = 0;
+    const int rc = current_device(&dev);
+    if (rc != ODSGD_OK) return rc;
+    if (dev >= kMaxDevices || !done[dev].load(std::memory_order_relaxed)) {
+        const cudaError_t e = cudaFuncSetAttribute(row_kernel<T, true, THREADS, CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, hold_bytes);
+        if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute", e);
+        if (dev < kMaxDevices) done[dev].store(true, std::memory_order_relaxed);
+    }
+    // as many whole batches as fit, but for the row's last, which stays in registers
+    const int64_t batch = (int64_t)s.threads * kRowVectors * 16;
+    const int64_t batches = ceil_div(ceil_div(a.vocab / kLanes<T>, s.cluster) * 16, batch);
+    a.hold = (int)std::max<int64_t>(0, std::min(hold_bytes / batch, batches - 1));
+    return launch("policy loss kernel", row_kernel<T, true, THREADS, CTAS>, dim3(a.rows * (unsigned)s.cluster), dim3((unsigned)s.threads),
+                  (size_t)(a.hold * batch), s.cluster, stream, a);
+}
+
 template <typename T>
 int launch_rows_t(const RowArgs& a, const RowShape& s, bool loss, void* stream) {
-    const dim3 grid(a.rows * (unsigned)s.cluster), block((unsigned)s.threads);
-    if (!loss) return launch("score kernel", row_kernel<T, false, kScoreThreads, kScoreCtas>, grid, block, 0, s.cluster, stream, a);
-    return s.wide ? launch("policy loss kernel", row_kernel<T, true, kWideThreads, kWideCtas>, grid, block, 0, s.cluster, stream, a)
-                  : launch("policy loss kernel", row_kernel<T, true, kNarrowThreads, kNarrowCtas>, grid, block, 0, s.cluster, stream, a);
+    if (!loss)
+        return launch("score kernel", row_kernel<T, false, kScoreThreads, kScoreCtas>, dim3(a.rows * (unsigned)s.cluster),
+                      dim3((unsigned)s.threads), 0, s.cluster, stream, a);
+    return s.wide ? launch_loss<T, kWideThreads, kWideCtas>(a, s, kHoldWide, stream)
+                  : launch_loss<T, kNarrowThreads, kNarrowCtas>(a, s, kHoldNarrow, stream);
 }
 
 int launch_rows(const odsgd_policy_desc* d, bool loss, float* terms, void* stream) {

@@ -197,6 +197,7 @@ struct RowArgs {
     unsigned rows, n_inner;
     int wide_labels;
     int cluster;
+    int hold;  // losses: batches of a row that a CTA holds in shared memory
     float inv_temp, clip_low, clip_high, kl_coef, grad_scale;
 };
 
@@ -403,15 +404,15 @@ __device__ __forceinline__ MaxSum single(float z) { return MaxSum{z, z == -CUDAR
 
 // Scores, and the loss with its gradient.  One CTA takes a row (a cluster shares it where rows are
 // few, or so long that the rows in flight would not stay in the L2) and goes over it twice: maximum
-// and sum, then the gradient.  The second reading finds the row in the L2, its last vectors still in
-// registers; DRAM sees about one read and one write (8192 rows of 131072 bf16: 0.66 ms against 0.55
-// for those bytes at the copy rate; 1024 of them: 289 + 210 MB where 250 + 268 are the logits that
-// count and the gradient, part of it still in the L2 at the end).
+// and sum, then the gradient.  The second reading finds the row's first batches in the CTA's shared
+// memory, its last in registers and the rest in the L2; DRAM sees about one read and one write (8192
+// rows of 131072 bf16: 0.62 ms against 0.55 for those bytes at the copy rate; 0.66 with the whole
+// second reading from the L2, which by then has lost a sixth of it).
 // Scores: 8184 rows of 50021 bf16 125 us, 0.98 of the copy rate, in 128-thread CTAs, twelve an SM
 // (182 in 512-thread ones: the more rows in flight, the less the latency of label, row and join
 // shows).  Losses: 256 threads, five an SM, and for rows the L2 holds fewer of 512, two an SM.
 // Four vectors a thread in flight rather than eight: 881 -> 681 us for the wide loss, by the warps
-// that fit.  Without its arithmetic the wide loss takes 617 us.
+// that fit.
 // Measured slower: the row held in registers, or in shared memory with the next rows on their way by
 // asynchronous copies, across a cluster of 4 or 8 CTAs (716-990 us: the cluster's sums are waited for,
 // and clusters of eight leave 16 SMs empty); a quarter or half of the exponentials by a polynomial on
@@ -421,6 +422,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) row_kernel(const __grid_constan
     constexpr int L = kLanes<T>;
     __shared__ MaxSum warp_part[THREADS / 32];
     __shared__ MaxSum cta_part[kRowCluster];
+    extern __shared__ uint4 held[];  // [a.hold][kRowVectors][threads]: each thread's vectors of the first batches
     dependent_launch_prologue();
     const unsigned cs = (unsigned)a.cluster;
     const unsigned row = blockIdx.x / cs, rank = blockIdx.x % cs;
@@ -459,9 +461,19 @@ __global__ void __launch_bounds__(THREADS, CTAS) row_kernel(const __grid_constan
     const int step = threads * kRowVectors;
     uint4 q[kRowVectors];
     int b = 0;
+    const int kept = LOSS ? a.hold * step : 0;  // vectors before this one are held
     for (; b + step <= n; b += step) {
+        if (LOSS && b >= kept) {
 #pragma unroll
-        for (int k = 0; k < kRowVectors; ++k) q[k] = LOSS ? zv[b + k * threads + tid] : __ldcs(zv + b + k * threads + tid);
+            for (int k = 0; k < kRowVectors; ++k) q[k] = zv[b + k * threads + tid];
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRowVectors; ++k) q[k] = __ldcs(zv + b + k * threads + tid);
+        }
+        if (LOSS && b < kept) {
+#pragma unroll
+            for (int k = 0; k < kRowVectors; ++k) held[b + k * threads + tid] = q[k];
+        }
         x = add_vectors<T>(x, q, a.inv_temp);
     }
     if (b < n) {
@@ -515,8 +527,13 @@ __global__ void __launch_bounds__(THREADS, CTAS) row_kernel(const __grid_constan
             if (v >= 0 && v < n) __stcs(to + v, grad(q[k]));
         }
         for (b -= step; b >= 0; b -= step) {
+            if (b < kept) {
 #pragma unroll
-            for (int k = 0; k < kRowVectors; ++k) q[k] = __ldcs(zv + b + k * threads + tid);
+                for (int k = 0; k < kRowVectors; ++k) q[k] = held[b + k * threads + tid];
+            } else {
+#pragma unroll
+                for (int k = 0; k < kRowVectors; ++k) q[k] = __ldcs(zv + b + k * threads + tid);
+            }
 #pragma unroll
             for (int k = 0; k < kRowVectors; ++k) __stcs(to + b + k * threads + tid, grad(q[k]));
         }
