@@ -361,16 +361,18 @@ struct RowShape {
 constexpr int kScoreThreads = 128, kScoreCtas = 12;
 constexpr int kNarrowThreads = 256, kNarrowCtas = 5;
 constexpr int kWideThreads = 512, kWideCtas = 2;
-// Rows in flight are read again from the L2 (126 MB) while their gradients pass through it.
+constexpr int kHoldNarrow = 40 << 10, kHoldWide = 108 << 10;  // shared memory of a full CTA: an SM's, over its CTAs
+// What the rows in flight do not hold on the chip is read again from the L2 (126 MB), while their
+// gradients pass through it.
 constexpr int64_t kRowsInFlightBytes = 80 << 20;
 
 RowShape row_shape(int64_t rows, int64_t vocab, int elem, bool loss, int sms) {
     RowShape s;
     const int64_t vectors = std::max<int64_t>(1, vocab / (16 / elem));
-    s.wide = loss && vectors * 16 * kNarrowCtas * sms > kRowsInFlightBytes;
+    s.wide = loss && (vectors * 16 - kHoldNarrow) * kNarrowCtas * sms > kRowsInFlightBytes;
     s.cluster = 1;
     if (loss)
-        while (s.cluster < kRowCluster && vectors * 16 * kWideCtas * sms > kRowsInFlightBytes * s.cluster) s.cluster *= 2;
+        while (s.cluster < kRowCluster && (vectors * 16 / s.cluster - kHoldWide) * kWideCtas * sms > kRowsInFlightBytes) s.cluster *= 2;
     while (s.cluster < kRowCluster && rows * s.cluster < sms && vectors > (int64_t)s.cluster * 256) s.cluster *= 2;
     const int64_t part = ceil_div(vectors, s.cluster);
     // four batches of vectors a thread when there are rows enough to fill the GPU (4096 rows of 4000
@@ -380,8 +382,6 @@ RowShape row_shape(int64_t rows, int64_t vocab, int elem, bool loss, int sms) {
     s.threads = (int)std::min(most, std::max<int64_t>(32, ceil_div(ceil_div(part, each), 32) * 32));
     return s;
 }
-
-constexpr int kHoldNarrow = 40 << 10, kHoldWide = 108 << 10;  // shared memory of a CTA: what an SM has, over its CTAs
 
 template <typename T, int THREADS, int CTAS>
 int launch_loss(RowArgs a, const RowShape& s, int hold_bytes, void* stream) {
@@ -394,10 +394,12 @@ int launch_loss(RowArgs a, const RowShape& s, int hold_bytes, void* stream) {
         if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute", e);
         if (dev < kMaxDevices) done[dev].store(true, std::memory_order_relaxed);
     }
-    // as many whole batches as fit, but for the row's last, which stays in registers
+    // as many whole batches as fit (smaller CTAs, of which an SM takes more, have less room each), but
+    // for the row's last, which stays in registers; nothing of short rows, which gain nothing by it
+    // (16 KB: 27 us against 26; 48 KB: 72 against 77)
     const int64_t batch = (int64_t)s.threads * kRowVectors * 16;
-    const int64_t batches = ceil_div(ceil_div(a.vocab / kLanes<T>, s.cluster) * 16, batch);
-    a.hold = (int)std::max<int64_t>(0, std::min(hold_bytes / batch, batches - 1));
+    const int64_t part = ceil_div(a.vocab / kLanes<T>, s.cluster) * 16, batches = ceil_div(part, batch);
+    a.hold = part < 32 << 10 ? 0 : (int)std::max<int64_t>(0, std::min((int64_t)hold_bytes * s.threads / THREADS / batch, batches - 1));
     return launch("policy loss kernel", row_kernel<T, true, THREADS, CTAS>, dim3(a.rows * (unsigned)s.cluster), dim3((unsigned)s.threads),
                   (size_t)(a.hold * batch), s.cluster, stream, a);
 }
