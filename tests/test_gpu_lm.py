@@ -401,6 +401,16 @@ def test_policy_loss_broadcast_inputs_and_empty():
     assert e.dlogits.shape == (5, 0, 300) and bool((e.stats == 0).all())
 
 
+def test_int32_labels():
+    z = randn(4, 19, 700, seed=47, dtype=BF16)
+    y = tokens_of((4, 20), 700, 48)[:, 1:].clamp(-100, 5000)
+    old, adv, w, _ = policy_inputs(z, y, 49, 1.0)
+    a, b = lm.token_logprob(z, y), lm.token_logprob(z, y.int())
+    assert torch.equal(a.logp, b.logp) and torch.equal(a.lse, b.lse)
+    p, q = lm.policy_loss(z, y, old, adv, w), lm.policy_loss(z, y.int(), old, adv, w)
+    assert all(torch.equal(s, t) for s, t in zip(p, q))
+
+
 def test_policy_loss_gradient_against_differences():
     """Central differences of the 64-bit loss.  Its third derivative along one logit is below
     8 c^3 |w| (|A| r + beta (e^d + 1)), so the difference quotient with step h is off by less than
