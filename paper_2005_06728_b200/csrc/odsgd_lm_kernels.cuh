@@ -765,22 +765,22 @@ __device__ __forceinline__ void clear_marks(const EmbedGradArgs& a, unsigned thr
 
 // Of the sorted tokens: marks the rows that are named, and lists the runs that cross a block
 // boundary (the first boundary inside the run does, with the block its last position lies in).
-__device__ __forceinline__ void list_runs(const EmbedGradArgs& a, unsigned thread, unsigned threads) {
-    const unsigned* key = a.key[a.passes & 1];
+template <typename Key>
+__device__ __forceinline__ void list_runs(const EmbedGradArgs& a, unsigned thread, unsigned threads, Key key) {
     if (a.fills > 0) {
 #pragma unroll 4
         for (unsigned t = thread; t < a.n; t += threads) {
-            const unsigned k = __ldcg(key + t), row = k - a.early;
-            if (k >= a.early && k < (unsigned)a.vocab && (t == 0 || __ldcg(key + t - 1) != k)) atomicOr(a.named + row / 32, 1u << row % 32);
+            const unsigned k = key(t), row = k - a.early;
+            if (k >= a.early && k < (unsigned)a.vocab && (t == 0 || key(t - 1) != k)) atomicOr(a.named + row / 32, 1u << row % 32);
         }
     }
     for (unsigned t = (thread + 1) * a.block; t < a.n; t += threads * a.block) {
-        const unsigned k = __ldcg(key + t);
-        if (k != (unsigned)a.vocab && __ldcg(key + t - 1) == k && (t == a.block || __ldcg(key + t - a.block - 1) != k)) {
+        const unsigned k = key(t);
+        if (k != (unsigned)a.vocab && key(t - 1) == k && (t == a.block || key(t - a.block - 1) != k)) {
             unsigned last = t / a.block, up = (a.n - 1) / a.block;  // key[last * block] == k
             while (last < up) {
                 const unsigned mid = last + (up - last + 1) / 2;
-                if (__ldcg(key + mid * (size_t)a.block) == k) last = mid; else up = mid - 1;
+                if (key(mid * a.block) == k) last = mid; else up = mid - 1;
             }
             a.runs[atomicAdd(a.counts, 1u)] = SpanRun{k, t / a.block - 1, last};
         }
@@ -887,7 +887,8 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
         }
         cluster_sync();  // the pass is complete, in memory, for all CTAs of the cluster
     }
-    list_runs(a, rank * kSortThreads + tid, kSortCluster * kSortThreads);
+    const unsigned* sorted = a.key[a.passes & 1];
+    list_runs(a, rank * kSortThreads + tid, kSortCluster * kSortThreads, [&](unsigned t) { return __ldcg(sorted + t); });
 }
 
 // At most one position a thread: token and position in one number, sorted by a bitonic network, the
@@ -921,7 +922,9 @@ __device__ __forceinline__ void sort_few_tokens(const EmbedGradArgs& a, unsigned
         a.pos[a.passes & 1][tid] = (unsigned)x;
     }
     __syncthreads();
-    list_runs(a, tid, kSortThreads);
+    smem[tid] = x;
+    __syncthreads();
+    list_runs(a, tid, kSortThreads, [&](unsigned t) { return (unsigned)(smem[t] >> 32); });
 }
 
 __global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kSortCluster, 1, 1)
@@ -1094,10 +1097,11 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const __grid_cons
     __shared__ float4 part[kJoinWarps][32];
     dependent_launch_prologue();
     const unsigned runs = a.counts[0];
+    SpanRun run = a.runs[blockIdx.x];  // not after the count is known (there is room for a run a block)
     const unsigned lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long col = (long long)blockIdx.y * kJoinColumns + 4 * lane;  // the parts' pitch is a multiple of four
     for (unsigned r = blockIdx.x; r < runs; r += gridDim.x) {
-        const SpanRun run = a.runs[r];
+        if (r != blockIdx.x) run = a.runs[r];
         float4 s = make_float4(0, 0, 0, 0);
         if (col < a.dim) {
 #pragma unroll 4
