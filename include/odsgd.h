@@ -594,8 +594,8 @@ int odsgd_token_logprob(const odsgd_policy_desc* desc, void* stream);
 
 /*
  * The loss and its gradient in one call.  Each row is gone over twice, for its softmax statistics
- * and for its gradient, by the same CTA, the second time out of the L2: DRAM sees one read of the
- * logits and one write of their gradient.  `workspace` as for odsgd_embed_grad (12 bytes a row).
+ * and for its gradient, by the same CTA, the second time out of its shared memory and the L2: DRAM
+ * sees about one read of the logits and one write of their gradient.  `workspace` as for odsgd_embed_grad (12 bytes a row).
  * Errors of both calls: ERR_ARG, ERR_ALIGN, ERR_OVERLAP (an output overlaps an input or another
  * output), ERR_UNSUPPORTED, ERR_CUDA.
  */

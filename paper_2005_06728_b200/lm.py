@@ -12,7 +12,8 @@ What a worker runs on either side of its model when the parameter set is a langu
 
 include/odsgd.h has the formulas and the treatment of padding, masks and special values.  Every
 call is asynchronous on `stream` (default: the current stream), on the current device; results are
-new tensors unless a buffer is given.  Tensors may be strided in their leading axes (a shifted
+new tensors, in memory of that stream, unless a buffer is given.  With another stream than the one a
+tensor belongs to, ordering the two and keeping the memory (record_stream) are the caller's.  Tensors may be strided in their leading axes (a shifted
 view, an expanded value) as long as the last axis is contiguous and the leading ones fold into two
 levels.  There is no CPU fallback and no autograd: the gradient calls are the backward pass.
 """
@@ -286,7 +287,8 @@ class GradSet:
              worker)
 
     The set keeps its tensors alive; they must stay where they are, and calls of one set must not
-    overlap on the GPU.  Like a context it can be closed; it frees its table when dropped.
+    overlap on the GPU.  Its table is filled on `stream`: calls on other streams have to be ordered
+    behind that.  Like a context it can be closed; it frees its table when dropped.
     """
 
     def __init__(self, groups: Sequence[Sequence[torch.Tensor]], *, offsets: Optional[Sequence] = None,
