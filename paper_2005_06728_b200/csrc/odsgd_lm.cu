@@ -306,7 +306,9 @@ int allow_sort_smem() {
     const int rc = current_device(&dev);
     if (rc != ODSGD_OK) return rc;
     if (dev < kMaxDevices && done[dev].load(std::memory_order_relaxed)) return ODSGD_OK;
-    const cudaError_t e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmem);
+    cudaError_t e = cudaSuccess;
+    for (auto kernel : {sort_kernel<false, 2>, sort_kernel<true, 1>, sort_kernel<true, 2>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmem);
     if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute", e);
     if (dev < kMaxDevices) done[dev].store(true, std::memory_order_relaxed);
     return ODSGD_OK;
@@ -709,7 +711,11 @@ int odsgd_embed_grad(const odsgd_embed_desc* d, void* workspace, size_t workspac
         a.early = (unsigned)early;
         a.named = reinterpret_cast<unsigned*>(ws + s.at_named);
         const unsigned fill = (unsigned)std::min<int64_t>(kFillClusters, ceil_div(early * a.dim * 4, kFillBytes));
-        rc = launch("token sort kernel", sort_kernel, dim3((1 + fill) * kSortCluster), dim3(kSortThreads), kSortSmem, 1, stream, a);
+        // one CTA an SM where it still writes the zeros within the digit passes' time (32760 tokens, 51 MB: 39 us
+        // with one, 41 with two; 102 MB: 57, 49; 131072 tokens, 102 MB: 101, 105; 205 MB: 150, 148)
+        const bool few_zeros = early * a.dim * 4 <= (45 << 20) + (int64_t)s.n * 500;
+        const auto sort = s.n <= (unsigned)(kSortCluster * kSortThreads) ? sort_kernel<false, 2> : few_zeros ? sort_kernel<true, 1> : sort_kernel<true, 2>;
+        rc = launch("token sort kernel", sort, dim3((1 + fill) * kSortCluster), dim3(kSortThreads), kSortSmem, 1, stream, a);
         if (rc != ODSGD_OK || s.n == 0) return rc;
         a.wide = rows_aligned(a.table, 4, 0, a.stride, 1, a.vocab, 32);
         const bool vec = aligned16(a.table) && a.stride % 4 == 0 &&

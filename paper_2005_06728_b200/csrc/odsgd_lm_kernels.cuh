@@ -173,7 +173,6 @@ __device__ __forceinline__ uint32_t cluster_load(uint32_t addr) {
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(addr) : "memory");
     return x;
 }
-
 // ------------------------------------------------------------------ rows of logits
 // A cluster of `cluster` CTAs takes a row; the row's 16-byte vectors are split evenly over it.
 constexpr int kRowVectors = 4;  // vectors a thread has in flight
@@ -689,8 +688,9 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
 
 // ------------------------------------------------------------------ embedding gradient
 // Three launches.
-//   sort_kernel  One cluster sorts the tokens' positions by token, stably (least significant digit
-//                first, up to 9 bits a pass), marks the tokens that occur, and lists those whose run crosses a
+//   sort_kernel  One cluster sorts the tokens' positions by token, stably (up to 8192 by a bitonic
+//                network in each CTA and a merge: 2040 tokens 18.5 -> 13.6 us in all; more, least significant
+//                digit first, up to 9 bits a pass), marks the tokens that occur, and lists those whose run crosses a
 //                block boundary.  The other CTAs of the grid meanwhile write zeros to the first
 //                `early` rows of the table, as many as the sort takes time for, named or not.
 //   sum_kernel   A CTA takes `block` consecutive sorted positions and a slab of columns, and adds
@@ -710,6 +710,7 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortBits = 9;
 constexpr int kSortRadix = 1 << kSortBits;
 constexpr int kSortSmem = (kSortWarps * kSortRadix + 2 * kSortRadix + kSortWarps) * 4;
+static_assert(kSortSmem >= (kSortCluster * 4 + 2 * 8) * kSortThreads, "the parts and buffers of sort_some_tokens");
 constexpr int kFillClusters = 1000;  // most clusters that write zeros beside the sort, ...
 constexpr int kFillBytes = 1 << 18;  // ... each at least so many of the table
 constexpr int kFillRows = 32;        // rows of a CTA that writes zeros beside the sums: one word of marks
@@ -764,9 +765,10 @@ __device__ __forceinline__ void clear_marks(const EmbedGradArgs& a, unsigned thr
 }
 
 // Of the sorted tokens: marks the rows that are named, and lists the runs that cross a block
-// boundary (the first boundary inside the run does, with the block its last position lies in).
+// boundary (the first boundary inside the run does, with the block its last position lies in),
+// counting them at `count`.
 template <typename Key>
-__device__ __forceinline__ void list_runs(const EmbedGradArgs& a, unsigned thread, unsigned threads, Key key) {
+__device__ __forceinline__ void list_runs(const EmbedGradArgs& a, unsigned thread, unsigned threads, unsigned* count, Key key) {
     if (a.fills > 0) {
 #pragma unroll 4
         for (unsigned t = thread; t < a.n; t += threads) {
@@ -775,15 +777,23 @@ __device__ __forceinline__ void list_runs(const EmbedGradArgs& a, unsigned threa
         }
     }
     for (unsigned t = (thread + 1) * a.block; t < a.n; t += threads * a.block) {
-        const unsigned k = key(t);
-        if (k != (unsigned)a.vocab && key(t - 1) == k && (t == a.block || key(t - a.block - 1) != k)) {
-            unsigned last = t / a.block, up = (a.n - 1) / a.block;  // key[last * block] == k
-            while (last < up) {
-                const unsigned mid = last + (up - last + 1) / 2;
-                if (key(mid * a.block) == k) last = mid; else up = mid - 1;
+        const unsigned k = key(t), before = key(t - 1), earlier = key(t - min(t, a.block + 1));
+        if (k == (unsigned)a.vocab || before != k || (t != a.block && earlier == k)) continue;
+        // The block of the run's end: eight places are looked at together, 1, 2, 4, ... blocks on (most
+        // runs cross one boundary), then at the eighths of what is left.
+        unsigned last = t / a.block, up = (a.n - 1) / a.block;  // key(last * block) == k
+        for (bool grown = false; last < up; grown = true) {
+            const unsigned left = up - last, eighth = (left + 7) / 8;
+            unsigned same = 0;  // of the places, the first so many are in the run
+#pragma unroll
+            for (unsigned j = 0; j < 8; ++j) {
+                const unsigned d = grown ? (j + 1) * eighth : 1u << j;
+                same += key((last + min(d, left)) * a.block) == k && d <= left;
             }
-            a.runs[atomicAdd(a.counts, 1u)] = SpanRun{k, t / a.block - 1, last};
+            if (same < 8) up = min(up, last + (grown ? (same + 1) * eighth : 1u << same) - 1);
+            if (same > 0) last += grown ? same * eighth : 1u << (same - 1);
         }
+        a.runs[atomicAdd(count, 1u)] = SpanRun{k, t / a.block - 1, last};
     }
 }
 
@@ -832,6 +842,7 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
         __syncthreads();
         if (tid < radix) {  // exclusive scan over the warps, digit by digit
             unsigned run = 0;
+#pragma unroll 1
             for (int v0 = 0; v0 < kSortWarps; v0 += 8) {
                 unsigned c[8];
 #pragma unroll
@@ -888,52 +899,139 @@ __device__ __forceinline__ void sort_tokens(const EmbedGradArgs& a, unsigned* sm
         cluster_sync();  // the pass is complete, in memory, for all CTAs of the cluster
     }
     const unsigned* sorted = a.key[a.passes & 1];
-    list_runs(a, rank * kSortThreads + tid, kSortCluster * kSortThreads, [&](unsigned t) { return __ldcg(sorted + t); });
+    list_runs(a, rank * kSortThreads + tid, kSortCluster * kSortThreads, a.counts, [&](unsigned t) { return __ldcg(sorted + t); });
 }
 
-// At most one position a thread: token and position in one number, sorted by a bitonic network, the
-// exchanges inside a warp by shuffles (2 us where the digit passes and their barriers take 10).
-__device__ __forceinline__ void sort_few_tokens(const EmbedGradArgs& a, unsigned long long* smem) {
+// A token and its place in the CTA (10 bits) in one number: 32 bits where the vocabulary leaves them
+// (sorting 1020 tokens takes 2.4 us so, 3.6 with 64), else 64.
+template <typename N>
+constexpr int kPlaceBits = sizeof(N) == 4 ? 10 : 32;
+constexpr long long kNarrowVocab = (1ll << 22) - 1;  // below: no number is ~0
+
+// Sorts the numbers that a CTA's threads hold by a bitonic network, the exchanges inside a warp by
+// shuffles, the others through two buffers in turn.  Those of the threads from n on are the largest.
+template <typename N>
+__device__ __forceinline__ N sort_across(N x, unsigned n, N* smem) {
     const unsigned tid = threadIdx.x;
-    unsigned key[kKeyBatch];
-    token_keys(a, tid, a.n, key);  // the first of the batch; the others lie beyond n
-    if (tid == 0) a.counts[0] = 0;
-    clear_marks(a, tid, kSortThreads);
-    unsigned long long x = (unsigned long long)key[0] << 32 | tid;
+    unsigned turn = 0;
+#pragma unroll
     for (unsigned size = 2; size <= kSortThreads; size *= 2) {
-        if (size > 32 && size / 2 >= a.n) break;  // what lies beyond n is in its place already
+        if (size > 32 && size / 2 >= n) break;  // what lies beyond n is in its place already
         const bool up = (tid & size) == 0;
+#pragma unroll
         for (unsigned d = size / 2; d > 0; d /= 2) {
-            unsigned long long y;
+            N y;
             if (d >= 32) {
+                N* buffer = smem + turn * kSortThreads;
+                turn ^= 1;
+                buffer[tid] = x;
                 __syncthreads();
-                smem[tid] = x;
-                __syncthreads();
-                y = smem[tid ^ d];
+                y = buffer[tid ^ d];
             } else {
                 y = __shfl_xor_sync(0xffffffffu, x, d);
             }
             const bool lower = (tid & d) == 0;
-            x = (lower == up) == (x < y) ? x : y;
+            x = lower == up ? min(x, y) : max(x, y);
         }
     }
-    if (tid < a.n) {
-        a.key[a.passes & 1][tid] = (unsigned)(x >> 32);
-        a.pos[a.passes & 1][tid] = (unsigned)x;
-    }
-    __syncthreads();
-    smem[tid] = x;
-    __syncthreads();
-    list_runs(a, tid, kSortThreads, [&](unsigned t) { return (unsigned)(smem[t] >> 32); });
+    return x;
 }
 
-__global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kSortCluster, 1, 1)
+// At most one position a thread of one CTA.
+template <typename N>
+__device__ __forceinline__ void sort_few_tokens(const EmbedGradArgs& a, void* smem) {
+    __shared__ unsigned count;
+    const unsigned tid = threadIdx.x;
+    unsigned* sorted = static_cast<unsigned*>(smem);
+    unsigned key[kKeyBatch];
+    token_keys(a, tid, a.n, key);  // the first of the batch; the others lie beyond n
+    if (tid == 0) count = 0;
+    clear_marks(a, tid, kSortThreads);
+    const N x = sort_across<N>((N)key[0] << kPlaceBits<N> | tid, a.n, reinterpret_cast<N*>(sorted + kSortThreads));
+    key[0] = (unsigned)(x >> kPlaceBits<N>);
+    if (tid < a.n) {
+        a.key[a.passes & 1][tid] = key[0];
+        a.pos[a.passes & 1][tid] = (unsigned)x % kSortThreads;
+    }
+    sorted[tid] = key[0];
+    __syncthreads();
+    list_runs(a, tid, kSortThreads, &count, [&](unsigned t) { return sorted[t]; });
+    __syncthreads();
+    if (tid == 0) a.counts[0] = count;
+}
+
+// At most one position a thread of the cluster: each CTA sorts its part, and finds for each of its
+// tokens how many of every other part come before it (equal ones do from the parts before its own).
+template <typename N>
+__device__ __forceinline__ void sort_some_tokens(const EmbedGradArgs& a, void* smem) {
+    const unsigned rank = blockIdx.x, tid = threadIdx.x;
+    const unsigned per = (a.n + kSortCluster - 1) / kSortCluster, t = rank * per + tid;
+    unsigned* parts = static_cast<unsigned*>(smem);  // [cluster][threads]
+    unsigned* mine = parts + rank * kSortThreads;
+    const bool in = tid < per && t < a.n;
+    unsigned key[kKeyBatch];
+    token_keys(a, in ? t : a.n, a.n, key);
+    if (rank == 0 && tid == 0) a.counts[0] = 0;
+    clear_marks(a, rank * kSortThreads + tid, kSortCluster * kSortThreads);
+    const N none = ~(N)0;
+    const N x = sort_across<N>(in ? (N)key[0] << kPlaceBits<N> | tid : none, per, reinterpret_cast<N*>(parts + kSortCluster * kSortThreads));
+    const unsigned k = x == none ? ~0u : (unsigned)(x >> kPlaceBits<N>);
+    mine[tid] = k;
+    cluster_sync();
+    unsigned size = 32;  // of the parts, in whole steps of the search
+    while (size < per) size *= 2;
+    unsigned got[kSortCluster - 1];
+    if (tid < size) {
+#pragma unroll
+        for (unsigned c = 0; c < kSortCluster - 1; ++c) {
+            const unsigned other = (rank + 1 + c) % kSortCluster;
+            got[c] = cluster_load(cluster_address(parts + other * kSortThreads + tid, other));
+        }
+#pragma unroll
+        for (unsigned c = 0; c < kSortCluster - 1; ++c) parts[(rank + 1 + c) % kSortCluster * kSortThreads + tid] = got[c];
+    }
+    __syncthreads();
+    if (x != none) {
+        // neighbours in a warp are neighbours in order: their searches take nearly one path
+        unsigned to[kSortCluster - 1];
+#pragma unroll
+        for (unsigned c = 0; c < kSortCluster - 1; ++c) to[c] = (rank + 1 + c) % kSortCluster * kSortThreads;
+        const auto smaller = [&](unsigned c, unsigned i) { return parts[i] < k + (rank + 1 + c >= kSortCluster ? 1 : 0); };
+        for (unsigned step = size / 2; step > 0; step /= 2) {
+#pragma unroll
+            for (unsigned c = 0; c < kSortCluster - 1; ++c)
+                if (smaller(c, to[c] + step - 1)) to[c] += step;
+        }
+        unsigned at = tid;
+#pragma unroll
+        for (unsigned c = 0; c < kSortCluster - 1; ++c) at += to[c] % kSortThreads + (smaller(c, to[c]) ? 1 : 0);
+        a.key[a.passes & 1][at] = k;
+        a.pos[a.passes & 1][at] = rank * per + (unsigned)x % kSortThreads;
+    }
+    cluster_sync();  // in memory, for all CTAs of the cluster; and no part is read any more
+    const unsigned* sorted = a.key[a.passes & 1];
+    list_runs(a, rank * kSortThreads + tid, kSortCluster * kSortThreads, a.counts, [&](unsigned t) { return __ldcg(sorted + t); });
+}
+
+// DIGITS: more tokens than the cluster has threads.  CTAS: of an SM.  What writes zeros needs two (32760
+// tokens, 205 MB of zeros: 66 us, with one 92), for which a thread has 32 registers; the digit
+// passes alone are faster with more (131072 tokens, 13 MB of zeros: 84 us, else 89).
+template <bool DIGITS, int CTAS>
+__global__ void __launch_bounds__(kSortThreads, CTAS) __cluster_dims__(kSortCluster, 1, 1)
     sort_kernel(const __grid_constant__ EmbedGradArgs a) {
     extern __shared__ __align__(8) unsigned smem[];
     dependent_launch_prologue();
     if (blockIdx.x < kSortCluster) {
-        if (a.n > kSortThreads) sort_tokens(a, smem);
-        else if (blockIdx.x == 0) sort_few_tokens(a, reinterpret_cast<unsigned long long*>(smem));
+        const bool narrow = a.vocab < kNarrowVocab;
+        if constexpr (DIGITS) {
+            sort_tokens(a, smem);
+        } else if (a.n > kSortThreads) {
+            if (narrow) sort_some_tokens<unsigned>(a, smem);
+            else sort_some_tokens<unsigned long long>(a, smem);
+        } else if (blockIdx.x == 0) {
+            if (narrow) sort_few_tokens<unsigned>(a, smem);
+            else sort_few_tokens<unsigned long long>(a, smem);
+        }
         return;
     }
     const unsigned ctas = gridDim.x - kSortCluster, me = blockIdx.x - kSortCluster;

@@ -168,6 +168,32 @@ def test_embed_grad_digits(vocab, n):
     check_grad(tokens_of((n,), vocab, 17), randn(n, 4, seed=18), vocab)
 
 
+@pytest.mark.parametrize("n", [1023, 1024, 1026, 1031, 2047, 2048, 2049, 4095, 4097, 8183, 8191, 8192, 8193, 8201, 12007])
+@pytest.mark.parametrize("kind", ["all different", "few tokens", "one and none"])
+def test_embed_grad_sort_borders(n, kind):
+    """Around the powers of two and the borders between the three sorts, at parts that are full, ragged and empty."""
+    if kind == "all different":
+        vocab = n + 5
+        tok = (torch.arange(n, device=DEV) * 4799 + 11) % n
+    elif kind == "few tokens":
+        vocab = 3
+        tok = torch.arange(n, device=DEV) % 4 - 1
+    else:
+        vocab = 70001
+        tok = torch.where(torch.arange(n, device=DEV) * 13 % 8 < 5, 70000, vocab)
+    check_grad(tok, randn(n, 8, seed=19, dtype=BF16), vocab)
+
+
+@pytest.mark.parametrize("vocab", [4194302, 4194303, 4194304, 5000001])
+@pytest.mark.parametrize("n", [1, 33, 700, 1024, 1500, 8192])
+def test_embed_grad_large_vocabularies(n, vocab):
+    """On either side of the vocabulary whose tokens are sorted in 32 bits with their place."""
+    tok = tokens_of((n,), vocab, 21)
+    tok[::3] = vocab - 1
+    tok[1::7] = vocab
+    check_grad(tok, randn(n, 1, seed=22), vocab)
+
+
 @pytest.mark.parametrize("n,dim", [(70001, 32), (300000, 8), (4096, 2056)])
 def test_embed_grad_many_tokens(n, dim):
     vocab = 5000
