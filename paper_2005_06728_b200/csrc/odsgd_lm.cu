@@ -218,9 +218,9 @@ int check_embed(const odsgd_embed_desc* d, bool lookup, const void* ws = nullptr
     return ODSGD_OK;
 }
 
-// Whether all rows of a strided buffer start on `bytes` bytes (a power of two).
-bool rows_aligned(const void* p, int elem, int64_t so, int64_t si, int64_t n_outer, int64_t n_inner, int bytes = 16) {
-    return reinterpret_cast<uintptr_t>(p) % bytes == 0 && (n_outer <= 1 || so * elem % bytes == 0) && (n_inner <= 1 || si * elem % bytes == 0);
+// Whether all rows of a strided buffer start on 16 bytes.
+bool rows_aligned(const void* p, int elem, int64_t so, int64_t si, int64_t n_outer, int64_t n_inner) {
+    return aligned16(p) && (n_outer <= 1 || so * elem % 16 == 0) && (n_inner <= 1 || si * elem % 16 == 0);
 }
 
 template <typename TT, typename TA>
@@ -717,7 +717,6 @@ int odsgd_embed_grad(const odsgd_embed_desc* d, void* workspace, size_t workspac
         const auto sort = s.n <= (unsigned)(kSortCluster * kSortThreads) ? sort_kernel<false, 2> : few_zeros ? sort_kernel<true, 1> : sort_kernel<true, 2>;
         rc = launch("token sort kernel", sort, dim3((1 + fill) * kSortCluster), dim3(kSortThreads), kSortSmem, 1, stream, a);
         if (rc != ODSGD_OK || s.n == 0) return rc;
-        a.wide = rows_aligned(a.table, 4, 0, a.stride, 1, a.vocab, 32);
         const bool vec = aligned16(a.table) && a.stride % 4 == 0 &&
                          rows_aligned(d->act, size_of(d->act_type), a.a_so, a.a_si, d->n_outer, d->n_inner);
         switch (d->act_type) {

@@ -727,7 +727,6 @@ struct EmbedGradArgs {
     unsigned n, n_inner;
     int wide_tokens, accumulate;
     int flat;  // token t lies at t * t_si
-    int wide;  // the table's rows start on 32 bytes
     float scale;
     // workspace
     unsigned* key[2];
@@ -1106,7 +1105,7 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
             float* p = a.table + (r0 + r) * a.stride + col;
             const float zero[8] = {};
             if constexpr (VEC) {
-                if (W == 8 && a.wide) {
+                if (W == 8 && aligned32(p)) {
                     store_eight(p, zero);
                 } else {
 #pragma unroll
@@ -1168,11 +1167,14 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) sum_kernel(const __grid
                 }
             }
             if constexpr (VEC) {
+                // every place by its own address: the table's rows, and the parts in the workspace, need only
+                // start on 16 bytes
+                const bool wide = W == 8 && aligned32(dst);
                 if constexpr (W == 8) {
-                    if (a.wide) store_eight(dst, acc);
+                    if (wide) store_eight(dst, acc);
                 }
 #pragma unroll
-                for (int l = 0; l < W && !(W == 8 && a.wide); l += 4)
+                for (int l = 0; l < W && !wide; l += 4)
                     *reinterpret_cast<float4*>(dst + l) = make_float4(acc[l], acc[l + 1], acc[l + 2], acc[l + 3]);
             } else {
 #pragma unroll

@@ -1,0 +1,63 @@
+"""The language-model operators where alignment, run lengths and special values meet: cases beside
+those of test_gpu_lm, against the same 64-bit forms and bounds."""
+import pytest
+import torch
+
+import lm_reference as R
+from paper_2005_06728_b200 import lm
+from test_gpu_lm import BF16, DEV, F16, F32, check_grad, in_poison, randn, tokens_of
+
+pytestmark = pytest.mark.gpu
+
+
+# --------------------------------------------------------------------------- embedding gradient: alignment
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("dim", [24, 2048])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embed_grad_workspace_on_16_bytes(dtype, dim, accumulate):
+    """A workspace needs 16-byte alignment and no more: runs that cross blocks leave the same bits in it
+    wherever it starts."""
+    vocab = 7
+    tok = torch.cat([torch.full((k,), i % vocab, device=DEV) for i, k in enumerate([1, 40, 16, 100, 3, 64, 15, 17])])
+    grad = randn(tok.numel(), dim, seed=130, dtype=dtype)
+    old = randn(vocab, dim, seed=131) if accumulate else torch.zeros(vocab, dim, device=DEV)
+    ref, bound = R.embed_grad(tok, grad, vocab, 1.5, None, old if accumulate else None)
+    need = lm.embed_grad_workspace(tok, grad, old)
+    got = []
+    for base in (0, 16, 48, 112):
+        buffer = torch.full((need + 512,), 0x5A, dtype=torch.uint8, device=DEV)
+        assert buffer.data_ptr() % 256 == 0
+        dt = old.clone()
+        lm.embed_grad(tok, grad, dt, scale=1.5, accumulate=accumulate, workspace=buffer[base:base + need])
+        assert bool((buffer[:base] == 0x5A).all()) and bool((buffer[base + need:] == 0x5A).all()), "written outside the workspace"
+        got.append(dt)
+    R.within(got[0], ref, bound, "embedding gradient")
+    assert all(torch.equal(got[0], x) for x in got[1:])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("offset,pad", [(4, 0), (4, 4), (0, 4), (4, 8), (8, 8), (2, 0), (0, 2)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_embed_grad_16_bit_rows_into_tables_on_16_bytes(dtype, offset, pad, accumulate):
+    """Eight columns a thread, into table rows of which all, some or none start on 32 bytes."""
+    vocab, dim = 50, 24
+    tok = tokens_of((6, 90), vocab, 132)
+    tok[2] = 11  # a run over several blocks
+    grad = randn(6, 90, dim + 8, seed=133, dtype=dtype)[..., :dim]
+    check_grad(tok, grad, vocab, 1.5, 3, accumulate, offset, pad)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("offset,pad", [(0, 0), (4, 0), (0, 4), (4, 4)])
+def test_embed_grad_late_zeros_into_tables_on_16_bytes(dtype, offset, pad):
+    """A table with more rows than are zeroed beside the sort: those behind are zeroed beside the sums."""
+    vocab, dim, n = 9003, 2048, 1500  # 74 MB, of which 58 MB are written beside the sort
+    tok = tokens_of((n,), vocab, 134)
+    tok[::4] = vocab - 1
+    grad = randn(n, dim, seed=135, dtype=dtype)
+    dt, check = in_poison((vocab, dim), F32, offset, pad)
+    lm.embed_grad(tok, grad, dt, scale=0.5)
+    ref, bound = R.embed_grad(tok, grad, vocab, 0.5)
+    R.within(dt, ref, bound, "embedding gradient")
+    check()
