@@ -100,6 +100,8 @@ def _levels(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int]:
         return stride[:2]
     if lead < 2:
         return (0, stride[0]) if lead else (0, 0)
+    if 0 in t.shape[:lead]:
+        return 0, 0  # no element, no stride
     outer, step = 1, 0  # all but the last leading axis fold into one level
     for n, s in reversed(list(zip(t.shape[:lead - 1], stride[:lead - 1]))):
         if n == 1:

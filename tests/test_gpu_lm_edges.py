@@ -61,3 +61,21 @@ def test_embed_grad_late_zeros_into_tables_on_16_bytes(dtype, offset, pad):
     ref, bound = R.embed_grad(tok, grad, vocab, 0.5)
     R.within(dt, ref, bound, "embedding gradient")
     check()
+
+
+# --------------------------------------------------------------------------- no rows
+
+@pytest.mark.parametrize("shape", [(2, 0, 3), (0, 2, 3), (2, 3, 0), (2, 0, 3, 5)])
+def test_empty_batches_of_many_axes(shape):
+    tok = torch.zeros(shape, dtype=torch.int64, device=DEV)
+    table = randn(10, 8)
+    assert lm.embed_lookup(tok, table).shape == (*shape, 8)
+    dt = torch.full((10, 8), 5.0, device=DEV)
+    lm.embed_grad(tok, torch.zeros(*shape, 8, device=DEV), dt, accumulate=True)
+    assert bool((dt == 5).all())
+    assert bool((lm.embed_grad(tok, torch.zeros(*shape, 8, device=DEV), dt) == 0).all())
+    z = torch.zeros(*shape, 12, device=DEV)
+    assert lm.token_logprob(z, tok).logp.shape == shape
+    v = torch.zeros(shape, device=DEV)
+    r = lm.policy_loss(z, tok, v, v, v)
+    assert r.dlogits.shape == z.shape and r.logp.shape == shape and bool((r.stats == 0).all())
