@@ -562,7 +562,7 @@ typedef struct odsgd_policy_desc {
     const void* logits;           /* device, [n_outer][n_inner][vocab] of type */
     const void* labels;           /* device, [n_outer][n_inner] of label_type */
     const float* old_logp;        /* device, the same, as are the next three: log-probability under the acting policy */
-    const float* ref_logp;        /* under the reference policy; NULL only with kl_coef == 0 (the KL sum is then 0) */
+    const float* ref_logp;        /* under the reference policy; NULL only with kl_coef == 0 (the KL sum is then 0) or without rows */
     const float* advantages;
     const float* weights;
     void* dlogits;                /* device, as logits and of its type; may be the logits themselves (same pointer and strides) */

@@ -339,7 +339,7 @@ int check_policy(const odsgd_policy_desc* d, bool loss, const void* ws = nullptr
     if (!std::isfinite(d->kl_coef) || !std::isfinite(d->grad_scale)) return fail(ODSGD_ERR_ARG, "kl_coef and grad_scale must be finite");
     if (!d->stats) return fail(ODSGD_ERR_ARG, "stats is NULL");
     if (reinterpret_cast<uintptr_t>(d->stats) % 4 != 0) return fail(ODSGD_ERR_ALIGN, "stats is not 4-byte aligned");
-    if (!d->ref_logp && d->kl_coef != 0.0f) return fail(ODSGD_ERR_ARG, "kl_coef needs ref_logp");
+    if (!d->ref_logp && d->kl_coef != 0.0f && d->n_outer > 0 && ni > 0) return fail(ODSGD_ERR_ARG, "kl_coef needs ref_logp");
     bufs[n++] = {"old_logp", d->old_logp, 4, d->old_stride_outer, d->old_stride_inner, 1, false};
     if (d->ref_logp) bufs[n++] = {"ref_logp", d->ref_logp, 4, d->ref_stride_outer, d->ref_stride_inner, 1, false};
     bufs[n++] = {"advantages", d->advantages, 4, d->adv_stride_outer, d->adv_stride_inner, 1, false};

@@ -79,3 +79,5 @@ def test_empty_batches_of_many_axes(shape):
     v = torch.zeros(shape, device=DEV)
     r = lm.policy_loss(z, tok, v, v, v)
     assert r.dlogits.shape == z.shape and r.logp.shape == shape and bool((r.stats == 0).all())
+    r = lm.policy_loss(z, tok, v, v, v, ref_logp=v, kl_coef=0.1)
+    assert bool((r.stats == 0).all())

@@ -3,7 +3,8 @@ launched here."""
 import pytest
 import torch
 
-from paper_2005_06728_b200 import lm
+from paper_2005_06728_b200 import binding, lm
+from test_lm_host import policy
 
 
 @pytest.mark.parametrize("shape", [(3, 0, 4), (0, 3, 4), (3, 4, 0), (5, 0, 3, 8), (5, 3, 0, 8), (2, 0, 0, 8), (0, 2, 3, 4, 5)])
@@ -21,3 +22,12 @@ def test_empty_tensors_fold(shape):
 def test_axes_that_do_not_fold_are_still_refused():
     with pytest.raises(ValueError, match="two strided levels"):
         lm._levels(torch.zeros(2, 3, 4, 5)[:, 1:], 3, "t")
+
+
+def test_a_loss_without_rows_needs_no_reference():
+    """An empty tensor has no address: the KL term of no rows is taken from none."""
+    lib = binding.load_library()
+    for over in (dict(n_outer=0), dict(n_inner=0)):
+        # refused for its workspace, which is looked at after the rows' buffers
+        d = policy(logits=0, labels=0, old_logp=0, ref_logp=0, advantages=0, weights=0, dlogits=0, logp=0, **over)
+        assert lib.odsgd_policy_loss(d, None, 16, None) == binding.ERR_ARG and "workspace" in lib.odsgd_last_error(None).decode()
