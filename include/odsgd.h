@@ -555,7 +555,8 @@ int odsgd_embed_grad(const odsgd_embed_desc* desc, void* workspace, size_t works
  *         k = w ((r A <= clip(r) A ? -A r : 0) + kl_coef (1 - exp(d)))
  * w is the row's weight (mask and normalisation in one: 1 / tokens, say).  Rows with w == 0 or a
  * label outside [0, vocab) are not read: logp 0, no part in the sums, a gradient row of zeros,
- * whatever their logits hold.  A vocabulary entry of -inf has probability 0 and gradient 0; a
+ * whatever their logits hold.  With kl_coef == 0 a reference only serves the KL sum: loss and gradient do
+ * not see it, finite or not.  A vocabulary entry of -inf has probability 0 and gradient 0; a
  * row with nothing but -inf, or with NaN or +inf, gives NaN, as the formula does.
  */
 typedef struct odsgd_policy_desc {

@@ -364,7 +364,7 @@ struct RowLoss {
             const float d = in.ref_logp - logp;
             const float em = expm1f(d);  // exp(d) - 1 without its cancellation near d = 0
             kl = w * (em - d);
-            g -= a.kl_coef * em;
+            if (a.kl_coef != 0.0f) g -= a.kl_coef * em;  // (0 times an em that overflows would be NaN)
         }
         k = w * g * a.inv_temp * a.grad_scale;
     }
@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(kStatsThreads) stats_kernel(const __grid_const
     }
     block_sum<3, kStatsThreads>(x, part);
     if (threadIdx.x == 0) {
-        a.stats[0] = (float)(x[0] + (double)a.kl_coef * x[1]);
+        a.stats[0] = (float)(a.kl_coef != 0.0f ? x[0] + (double)a.kl_coef * x[1] : x[0]);
         a.stats[1] = (float)x[0];
         a.stats[2] = (float)x[1];
         a.stats[3] = (float)x[2];

@@ -81,3 +81,32 @@ def test_empty_batches_of_many_axes(shape):
     assert r.dlogits.shape == z.shape and r.logp.shape == shape and bool((r.stats == 0).all())
     r = lm.policy_loss(z, tok, v, v, v, ref_logp=v, kl_coef=0.1)
     assert bool((r.stats == 0).all())
+
+
+# --------------------------------------------------------------------------- policy loss: special values
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("vocab", [40, 5003])
+def test_reference_for_the_kl_sum_alone(dtype, vocab):
+    """With kl_coef 0 the reference is there for the KL sum: loss and gradient do not depend on it, whatever
+    exp(ref - logp) is."""
+    z = randn(6, vocab, seed=140, dtype=dtype, sigma=2.0)
+    z[1, 3] = float("-inf")
+    y = torch.tensor([0, 3, 5, 7, -1, 9], device=DEV)
+    old, adv = randn(6, seed=141, sigma=0.1) - 8.0, randn(6, seed=142)
+    w = torch.full((6,), 1 / 6, device=DEV)
+    old[1] = -200.0
+    want = lm.policy_loss(z, y, old, adv, w)
+    ref = old.clone()
+    ref[0] = 300.0  # exp overflows
+    ref[2] = float("inf")
+    ref[3] = float("-inf")
+    got = lm.policy_loss(z, y, old, adv, w, ref_logp=ref)
+    assert torch.equal(got.dlogits, want.dlogits) and torch.equal(got.logp, want.logp)
+    assert bool(torch.isfinite(got.dlogits).all()) and bool(torch.isfinite(got.stats[0]))
+    assert torch.equal(got.stats[[0, 1, 3]], want.stats[[0, 1, 3]]) and not bool(torch.isfinite(got.stats[2]))
+    # without rows that overflow, the sum itself
+    ref = want.logp + 0.3
+    got = lm.policy_loss(z[2:4], y[2:4], old[2:4], adv[2:4], w[2:4], ref_logp=ref[2:4])
+    kl = 2 / 6 * (torch.exp(torch.tensor(0.3, dtype=torch.float64)) - 1.3)
+    assert abs(float(got.stats[2]) - float(kl)) < 1e-5
