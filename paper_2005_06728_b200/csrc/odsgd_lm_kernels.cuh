@@ -19,7 +19,9 @@ namespace odsgd_lm {
 using bf16 = __nv_bfloat16;
 using f16 = __half;
 
-// Scheduled early, run in order: see the update kernels.
+// Scheduled early, run in order: see the update kernels.  A grid can have begun while the one ahead of it still
+// writes, so what is read behind the wait goes through ordinary loads: the read-only path asks for memory
+// that nothing writes in all the time the grid exists (it measured no faster: norms, lookups and clips within 0.5 %).
 __device__ __forceinline__ void dependent_launch_prologue() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -618,10 +620,10 @@ __device__ __forceinline__ void load_columns(const T* row, long long col, long l
         for (int l = 0; l < W; ++l)
             if (col + l * (int)blockDim.x < dim) x[l] = to_f32(p[l * (int)blockDim.x]);
     } else if constexpr (W == kLanes<T>) {
-        unpack<T>(__ldg(reinterpret_cast<const uint4*>(p)), x);
+        unpack<T>(*reinterpret_cast<const uint4*>(p), x);
     } else {
         float y[8];
-        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
+        const uint2 q = *reinterpret_cast<const uint2*>(p);
         unpack<T>(make_uint4(q.x, q.y, 0, 0), y);
 #pragma unroll
         for (int l = 0; l < W; ++l) x[l] = y[l];
@@ -1298,7 +1300,7 @@ __device__ __forceinline__ double chunk_squares(const GradChunk& c) {
 #pragma unroll
             for (int k = 0; k < kClipVectors; ++k) {
                 const unsigned v = b + k * kClipThreads + threadIdx.x;
-                q[k] = v < nv ? __ldg(reinterpret_cast<const uint4*>(p) + v) : make_uint4(0, 0, 0, 0);
+                q[k] = v < nv ? reinterpret_cast<const uint4*>(p)[v] : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
             for (int k = 0; k < kClipVectors; ++k) s += vector_squares<T>(q[k]);

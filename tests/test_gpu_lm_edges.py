@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import lm_reference as R
-from paper_2005_06728_b200 import lm
+from paper_2005_06728_b200 import binding, lm
 from test_gpu_lm import BF16, DEV, F16, F32, check_grad, in_poison, randn, tokens_of
 
 pytestmark = pytest.mark.gpu
@@ -110,3 +110,49 @@ def test_reference_for_the_kl_sum_alone(dtype, vocab):
     got = lm.policy_loss(z[2:4], y[2:4], old[2:4], adv[2:4], w[2:4], ref_logp=ref[2:4])
     kl = 2 / 6 * (torch.exp(torch.tensor(0.3, dtype=torch.float64)) - 1.3)
     assert abs(float(got.stats[2]) - float(kl)) < 1e-5
+
+
+# --------------------------------------------------------------------------- calls back to back
+
+@pytest.mark.parametrize("vocab,dim", [(64, 40), (3001, 512)])
+def test_back_to_back_calls_see_what_the_ones_ahead_wrote(vocab, dim):
+    """Every kernel may be scheduled while the one ahead of it still runs.  Clip into an arena, update,
+    lookup in the updated weights, clip in place, norm: the same bits with and without waiting in between."""
+    rounds = 12
+    tok = tokens_of((257,), vocab, 150)
+    g = [randn(vocab, dim, seed=151, dtype=BF16), randn(vocab, dim, seed=152, dtype=BF16)]
+    w0 = randn(vocab * dim, seed=153)
+
+    def chain(wait):
+        w, v = w0.clone(), torch.zeros_like(w0)
+        arenas = [torch.zeros_like(w0) for _ in range(2)]
+        ctx = binding.Odsgd(w, v, n_workers=2, lr=0.5, local_lr=0.5, momentum=0.9, wd=0.01)
+        into = lm.GradSet([[g[0]], [g[1]]], offsets=[0], arenas=arenas)
+        own = [[t.float()] for t in g]
+        place = lm.GradSet(own)
+        outs = torch.zeros(rounds, 257, dim, dtype=BF16, device=DEV)
+        norms = torch.zeros(rounds, 3, 2, device=DEV)
+        torch.cuda.synchronize()
+        sync = torch.cuda.synchronize if wait else (lambda: None)
+        table = w.view(vocab, dim)
+        for k in range(rounds):
+            into.clip(10.0 + 3.0 * (k * 5 % rounds), out=norms[k, 0])
+            sync()
+            ctx.ssgd_step(arenas)
+            sync()
+            lm.embed_lookup(tok, table, out=outs[k])
+            sync()
+            place.clip(30.0 - 2.0 * k, out=norms[k, 1])
+            sync()
+            place.norm(out=norms[k, 2])
+            sync()
+        torch.cuda.synchronize()
+        ctx.close()
+        return w, outs, norms, own
+
+    want, got = chain(True), chain(False)
+    assert all(torch.equal(a, b) for a, b in zip(want[:3], got[:3]))
+    assert all(torch.equal(a[0], b[0]) for a, b in zip(want[3], got[3]))
+    for k in range(rounds):  # clipped in place to ever smaller norms
+        assert bool(((got[2][k, 2] / (30.0 - 2.0 * k) - 1).abs() < 1e-5).all())
+    assert not torch.equal(got[1][0], got[1][-1])

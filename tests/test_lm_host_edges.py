@@ -1,9 +1,11 @@
 """Host side of the language-model calls: shapes and buffers beside those of test_lm_host.  No kernel is
 launched here."""
+import os
+
 import pytest
 import torch
 
-from paper_2005_06728_b200 import binding, lm
+from paper_2005_06728_b200 import binding, build, lm
 from test_lm_host import policy
 
 
@@ -31,3 +33,11 @@ def test_a_loss_without_rows_needs_no_reference():
         # refused for its workspace, which is looked at after the rows' buffers
         d = policy(logits=0, labels=0, old_logp=0, ref_logp=0, advantages=0, weights=0, dlogits=0, logp=0, **over)
         assert lib.odsgd_policy_loss(d, None, 16, None) == binding.ERR_ARG and "workspace" in lib.odsgd_last_error(None).decode()
+
+
+def test_no_load_of_the_read_only_path():
+    """A grid that may begin while the one ahead of it writes must not read through the path for memory that
+    nothing writes while the grid exists."""
+    with open(os.path.join(build.CSRC, "odsgd_lm_kernels.cuh")) as f:
+        text = f.read()
+    assert "griddepcontrol.wait" in text and "__ldg" not in text and "global.nc" not in text
