@@ -267,7 +267,7 @@ GradShape grad_shape(const odsgd_embed_desc* d) {
     // positions of a block: enough CTAs to fill the machine several times over before blocks grow
     const int64_t slabs = ceil_div(d->dim, (int64_t)kSumThreads * (16 / size_of(d->act_type)));
     s.block = 16;
-    while (2 * s.block <= (unsigned)kSumMaxBlock && (int64_t)(s.n / s.block) * slabs > 148 * 16) s.block *= 2;
+    while (s.block < (unsigned)kSumMaxBlock && (int64_t)(s.n / s.block) * slabs > 148 * 16) s.block *= 2;
     s.blocks = (unsigned)ceil_div(s.n, s.block);
     s.pitch = ceil_div(d->dim, 8) * 8;
     size_t at = 0;

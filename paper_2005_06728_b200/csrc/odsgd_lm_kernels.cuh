@@ -698,9 +698,11 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
 //   sum_kernel   A CTA takes `block` consecutive sorted positions and a slab of columns, and adds
 //                runs of equal tokens in 32 bits.  A run inside the block is written to the table,
 //                the part of one that crosses a boundary to the workspace.  Work is split by
-//                position, so a token that fills half the batch costs no more than rare ones.
+//                position, so that a token that fills half the batch holds up no CTA here; its parts, one a
+//                block, are left to the join.
 //                Further CTAs, spread among these, write zeros to the other rows that no token names.
-//   join_kernel  Adds the parts of the runs that cross boundaries, in order.
+//   join_kernel  Adds the parts of the runs that cross boundaries, in an order that the sizes fix: a CTA takes a run and a
+//                slab of columns, so one very long run is added by few.
 // The order of every sum depends on sizes and tokens alone.
 // 32760 tokens, 2048 bf16 columns, a table of 50021 rows (544 MB): 108 us, 0.77 of the copy rate: 25 us of
 // zeros beside the sort (of which the sort takes 20), 75 for sums and the other zeros, 8 for the join.
@@ -1057,7 +1059,7 @@ __global__ void __launch_bounds__(kSortThreads, CTAS) __cluster_dims__(kSortClus
 constexpr int kSumThreads = 128;
 constexpr int kSumCtas = 8;
 constexpr int kSumBatch = 8;       // rows a thread has in flight
-constexpr int kSumMaxBlock = 126;  // most positions of a block
+constexpr int kSumMaxBlock = 64;   // most positions of a block: 16, 32 or 64
 
 // A thread's columns of a row: a vector of T, or (rows that are not aligned) T's blockDim.x apart, of
 // which `left` columns remain.

@@ -156,3 +156,22 @@ def test_back_to_back_calls_see_what_the_ones_ahead_wrote(vocab, dim):
     for k in range(rounds):  # clipped in place to ever smaller norms
         assert bool(((got[2][k, 2] / (30.0 - 2.0 * k) - 1).abs() < 1e-5).all())
     assert not torch.equal(got[1][0], got[1][-1])
+
+
+# --------------------------------------------------------------------------- embedding gradient: lengths of runs
+
+@pytest.mark.parametrize("n", [2300, 37903, 37904, 75807, 75808, 80001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_embed_grad_runs_around_blocks(n, dtype):
+    """Blocks of 16, 32 and 64 positions (37904 and 75808 tokens are the first of the larger ones): runs that are
+    one shorter and longer than one, two and more blocks, one after another, and one that fills half."""
+    lens = [15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 64, 65, 1, 95, 96, 97, 127, 128, 129, 2, 191, 192, 193, 255, 257]
+    tok, i = [torch.full((n // 2,), 1, device=DEV)], 0
+    left = n - n // 2
+    while left > 0:
+        k = min(left, lens[i % len(lens)])
+        tok.append(torch.full((k,), 2 + i, device=DEV))
+        left, i = left - k, i + 1
+    tok = torch.cat(tok)
+    order = torch.randperm(n, generator=torch.Generator().manual_seed(160))
+    check_grad(tok[order.to(DEV)], randn(n, 8, seed=161, dtype=dtype), i + 5, 0.5)
