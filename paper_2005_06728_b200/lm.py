@@ -15,7 +15,9 @@ call is asynchronous on `stream` (default: the current stream), on the current d
 new tensors, in memory of that stream, unless a buffer is given.  With another stream than the one a
 tensor belongs to, ordering the two and keeping the memory (record_stream) are the caller's.  Tensors may be strided in their leading axes (a shifted
 view, an expanded value) as long as the last axis is contiguous and the leading ones fold into two
-levels.  There is no CPU fallback and no autograd: the gradient calls are the backward pass.
+levels.  There is no CPU fallback and no autograd: the gradient calls are the backward pass.  Tensors that a
+caller hands over to be written (out, dtable, dlogits, arenas, gradients clipped in place) count as changed in
+place, so that a backward pass of torch that saved one of them fails; replays of a captured graph do not count.
 """
 from __future__ import annotations
 
@@ -24,6 +26,7 @@ import struct
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import binding
 from .binding import OK, OdsgdError
@@ -162,7 +165,8 @@ def embed_lookup(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.
     table_type = _need(table, "table", _FLOATS, dev)
     vocab, dim, stride = _table(table, "table")
     shape = (*tokens.shape, dim)
-    if out is None:
+    given = out is not None
+    if not given:
         out = _new(table, shape, table.dtype if dtype is None else dtype, stream)
     elif dtype is not None and out.dtype != dtype:
         raise ValueError("out and dtype disagree")
@@ -172,6 +176,8 @@ def embed_lookup(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.
     d = _EMBED.pack(tokens.data_ptr(), out.data_ptr(), table.data_ptr(), token_type, out_type, table_type, 0,
                     *_sizes(tokens.shape), *_levels(tokens, lead, "tokens"), *_rows(out, lead, "out"), vocab, dim, stride, -1, scale)
     _check(binding.load_library().odsgd_embed_lookup(d, _handle(stream, dev)))
+    if given:
+        increment_version(out)
     return out
 
 
@@ -199,6 +205,7 @@ def embed_grad(tokens: torch.Tensor, grad: torch.Tensor, dtable: torch.Tensor, *
     elif not workspace.is_contiguous() or workspace.get_device() != dev:
         raise ValueError("workspace: need a contiguous tensor on the current device")
     _check(lib.odsgd_embed_grad(d, workspace.data_ptr(), workspace.nbytes, _handle(stream, dev)))
+    increment_version(dtable)
     return dtable
 
 
@@ -258,7 +265,8 @@ def policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tens
     strides = (*_rows(logits, lead, "logits"), *_levels(labels, lead, "labels"), *vector(old_logp, "old_logp"),
                *((0, 0) if ref_logp is None else vector(ref_logp, "ref_logp")),
                *vector(advantages, "advantages"), *vector(weights, "weights"))
-    if dlogits is None:
+    given = dlogits is not None
+    if not given:
         dlogits = _new(logits, None, None, stream)
     else:
         _need(dlogits, "dlogits", {logits.dtype: kind}, dev)
@@ -273,6 +281,8 @@ def policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tens
                      outer, inner, whole[-1], *strides, *_rows(dlogits, lead, "dlogits"),
                      inv_temp, clip_low, clip_high, kl_coef, grad_scale)
     _check(binding.load_library().odsgd_policy_loss(d, at + 16, 12 * n if n > 1 else 16, _handle(stream, dev)))
+    if given:
+        increment_version(dlogits)
     return PolicyLoss(head[:4], logp, dlogits)
 
 
@@ -308,6 +318,8 @@ class GradSet:
             if len({a.numel() for a in arenas}) != 1:
                 raise ValueError("the arenas differ in length")
         self._keep = ([list(g) for g in groups], list(arenas) if arenas is not None else None)
+        # what clip() writes besides the norms
+        self._written = [t for g in self._keep[0] for t in g] if arenas is None else self._keep[1]
         self._dev = dev = torch.cuda.current_device()
         per_group = offsets is not None and len(offsets) > 0 and isinstance(offsets[0], (list, tuple))
         rows = []
@@ -348,6 +360,7 @@ class GradSet:
         """The 2-norm of each group over all its tensors (float32); nothing else is written."""
         out = self._out(out, stream)
         _check(self._lib.odsgd_grad_set_norm(self._h, out.data_ptr(), _handle(stream, self._dev)))
+        increment_version(out)
         return out
 
     def clip(self, max_norm: float, *, out: Optional[torch.Tensor] = None,
@@ -356,6 +369,7 @@ class GradSet:
         norms of before."""
         out = self._out(out, stream)
         _check(self._lib.odsgd_grad_set_clip(self._h, max_norm, out.data_ptr(), _handle(stream, self._dev)))
+        increment_version([*self._written, out])
         return out
 
     def close(self) -> None:

@@ -175,3 +175,56 @@ def test_embed_grad_runs_around_blocks(n, dtype):
     tok = torch.cat(tok)
     order = torch.randperm(n, generator=torch.Generator().manual_seed(160))
     check_grad(tok[order.to(DEV)], randn(n, 8, seed=161, dtype=dtype), i + 5, 0.5)
+
+
+# --------------------------------------------------------------------------- autograd
+
+@pytest.mark.parametrize("call", ["lookup", "gradient", "loss", "clip in place", "clip into arenas", "norms", "norm"])
+def test_writing_over_what_autograd_saved_is_noticed(call):
+    """Buffers that a caller hands over to be written count as changed in place: a backward pass that saved one
+    of them fails instead of using what was written over it."""
+    x = randn(4, 16, seed=170).requires_grad_()
+    y = x.exp()  # its backward needs y itself
+    buf = y.detach()
+    tok = torch.tensor([1, 0, 3, 2], device=DEV)
+    if call == "lookup":
+        lm.embed_lookup(tok, randn(4, 16, seed=171), out=buf)
+    elif call == "gradient":
+        lm.embed_grad(tok, randn(4, 16, seed=172), buf)
+    elif call == "loss":
+        v = torch.ones(4, device=DEV)
+        lm.policy_loss(buf, tok, -v, v, v, dlogits=buf)
+    elif call == "clip in place":
+        lm.GradSet([[randn(9, seed=173)], [buf]]).clip(0.1)
+    elif call == "clip into arenas":
+        lm.GradSet([[randn(9, seed=173)]], offsets=[3], arenas=[buf.view(-1)]).clip(0.1)
+    else:
+        s = lm.GradSet([[randn(9, seed=173 + k)] for k in range(64)])
+        s.clip(0.1, out=buf.view(-1)) if call == "norms" else s.norm(out=buf.view(-1))
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.sum().backward()
+
+
+def test_reading_changes_no_version():
+    z, tok = randn(4, 16, seed=175), torch.tensor([1, 0, 3, 2], device=DEV)
+    v = torch.ones(4, device=DEV)
+    s = lm.GradSet([[z]])
+    before = [t._version for t in (z, tok, v)]
+    lm.embed_lookup(tok, z)
+    lm.token_logprob(z, tok)
+    lm.policy_loss(z, tok, -v, v, v)
+    lm.embed_grad(tok, z, torch.zeros(4, 16, device=DEV))
+    s.norm()
+    assert [t._version for t in (z, tok, v)] == before
+
+
+def test_inference_tensors():
+    """Tensors without a version counter."""
+    with torch.inference_mode():
+        table, tok = randn(6, 8, seed=176), torch.tensor([5, 1], device=DEV)
+        out = torch.empty(2, 8, device=DEV)
+        assert lm.embed_lookup(tok, table, out=out) is out and torch.equal(out, table[tok])
+        g = [[randn(40, seed=177)]]
+        assert float(lm.GradSet(g).clip(0.5)[0]) > 0.5
+    lm.embed_lookup(tok, table, out=out)
+    assert abs(float(lm.GradSet(g).norm()[0]) - 0.5) < 1e-6
