@@ -318,8 +318,9 @@ class GradSet:
             if len({a.numel() for a in arenas}) != 1:
                 raise ValueError("the arenas differ in length")
         self._keep = ([list(g) for g in groups], list(arenas) if arenas is not None else None)
-        # what clip() writes besides the norms
-        self._written = [t for g in self._keep[0] for t in g] if arenas is None else self._keep[1]
+        # what clip() writes besides the norms, of the views of one tensor (which share its version) one
+        written = [t for g in self._keep[0] for t in g] if arenas is None else self._keep[1]
+        self._written = list({id(t._base if t._is_view() else t): t for t in written}.values())
         self._dev = dev = torch.cuda.current_device()
         per_group = offsets is not None and len(offsets) > 0 and isinstance(offsets[0], (list, tuple))
         rows = []

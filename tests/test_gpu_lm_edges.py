@@ -205,6 +205,20 @@ def test_writing_over_what_autograd_saved_is_noticed(call):
         y.sum().backward()
 
 
+@pytest.mark.parametrize("in_place", [True, False])
+def test_views_of_one_tensor_and_others_are_all_noticed(in_place):
+    x = [randn(40, seed=178).requires_grad_() for _ in range(3)]
+    y = [t.exp() for t in x]
+    bufs = [y[0].detach()[:20], y[0].detach()[20:], y[1].detach(), y[2].detach()[4:24]]
+    if in_place:
+        lm.GradSet([bufs]).clip(0.1)
+    else:
+        lm.GradSet([[randn(9, seed=179)]] * 4, offsets=[0], arenas=[b[:20] for b in bufs]).clip(0.1)
+    for t in y:
+        with pytest.raises(RuntimeError, match="inplace"):
+            t.sum().backward()
+
+
 def test_reading_changes_no_version():
     z, tok = randn(4, 16, seed=175), torch.tensor([1, 0, 3, 2], device=DEV)
     v = torch.ones(4, device=DEV)
