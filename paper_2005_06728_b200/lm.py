@@ -273,17 +273,16 @@ def policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tens
         _shape(dlogits, whole, "dlogits")
     outer, inner = _sizes(shape)
     n = outer * inner
-    head = _new(logits, 4 + max(4, 3 * n), torch.float32, stream)  # the four sums, and the workspace (12 bytes a row)
-    logp = _new(labels, None, torch.float32, stream)
-    at = head.data_ptr()
+    stats, logp = _new(logits, 4, torch.float32, stream), _new(labels, None, torch.float32, stream)
+    workspace = _new(logits, max(4, 3 * n), torch.float32, stream)  # 12 bytes a row
     d = _POLICY.pack(logits.data_ptr(), labels.data_ptr(), old_logp.data_ptr(), 0 if ref_logp is None else ref_logp.data_ptr(),
-                     advantages.data_ptr(), weights.data_ptr(), dlogits.data_ptr(), logp.data_ptr(), 0, at, kind, label_type,
+                     advantages.data_ptr(), weights.data_ptr(), dlogits.data_ptr(), logp.data_ptr(), 0, stats.data_ptr(), kind, label_type,
                      outer, inner, whole[-1], *strides, *_rows(dlogits, lead, "dlogits"),
                      inv_temp, clip_low, clip_high, kl_coef, grad_scale)
-    _check(binding.load_library().odsgd_policy_loss(d, at + 16, 12 * n if n > 1 else 16, _handle(stream, dev)))
+    _check(binding.load_library().odsgd_policy_loss(d, workspace.data_ptr(), 12 * n if n > 1 else 16, _handle(stream, dev)))
     if given:
         increment_version(dlogits)
-    return PolicyLoss(head[:4], logp, dlogits)
+    return PolicyLoss(stats, logp, dlogits)
 
 
 # --------------------------------------------------------------------------- gradient norm and clip

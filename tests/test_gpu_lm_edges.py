@@ -242,3 +242,14 @@ def test_inference_tensors():
         assert float(lm.GradSet(g).clip(0.5)[0]) > 0.5
     lm.embed_lookup(tok, table, out=out)
     assert abs(float(lm.GradSet(g).norm()[0]) - 0.5) < 1e-6
+
+
+# --------------------------------------------------------------------------- memory
+
+def test_a_kept_result_keeps_no_workspace():
+    """The four sums of a loss may be kept for as long as one likes: they hold 16 bytes."""
+    z, tok = randn(3, 1000, 4, seed=180), torch.zeros(3, 1000, dtype=torch.int64, device=DEV)
+    v = torch.ones(3, 1000, device=DEV)
+    r = lm.policy_loss(z, tok, -v, v, v)
+    assert r.stats.untyped_storage().nbytes() == 16
+    assert r.logp.untyped_storage().nbytes() == 4 * 3000 and r.dlogits.untyped_storage().nbytes() == 4 * z.numel()
