@@ -98,7 +98,9 @@ int check_buffers(const Buf* bufs, int n, int64_t n_outer, int64_t n_inner, int 
     for (int i = 0; i < n; ++i) {
         for (int j = 0; j < n; ++j) {
             if (i == j || !bufs[i].written || (bufs[j].written && j < i)) continue;
-            if (i == same_ok && j == 0 && bufs[i].p == bufs[0].p && bufs[i].so == bufs[0].so && bufs[i].si == bufs[0].si) continue;
+            if (i == same_ok && j == 0 && bufs[i].p == bufs[0].p && (n_outer == 1 || bufs[i].so == bufs[0].so) &&
+                (n_inner == 1 || bufs[i].si == bufs[0].si))
+                continue;
             if (r[i].lo < r[j].hi && r[j].lo < r[i].hi)
                 return fail(ODSGD_ERR_OVERLAP, std::string(bufs[i].name) + " overlaps " + bufs[j].name);
         }

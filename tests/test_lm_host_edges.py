@@ -41,3 +41,24 @@ def test_no_load_of_the_read_only_path():
     with open(os.path.join(build.CSRC, "odsgd_lm_kernels.cuh")) as f:
         text = f.read()
     assert "griddepcontrol.wait" in text and "__ldg" not in text and "global.nc" not in text
+
+
+@pytest.mark.parametrize("over", [
+    dict(n_outer=1, dlogits_stride_outer=0),
+    dict(n_outer=1, logits_stride_outer=0, dlogits_stride_outer=12345),
+    dict(n_inner=1, dlogits_stride_inner=7),
+    dict(n_outer=1, n_inner=1, dlogits_stride_outer=3, dlogits_stride_inner=0),
+])
+def test_a_gradient_in_place_of_one_row_has_any_stride(over):
+    """The stride of a level with one place says nothing about where its rows lie."""
+    lib = binding.load_library()
+    # refused for its workspace, which is looked at after the buffers
+    d = policy(dlogits=0x1000000, **over)
+    assert lib.odsgd_policy_loss(d, None, 1 << 20, None) == binding.ERR_ARG and "workspace" in lib.odsgd_last_error(None).decode()
+
+
+@pytest.mark.parametrize("over", [dict(n_outer=2, dlogits_stride_outer=900), dict(n_inner=2, dlogits_stride_inner=200),
+                                  dict(n_outer=1, n_inner=2, dlogits_stride_inner=150)])
+def test_a_gradient_over_the_logits_of_other_strides_is_still_refused(over):
+    lib = binding.load_library()
+    assert lib.odsgd_policy_loss(policy(dlogits=0x1000000, **over), None, 1 << 20, None) == binding.ERR_OVERLAP
