@@ -409,7 +409,8 @@ int launch_loss(RowArgs a, const RowShape& s, int hold_bytes, void* stream) {
 }
 
 template <typename T>
-int launch_rows_t(const RowArgs& a, const RowShape& s, bool loss, void* stream) {
+int launch_rows_t(RowArgs a, const RowShape& s, bool loss, void* stream) {
+    a.exp_temp = RowExp<T>::bounded(a.inv_temp);
     if (!loss)
         return launch("score kernel", row_kernel<T, false, kScoreThreads, kScoreCtas>, dim3(a.rows * (unsigned)s.cluster),
                       dim3((unsigned)s.threads), 0, s.cluster, stream, a);

@@ -200,6 +200,7 @@ struct RowArgs {
     int cluster;
     int hold;  // losses: batches of a row that a CTA holds in shared memory
     float inv_temp, clip_low, clip_high, kl_coef, grad_scale;
+    float exp_temp;  // inv_temp as RowExp takes it
 };
 
 // Maximum m of a set of z and sum of exp(c (z - m)); m = -inf, s = 0 for the empty set.
@@ -211,10 +212,14 @@ struct MaxSum {
 // through the base-2 exponential of the special-function unit (2^-22 relative, far below the 2^-8 or
 // 2^-11 that the gradient is rounded to).  The difference comes first: the largest element has
 // exactly 1, and c m alone would overflow where a mask holds the type's lowest value.
+// For 16-bit rows the inverse temperature is bounded where its product with log2 e is still finite, so that
+// the largest element's difference of 0 stays 0 (beyond, only logits less than 1e-36 apart would notice).
 template <typename T>
 struct RowExp {
     float c, m;
-    __device__ __forceinline__ RowExp(float inv_temp, float m_) : c(sizeof(T) == 4 ? inv_temp : inv_temp * 1.4426950408889634f), m(m_) {}
+    static float bounded(float inv_temp) { return sizeof(T) == 4 ? inv_temp : fminf(inv_temp, 2.3e38f); }
+    __device__ __forceinline__ RowExp(float bounded_temp, float m_)
+        : c(sizeof(T) == 4 ? bounded_temp : bounded_temp * 1.4426950408889634f), m(m_) {}
     __device__ __forceinline__ F2 exponent(float z0, float z1) const { return (f2(z0, z1) + f2(-m, -m)) * f2(c, c); }
     __device__ __forceinline__ F2 operator()(float z0, float z1) const {
         float t0, t1;
@@ -321,10 +326,10 @@ __device__ __forceinline__ void store_vector(T* p, const uint4& q, bool aligned)
 
 // x joined with the elements of some vectors.
 template <typename T>
-__device__ __forceinline__ MaxSum add_vectors(MaxSum x, const uint4 (&q)[kRowVectors], float inv_temp) {
+__device__ __forceinline__ MaxSum add_vectors(MaxSum x, const uint4 (&q)[kRowVectors], float inv_temp, float exp_temp) {
     constexpr int L = kLanes<T>;
     const float m = fmaxf(x.m, vectors_max<T>(q));
-    const RowExp<T> e(inv_temp, m == -CUDART_INF_F ? 0.0f : m);
+    const RowExp<T> e(exp_temp, m == -CUDART_INF_F ? 0.0f : m);
     F2 sum = f2(0.0f, 0.0f);
 #pragma unroll
     for (int k = 0; k < kRowVectors; ++k) {
@@ -384,7 +389,7 @@ template <typename T>
 struct RowGradient {
     RowExp<T> e;
     float neg;  // -k / s
-    __device__ __forceinline__ RowGradient(float inv_temp, float m, float neg_) : e(inv_temp, m), neg(neg_) {}
+    __device__ __forceinline__ RowGradient(float exp_temp, float m, float neg_) : e(exp_temp, m), neg(neg_) {}
     __device__ __forceinline__ uint4 operator()(const uint4& q) const {
         constexpr int L = kLanes<T>;
         float p[L];
@@ -475,12 +480,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) row_kernel(const __grid_constan
 #pragma unroll
             for (int k = 0; k < kRowVectors; ++k) held[b + k * threads + tid] = q[k];
         }
-        x = add_vectors<T>(x, q, a.inv_temp);
+        x = add_vectors<T>(x, q, a.inv_temp, a.exp_temp);
     }
     if (b < n) {
 #pragma unroll
         for (int k = 0; k < kRowVectors; ++k) q[k] = b + k * threads + tid < n ? __ldcs(zv + b + k * threads + tid) : neg_inf_vector<T>();
-        x = add_vectors<T>(x, q, a.inv_temp);
+        x = add_vectors<T>(x, q, a.inv_temp, a.exp_temp);
     } else {
         b -= step;  // the batch that q holds
     }
@@ -519,7 +524,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) row_kernel(const __grid_constan
     }
     const RowLoss loss(a, in, logp, w);
     if (first) loss.store(a, row, logp);
-    const RowGradient<T> grad(a.inv_temp, x.m, -loss.k / x.s);
+    const RowGradient<T> grad(a.exp_temp, x.m, -loss.k / x.s);
     if (aligned) {
         uint4* to = reinterpret_cast<uint4*>(dv);
 #pragma unroll

@@ -253,3 +253,25 @@ def test_a_kept_result_keeps_no_workspace():
     r = lm.policy_loss(z, tok, -v, v, v)
     assert r.stats.untyped_storage().nbytes() == 16
     assert r.logp.untyped_storage().nbytes() == 4 * 3000 and r.dlogits.untyped_storage().nbytes() == 4 * z.numel()
+
+
+# --------------------------------------------------------------------------- temperature
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("vocab", [7, 3000])
+def test_scores_at_the_ends_of_the_temperature(dtype, vocab):
+    """Any positive finite inverse temperature: the largest leaves the rows' maxima, the smallest all entries alike.
+    A product with it may leave the range of binary32, the maximum's own difference (0) may not."""
+    z = torch.arange(vocab, device=DEV).remainder(5).to(dtype) * 0.25
+    z = torch.stack([z, -z, torch.zeros_like(z)])
+    y = torch.tensor([4, 0, 1], device=DEV)
+    top = (z.float() == z.float().amax(-1, keepdim=True)).sum(-1)
+    for c in (2.0 ** 127 * 1.9, 3e38, 2.3e38, 1e30):
+        got = lm.token_logprob(z, y, inv_temp=c).logp.cpu()
+        R.within(got, -torch.log(top.double().cpu()), torch.full((3,), 1e-5, dtype=torch.float64), f"logp at {c}")
+    for c in (1e-45, 1e-38, 1e-20):
+        got = lm.token_logprob(z, y, inv_temp=c).logp.cpu()
+        R.within(got, torch.full((3,), vocab, dtype=torch.float64).log().neg(), torch.full((3,), 1e-5, dtype=torch.float64), f"logp at {c}")
+    v = torch.ones(3, device=DEV)
+    p = lm.policy_loss(z, y, v * 0, v, v, inv_temp=3e38, grad_scale=1e-38)
+    assert bool(torch.isfinite(p.stats).all()) and bool(torch.isfinite(p.dlogits).all())
