@@ -29,13 +29,18 @@ int fail(int code, const std::string& msg) {
     return code;
 }
 
-// Nothing may be thrown across the C boundary (building an error text can run out of memory).
+// Nothing may be thrown across the C boundary.  What the bodies can throw is that host memory has run out (a set's
+// tables, an error text).
 template <typename F>
 int guarded(F body) noexcept {
     try {
         return body();
     } catch (...) {
-        return ODSGD_ERR_ARG;
+        try {
+            return fail(ODSGD_ERR_ARG, "out of host memory");
+        } catch (...) {
+            return ODSGD_ERR_ARG;  // not even for the text
+        }
     }
 }
 

@@ -1,6 +1,8 @@
 """Host side of the language-model calls: shapes and buffers beside those of test_lm_host.  No kernel is
 launched here."""
 import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -62,3 +64,27 @@ def test_a_gradient_in_place_of_one_row_has_any_stride(over):
 def test_a_gradient_over_the_logits_of_other_strides_is_still_refused(over):
     lib = binding.load_library()
     assert lib.odsgd_policy_loss(policy(dlogits=0x1000000, **over), None, 1 << 20, None) == binding.ERR_OVERLAP
+
+
+LIMITED = """
+import ctypes, resource, sys
+sys.path.insert(0, {root!r})
+from paper_2005_06728_b200 import binding, lm
+lib = binding.load_library()
+assert lib.odsgd_token_logprob(None, None) == binding.ERR_ARG  # leaves its text
+with open("/proc/self/status") as f:
+    held = next(int(line.split()[1]) for line in f if line.startswith("VmSize")) * 1024
+resource.setrlimit(resource.RLIMIT_AS, (held + (1 << 30), held + (1 << 30)))
+h = ctypes.c_void_p(1)
+t = lm._GRAD_TENSOR.pack(0x1000000, 1 << 42, 0, lm.F32, 0)  # a table of 6 GB
+rc = lib.odsgd_grad_set_create(ctypes.byref(h), t, 1, 1, None, 0, None)
+print(rc, h.value, lib.odsgd_last_error(None).decode())
+"""
+
+
+def test_running_out_of_host_memory_says_so():
+    """Nothing is thrown across the boundary, and the text is not that of an earlier failure."""
+    code = LIMITED.format(root=build.ROOT)
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=600)
+    assert out.returncode == 0, out.stderr[-2000:]
+    assert out.stdout.split(maxsplit=2) == [str(binding.ERR_ARG), "None", "out of host memory\n"]
