@@ -619,7 +619,9 @@ int odsgd_policy_loss(const odsgd_policy_desc* desc, void* workspace, size_t wor
  * to stay where they are.  create() allocates one device table (32 bytes per 4096 or
  * 16384 elements) with cudaMalloc and fills it on `stream`: not while that stream is
  * capturing (ERR_STATE), and calls on other streams have to be ordered behind it.  The table also
- * holds the partial sums of a call, so the calls of one set must not overlap on the GPU.
+ * holds the partial sums of a call, so the calls of one set must not overlap on the GPU.  A graph
+ * that recorded a set's calls needs the set for as long as it is replayed; other sets may be made and destroyed
+ * while one is recorded.  destroy() frees the table (cudaFree, which waits for the GPU).
  *   norms  device, n_groups floats, out; NULL if not wanted (clip only)
  * Errors: ERR_ARG (NULL, bad type or group, a tensor beyond its arena, max_norm negative or NaN),
  * ERR_ALIGN, ERR_OVERLAP (tensors in place, or places in an arena, that overlap; an arena that

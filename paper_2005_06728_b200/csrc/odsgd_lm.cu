@@ -475,6 +475,21 @@ struct Span {
     uintptr_t lo, hi;
     int kind;
 };
+
+// Lets this thread allocate and free while a stream that is not the call's is being captured: both would
+// otherwise fail, and end that capture.
+struct BesideCapture {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    BesideCapture() { swap(); }
+    ~BesideCapture() { swap(); }
+    BesideCapture(const BesideCapture&) = delete;
+    BesideCapture& operator=(const BesideCapture&) = delete;
+
+private:
+    void swap() {
+        if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) cudaGetLastError();
+    }
+};
 }  // namespace
 
 struct odsgd_grad_set {
@@ -488,7 +503,9 @@ struct odsgd_grad_set {
     double* partial = nullptr;
     GradGroup* groups = nullptr;
     ~odsgd_grad_set() {
-        if (table) cudaFree(table);
+        if (!table) return;
+        const BesideCapture beside;
+        if (cudaFree(table) != cudaSuccess) cudaGetLastError();  // not left for the caller's next check
     }
 };
 
@@ -570,6 +587,7 @@ int make_set(odsgd_grad_set* s, const odsgd_grad_tensor* t, size_t n, int n_grou
     if (cap != cudaStreamCaptureStatusNone) return fail(ODSGD_ERR_STATE, "odsgd_grad_set_create cannot be recorded into a stream capture");
     const int rc = current_device(&s->device);
     if (rc != ODSGD_OK) return rc;
+    const BesideCapture beside;
     e = cudaMalloc(&s->table, filled + (size_t)s->n_chunks * 8);
     if (e != cudaSuccess) {
         s->table = nullptr;

@@ -299,7 +299,8 @@ class GradSet:
 
     The set keeps its tensors alive; they must stay where they are, and calls of one set must not
     overlap on the GPU.  Its table is filled on `stream`: calls on other streams have to be ordered
-    behind that.  Like a context it can be closed; it frees its table when dropped.
+    behind that.  Like a context it can be closed; it frees its table when dropped, so a graph that recorded its
+    calls needs the set for as long as it is replayed.
     """
 
     def __init__(self, groups: Sequence[Sequence[torch.Tensor]], *, offsets: Optional[Sequence] = None,

@@ -275,3 +275,25 @@ def test_scores_at_the_ends_of_the_temperature(dtype, vocab):
     v = torch.ones(3, device=DEV)
     p = lm.policy_loss(z, y, v * 0, v, v, inv_temp=3e38, grad_scale=1e-38)
     assert bool(torch.isfinite(p.stats).all()) and bool(torch.isfinite(p.dlogits).all())
+
+
+# --------------------------------------------------------------------------- capture
+
+def test_a_set_dropped_or_made_beside_a_capture():
+    """A set that goes while a graph is being recorded frees its table and leaves the recording intact; so does one
+    that is made on a stream that records nothing."""
+    g = [[randn(5000, seed=190)]]
+    kept, dropped = lm.GradSet(g), lm.GradSet([[randn(50, seed=191)]])
+    out = torch.zeros(1, device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept.norm(out=out)
+        dropped.close()
+        other = lm.GradSet([[g[0][0][:77]]], stream=side)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float(out[0]) == float(kept.norm()[0]) > 0
+    side.synchronize()
+    assert abs(float(other.norm()[0]) - float(g[0][0][:77].double().norm())) < 1e-4
