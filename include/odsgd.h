@@ -483,7 +483,8 @@ int odsgd_get_launch_count(odsgd_ctx* ctx, uint64_t* launches);
  *
  * These calls take no context.  They run on the current CUDA device, on `stream`, and allocate
  * nothing (odsgd_grad_set_create alone allocates a table); outputs and workspaces are the
- * caller's.  A failed call has written nothing; odsgd_last_error(NULL) has its text for the
+ * caller's.  A refused call (any error but ERR_CUDA) has written nothing; after ERR_CUDA a launch of
+ * the call may have run before the one that failed.  odsgd_last_error(NULL) has the text for the
  * calling thread.  Inputs are read and outputs written in stream order: memory that belongs to
  * another stream has to be ordered by the caller.
  *
@@ -493,8 +494,10 @@ int odsgd_get_launch_count(odsgd_ctx* ctx, uint64_t* launches);
  * table's or activation's `dim`, the vocabulary) is contiguous.  Strides are >= 0; rows that are
  * written must not overlap.  Pointers need the alignment of their element type only; 16-byte
  * aligned rows run fastest.  Sums and softmax statistics are held in 32 bits or more; results are
- * rounded once to the type they are stored in.  The order of every sum is fixed by the sizes of
- * the call: equal inputs give equal bits.
+ * rounded once to the type they are stored in.  No sum is added atomically.  Its order follows from sizes, types and
+ * tokens, for rows of logits and gradient tensors also from where they start on a 16-byte boundary, and for
+ * rows of logits from the number of SMs: a call repeated on the same buffers gives the same bits; equal
+ * values elsewhere, or on another GPU, may differ by a rounding (as the norm of a set may between its two calls).
  */
 #define ODSGD_F32 0
 #define ODSGD_BF16 1

@@ -2,8 +2,10 @@
 // its gradient, token scores, the clipped policy loss with its gradient, gradient norm and clip.
 //
 // All of them are bound by memory traffic; each kernel's comment says how it keeps to one read of
-// what it reads and one write of what it writes, and what was measured.  Times are of one B200, whose
-// copy rate is 6549 GB/s.
+// what it reads and one write of what it writes, and what was measured.  Times are of the kernels alone on
+// one B200, whose copy rate is 6549 GB/s, in a CUDA graph of a few passes.  Passes that go on for longer
+// run at the clock that the power limit leaves, which costs those with an exponential an element up to a
+// sixth, the others a few per cent; calls that are shorter than some 10 us wait for the host.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -317,7 +319,9 @@ __device__ __forceinline__ void store_elements(T* p, const uint4& q) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) h[i] = (unsigned short)(u[i / 2] >> (i % 2 * 16));
 }
-// `aligned`: the gradient's row starts as far behind a 16-byte boundary as the logits' does.
+// `aligned`: the gradient's row starts as far behind a 16-byte boundary as the logits' does.  Where it does not
+// (a shifted view of an odd vocabulary, with a contiguous gradient) elements are stored one by one: 8184 rows of
+// 50257 bf16 take 1084 us, of 50256 298.
 template <typename T>
 __device__ __forceinline__ void store_vector(T* p, const uint4& q, bool aligned) {
     if (aligned) __stcs(reinterpret_cast<uint4*>(p), q);
@@ -414,7 +418,7 @@ __device__ __forceinline__ MaxSum single(float z) { return MaxSum{z, z == -CUDAR
 // memory, its last in registers and the rest in the L2; DRAM sees about one read and one write (8192
 // rows of 131072 bf16: 0.62 ms against 0.55 for those bytes at the copy rate; 0.66 with the whole
 // second reading from the L2, which by then has lost a sixth of it).
-// Scores: 8184 rows of 50021 bf16 125 us, 0.98 of the copy rate, in 128-thread CTAs, twelve an SM
+// Scores: 8184 rows of 50021 bf16 126 us, 0.97 of the copy rate, in 128-thread CTAs, twelve an SM
 // (182 in 512-thread ones: the more rows in flight, the less the latency of label, row and join
 // shows).  Losses: 256 threads, five an SM, and for rows the L2 holds fewer of 512, two an SM.
 // Four vectors a thread in flight rather than eight: 881 -> 681 us for the wide loss, by the warps
@@ -709,7 +713,7 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(const __grid_con
 //   join_kernel  Adds the parts of the runs that cross boundaries, in an order that the sizes fix: a CTA takes a run and a
 //                slab of columns, so one very long run is added by few.
 // The order of every sum depends on sizes and tokens alone.
-// 32760 tokens, 2048 bf16 columns, a table of 50021 rows (544 MB): 108 us, 0.77 of the copy rate: 25 us of
+// 32760 tokens, 2048 bf16 columns, a table of 50021 rows (544 MB): 109 us, 0.76 of the copy rate: 25 us of
 // zeros beside the sort (of which the sort takes 20), 75 for sums and the other zeros, 8 for the join.
 // Rows kept packed until they are added, so that eight rows a thread and eight CTAs an SM are in flight:
 // sums 77 -> 36 us.
