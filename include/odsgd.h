@@ -645,6 +645,60 @@ int odsgd_grad_set_norm(odsgd_grad_set* set, float* norms, void* stream);
 int odsgd_grad_set_clip(odsgd_grad_set* set, float max_norm, float* norms, void* stream);
 int odsgd_grad_set_destroy(odsgd_grad_set* set);
 
+/*
+ * Gated feed-forward block over rows of tokens x, with weights [width][dim]:
+ *     gate = x Wg^T    up = x Wu^T    h = act(gate) * up
+ *     act  = SILU: t / (1 + exp(-t))    GELU: t (1 + erf(t / sqrt 2)) / 2
+ * and its gradient from dh and the kept gate and up:
+ *     dg = dh up act'(gate)    du = dh act(gate)
+ *     dx = dg Wg + du Wu    dWg (+)= dg^T x    dWu (+)= du^T x
+ * x, h, gate, up, dh and dx are of `type`, 16 bits.  Weights are of `type`, or stand in an arena in 32 bits and are
+ * rounded to `type` by the call (they are operands of products of that type, as are dg and du, which are rounded to it
+ * too).  Sums and activation are held in 32 bits and rounded once.  Gradients of weights come in `type`, or in 32 bits
+ * where they go to a gradient arena, there added to what it holds if `accumulate` is set.  NaN and infinities
+ * act as the formulas say, within their token (and, as in any such product, in all gradients of weights).
+ * `workspace`: device memory of at least the size that odsgd_gated_workspace() reports for this descriptor (operands that
+ * have to be laid out, dg and du), 16-byte aligned, free again when the call's work is done.
+ * Errors: ERR_ARG, ERR_ALIGN, ERR_OVERLAP (what is written overlaps anything else), ERR_UNSUPPORTED, ERR_CUDA.
+ */
+#define ODSGD_SILU 0
+#define ODSGD_GELU 1
+typedef struct odsgd_gated_desc {
+    const void* x;                /* device, [n_outer][n_inner][dim] of type */
+    const void* w_gate;           /* device, [width][dim] of weight_type */
+    const void* w_up;             /* the same */
+    void* h;                      /* device, [n_outer][n_inner][width] of type: written by the forward call; the backward call reads dh here */
+    void* gate;                   /* the same shape: written by the forward call (NULL: not kept), read by the backward call */
+    void* up;                     /* the same */
+    void* dx;                     /* backward: out, as x; NULL: not wanted */
+    void* dw_gate;                /* backward: out, [width][dim] of dw_type; both NULL: not wanted */
+    void* dw_up;
+    int type;                     /* ODSGD_BF16 or ODSGD_F16 */
+    int weight_type;              /* type or ODSGD_F32 */
+    int dw_type;                  /* type or ODSGD_F32 */
+    int activation;               /* ODSGD_SILU or ODSGD_GELU */
+    int accumulate;               /* backward, ODSGD_F32 gradients: 1 adds to dw_gate and dw_up */
+    int64_t n_outer, n_inner;     /* either may be 0; the product at most ODSGD_MAX_TOKENS */
+    int64_t dim, width;           /* 1 .. 2^20 */
+    int64_t x_stride_outer, x_stride_inner;
+    int64_t h_stride_outer, h_stride_inner;
+    int64_t gate_stride_outer, gate_stride_inner;
+    int64_t up_stride_outer, up_stride_inner;
+    int64_t dx_stride_outer, dx_stride_inner;
+    int64_t w_gate_stride, w_up_stride;   /* >= dim */
+    int64_t dw_gate_stride, dw_up_stride; /* >= dim */
+} odsgd_gated_desc;
+
+int odsgd_gated_workspace(const odsgd_gated_desc* desc, int backward, size_t* bytes);
+int odsgd_gated_forward(const odsgd_gated_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+int odsgd_gated_backward(const odsgd_gated_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * How many waits inside the kernels of the gated block have given up on the current device since the library was loaded.  They wait for
+ * their own copies and products alone and give up after seconds: not 0 means that a result is void.  Waits for the GPU.
+ */
+int odsgd_stalled_waits(unsigned int* count);
+
 /* Text describing the last failure on `ctx` (or, for ctx == NULL, of the last failed
  * odsgd_create or context-free call on this thread).  Never NULL. */
 const char* odsgd_last_error(odsgd_ctx* ctx);

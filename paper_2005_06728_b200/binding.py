@@ -42,7 +42,8 @@ EXPORTS = (
     "odsgd_ssgd_step_bound", "odsgd_step_bound", "odsgd_worker_local_update", "odsgd_shard_range",
     "odsgd_set_weight_mirrors", "odsgd_embed_lookup", "odsgd_embed_grad_workspace", "odsgd_embed_grad",
     "odsgd_token_logprob", "odsgd_policy_loss_workspace", "odsgd_policy_loss", "odsgd_grad_set_create",
-    "odsgd_grad_set_norm", "odsgd_grad_set_clip", "odsgd_grad_set_destroy",
+    "odsgd_grad_set_norm", "odsgd_grad_set_clip", "odsgd_grad_set_destroy", "odsgd_gated_workspace",
+    "odsgd_gated_forward", "odsgd_gated_backward", "odsgd_stalled_waits",
 )
 
 
@@ -133,6 +134,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "odsgd_grad_set_norm": ([vp, vp, vp], ci),
         "odsgd_grad_set_clip": ([vp, cf, vp, vp], ci),
         "odsgd_grad_set_destroy": ([vp], ci),
+        "odsgd_gated_workspace": ([vp, ci, ctypes.POINTER(ctypes.c_size_t)], ci),
+        "odsgd_gated_forward": ([vp, vp, ctypes.c_size_t, vp], ci),
+        "odsgd_gated_backward": ([vp, vp, ctypes.c_size_t, vp], ci),
+        "odsgd_stalled_waits": ([ctypes.POINTER(ctypes.c_uint)], ci),
     }
     for name, (argtypes, restype) in sig.items():
         fn = getattr(lib, name)  # AttributeError if the library lacks a declared symbol

@@ -12,13 +12,14 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libodsgd.so")
-SOURCES = [os.path.join(CSRC, "odsgd.cu"), os.path.join(CSRC, "odsgd_lm.cu")]
-HEADERS = [os.path.join(CSRC, "odsgd_kernels.cuh"), os.path.join(CSRC, "odsgd_lm_kernels.cuh"), os.path.join(INCLUDE, "odsgd.h")]
+SOURCES = [os.path.join(CSRC, f) for f in ("odsgd.cu", "odsgd_lm.cu", "odsgd_gated.cu")]
+HEADERS = [os.path.join(CSRC, f) for f in ("odsgd_kernels.cuh", "odsgd_lm_host.h", "odsgd_lm_elements.cuh", "odsgd_lm_kernels.cuh",
+                                           "odsgd_gated_kernels.cuh")] + [os.path.join(INCLUDE, "odsgd.h")]
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-Xcompiler", "-fPIC", "-shared",
+    "-Xcompiler", "-fPIC", "-shared", "--threads", "0",
 ]
 
 

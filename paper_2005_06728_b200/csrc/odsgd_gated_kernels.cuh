@@ -1,0 +1,512 @@
+// Device code of the gated feed-forward block (sm_100a): act(x Wg^T) * (x Wu^T), and its gradient.
+//
+// All products run on the tensor cores (tcgen05): operands come to shared memory by TMA, sums stand in tensor
+// memory in 32 bits.  One kernel serves the three of them, which differ in how operands lie and what happens to a
+// finished tile:
+//   forward       rows of x against 128 rows of Wg and the same 128 of Wu: a tile holds both projections of a
+//                 token, so that activation and product are taken where the sums are
+//   gradient of x         [dg | du] [Wg; Wu]: one sum over both halves, the second begun where the first ends
+//   gradient of weights   dg^T x and du^T x: tiles of both in one launch
+#pragma once
+
+#include <cuda.h>
+
+#include "odsgd_lm_elements.cuh"
+
+namespace odsgd_lm {
+
+// ------------------------------------------------------------------ barriers, copies, tensor memory
+__device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, unsigned count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, unsigned bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// One arrival at a barrier that may be another CTA's of the cluster.
+__device__ __forceinline__ void barrier_arrive_at(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, unsigned parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+
+// Waits that have given up since the library was loaded (odsgd_stalled_waits).  None ever should.
+__device__ unsigned int stalled_waits;
+
+// No wait is without an end: after about four seconds it is given up, counted, and `stalled` ends the CTA's other
+// waits.  What comes out of that launch is void.
+__device__ __forceinline__ unsigned long long nanoseconds() {
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+__device__ __noinline__ bool barrier_wait_long(uint32_t bar, unsigned parity, volatile int* stalled) {
+    const unsigned long long until = nanoseconds() + 4000000000ull;
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (barrier_try(bar, parity)) return true;
+        if (*stalled) return false;
+        if (nanoseconds() > until) break;
+    }
+    *stalled = 1;
+    atomicAdd(&stalled_waits, 1u);
+    return false;
+}
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, unsigned parity, volatile int* stalled) {
+    return barrier_try(bar, parity) || barrier_wait_long(bar, parity, stalled);
+}
+
+// A box of a tensor, from column c and row r on, into this CTA's shared memory; counted at `bar`, which is in the
+// cluster's first CTA.
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int c, int r, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(c), "r"(r), "r"(bar)
+        : "memory");
+}
+
+template <int CTAS>
+__device__ __forceinline__ void tensor_alloc(uint32_t smem_out, unsigned columns) {
+    if constexpr (CTAS == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_out), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_out), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+}
+template <int CTAS>
+__device__ __forceinline__ void tensor_free(uint32_t base, unsigned columns) {
+    if constexpr (CTAS == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns));
+}
+__device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// d (+)= A B^T over 16 of the long axis; the pair's first CTA issues it for both.
+__device__ __forceinline__ void multiply_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a),
+                 "l"(b), "r"(instr), "r"((uint32_t)add)
+                 : "memory");
+}
+// An arrival at the barrier of this offset in both CTAs, when all products issued so far are done.
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+
+// 32 columns of a warp's 32 lanes: x[i] is column i of the thread's lane.
+__device__ __forceinline__ void tensor_load(uint32_t addr, float (&x)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+        "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tensor_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// Operands lie in shared memory as TMA's 128-byte swizzle writes them, 1024-byte aligned: rows of 128 bytes (64
+// elements of 16 bits), eight rows to a unit of 1024 bytes.
+//   long axis inside the rows (`lines` false): a row is one of the tile's rows, units follow one another; 16 further
+//     elements of the long axis are 32 bytes on.
+//   tile's axis inside the rows (`lines` true): a row is one place of the long axis with 64 of the tile's rows; the
+//     next 64 of the tile's rows are kBlockK rows further on, 16 further places of the long axis 16 rows.
+constexpr int kBlockK = 64;  // of the long axis, in one stage
+__device__ __forceinline__ uint64_t operand(uint32_t addr, bool lines) {
+    const uint64_t chunk = lines ? (uint64_t)(kBlockK * 128 >> 4) : 1, unit = 1024 >> 4;
+    return (uint64_t)(addr >> 4 & 0x3fff) | chunk << 16 | unit << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__host__ __device__ constexpr uint32_t operand_step(bool lines) { return (lines ? 16 * 128 : 32) >> 4; }  // to the next 16 of the long axis
+
+// 32-bit sums of 16-bit products, rows x columns of the pair's tile.
+__host__ __device__ constexpr uint32_t instruction(bool is_bf16, bool a_lines, bool b_lines, int rows, int columns) {
+    return 1u << 4 | (is_bf16 ? 1u << 7 | 1u << 10 : 0u) | (a_lines ? 1u << 15 : 0u) | (b_lines ? 1u << 16 : 0u) | (uint32_t)(columns >> 3) << 17 |
+           (uint32_t)(rows >> 4) << 24;
+}
+
+// ------------------------------------------------------------------ activation
+// Both by their formulas in 32 bits; `slope` is the derivative.
+struct Activated {
+    float value, slope;
+};
+__device__ __forceinline__ float activate(float t, bool gelu) {
+    if (gelu) return 0.5f * t * (1.0f + erff(t * 0.70710678f));
+    return __fdividef(t, 1.0f + __expf(-t));
+}
+__device__ __forceinline__ Activated activate_with_slope(float t, bool gelu) {
+    if (gelu) {
+        const float cdf = 0.5f * (1.0f + erff(t * 0.70710678f));
+        return {t * cdf, cdf + t * 0.39894228f * __expf(-0.5f * t * t)};
+    }
+    const float s = __fdividef(1.0f, 1.0f + __expf(-t));
+    return {t * s, s * (1.0f + t * (1.0f - s))};
+}
+
+// ------------------------------------------------------------------ tiles
+enum GatedKind { kForward, kGradX, kGradW };
+
+// Rows of an output: row r lies at (r / n_inner) * so + (r % n_inner) * si.
+struct RowsOut {
+    void* p;
+    long long so, si;
+};
+
+struct GatedArgs {
+    CUtensorMap a[2], b[2];
+    RowsOut out[3];          // forward: h, gate, up; gradient of x: dx; of weights: dw_gate, dw_up
+    unsigned rows, columns;  // of the product (forward: columns of each projection)
+    unsigned n_inner;        // rows of an outer level of the outputs
+    unsigned depth;          // the long axis (gradient of x: of one half)
+    int is_bf16, out_f32, accumulate, gelu, save;
+};
+
+constexpr int kTileRows = 256;       // of a pair of CTAs: 128 each
+constexpr int kTileColumns = 256;    // sums a row: forward 128 gates and 128 ups
+constexpr int kGatedStages = 6;
+constexpr int kHalfBytes = 128 * kBlockK * 2;     // 128 rows of an operand, one stage
+constexpr int kStageBytes = 2 * kHalfBytes;       // of one CTA: its 128 rows of A, its half of B
+constexpr int kGatedThreads = 256;                // copy, products, tensor memory, one idle warp; four that finish tiles
+constexpr int kPatchPitch = 33;                   // words of a row of the patch through which unaligned rows are written
+constexpr int kGatedSmem = 1024 + kGatedStages * kStageBytes + 4 * 32 * kPatchPitch * 4;
+constexpr int kGroupTiles = 8;                    // tiles of rows that follow one another before the columns move on
+
+struct GatedBarriers {
+    unsigned long long full[kGatedStages], empty[kGatedStages];
+    unsigned long long sums_full[2], sums_empty[2];
+    uint32_t tensor_base;
+    int stalled;
+};
+
+// 32 consecutive columns of a row from registers to memory.  Rows that start on 16 bytes are written by their
+// threads, 16 bytes at a time.  Others go through a patch of shared memory, from which the warp writes row by row.
+// Out-of-range rows have p == nullptr.
+template <typename T>
+__device__ __forceinline__ void store_32(T* p, int valid, bool vec, const float (&x)[32], uint32_t* patch, unsigned lane) {
+    if (vec) {
+        if (p != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 32; i += kLanes<T>) {
+                float y[kLanes<T>];
+#pragma unroll
+                for (int l = 0; l < kLanes<T>; ++l) y[l] = x[i + l];
+                if (i + kLanes<T> <= valid) {
+                    *reinterpret_cast<uint4*>(p + i) = pack<T>(y);
+                } else {
+#pragma unroll
+                    for (int l = 0; l < kLanes<T>; ++l)
+                        if (i + l < valid) p[i + l] = from_f32<T>(y[l]);
+                }
+            }
+        }
+        return;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) patch[lane * kPatchPitch + i] = __float_as_uint(x[i]);
+    __syncwarp();
+#pragma unroll 4
+    for (int r = 0; r < 32; ++r) {
+        T* const to = reinterpret_cast<T*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(p), r));
+        if (to != nullptr && (int)lane < valid) to[lane] = from_f32<T>(__uint_as_float(patch[r * kPatchPitch + lane]));
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ T* row_of(const RowsOut& o, const GatedArgs& a, unsigned row) {
+    return static_cast<T*>(o.p) + (row / a.n_inner) * o.so + (row % a.n_inner) * o.si;
+}
+template <typename T>
+__device__ __forceinline__ bool rows_on_16(const RowsOut& o) {
+    return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.so * (long long)sizeof(T)) | (uintptr_t)(o.si * (long long)sizeof(T))) & 15) == 0;
+}
+
+// A persistent pair of CTAs per two SMs goes over tiles of 256 rows x 256 sums.  In each CTA one thread copies (its own 128 rows of
+// A and its half of B: in the forward pass the first CTA's half is Wg's, the second's Wu's), four warps finish
+// tiles; one thread of the first CTA issues the products of both.  Two sets of sums, so that one tile is finished
+// while the next is computed.
+template <int KIND, typename T>
+__global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) gated_kernel(const __grid_constant__ GatedArgs a) {
+    constexpr bool A_LINES = KIND == kGradW, B_LINES = KIND != kForward;
+    extern __shared__ unsigned char raw[];
+    __shared__ GatedBarriers s;
+    const uint32_t stages = (smem_address(raw) + 1023) & ~1023u;
+    uint32_t* const patches = reinterpret_cast<uint32_t*>(raw + (stages - smem_address(raw)) + kGatedStages * kStageBytes);
+    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x & 1;
+    const unsigned pairs = gridDim.x / 2, pair = blockIdx.x / 2;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kGatedStages; ++i) {
+            barrier_init(smem_address(&s.full[i]), 1);
+            barrier_init(smem_address(&s.empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            barrier_init(smem_address(&s.sums_full[i]), 1);
+            barrier_init(smem_address(&s.sums_empty[i]), 8);  // the finishing warps of both CTAs
+        }
+        s.stalled = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    dependent_launch_prologue();
+    if (warp == 2) tensor_alloc<2>(smem_address(&s.tensor_base), 512);
+    tensor_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tensor_fence_after();
+    const uint32_t base = *reinterpret_cast<volatile uint32_t*>(&s.tensor_base);
+
+    const unsigned col_step = KIND == kForward ? kTileColumns / 2 : kTileColumns;
+    const unsigned row_tiles = (a.rows + kTileRows - 1) / kTileRows, col_tiles = (a.columns + col_step - 1) / col_step;
+    const unsigned per_product = row_tiles * col_tiles, tiles = per_product * (KIND == kGradW ? 2 : 1);
+    const unsigned half_blocks = (a.depth + kBlockK - 1) / kBlockK, blocks = half_blocks * (KIND == kGradX ? 2 : 1);
+
+    // tile t: which product, first row, first column
+    struct Tile {
+        unsigned product, row, col;
+    };
+    const auto tile_at = [&](unsigned t) {
+        Tile out;
+        out.product = t / per_product;
+        t -= out.product * per_product;
+        const unsigned group = t / (kGroupTiles * col_tiles), first = group * kGroupTiles, many = min((unsigned)kGroupTiles, row_tiles - first);
+        t -= first * col_tiles;
+        out.row = (first + t % many) * kTileRows;
+        out.col = (t / many) * col_step;
+        return out;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            unsigned stage = 0, phase = 0;
+            bool ok = true;
+            for (unsigned t = pair; t < tiles && ok; t += pairs) {
+                const Tile tile = tile_at(t);
+                const int row = (int)(tile.row + rank * 128);
+                for (unsigned k = 0; k < blocks; ++k) {
+                    ok = barrier_wait(smem_address(&s.empty[stage]), phase ^ 1, &s.stalled);
+                    if (!ok) break;
+                    if (rank == 0) barrier_expect(smem_address(&s.full[stage]), 2 * kStageBytes);
+                    const uint32_t bar = cluster_address(&s.full[stage], 0);
+                    const uint32_t to_a = stages + stage * kStageBytes, to_b = to_a + kHalfBytes;
+                    const bool second = KIND == kGradX && k >= half_blocks;
+                    const int at = (int)((second ? k - half_blocks : k) * kBlockK);
+                    const CUtensorMap* ma = KIND == kGradW ? &a.a[tile.product] : &a.a[second];
+                    const CUtensorMap* mb = KIND == kForward ? &a.b[rank] : KIND == kGradX ? &a.b[second] : &a.b[0];
+                    const int col = (int)(KIND == kForward ? tile.col : tile.col + rank * 128);
+                    if constexpr (A_LINES) {
+                        load_box(to_a, ma, row, at, bar);
+                        load_box(to_a + kHalfBytes / 2, ma, row + 64, at, bar);
+                    } else {
+                        load_box(to_a, ma, at, row, bar);
+                    }
+                    if constexpr (B_LINES) {
+                        load_box(to_b, mb, col, at, bar);
+                        load_box(to_b + kHalfBytes / 2, mb, col + 64, at, bar);
+                    } else {
+                        load_box(to_b, mb, at, col, bar);
+                    }
+                    if (++stage == kGatedStages) stage = 0, phase ^= 1;
+                }
+            }
+            // every stage free again: the other CTA's arrivals here are in, and no copy is under way
+            for (int i = 0; i < kGatedStages && ok; ++i) {
+                ok = barrier_wait(smem_address(&s.empty[stage]), phase ^ 1, &s.stalled);
+                if (++stage == kGatedStages) stage = 0, phase ^= 1;
+            }
+            if (!ok) {  // copies under way land within this time
+                for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t instr = instruction(a.is_bf16 != 0, A_LINES, B_LINES, kTileRows, kTileColumns);
+            unsigned stage = 0, phase = 0, set = 0, set_phase = 0;
+            bool ok = true;
+            for (unsigned t = pair; t < tiles && ok; t += pairs) {
+                ok = barrier_wait(smem_address(&s.sums_empty[set]), set_phase ^ 1, &s.stalled);
+                if (!ok) break;
+                tensor_fence_after();
+                const uint32_t d = base + set * kTileColumns;
+                for (unsigned k = 0; k < blocks; ++k) {
+                    ok = barrier_wait(smem_address(&s.full[stage]), phase, &s.stalled);
+                    if (!ok) break;
+                    tensor_fence_after();
+                    const uint64_t da = operand(stages + stage * kStageBytes, A_LINES);
+                    const uint64_t db = operand(stages + stage * kStageBytes + kHalfBytes, B_LINES);
+#pragma unroll
+                    for (int i = 0; i < kBlockK / 16; ++i)
+                        multiply_pair(d, da + i * operand_step(A_LINES), db + i * operand_step(B_LINES), instr, k > 0 || i > 0);
+                    commit_pair(smem_address(&s.empty[stage]));
+                    if (++stage == kGatedStages) stage = 0, phase ^= 1;
+                }
+                if (!ok) break;
+                commit_pair(smem_address(&s.sums_full[set]));
+                if (++set == 2) set = 0, set_phase ^= 1;
+            }
+        }
+    } else if (warp >= 4) {
+        const unsigned quarter = warp & 3;
+        uint32_t* const patch = patches + quarter * 32 * kPatchPitch;
+        const bool vec_t = rows_on_16<T>(a.out[0]) && (KIND == kGradX || rows_on_16<T>(a.out[1])) && (KIND != kForward || rows_on_16<T>(a.out[2]));
+        const bool vec_f = rows_on_16<float>(a.out[0]) && rows_on_16<float>(a.out[1]);
+        unsigned set = 0, set_phase = 0;
+        for (unsigned t = pair; t < tiles; t += pairs) {
+            const Tile tile = tile_at(t);
+            const unsigned row = tile.row + rank * 128 + quarter * 32 + lane;
+            if (!__all_sync(~0u, barrier_wait(smem_address(&s.sums_full[set]), set_phase, &s.stalled))) break;
+            tensor_fence_after();
+            const uint32_t from = base + set * kTileColumns + (quarter * 32 << 16);
+            if constexpr (KIND == kForward) {
+                T* const h = row < a.rows ? row_of<T>(a.out[0], a, row) : nullptr;
+                T* const gate = row < a.rows && a.save ? row_of<T>(a.out[1], a, row) : nullptr;
+                T* const up = row < a.rows && a.save ? row_of<T>(a.out[2], a, row) : nullptr;
+#pragma unroll 1
+                for (unsigned c = 0; c < 128; c += 32) {
+                    float g[32], u[32];
+                    tensor_load(from + c, g);
+                    tensor_load(from + 128 + c, u);
+                    tensor_load_wait();
+                    const unsigned col = tile.col + c;
+                    if (col >= a.columns) break;
+                    const int valid = (int)min(32u, a.columns - col);
+                    if (a.save) {
+                        store_32<T>(gate ? gate + col : nullptr, valid, vec_t, g, patch, lane);
+                        store_32<T>(up ? up + col : nullptr, valid, vec_t, u, patch, lane);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) g[i] = activate(g[i], a.gelu != 0) * u[i];
+                    store_32<T>(h ? h + col : nullptr, valid, vec_t, g, patch, lane);
+                }
+            } else {
+                const RowsOut& o = a.out[KIND == kGradW ? tile.product : 0];
+#pragma unroll 1
+                for (unsigned c = 0; c < kTileColumns; c += 32) {
+                    float x[32];
+                    tensor_load(from + c, x);
+                    tensor_load_wait();
+                    const unsigned col = tile.col + c;
+                    if (col >= a.columns) break;
+                    const int valid = (int)min(32u, a.columns - col);
+                    if (KIND == kGradW && a.out_f32) {
+                        float* const p = row < a.rows ? row_of<float>(o, a, row) + col : nullptr;
+                        if (a.accumulate && p != nullptr) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (i < valid) x[i] += p[i];
+                        }
+                        store_32<float>(p, valid, vec_f, x, patch, lane);
+                    } else {
+                        store_32<T>(row < a.rows ? row_of<T>(o, a, row) + col : nullptr, valid, vec_t, x, patch, lane);
+                    }
+                }
+            }
+            tensor_fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive_at(cluster_address(&s.sums_empty[set], 0));
+            if (++set == 2) set = 0, set_phase ^= 1;
+        }
+    }
+    __syncwarp();
+    tensor_fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (warp == 2) {
+        tensor_fence_after();
+        tensor_free<2>(base, 512);
+    }
+}
+
+// ------------------------------------------------------------------ operands laid out
+// Rows that TMA cannot address (a row that does not start on 16 bytes, leading axes that do not fold into one), and
+// weights that stand in the arena in 32 bits, are copied once, rounded to the type of the products.
+struct LayArgs {
+    const void* from;
+    void* to;  // [rows][pitch]
+    long long so, si;
+    unsigned rows, n_inner, columns, pitch;
+};
+constexpr int kLayThreads = 256;
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(kLayThreads) lay_kernel(const __grid_constant__ LayArgs a) {
+    dependent_launch_prologue();
+    const unsigned col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
+    if (col >= a.columns) return;
+    for (unsigned row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const TI* const p = static_cast<const TI*>(a.from) + (row / a.n_inner) * a.so + (row % a.n_inner) * a.si + col;
+        float x[8] = {};
+        if (sizeof(TI) == 4 && col + 8 <= a.columns && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+            float y[kLanes<TI>];
+#pragma unroll
+            for (int h = 0; h < 8; h += kLanes<TI>) {
+                unpack<TI>(*reinterpret_cast<const uint4*>(p + h), y);
+#pragma unroll
+                for (int l = 0; l < kLanes<TI>; ++l) x[h + l] = y[l];
+            }
+        } else {
+#pragma unroll
+            for (int l = 0; l < 8; ++l)
+                if (col + l < a.columns) x[l] = to_f32<TI>(p[l]);
+        }
+        *reinterpret_cast<uint4*>(static_cast<TO*>(a.to) + (size_t)row * a.pitch + col) = pack<TO>(x);
+    }
+}
+
+// ------------------------------------------------------------------ gradient of the two projections
+// dg = dh up act'(gate), du = dh act(gate), rounded to 16 bits: they are operands of the products that follow.
+struct SlopeArgs {
+    RowsOut gate, up, dh;
+    void* dg;
+    void* du;  // [rows][pitch]
+    unsigned rows, n_inner, columns, pitch;
+    int gelu, vec;
+};
+template <typename T>
+__global__ void __launch_bounds__(kLayThreads) slope_kernel(const __grid_constant__ SlopeArgs a) {
+    dependent_launch_prologue();
+    const unsigned col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
+    if (col >= a.columns) return;
+    for (unsigned row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const unsigned o = row / a.n_inner, i = row % a.n_inner;
+        const T* const pg = static_cast<const T*>(a.gate.p) + o * a.gate.so + i * a.gate.si + col;
+        const T* const pu = static_cast<const T*>(a.up.p) + o * a.up.so + i * a.up.si + col;
+        const T* const pd = static_cast<const T*>(a.dh.p) + o * a.dh.so + i * a.dh.si + col;
+        float g[8] = {}, u[8] = {}, d[8] = {};
+        if (a.vec && col + 8 <= a.columns) {
+            unpack<T>(*reinterpret_cast<const uint4*>(pg), g);
+            unpack<T>(*reinterpret_cast<const uint4*>(pu), u);
+            unpack<T>(*reinterpret_cast<const uint4*>(pd), d);
+        } else {
+#pragma unroll
+            for (int l = 0; l < 8; ++l) {
+                if (col + l < a.columns) g[l] = to_f32<T>(pg[l]), u[l] = to_f32<T>(pu[l]), d[l] = to_f32<T>(pd[l]);
+            }
+        }
+#pragma unroll
+        for (int l = 0; l < 8; ++l) {
+            const Activated act = activate_with_slope(g[l], a.gelu != 0);
+            g[l] = d[l] * u[l] * act.slope;
+            u[l] = d[l] * act.value;
+        }
+        const size_t at = (size_t)row * a.pitch + col;
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.dg) + at) = pack<T>(g);
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.du) + at) = pack<T>(u);
+    }
+}
+
+}  // namespace odsgd_lm

@@ -37,12 +37,15 @@ MAX_TOKENS = 1 << 24
 _FLOATS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _FLOAT32 = {torch.float32: F32}
 _INTS = {torch.int32: I32, torch.int64: I64}
+_HALVES = {torch.bfloat16: BF16, torch.float16: F16}
+_ACTIVATIONS = {"silu": 0, "gelu": 1}
 
 # odsgd_embed_desc, odsgd_policy_desc and odsgd_grad_tensor of include/odsgd.h, packed by struct: a call is
 # a few microseconds, and filling a ctypes structure would be one of them.
 _EMBED = struct.Struct("3P4i10qf4x")
 _POLICY = struct.Struct("10P2i17q5f4x")
 _GRAD_TENSOR = struct.Struct("PNN2i")
+_GATED = struct.Struct("9P5i4x18q")
 
 
 class TokenLogprob(NamedTuple):
@@ -58,6 +61,18 @@ class PolicyLoss(NamedTuple):
     @property
     def loss(self) -> torch.Tensor:
         return self.stats[0]
+
+
+class GatedFfn(NamedTuple):
+    h: torch.Tensor               # [..., width], x's type
+    gate: Optional[torch.Tensor]  # the projections before the activation, the same; None unless kept
+    up: Optional[torch.Tensor]
+
+
+class GatedFfnGrad(NamedTuple):
+    dx: Optional[torch.Tensor]       # x's shape and type
+    dw_gate: Optional[torch.Tensor]  # the weights' shape
+    dw_up: Optional[torch.Tensor]
 
 
 # --------------------------------------------------------------------------- checks
@@ -283,6 +298,118 @@ def policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tens
     if given:
         increment_version(dlogits)
     return PolicyLoss(stats, logp, dlogits)
+
+
+# --------------------------------------------------------------------------- gated feed-forward block
+
+def _gated_inputs(x, w_gate, w_up, activation, dev):
+    kind = _need(x, "x", _HALVES, dev)
+    codes = {x.dtype: kind, torch.float32: F32}
+    weight_type = _need(w_gate, "w_gate", codes, dev)
+    _need(w_up, "w_up", {w_gate.dtype: weight_type}, dev)
+    if x.dim() < 1:
+        raise ValueError("x: need [..., dim]")
+    width, dim, gate_stride = _table(w_gate, "w_gate")
+    _shape(w_up, (width, dim), "w_up")
+    up_stride = _table(w_up, "w_up")[2]
+    if x.shape[-1] != dim:
+        raise ValueError(f"x: last axis {x.shape[-1]}, expected {dim}")
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation: {activation!r}, expected one of {sorted(_ACTIVATIONS)}")
+    return kind, weight_type, width, dim, gate_stride, up_stride
+
+
+def _workspace(need: int, given: Optional[torch.Tensor], like: torch.Tensor, dev: int, stream) -> torch.Tensor:
+    if given is None:
+        return _new(like, max(16, need), torch.uint8, stream)
+    if not given.is_contiguous() or given.get_device() != dev:
+        raise ValueError("workspace: need a contiguous tensor on the current device")
+    return given
+
+
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, *, activation: str = "silu", save: bool = False,
+              out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> GatedFfn:
+    """h = act(x w_gate^T) * (x w_up^T) for x [..., dim] of bfloat16 or float16 and weights [width, dim] of x's type, or
+    float32 (views of a weight arena, rounded to x's type by the call).  `save`: gate and up are kept for gated_ffn_grad.
+    activation: "silu" or "gelu" (by the error function)."""
+    dev = torch.cuda.current_device()
+    kind, weight_type, width, dim, gate_stride, up_stride = _gated_inputs(x, w_gate, w_up, activation, dev)
+    lead = x.dim() - 1
+    shape = (*x.shape[:-1], width)
+    given = out is not None
+    if not given:
+        out = _new(x, shape, x.dtype, stream)
+    else:
+        _need(out, "out", {x.dtype: kind}, dev)
+        _shape(out, shape, "out")
+    gate = up = None
+    kept, at, up_at = (0, 0), 0, 0
+    if save:
+        gate, up = _new(x, shape, x.dtype, stream), _new(x, shape, x.dtype, stream)
+        kept, at, up_at = _levels(gate, lead, "gate"), gate.data_ptr(), up.data_ptr()
+    d = _GATED.pack(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), out.data_ptr(), at, up_at, 0, 0, 0, kind, weight_type, kind,
+                    _ACTIVATIONS[activation], 0, *_sizes(x.shape[:-1]), dim, width, *_rows(x, lead, "x"), *_rows(out, lead, "out"),
+                    *kept, *kept, 0, 0, gate_stride, up_stride, 0, 0)
+    lib = binding.load_library()
+    need = ctypes.c_size_t()
+    _check(lib.odsgd_gated_workspace(d, 0, ctypes.byref(need)))
+    workspace = _workspace(need.value, workspace, x, dev, stream)
+    _check(lib.odsgd_gated_forward(d, workspace.data_ptr(), workspace.nbytes, _handle(stream, dev)))
+    if given:
+        increment_version(out)
+    return GatedFfn(out, gate, up)
+
+
+def gated_ffn_grad(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, dh: torch.Tensor, *,
+                   activation: str = "silu", want_dx: bool = True, want_dw: bool = True, dx: Optional[torch.Tensor] = None,
+                   dw_gate: Optional[torch.Tensor] = None, dw_up: Optional[torch.Tensor] = None, accumulate: bool = False,
+                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> GatedFfnGrad:
+    """The gradients of x and of both weights, from dh and what gated_ffn kept.  dw_gate and dw_up may be float32 views of a
+    gradient arena (accumulate: added to what is there); new ones are of x's type."""
+    dev = torch.cuda.current_device()
+    kind, weight_type, width, dim, gate_stride, up_stride = _gated_inputs(x, w_gate, w_up, activation, dev)
+    lead = x.dim() - 1
+    shape = (*x.shape[:-1], width)
+    for t, name in ((gate, "gate"), (up, "up"), (dh, "dh")):
+        _need(t, name, {x.dtype: kind}, dev)
+        _shape(t, shape, name)
+    want_dx, want_dw = want_dx or dx is not None, want_dw or dw_gate is not None or dw_up is not None
+    if (dw_gate is None) != (dw_up is None):
+        raise ValueError("dw_gate and dw_up go together")
+    if accumulate and dw_gate is None:
+        raise ValueError("accumulate: need dw_gate and dw_up to add to")
+    written = [t for t in (dx, dw_gate, dw_up) if t is not None]
+    dx_strides, dx_at = (0, 0), 0
+    if want_dx:
+        if dx is None:
+            dx = _new(x, tuple(x.shape), x.dtype, stream)
+        else:
+            _need(dx, "dx", {x.dtype: kind}, dev)
+            _shape(dx, x.shape, "dx")
+        dx_strides, dx_at = _rows(dx, lead, "dx"), dx.data_ptr()
+    dw_type, dg_stride, du_stride, dg_at, du_at = kind, 0, 0, 0, 0
+    if want_dw:
+        if dw_gate is None:
+            dw_gate, dw_up = _new(x, (width, dim), x.dtype, stream), _new(x, (width, dim), x.dtype, stream)
+        dw_type = _need(dw_gate, "dw_gate", {x.dtype: kind, torch.float32: F32}, dev)
+        _need(dw_up, "dw_up", {dw_gate.dtype: dw_type}, dev)
+        _shape(dw_gate, (width, dim), "dw_gate")
+        _shape(dw_up, (width, dim), "dw_up")
+        dg_stride, du_stride = _table(dw_gate, "dw_gate")[2], _table(dw_up, "dw_up")[2]
+        dg_at, du_at = dw_gate.data_ptr(), dw_up.data_ptr()
+    d = _GATED.pack(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), dh.data_ptr(), gate.data_ptr(), up.data_ptr(), dx_at, dg_at, du_at,
+                    kind, weight_type, dw_type, _ACTIVATIONS[activation], 1 if accumulate else 0, *_sizes(x.shape[:-1]), dim, width,
+                    *_rows(x, lead, "x"), *_rows(dh, lead, "dh"), *_rows(gate, lead, "gate"), *_rows(up, lead, "up"), *dx_strides,
+                    gate_stride, up_stride, dg_stride, du_stride)
+    lib = binding.load_library()
+    need = ctypes.c_size_t()
+    _check(lib.odsgd_gated_workspace(d, 1, ctypes.byref(need)))
+    workspace = _workspace(need.value, workspace, x, dev, stream)
+    _check(lib.odsgd_gated_backward(d, workspace.data_ptr(), workspace.nbytes, _handle(stream, dev)))
+    if written:
+        increment_version(written)
+    return GatedFfnGrad(dx, dw_gate, dw_up)
 
 
 # --------------------------------------------------------------------------- gradient norm and clip
