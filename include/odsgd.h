@@ -699,6 +699,74 @@ int odsgd_gated_backward(const odsgd_gated_desc* desc, void* workspace, size_t w
  */
 int odsgd_stalled_waits(unsigned int* count);
 
+/*
+ * Dropout whose mask is never stored.  Element e of x, in the order [n_outer][n_inner][dim], is kept where its 16 random
+ * bits are at least t = round(65536 p), so that it is dropped with probability t / 65536:
+ *     out = residual + (kept ? x * 65536 / (65536 - t) : 0)
+ * in 32 bits, rounded once.  The bits are those of half e % 2 (0: the low one) of word e % 8 / 2 of the generator
+ * Philox4x32-10 at counter (e / 8, offset), both of 64 bits, under the key `seed`: a call with the same seed, offset and
+ * shape has the same mask whatever types, strides and residual are, so that the backward pass is this call on the
+ * gradient, without a residual.  `counter`: a number in device memory that is added to the offset when the call runs, so that replays of
+ * a captured graph can differ.  What is dropped does not count, be it NaN.  `out` may be x (of the same type) or the
+ * residual (same pointer and strides).
+ * Errors: ERR_ARG, ERR_ALIGN, ERR_OVERLAP, ERR_UNSUPPORTED (sizes beyond the limits), ERR_CUDA.
+ */
+typedef struct odsgd_dropout_desc {
+    const void* x;                /* device, [n_outer][n_inner][dim] of type */
+    const void* residual;         /* device, the same shape of out_type; NULL: none */
+    void* out;                    /* device, the same shape of out_type */
+    const uint64_t* counter;      /* device, one number, or NULL */
+    int type;                     /* ODSGD_F32, ODSGD_BF16 or ODSGD_F16 */
+    int out_type;                 /* the same */
+    int64_t n_outer, n_inner;     /* either may be 0; the product at most ODSGD_MAX_TOKENS */
+    int64_t dim;                  /* 1 .. 2^20 */
+    int64_t x_stride_outer, x_stride_inner;
+    int64_t residual_stride_outer, residual_stride_inner;
+    int64_t out_stride_outer, out_stride_inner;
+    uint64_t seed, offset;
+    double p;                     /* >= 0, below 65535.5 / 65536 */
+} odsgd_dropout_desc;
+
+int odsgd_dropout(const odsgd_dropout_desc* desc, void* stream);
+
+/*
+ * Verification of drafted tokens, and the drawing of one more, so that what comes out is distributed as the target is.
+ * For each sequence, with p_i = softmax(inv_temp target_i), q_i = softmax(draft_inv_temp draft_i) and its random
+ * numbers u in [0, 1), drafts x_0, x_1, ... are accepted in order while
+ *     u_i q_i(x_i) < p_i(x_i)
+ * At the first place n where one is not, a token is drawn from max(0, p_n - q_n) (from p_n if that is nothing at all);
+ * behind the last draft from p_n.  It is the lowest one at which the running sum is above u_last times the whole, u_last
+ * being the sequence's last random number.  Without draft logits a draft has all of its distribution (q_i(x_i) = 1).
+ *     accepted = n    out_tokens = x_0 .. x_(n-1), the drawn one, -1 ...    logp = log p_i(out_i), 0 behind the drawn one
+ * logp is what odsgd_policy_loss takes as old_logp.  A token outside [0, vocab) ends the sequence's drafts (shorter
+ * drafts are padded with -1); `drafts` 0 draws a token alone.  -inf has probability 0.  Where a row that counts is
+ * nothing but -inf, or holds NaN or +inf, nothing is drawn: the token is -1 and its logp NaN.
+ * Rows are read once for their sums in 32 bits; the two rows of place n, and of any draft that comes within 1e-4 of the border,
+ * again in 64 bits, in which all decisions stand.  `workspace` as for odsgd_embed_grad.
+ * Errors: ERR_ARG, ERR_ALIGN, ERR_OVERLAP, ERR_UNSUPPORTED, ERR_CUDA.
+ */
+#define ODSGD_MAX_DRAFTS 255
+typedef struct odsgd_verify_desc {
+    const void* target;           /* device, [batch][drafts + 1][vocab] of type: the logits of what follows each draft */
+    const void* draft;            /* device, [batch][drafts][vocab] of type, or NULL */
+    const void* tokens;           /* device, [batch][drafts] of token_type */
+    const float* uniforms;        /* device, [batch][drafts + 1] */
+    void* out_tokens;             /* device, out, batch * (drafts + 1) of token_type */
+    int32_t* accepted;            /* device, out, batch */
+    float* logp;                  /* device, out, batch * (drafts + 1) */
+    int type;                     /* ODSGD_F32, ODSGD_BF16 or ODSGD_F16 */
+    int token_type;               /* ODSGD_I32 or ODSGD_I64 */
+    int64_t batch, drafts, vocab; /* 0 .. 2^16, 0 .. ODSGD_MAX_DRAFTS, 1 .. 2^30 */
+    int64_t target_stride_batch, target_stride_row;
+    int64_t draft_stride_batch, draft_stride_row;
+    int64_t token_stride_batch, token_stride_row;
+    int64_t uniform_stride_batch, uniform_stride_row;
+    float inv_temp, draft_inv_temp; /* > 0 */
+} odsgd_verify_desc;
+
+int odsgd_verify_workspace(const odsgd_verify_desc* desc, size_t* bytes);
+int odsgd_verify_draft(const odsgd_verify_desc* desc, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Text describing the last failure on `ctx` (or, for ctx == NULL, of the last failed
  * odsgd_create or context-free call on this thread).  Never NULL. */
 const char* odsgd_last_error(odsgd_ctx* ctx);

@@ -43,7 +43,8 @@ EXPORTS = (
     "odsgd_set_weight_mirrors", "odsgd_embed_lookup", "odsgd_embed_grad_workspace", "odsgd_embed_grad",
     "odsgd_token_logprob", "odsgd_policy_loss_workspace", "odsgd_policy_loss", "odsgd_grad_set_create",
     "odsgd_grad_set_norm", "odsgd_grad_set_clip", "odsgd_grad_set_destroy", "odsgd_gated_workspace",
-    "odsgd_gated_forward", "odsgd_gated_backward", "odsgd_stalled_waits",
+    "odsgd_gated_forward", "odsgd_gated_backward", "odsgd_stalled_waits", "odsgd_dropout", "odsgd_verify_workspace",
+    "odsgd_verify_draft",
 )
 
 
@@ -138,6 +139,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "odsgd_gated_forward": ([vp, vp, ctypes.c_size_t, vp], ci),
         "odsgd_gated_backward": ([vp, vp, ctypes.c_size_t, vp], ci),
         "odsgd_stalled_waits": ([ctypes.POINTER(ctypes.c_uint)], ci),
+        "odsgd_dropout": ([vp, vp], ci),
+        "odsgd_verify_workspace": ([vp, ctypes.POINTER(ctypes.c_size_t)], ci),
+        "odsgd_verify_draft": ([vp, vp, ctypes.c_size_t, vp], ci),
     }
     for name, (argtypes, restype) in sig.items():
         fn = getattr(lib, name)  # AttributeError if the library lacks a declared symbol

@@ -12,9 +12,10 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libodsgd.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("odsgd.cu", "odsgd_lm.cu", "odsgd_gated.cu")]
-HEADERS = [os.path.join(CSRC, f) for f in ("odsgd_kernels.cuh", "odsgd_lm_host.h", "odsgd_lm_elements.cuh", "odsgd_lm_kernels.cuh",
-                                           "odsgd_gated_kernels.cuh")] + [os.path.join(INCLUDE, "odsgd.h")]
+SOURCES = [os.path.join(CSRC, f) for f in ("odsgd.cu", "odsgd_lm.cu", "odsgd_gated.cu", "odsgd_dropout.cu", "odsgd_verify.cu")]
+HEADERS = [os.path.join(CSRC, f) for f in ("odsgd_kernels.cuh", "odsgd_lm_host.h", "odsgd_lm_elements.cuh", "odsgd_lm_softmax.cuh",
+                                           "odsgd_lm_kernels.cuh", "odsgd_gated_kernels.cuh", "odsgd_dropout_kernels.cuh",
+                                           "odsgd_verify_kernels.cuh")] + [os.path.join(INCLUDE, "odsgd.h")]
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",

@@ -1,0 +1,129 @@
+// Host side of the verification of drafted tokens: checks of arguments and launches.  No allocation, no
+// synchronisation, nothing thrown across the boundary.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "odsgd.h"
+#include "odsgd_lm_host.h"
+#include "odsgd_verify_kernels.cuh"
+
+using namespace odsgd_lm;
+
+namespace {
+
+static_assert(kVerifyDrafts == ODSGD_MAX_DRAFTS, "the shared arrays of draw_kernel");
+
+int check_verify(const odsgd_verify_desc* d, const void* ws, size_t have) {
+    if (!d) return fail(ODSGD_ERR_ARG, "desc is NULL");
+    if (!is_float_type(d->type)) return fail(ODSGD_ERR_ARG, "type must be ODSGD_F32, ODSGD_BF16 or ODSGD_F16");
+    if (!is_token_type(d->token_type)) return fail(ODSGD_ERR_ARG, "token_type must be ODSGD_I32 or ODSGD_I64");
+    if (d->batch < 0 || d->drafts < 0) return fail(ODSGD_ERR_ARG, "batch / drafts is negative");
+    if (d->vocab < 1) return fail(ODSGD_ERR_ARG, "vocab must be at least 1");
+    if (d->drafts > ODSGD_MAX_DRAFTS || d->batch > 1 << 16 || d->vocab > 1 << 30)
+        return fail(ODSGD_ERR_UNSUPPORTED, "batch, drafts or vocab beyond the limits");
+    if (!(d->inv_temp > 0.0f) || !(d->draft_inv_temp > 0.0f) || std::isinf(d->inv_temp) || std::isinf(d->draft_inv_temp))
+        return fail(ODSGD_ERR_ARG, "inv_temp and draft_inv_temp must be positive and finite");
+    const int es = size_of(d->type), ts = size_of(d->token_type);
+    const int64_t many = d->drafts + 1;
+    const Buf rows[6] = {{"target", d->target, es, d->target_stride_batch, d->target_stride_row, d->vocab, false},
+                         {"uniforms", d->uniforms, 4, d->uniform_stride_batch, d->uniform_stride_row, 1, false},
+                         {"out_tokens", d->out_tokens, ts, many, 1, 1, true},
+                         {"logp", d->logp, 4, many, 1, 1, true},
+                         {"draft", d->draft, es, d->draft_stride_batch, d->draft_stride_row, d->vocab, false},
+                         {"tokens", d->tokens, ts, d->token_stride_batch, d->token_stride_row, 1, false}};
+    const Buf accepted = {"accepted", d->accepted, 4, 1, 0, 1, true};
+    int rc = check_buffers(rows, 4, d->batch, many, -1);
+    if (rc == ODSGD_OK) rc = check_buffers(rows + (d->draft ? 4 : 5), d->draft ? 2 : 1, d->batch, d->drafts, -1);
+    if (rc == ODSGD_OK) rc = check_buffers(&accepted, 1, d->batch, 1, -1);
+    if (rc != ODSGD_OK || d->batch == 0) return rc;
+    // what is written against everything else
+    struct Out {
+        const char* name;
+        const void* p;
+        size_t bytes;
+    };
+    const size_t n = (size_t)(d->batch * many);
+    const Out out[4] = {{"accepted", d->accepted, (size_t)d->batch * 4}, {"out_tokens", d->out_tokens, n * ts}, {"logp", d->logp, n * 4}, {"workspace", ws, have}};
+    for (int i = 0; i < (ws ? 4 : 3) && rc == ODSGD_OK; ++i) {
+        rc = check_outside(out[i].name, out[i].p, out[i].bytes, rows, 2, d->batch, many);
+        if (rc == ODSGD_OK) rc = check_outside(out[i].name, out[i].p, out[i].bytes, rows + 5, 1, d->batch, d->drafts);
+        if (rc == ODSGD_OK && d->draft) rc = check_outside(out[i].name, out[i].p, out[i].bytes, rows + 4, 1, d->batch, d->drafts);
+        for (int j = 0; j < i && rc == ODSGD_OK; ++j) {
+            const uintptr_t a = reinterpret_cast<uintptr_t>(out[i].p), b = reinterpret_cast<uintptr_t>(out[j].p);
+            if (a < b + out[j].bytes && b < a + out[i].bytes) return fail(ODSGD_ERR_OVERLAP, std::string(out[i].name) + " overlaps " + out[j].name);
+        }
+    }
+    return rc;
+}
+
+// Parts of a row: of at least 4096 elements, as many as give every SM four CTAs.
+int64_t verify_chunks(const odsgd_verify_desc* d) {
+    const int64_t rows = d->batch * (2 * d->drafts + 1);
+    return std::max<int64_t>(1, std::min(ceil_div(148 * 4, std::max<int64_t>(rows, 1)), d->vocab / 4096));
+}
+size_t verify_bytes(const odsgd_verify_desc* d) {
+    return std::max<size_t>(16, (size_t)(d->batch * (2 * d->drafts + 1) * verify_chunks(d)) * sizeof(MaxSum));
+}
+
+template <typename T>
+int launch_verify(VerifyArgs a, void* stream) {
+    a.exp_temp = RowExp<T>::bounded(a.inv_temp);
+    a.draft_exp = RowExp<T>::bounded(a.draft_temp);
+    const unsigned rows = a.target_rows + (a.draft ? a.batch * a.drafts : 0);
+    const int rc = launch("verification kernel (rows)", parts_kernel<T>, dim3(rows * a.chunks), dim3(kPartThreads), 0, 1, stream, a);
+    if (rc != ODSGD_OK) return rc;
+    return launch("verification kernel (draw)", draw_kernel<T>, dim3(a.batch * (unsigned)a.cluster), dim3(kDrawThreads), 0, a.cluster, stream, a);
+}
+
+int verify(const odsgd_verify_desc* d, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_verify(d, nullptr, 0);
+    if (rc != ODSGD_OK) return rc;
+    rc = check_workspace(ws, ws_bytes, verify_bytes(d));
+    if (rc == ODSGD_OK) rc = check_verify(d, ws, verify_bytes(d));
+    if (rc != ODSGD_OK || d->batch == 0) return rc;
+    VerifyArgs a = {};
+    a.target = d->target, a.draft = d->drafts > 0 ? d->draft : nullptr, a.tokens = d->tokens, a.uniforms = d->uniforms;
+    a.out_tokens = d->out_tokens, a.accepted = d->accepted, a.logp = d->logp;
+    a.parts = static_cast<MaxSum*>(ws);
+    a.t_sb = d->target_stride_batch, a.t_sr = d->target_stride_row;
+    a.d_sb = d->draft_stride_batch, a.d_sr = d->draft_stride_row;
+    a.k_sb = d->token_stride_batch, a.k_sr = d->token_stride_row;
+    a.u_sb = d->uniform_stride_batch, a.u_sr = d->uniform_stride_row;
+    a.batch = (unsigned)d->batch, a.drafts = (unsigned)d->drafts, a.target_rows = (unsigned)(d->batch * (d->drafts + 1));
+    a.chunks = (unsigned)verify_chunks(d);
+    a.vocab = (int)d->vocab;
+    a.wide_tokens = d->token_type == ODSGD_I64;
+    // a CTA for every 4096 elements of a row, up to eight
+    a.cluster = 1;
+    while (a.cluster < kDrawCluster && d->vocab > 4096 * a.cluster) a.cluster *= 2;
+    a.inv_temp = d->inv_temp, a.draft_temp = d->draft_inv_temp;
+    switch (d->type) {
+        case ODSGD_F32: return launch_verify<float>(a, stream);
+        case ODSGD_BF16: return launch_verify<bf16>(a, stream);
+        default: return launch_verify<f16>(a, stream);
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+int odsgd_verify_workspace(const odsgd_verify_desc* desc, size_t* bytes) {
+    return guarded([&] {
+        if (!desc || !bytes) return fail(ODSGD_ERR_ARG, "desc / bytes is NULL");
+        *bytes = 0;
+        if (desc->batch < 0 || desc->drafts < 0 || desc->vocab < 1) return fail(ODSGD_ERR_ARG, "sizes out of range");
+        if (desc->drafts > ODSGD_MAX_DRAFTS || desc->batch > 1 << 16 || desc->vocab > 1 << 30)
+            return fail(ODSGD_ERR_UNSUPPORTED, "batch, drafts or vocab beyond the limits");
+        *bytes = verify_bytes(desc);
+        return (int)ODSGD_OK;
+    });
+}
+
+int odsgd_verify_draft(const odsgd_verify_desc* desc, void* workspace, size_t workspace_bytes, void* stream) {
+    return guarded([&] { return verify(desc, workspace, workspace_bytes, stream); });
+}
+
+}  // extern "C"

@@ -46,6 +46,8 @@ _EMBED = struct.Struct("3P4i10qf4x")
 _POLICY = struct.Struct("10P2i17q5f4x")
 _GRAD_TENSOR = struct.Struct("PNN2i")
 _GATED = struct.Struct("9P5i4x18q")
+_DROPOUT = struct.Struct("4P2i9q2Qd")
+_VERIFY = struct.Struct("7P2i11q2f")
 
 
 class TokenLogprob(NamedTuple):
@@ -73,6 +75,12 @@ class GatedFfnGrad(NamedTuple):
     dx: Optional[torch.Tensor]       # x's shape and type
     dw_gate: Optional[torch.Tensor]  # the weights' shape
     dw_up: Optional[torch.Tensor]
+
+
+class Verified(NamedTuple):
+    accepted: torch.Tensor  # int32 [batch]: drafts accepted
+    tokens: torch.Tensor    # [batch, drafts + 1] of the drafts' type: those, the drawn token, -1
+    logp: torch.Tensor      # float32 [batch, drafts + 1]: under the target, 0 behind the drawn token
 
 
 # --------------------------------------------------------------------------- checks
@@ -410,6 +418,88 @@ def gated_ffn_grad(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, ga
     if written:
         increment_version(written)
     return GatedFfnGrad(dx, dw_gate, dw_up)
+
+
+# --------------------------------------------------------------------------- dropout
+
+def dropout(x: torch.Tensor, p: float, seed: int, *, offset: int = 0, counter: Optional[torch.Tensor] = None,
+            residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """residual + dropout(x) in the residual's type (without one: x's), by a mask that follows from seed, offset, shape and p
+    alone.  The gradient of x is dropout(grad, p, seed, offset=offset), that of the residual is grad.  `offset`: a number of the call
+    (step, layer); `counter`: an int64 tensor of one element that is added to it on the device, for captured graphs."""
+    dev = torch.cuda.current_device()
+    kind = _need(x, "x", _FLOATS, dev)
+    if x.dim() < 1:
+        raise ValueError("x: need [..., dim]")
+    lead = x.dim() - 1
+    r_at, r_strides, dtype = 0, (0, 0), x.dtype
+    if residual is not None:
+        _need(residual, "residual", _FLOATS, dev)
+        _shape(residual, x.shape, "residual")
+        r_at, r_strides, dtype = residual.data_ptr(), _rows(residual, lead, "residual"), residual.dtype
+    given = out is not None
+    if not given:
+        out = _new(x, None, dtype, stream)
+    else:
+        _shape(out, x.shape, "out")
+    out_type = _need(out, "out", _FLOATS if residual is None else {dtype: _FLOATS[dtype]}, dev)
+    c_at = 0
+    if counter is not None:
+        _need(counter, "counter", {torch.int64: I64}, dev)
+        if counter.numel() != 1:
+            raise ValueError("counter: need one element")
+        c_at = counter.data_ptr()
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    if x.shape[-1] == 0:
+        return out
+    d = _DROPOUT.pack(x.data_ptr(), r_at, out.data_ptr(), c_at, kind, out_type, *_sizes(x.shape[:-1]), x.shape[-1],
+                      *_rows(x, lead, "x"), *r_strides, *_rows(out, lead, "out"), seed, offset, p)
+    _check(binding.load_library().odsgd_dropout(d, _handle(stream, dev)))
+    if given:
+        increment_version(out)
+    return out
+
+
+# --------------------------------------------------------------------------- drafted tokens
+
+def verify_draft(target: torch.Tensor, draft_tokens: torch.Tensor, uniforms: torch.Tensor, *, draft: Optional[torch.Tensor] = None,
+                 inv_temp: float = 1.0, draft_inv_temp: Optional[float] = None, workspace: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> Verified:
+    """Drafts accepted against the target's probabilities, and one token more, drawn so that all are distributed as the target is.
+
+    target [batch, drafts + 1, vocab] logits (the last row follows the last draft); draft_tokens [batch, drafts], -1 behind a
+    shorter draft; draft [batch, drafts, vocab] the logits that they were drawn from, of the target's type, at draft_inv_temp (default:
+    inv_temp), or None where they were not drawn; uniforms [batch, drafts + 1] float32 in [0, 1)."""
+    dev = torch.cuda.current_device()
+    kind = _need(target, "target", _FLOATS, dev)
+    token_type = _need(draft_tokens, "draft_tokens", _INTS, dev)
+    _need(uniforms, "uniforms", _FLOAT32, dev)
+    if target.dim() != 3:
+        raise ValueError("target: need [batch, drafts + 1, vocab]")
+    batch, many, vocab = target.shape
+    if many < 1:
+        raise ValueError("target: need [batch, drafts + 1, vocab]")
+    _shape(draft_tokens, (batch, many - 1), "draft_tokens")
+    _shape(uniforms, (batch, many), "uniforms")
+    at, strides = 0, (0, 0)
+    if draft is not None:
+        _need(draft, "draft", {target.dtype: kind}, dev)
+        _shape(draft, (batch, many - 1, vocab), "draft")
+        at, strides = draft.data_ptr(), _rows(draft, 2, "draft")
+    accepted, tokens = _new(target, (batch,), torch.int32, stream), _new(target, (batch, many), draft_tokens.dtype, stream)
+    logp = _new(target, (batch, many), torch.float32, stream)
+    d = _VERIFY.pack(target.data_ptr(), at, draft_tokens.data_ptr(), uniforms.data_ptr(), tokens.data_ptr(), accepted.data_ptr(),
+                     logp.data_ptr(), kind, token_type, batch, many - 1, vocab, *_rows(target, 2, "target"), *strides,
+                     *_levels(draft_tokens, 2, "draft_tokens"), *_levels(uniforms, 2, "uniforms"), inv_temp,
+                     inv_temp if draft_inv_temp is None else draft_inv_temp)
+    lib = binding.load_library()
+    need = ctypes.c_size_t()
+    _check(lib.odsgd_verify_workspace(d, ctypes.byref(need)))
+    workspace = _workspace(need.value, workspace, target, dev, stream)
+    _check(lib.odsgd_verify_draft(d, workspace.data_ptr(), workspace.nbytes, _handle(stream, dev)))
+    return Verified(accepted, tokens, logp)
 
 
 # --------------------------------------------------------------------------- gradient norm and clip

@@ -81,3 +81,74 @@ def within(got, ref, bound, what):
     bad = ~(same | ((got - ref).abs() <= bound))
     assert not bool(bad.any()), (f"{what}: {int(bad.sum())} of {bad.numel()} outside the bound, worst "
                                  f"{float(((got - ref).abs() / bound)[bad].max()):.3g} times")
+
+
+# --------------------------------------------------------------------------- dropout
+
+def philox(block, offset, seed):
+    """Four 32-bit words of Philox4x32-10, by Python integers."""
+    c = [block & 0xFFFFFFFF, block >> 32, offset & 0xFFFFFFFF, offset >> 32]
+    k = [seed & 0xFFFFFFFF, seed >> 32]
+    for _ in range(10):
+        a, b = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+        c = [(b >> 32) ^ c[1] ^ k[0], b & 0xFFFFFFFF, (a >> 32) ^ c[3] ^ k[1], a & 0xFFFFFFFF]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c
+
+
+def kept(shape, p, seed, offset):
+    t, n = round(p * 65536), math.prod(shape)
+    bits = []
+    for block in range(-(-n // 8)):
+        for word in philox(block, offset, seed):
+            bits += [word & 0xFFFF, word >> 16]
+    return torch.tensor([b >= t for b in bits[:n]], dtype=torch.bool).view(shape)
+
+
+def dropout(x, p, seed, offset, residual, kind):
+    """Value and bound: the factor, the product, the addition and the result are rounded once each."""
+    t = round(p * 65536)
+    keep = kept(tuple(x.shape), p, seed, offset).to(x.device)
+    y = torch.where(keep, x.double() * (65536 / (65536 - t)), torch.zeros((), dtype=torch.float64, device=x.device))
+    r = torch.zeros_like(y) if residual is None else residual.double()
+    return y + r, rounded(y + r, (3 * y.abs() + r.abs()) * U * 1.01, kind)
+
+
+# --------------------------------------------------------------------------- drafted tokens
+
+def verify(target, tokens, uniforms, draft, inv_temp, draft_inv_temp):
+    """Sequence by sequence, in 64 bits: accepted, tokens, logp, and how near any decision was to its border."""
+    c, e = (float(torch.tensor(v, dtype=torch.float32)) for v in (inv_temp, draft_inv_temp))
+    z, u, tok = target.cpu().double() * c, uniforms.cpu().double(), tokens.cpu().long()
+    zq = None if draft is None else draft.cpu().double() * e
+    b, many, v = z.shape
+    accepted, out, logp = torch.zeros(b, dtype=torch.int64), torch.full((b, many), -1), torch.zeros(b, many, dtype=torch.float64)
+    near = 1.0
+    for s in range(b):
+        for i in range(many):
+            p = torch.softmax(z[s, i], -1)
+            x = int(tok[s, i]) if i < many - 1 else -1
+            left = p
+            if 0 <= x < v:
+                q = torch.zeros(v, dtype=torch.float64) if zq is None else torch.softmax(zq[s, i], -1)
+                if zq is None:
+                    q[x] = 1.0
+                if q[x] > 0 or p[x] > 0:  # (0 < 0 is no matter of rounding)
+                    near = min(near, abs(float(u[s, i] * q[x] - p[x])) / max(float(p[x]), 1e-300))
+                if u[s, i] * q[x] < p[x]:
+                    out[s, i], logp[s, i] = x, torch.log_softmax(z[s, i], -1)[x]
+                    continue
+                left = (p - q).clamp(min=0)
+                if not bool(left.sum() != 0):
+                    left = p
+            accepted[s] = i
+            total = left.cumsum(0)
+            if not bool(total[-1] > 0):
+                logp[s, i] = float("nan")
+                break
+            bound = u[s, many - 1] * total[-1]
+            j = int(((total > bound) & (left > 0)).long().argmax())
+            near = min(near, float((total - bound).abs().min() / total[-1]))
+            out[s, i], logp[s, i] = j, torch.log_softmax(z[s, i], -1)[j]
+            break
+    return accepted, out, logp, near

@@ -271,3 +271,298 @@ def test_gated_refusals():
     before = out._version
     lm.gated_ffn(x, wg, wu, out=out)
     assert out._version > before, "what is written counts as changed"
+
+
+# --------------------------------------------------------------------------- dropout
+
+@pytest.mark.parametrize("kind,other", [(F32, None), (BF16, None), (F16, None), (BF16, BF16), (BF16, F32), (F16, F32), (F32, F16), (F16, F16), (F32, F32)])
+@pytest.mark.parametrize("shape", [(1,), (8,), (7,), (3, 8), (5, 13), (2, 3, 40), (4, 1, 257)])
+def test_dropout(kind, other, shape):
+    x = randn(*shape, seed=1, dtype=kind)
+    r = None if other is None else randn(*shape, seed=2, dtype=other, sigma=3.0)
+    for p, seed, offset in ((0.1, 12345, 0), (0.5, (1 << 64) - 3, (1 << 63) + 7), (0.0, 1, 2), (0.999, 5, 1 << 32)):
+        got = lm.dropout(x, p, seed, offset=offset, residual=r)
+        assert got.dtype == (kind if other is None else other) and got.shape == x.shape
+        ref, bound = R.dropout(x, p, seed, offset, r, got.dtype)
+        R.within(got, ref, bound, "dropout")
+        if p == 0.0 and r is None:
+            assert torch.equal(got, x)
+
+
+@pytest.mark.parametrize("offset,pad", [(0, 0), (0, 8), (8, 16), (1, 0), (0, 3), (4, 4)])
+@pytest.mark.parametrize("dim", [24, 29])
+def test_dropout_strides_and_alignment(offset, pad, dim):
+    def place(t):
+        whole = torch.zeros(offset + 10 * (dim + pad), dtype=t.dtype, device=DEV)
+        return whole[offset:].view(2, 5, dim + pad)[..., :dim].copy_(t)
+
+    x, r = place(randn(2, 5, dim, seed=3, dtype=BF16)), place(randn(2, 5, dim, seed=4))
+    for view, res in ((x, r), (x, None), (x.transpose(0, 1), r.transpose(0, 1)), (x[:, 1:], r[:, 1:]), (x[:1].expand(3, 5, dim), None)):
+        out, check = in_poison(tuple(view.shape), F32 if res is not None else BF16, offset, pad)
+        lm.dropout(view, 0.3, 77, offset=9, residual=res, out=out)
+        ref, bound = R.dropout(view, 0.3, 77, 9, res, out.dtype)
+        R.within(out, ref, bound, "dropout")
+        check()
+
+
+def test_dropout_in_place_and_backward():
+    x, r = randn(6, 40, seed=5, dtype=BF16), randn(6, 40, seed=6, dtype=BF16)
+    want = lm.dropout(x, 0.25, 8, offset=1, residual=r)
+    a, b = x.clone(), r.clone()
+    assert lm.dropout(x, 0.25, 8, offset=1, residual=b, out=b) is b and torch.equal(b, want)
+    lm.dropout(a, 0.25, 8, offset=1, out=a)
+    assert torch.equal(a, lm.dropout(x, 0.25, 8, offset=1))
+    # the gradient goes through the same mask, whatever the gradient's type and strides
+    dy = randn(6, 44, seed=7)[:, 3:43]
+    keep = R.kept((6, 40), 0.25, 8, 1).to(DEV)
+    dx = lm.dropout(dy, 0.25, 8, offset=1)
+    assert torch.equal(dx != 0, keep & (dy != 0)) and torch.equal(want != r, keep & (want != r))
+    assert not torch.equal(lm.dropout(x, 0.25, 8, offset=2), lm.dropout(x, 0.25, 8, offset=1))
+    assert not torch.equal(lm.dropout(x, 0.25, 9, offset=1), lm.dropout(x, 0.25, 8, offset=1))
+    n = randn(4, 16, seed=8)
+    n[1] = float("nan")
+    n[2] = float("inf")
+    keep = R.kept((4, 16), 0.5, 3, 0).to(DEV)
+    y = lm.dropout(n, 0.5, 3)
+    assert torch.equal(y.isfinite(), n.isfinite() | ~keep) and not bool(y[~keep].any())
+
+
+def test_dropout_many_elements():
+    """Shares of dropped elements, neighbours and calls independent, beyond 2^32 elements."""
+    n = (1 << 32) + 4096
+    x = torch.ones(n // 4096, 4096, dtype=BF16, device=DEV)
+    y = lm.dropout(x, 0.25, 11, out=x)
+    share = float((y == 0).sum(dtype=torch.int64)) / n
+    assert abs(share - 0.25) < 6 * math.sqrt(0.25 * 0.75 / n)
+    tail = y.view(-1)[-4096:].float()
+    first = (n - 4096) // 8
+    want = [h >= 16384 for b in range(first, first + 512) for w in R.philox(b, 0, 11) for h in (w & 0xFFFF, w >> 16)]
+    assert torch.equal(tail != 0, torch.tensor(want, device=DEV))
+    keep = y.view(-1)[:1 << 24] != 0
+    both = float((keep[1:] & keep[:-1]).double().mean())
+    assert abs(both - 0.5625) < 6 * math.sqrt(0.5625 * 0.4375 / (1 << 24)) * 1.5
+
+
+def test_dropout_counter_and_graph():
+    x = randn(50, 64, seed=10, dtype=BF16)
+    step = torch.zeros(1, dtype=torch.int64, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    lm.dropout(x, 0.1, 4, offset=3, counter=step)
+    with torch.cuda.graph(graph):
+        y = lm.dropout(x, 0.1, 4, offset=3, counter=step)
+        step += 1
+    for k in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, lm.dropout(x, 0.1, 4, offset=3 + k))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    z = lm.dropout(x, 0.1, 4, offset=3, stream=side)
+    side.synchronize()
+    assert torch.equal(z, lm.dropout(x, 0.1, 4, offset=3))
+
+
+def test_dropout_refusals_and_empty():
+    x = randn(4, 16)
+    assert lm.dropout(x[:0], 0.1, 1).shape == (0, 16) and lm.dropout(x[:, :0], 0.1, 1).shape == (4, 0)
+    for p in (-0.1, 1.0, float("nan"), 0.99999999):
+        with pytest.raises(binding.OdsgdError):
+            lm.dropout(x, p, 1)
+    with pytest.raises(ValueError):
+        lm.dropout(x, 0.1, -1)
+    with pytest.raises(ValueError):
+        lm.dropout(x, 0.1, 1, offset=1 << 64)
+    with pytest.raises(ValueError):
+        lm.dropout(x, 0.1, 1, residual=x[:2])
+    with pytest.raises(ValueError):
+        lm.dropout(x.t(), 0.1, 1)
+    with pytest.raises(TypeError):
+        lm.dropout(x.double(), 0.1, 1)
+    with pytest.raises(TypeError):
+        lm.dropout(x, 0.1, 1, residual=x, out=torch.empty_like(x, dtype=BF16))
+    with pytest.raises(TypeError):
+        lm.dropout(x, 0.1, 1, counter=torch.zeros(1, dtype=torch.int64))
+    with pytest.raises(ValueError):
+        lm.dropout(x, 0.1, 1, counter=torch.zeros(2, dtype=torch.int64, device=DEV))
+    whole = randn(5, 16)
+    with pytest.raises(binding.OdsgdError):
+        lm.dropout(whole[:4], 0.1, 1, out=whole[1:])
+    with pytest.raises(binding.OdsgdError):
+        lm.dropout(x, 0.1, 1, out=torch.empty(1, 16, device=DEV).expand(4, 16))
+    with pytest.raises(binding.OdsgdError):
+        lm.dropout(x, 0.1, 1, out=x.view(-1).view(BF16)[:64].view(4, 16))
+    before = x._version
+    lm.dropout(x, 0.1, 1, out=x)
+    assert x._version > before
+
+
+# --------------------------------------------------------------------------- drafted tokens
+
+def drafted(batch, drafts, vocab, kind, seed, with_draft=True, sigma=2.5, int_kind=torch.int64):
+    base = randn(batch, drafts + 1, vocab, seed=seed, sigma=sigma)
+    target = base.to(kind)
+    draft = (base[:, :drafts] + randn(batch, drafts, vocab, seed=seed + 1, sigma=0.6)).to(kind)
+    probs = torch.softmax(draft.float() * (1.25 if with_draft else 4.0), -1)
+    tok = torch.multinomial(probs.view(-1, vocab), 1, generator=gen(seed + 2)).view(batch, drafts) if drafts else torch.zeros(batch, 0, dtype=torch.int64, device=DEV)
+    u = torch.rand(batch, drafts + 1, generator=gen(seed + 3), device=DEV)
+    return target, tok.to(int_kind), u, draft if with_draft else None
+
+
+def check_verify(target, tok, u, draft, inv_temp=1.25, draft_inv_temp=None, **kw):
+    """Decisions are equal where the 64-bit form is further than 1e-11 from any border (its own sums are off by 1e-13 or so);
+    the seeds of these tests are."""
+    r = lm.verify_draft(target, tok, u, draft=draft, inv_temp=inv_temp, draft_inv_temp=draft_inv_temp, **kw)
+    accepted, tokens, logp, near = R.verify(target, tok, u, draft, inv_temp, inv_temp if draft_inv_temp is None else draft_inv_temp)
+    assert near > 1e-11, "a draw on the border: choose another seed"
+    assert torch.equal(r.accepted.cpu().long(), accepted)
+    assert torch.equal(r.tokens.cpu().long(), tokens) and r.tokens.dtype == tok.dtype
+    # the sum is added in 32 bits in parts, exponentials are off by 2^-21: bound as for a sum of so many terms in a tree
+    mag = float((target.double().nan_to_num(0, 0, 0).abs().amax() * inv_temp).clamp(max=1e30))
+    bound = torch.full_like(logp, 2.0 ** -19 + mag * 2.0 ** -21)
+    R.within(r.logp.cpu(), logp, bound, "logp")
+    return r
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("batch,drafts,vocab", [(1, 0, 1), (1, 1, 1), (3, 2, 7), (2, 4, 33), (5, 3, 1000), (4, 2, 4099), (3, 5, 20001), (9, 1, 513),
+                                                (2, 9, 64), (40, 0, 100), (2, 3, 70000)])
+@pytest.mark.parametrize("with_draft", [True, False])
+def test_verify(kind, batch, drafts, vocab, with_draft):
+    check_verify(*drafted(batch, drafts, vocab, kind, 100 + vocab + drafts, with_draft, int_kind=torch.int32 if vocab % 2 else torch.int64))
+
+
+def test_verify_many_sequences_accept_and_refuse():
+    r = check_verify(*drafted(300, 4, 50, BF16, 300, sigma=1.0))
+    assert len(set(r.accepted.tolist())) == 5, "every number of accepted drafts occurs"
+    again = lm.verify_draft(*drafted(300, 4, 50, BF16, 300, sigma=1.0)[:3], draft=drafted(300, 4, 50, BF16, 300, sigma=1.0)[3], inv_temp=1.25)
+    for a, b in zip(r, again):
+        assert torch.equal(a, b)
+
+
+def test_verify_most_drafts():
+    target, tok, u, _ = drafted(2, 255, 40, F16, 310, False)
+    check_verify(target, tok, u * 1e-3, None)  # low numbers: long runs are accepted
+
+
+def test_verify_strides_and_padding():
+    target, tok, u, draft = drafted(4, 3, 1001, BF16, 320)
+    tok[1, 2:], tok[2, 0], tok[3] = -1, 1001, -5
+    check_verify(target, tok, u, draft)
+    wide_t, wide_d = torch.zeros(4, 4, 1010, dtype=BF16, device=DEV), torch.zeros(3, 4, 1003, dtype=BF16, device=DEV).transpose(0, 1)
+    wide_t[..., 5:1006], wide_d[..., 1:1002] = target, draft
+    check_verify(wide_t[..., 5:1006], tok.t().contiguous().t(), u.t().contiguous().t(), wide_d[..., 1:1002])
+    check_verify(target.transpose(0, 1).contiguous().transpose(0, 1), tok, u[:1].expand(4, 4), draft)
+    check_verify(target, tok, u, draft, inv_temp=0.7, draft_inv_temp=3.0)
+
+
+def test_verify_borders():
+    """Random numbers on the border itself, decided in 64 bits: u q = p refuses, the next number below accepts."""
+    z = torch.zeros(1, 2, 4, device=DEV)  # uniform target: p = 1/4
+    tok = torch.tensor([[2]], device=DEV)
+    u = torch.tensor([[0.25, 0.0]], device=DEV)
+    assert lm.verify_draft(z, tok, u).accepted.tolist() == [0]
+    r = lm.verify_draft(z, tok, torch.tensor([[0.25 - 2.0 ** -26, 0.0]], device=DEV))
+    assert r.accepted.tolist() == [1] and r.tokens.tolist() == [[2, 0]]
+    # what is left of a uniform target without token 2: a third each, drawn at its borders
+    for last, want in ((0.0, 0), (0.33, 0), (0.34, 1), (0.66, 1), (0.67, 3), (1.0 - 2.0 ** -24, 3)):
+        assert lm.verify_draft(z, tok, torch.tensor([[0.9, last]], device=DEV)).tokens.tolist() == [[want, -1]]
+    same = drafted(6, 2, 300, BF16, 330)
+    r = lm.verify_draft(same[0], same[1], same[2], draft=same[0][:, :2].contiguous())
+    assert r.accepted.tolist() == [2] * 6, "equal distributions accept everything"
+    for last, want in ((0.0, 0), (0.25, 1), (0.5, 2), (0.75, 3)):  # cum > u whole: at a border the next one
+        assert lm.verify_draft(z[:, :1], tok[:, :0], torch.tensor([[last]], device=DEV)).tokens.tolist() == [[want]]
+
+
+def test_verify_masked_and_void_rows():
+    target, tok, u, draft = drafted(6, 2, 500, F32, 340)
+    target[..., 100:] = float("-inf")
+    draft[..., 100:] = float("-inf")
+    tok.clamp_(max=99)
+    tok[0, 0] = 400  # neither gives it a probability
+    check_verify(target, tok, u, draft)
+    low = target.clone()
+    low[..., 100:] = torch.finfo(F32).min
+    for a, b in zip(lm.verify_draft(low, tok, u, draft=draft), lm.verify_draft(target, tok, u, draft=draft)):
+        assert torch.equal(a, b)
+    one = torch.full((1, 1, 300), float("-inf"), device=DEV)
+    one[0, 0, 299] = -5.0
+    r = lm.verify_draft(one, tok[:1, :0], u[:1, :1])
+    assert r.tokens.tolist() == [[299]] and r.logp.tolist() == [[0.0]]
+    for bad in (float("nan"), float("inf"), None):
+        void = target.clone()
+        if bad is None:
+            void[2, 0] = float("-inf")
+        else:
+            void[2, 0, 50] = bad
+        r = lm.verify_draft(void, tok, u, draft=draft)
+        want = lm.verify_draft(target, tok, u, draft=draft)
+        assert r.accepted[2] == 0 and r.tokens[2].tolist() == [-1, -1, -1] and math.isnan(float(r.logp[2, 0]))
+        keep = [0, 1, 3, 4, 5]
+        for a, b in zip(r, want):
+            assert torch.equal(a[keep], b[keep])
+
+
+def test_verify_draws_as_the_target_does():
+    """Drafts of another distribution, verified: what comes out first is distributed as the target (5 tokens, 200000 sequences)."""
+    n, v = 65536, 5
+    zt, zq = torch.tensor([0.3, -1.0, 1.2, 0.0, -0.4], device=DEV), torch.tensor([1.5, 0.2, -0.7, 0.1, 0.0], device=DEV)
+    counts = torch.zeros(v, device=DEV)
+    for k in range(3):
+        tok = torch.multinomial(torch.softmax(zq, 0), n, replacement=True, generator=gen(350 + k)).view(n, 1)
+        u = torch.rand(n, 2, generator=gen(360 + k), device=DEV)
+        r = lm.verify_draft(zt.expand(n, 2, v), tok, u, draft=zq.expand(n, 1, v))
+        counts += torch.bincount(r.tokens[:, 0], minlength=v)
+    p = torch.softmax(zt, 0)
+    off = (counts / (3 * n) - p).abs() / (p * (1 - p) / (3 * n)).sqrt()
+    assert float(off.max()) < 5
+
+
+def test_verify_streams_graphs_and_refusals():
+    target, tok, u, draft = drafted(3, 2, 5000, BF16, 370)
+    want = lm.verify_draft(target, tok, u, draft=draft)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = lm.verify_draft(target, tok, u, draft=draft, stream=side)
+    side.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    us, graph = u.clone(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = lm.verify_draft(target, tok, us, draft=draft)
+    for k in range(3):
+        us.copy_(torch.rand(3, 3, generator=gen(380 + k), device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(r, lm.verify_draft(target, tok, us, draft=draft)):
+            assert torch.equal(a, b)
+    assert lm.verify_draft(target[:0], tok[:0], u[:0], draft=draft[:0]).tokens.shape == (0, 3)
+    with pytest.raises(TypeError):
+        lm.verify_draft(target, tok, u, draft=draft.half())
+    with pytest.raises(TypeError):
+        lm.verify_draft(target, tok, u.double())
+    with pytest.raises(ValueError):
+        lm.verify_draft(target, tok[:, :1], u)
+    with pytest.raises(ValueError):
+        lm.verify_draft(target, tok, u[:, :2])
+    with pytest.raises(ValueError):
+        lm.verify_draft(target, tok, u, draft=draft[..., :100])
+    for t in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(binding.OdsgdError):
+            lm.verify_draft(target, tok, u, inv_temp=t)
+    with pytest.raises(binding.OdsgdError):
+        lm.verify_draft(target, tok, u, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+    with pytest.raises(binding.OdsgdError):
+        lm.verify_draft(randn(1, 258, 4), torch.zeros(1, 257, dtype=torch.int64, device=DEV), torch.zeros(1, 258, device=DEV))
+
+
+def test_verify_beyond_32_bit_offsets():
+    v = 1 << 20
+    target = torch.zeros(16, 256, v, dtype=BF16, device=DEV)  # 2^32 elements
+    target[15, 255, v - 1] = 60.0
+    target[15, :255, 7] = 60.0
+    tok = torch.full((16, 255), 7, device=DEV)
+    tok[:15] = -1
+    u = torch.full((16, 256), 0.5, device=DEV)
+    r = lm.verify_draft(target, tok, u)
+    assert r.accepted.tolist() == [0] * 15 + [255] and r.tokens[15].tolist() == [7] * 255 + [v - 1]
+    assert r.tokens[:15, 0].tolist() == [v // 2] * 15
