@@ -86,16 +86,66 @@ struct DrawState {
     float maxima[kVerifyDrafts + 1], draft_maxima[kVerifyDrafts + 1];
 };
 
+// 2^y in 64 bits, within 3e-14: the nearest whole number goes into the exponent, the rest, at most a half, through 1 + f r(f),
+// r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0, 0 below 2^-1000;
+// for y <= 1 or NaN.
+__device__ __forceinline__ double power_of_two(double y) {
+    const double whole = y + 6755399441055744.0;  // 1.5 * 2^52: the last bits are the whole number
+    const double f = y - (whole - 6755399441055744.0);
+    double r = 1.0203121063391729e-07;
+    r = fma(r, f, 1.3255224878668817e-06);
+    r = fma(r, f, 1.525268684626772e-05);
+    r = fma(r, f, 0.00015403455852453838);
+    r = fma(r, f, 0.0013333558179043112);
+    r = fma(r, f, 0.009618129159402558);
+    r = fma(r, f, 0.055504108664760424);
+    r = fma(r, f, 0.2402265069581299);
+    r = fma(r, f, 0.6931471805599453);
+    r = fma(r, f, 1.0);
+    r = __hiloint2double(__double2hiint(r) + (__double2loint(whole) << 20), __double2loint(r));
+    return y < -1000.0 ? 0.0 : r;
+}
+
 // One of the target's rows and the draft's beside it, element by element in 64 bits.
 template <typename T>
 struct RowPair {
     const T* p;
-    const T* q;       // nullptr: only `hot` has a probability
-    long long hot;    // -1: no draft to take off
-    double mp, mq, cp, cq;
-    __device__ __forceinline__ double target(int j) const { return exp(((double)to_f32(p[j]) - mp) * cp); }
-    __device__ __forceinline__ double draft(int j) const { return exp(((double)to_f32(q[j]) - mq) * cq); }
+    const T* q;     // nullptr: only `hot` has a probability
+    long long hot;  // -1: no draft to take off
+    double mp, mq, cp, cq;  // maxima, temperatures times log2 e
+    int vocab;
+    __device__ __forceinline__ static double one(float z, double m, double c) { return power_of_two(((double)z - m) * c); }
+    __device__ __forceinline__ double target(int j) const { return one(to_f32(p[j]), mp, cp); }
+    __device__ __forceinline__ double draft(int j) const { return one(to_f32(q[j]), mq, cq); }
+    // Elements j to j + 7 of a row; -inf behind its end.
+    __device__ __forceinline__ void load(const T* row, int j, float (&z)[8]) const {
+        if (j + 8 <= vocab && (reinterpret_cast<uintptr_t>(row + j) & 15) == 0) {
+#pragma unroll
+            for (int h = 0; h < 8; h += kLanes<T>) {
+                float y[kLanes<T>];
+                unpack<T>(*reinterpret_cast<const uint4*>(row + j + h), y);
+#pragma unroll
+                for (int l = 0; l < kLanes<T>; ++l) z[h + l] = y[l];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = j + i < vocab ? to_f32(row[j + i]) : -CUDART_INF_F;
+        }
+    }
+    __device__ __forceinline__ void target(int j, double (&e)[8]) const {
+        float z[8];
+        load(p, j, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = one(z[i], mp, cp);
+    }
+    __device__ __forceinline__ void draft(int j, double (&e)[8]) const {
+        float z[8];
+        load(q, j, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = one(z[i], mq, cq);
+    }
 };
+__device__ __forceinline__ double sum_of(const double (&x)[8]) { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); }
 
 // Sums of two values over the cluster, in the same order in every CTA.
 __device__ __forceinline__ void cluster_sums(DrawState& s, unsigned cs, double x, double y, double& all_x, double& all_y) {
@@ -166,9 +216,10 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
     }
     __syncthreads();
 
-    // this CTA's part of the vocabulary, and each warp's of that
-    const int per_warp = ((a.vocab + (int)(cs * kDrawWarps) - 1) / (int)(cs * kDrawWarps) + 31) / 32 * 32;
+    // this warp's part of the vocabulary: whole steps of eight elements a lane
+    const int per_warp = ((a.vocab + (int)(cs * kDrawWarps) - 1) / (int)(cs * kDrawWarps) + 255) / 256 * 256;
     const int lo = (int)min((long long)a.vocab, (long long)(rank * kDrawWarps + warp) * per_warp), hi = min(a.vocab, lo + per_warp);
+    const int own = lo + 8 * (int)lane;
 
     // The first draft that is not accepted; the sums of its two rows in 64 bits.
     RowPair<T> row;
@@ -179,11 +230,17 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         while (s.decision[n] == kAccepted) ++n;  // (behind the last draft it is kEnds)
         const bool ends = s.decision[n] == kEnds;
         const long long x = ends ? -1 : token(n);
-        row = RowPair<T>{target + n * a.t_sr, draft && !ends ? draft + n * a.d_sr : nullptr, x, s.maxima[n], s.draft_maxima[n], a.inv_temp, a.draft_temp};
+        row = RowPair<T>{target + n * a.t_sr, draft && !ends ? draft + n * a.d_sr : nullptr, x, s.maxima[n], s.draft_maxima[n],
+                         a.inv_temp * 1.4426950408889634, a.draft_temp * 1.4426950408889634, a.vocab};
         double p = 0.0, q = 0.0;
-        for (int j = lo + (int)lane; j < hi; j += 32) {
-            p += row.target(j);
-            if (row.q) q += row.draft(j);
+        for (int j = own; j < hi; j += 256) {
+            double e[8];
+            row.target(j, e);
+            p += sum_of(e);
+            if (row.q) {
+                row.draft(j, e);
+                q += sum_of(e);
+            }
         }
         cluster_sums(s, cs, p, q, sum_p, sum_q);
         if (ends) break;
@@ -191,16 +248,32 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         if (refused) break;
     }
 
-    // What is left of the target, and its sum in every warp's part.
-    const auto left = [&](int j) {
-        const double r = row.target(j) / sum_p;
-        if (!refused) return r;
-        return row.q ? fmax(0.0, r - row.draft(j) / sum_q) : j == row.hot ? 0.0 : r;
+    // What is left of the target (times sum_p), and its sum in every warp's part.
+    const double ratio = row.q ? sum_p / sum_q : 0.0;
+    const auto left = [&](int j, double (&e)[8]) {
+        row.target(j, e);
+        if (!refused) return;
+        if (row.q) {
+            double f[8];
+            row.draft(j, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double r = fma(-ratio, f[i], e[i]);
+                e[i] = r < 0.0 ? 0.0 : r;  // (NaN stays)
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
+        }
     };
     double all = 0.0;
     for (;;) {
         double mine = 0.0, none;
-        for (int j = lo + (int)lane; j < hi; j += 32) mine += left(j);
+        for (int j = own; j < hi; j += 256) {
+            double e[8];
+            left(j, e);
+            mine += sum_of(e);
+        }
         cluster_sums(s, cs, mine, 0.0, all, none);
         if (!refused || all != 0.0) break;
         refused = false;  // nothing is left (a draft that neither gives a probability): the whole target
@@ -225,24 +298,42 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         const int at = last_begin(kDrawWarps, begin, [&](unsigned w) { return s.warp_part[0][w]; }, begin);
         if (at == (int)warp) {
             int found = -1, last = -1;
-            for (int j0 = lo; j0 < hi && found < 0; j0 += 32) {
-                const int j = j0 + (int)lane;
-                const double r = j < hi ? left(j) : 0.0;
-                double run = r;
+            for (int j0 = lo; j0 < hi && found < 0; j0 += 256) {
+                const int j = j0 + 8 * (int)lane;
+                double e[8] = {};
+                if (j < hi) left(j, e);
+#pragma unroll
+                for (int i = 1; i < 8; ++i) e[i] += e[i - 1];
+                double run = e[7];
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
                     const double t = __shfl_up_sync(~0u, run, d);
                     if ((int)lane >= d) run += t;
                 }
-                const unsigned over = __ballot_sync(~0u, r > 0.0 && begin + run > bound), some = __ballot_sync(~0u, r > 0.0);
-                if (over != 0) found = j0 + __ffs((int)over) - 1;
-                if (some != 0) last = j0 + 31 - __clz((int)some);
+                double before = __shfl_up_sync(~0u, run, 1);
+                before = begin + (lane == 0 ? 0.0 : before);
+                int at_over = 8, at_last = -1;
+#pragma unroll
+                for (int i = 7; i >= 0; --i) {
+                    const bool some = e[i] > (i > 0 ? e[i - 1] : 0.0);
+                    if (some && before + e[i] > bound) at_over = i;
+                    if (some && at_last < 0) at_last = i;
+                }
+                const unsigned over = __ballot_sync(~0u, at_over < 8), some = __ballot_sync(~0u, at_last >= 0);
+                if (over != 0) {
+                    const int l = __ffs((int)over) - 1;
+                    found = j0 + 8 * l + __shfl_sync(~0u, at_over, l);
+                }
+                if (some != 0) {
+                    const int l = 31 - __clz((int)some);
+                    last = j0 + 8 * l + __shfl_sync(~0u, at_last, l);
+                }
                 begin += __shfl_sync(~0u, run, 31);
             }
             if (found < 0) found = last;  // (the bound is the whole sum, but for a rounding)
             if (lane == 0) {
                 store_token(a, seq, n, found);
-                a.logp[(size_t)seq * (a.drafts + 1) + n] = (float)(((double)to_f32(row.p[found]) - row.mp) * row.cp - log(sum_p));
+                a.logp[(size_t)seq * (a.drafts + 1) + n] = (float)(((double)to_f32(row.p[found]) - row.mp) * a.inv_temp - log(sum_p));
             }
         }
     }
