@@ -68,13 +68,15 @@ size_t verify_bytes(const odsgd_verify_desc* d) {
 }
 
 template <typename T>
-int launch_verify(VerifyArgs a, void* stream) {
+int launch_verify(VerifyArgs a, bool wide_ctas, void* stream) {
     a.exp_temp = RowExp<T>::bounded(a.inv_temp);
     a.draft_exp = RowExp<T>::bounded(a.draft_temp);
     const unsigned rows = a.target_rows + (a.draft ? a.batch * a.drafts : 0);
     const int rc = launch("verification kernel (rows)", parts_kernel<T>, dim3(rows * a.chunks), dim3(kPartThreads), 0, 1, stream, a);
     if (rc != ODSGD_OK) return rc;
-    return launch("verification kernel (draw)", draw_kernel<T>, dim3(a.batch * (unsigned)a.cluster), dim3(kDrawThreads), 0, a.cluster, stream, a);
+    const dim3 grid(a.batch * (unsigned)a.cluster);
+    return wide_ctas ? launch("verification kernel (draw)", draw_kernel<T, 16>, grid, dim3(512), 0, a.cluster, stream, a)
+                     : launch("verification kernel (draw)", draw_kernel<T, 8>, grid, dim3(256), 0, a.cluster, stream, a);
 }
 
 int verify(const odsgd_verify_desc* d, void* ws, size_t ws_bytes, void* stream) {
@@ -95,14 +97,17 @@ int verify(const odsgd_verify_desc* d, void* ws, size_t ws_bytes, void* stream) 
     a.chunks = (unsigned)verify_chunks(d);
     a.vocab = (int)d->vocab;
     a.wide_tokens = d->token_type == ODSGD_I64;
-    // a CTA for every 4096 elements of a row, up to eight
-    a.cluster = 1;
-    while (a.cluster < kDrawCluster && d->vocab > 4096 * a.cluster) a.cluster *= 2;
+    int sms = 0;
+    rc = sm_count(&sms);
+    if (rc != ODSGD_OK) return rc;
+    // a CTA for every 2048 elements of a row, up to eight, and no more than run at once (two an SM)
+    a.cluster = (int)std::max<int64_t>(1, std::min({(int64_t)kDrawCluster, ceil_div(d->vocab, 2048), (int64_t)sms * 2 / d->batch}));
+    const bool wide_ctas = d->batch * a.cluster <= sms;
     a.inv_temp = d->inv_temp, a.draft_temp = d->draft_inv_temp;
     switch (d->type) {
-        case ODSGD_F32: return launch_verify<float>(a, stream);
-        case ODSGD_BF16: return launch_verify<bf16>(a, stream);
-        default: return launch_verify<f16>(a, stream);
+        case ODSGD_F32: return launch_verify<float>(a, wide_ctas, stream);
+        case ODSGD_BF16: return launch_verify<bf16>(a, wide_ctas, stream);
+        default: return launch_verify<f16>(a, wide_ctas, stream);
     }
 }
 

@@ -6,14 +6,15 @@
 // where the running sum passes a random number is a matter of its last bits.
 #pragma once
 
+#include <limits.h>
+
 #include "odsgd_lm_softmax.cuh"
 
 namespace odsgd_lm {
 
 constexpr int kVerifyDrafts = 255;
 constexpr int kPartThreads = 256;
-constexpr int kDrawThreads = 512;
-constexpr int kDrawWarps = kDrawThreads / 32;
+constexpr int kDrawWarps = 16;  // most of a CTA that draws
 constexpr int kDrawCluster = 8;
 
 struct VerifyArgs {
@@ -65,10 +66,8 @@ __global__ void __launch_bounds__(kPartThreads) parts_kernel(const __grid_consta
     }
 }
 
-__device__ __forceinline__ double cluster_load_f64(uint32_t addr) {
-    double x;
-    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(x) : "r"(addr) : "memory");
-    return x;
+__device__ __forceinline__ void cluster_store_f64(uint32_t addr, double x) {
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(x) : "memory");
 }
 __device__ __forceinline__ double warp_sum(double x) {
 #pragma unroll
@@ -78,20 +77,22 @@ __device__ __forceinline__ double warp_sum(double x) {
 
 enum Decision { kRefused, kAccepted, kNear, kEnds };
 
+constexpr int kDrawSums = 5;
 struct DrawState {
-    double warp_part[2][kDrawWarps];
-    double cta_part[2];  // read by the other CTAs
+    double warp_part[kDrawSums][kDrawWarps];
+    double cta_part[2][kDrawSums][kDrawCluster];  // of every CTA, written by it; two sets in turn
     unsigned char decision[kVerifyDrafts + 1];
     float logp[kVerifyDrafts + 1];
-    float maxima[kVerifyDrafts + 1], draft_maxima[kVerifyDrafts + 1];
+    int found, last;
+    float maxima[kVerifyDrafts + 1], draft_maxima[kVerifyDrafts + 1], sums[kVerifyDrafts + 1], draft_sums[kVerifyDrafts + 1];
 };
 
-// 2^y in 64 bits, within 3e-14: the nearest whole number goes into the exponent, the rest, at most a half, through 1 + f r(f),
-// r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0, 0 below 2^-1000;
-// for y <= 1 or NaN.
-__device__ __forceinline__ double power_of_two(double y) {
-    const double whole = y + 6755399441055744.0;  // 1.5 * 2^52: the last bits are the whole number
-    const double f = y - (whole - 6755399441055744.0);
+// 2^(d c) in 64 bits, within 4e-14: the nearest whole number goes into the exponent, the rest f, at most a half, through 1 + f r(f),
+// r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0, 0 below 2^-1000 and
+// at -inf; for d c <= 1 or NaN.
+__device__ __forceinline__ double power_of_two(double d, double c) {
+    const double w = fma(d, c, 6755399441055744.0);  // 1.5 * 2^52: the lower half is the whole number
+    const double f = fma(d, c, 6755399441055744.0 - w);
     double r = 1.0203121063391729e-07;
     r = fma(r, f, 1.3255224878668817e-06);
     r = fma(r, f, 1.525268684626772e-05);
@@ -102,8 +103,9 @@ __device__ __forceinline__ double power_of_two(double y) {
     r = fma(r, f, 0.2402265069581299);
     r = fma(r, f, 0.6931471805599453);
     r = fma(r, f, 1.0);
-    r = __hiloint2double(__double2hiint(r) + (__double2loint(whole) << 20), __double2loint(r));
-    return y < -1000.0 ? 0.0 : r;
+    // (a number below -2^31 leaves another upper half)
+    const bool none = __double2hiint(w) < 0x4337ffff || __double2loint(w) < -1000;
+    return __hiloint2double(none ? 0 : __double2hiint(r) + (__double2loint(w) << 20), none ? 0 : __double2loint(r));
 }
 
 // One of the target's rows and the draft's beside it, element by element in 64 bits.
@@ -114,9 +116,8 @@ struct RowPair {
     long long hot;  // -1: no draft to take off
     double mp, mq, cp, cq;  // maxima, temperatures times log2 e
     int vocab;
-    __device__ __forceinline__ static double one(float z, double m, double c) { return power_of_two(((double)z - m) * c); }
-    __device__ __forceinline__ double target(int j) const { return one(to_f32(p[j]), mp, cp); }
-    __device__ __forceinline__ double draft(int j) const { return one(to_f32(q[j]), mq, cq); }
+    __device__ __forceinline__ double target(int j) const { return power_of_two((double)to_f32(p[j]) - mp, cp); }
+    __device__ __forceinline__ double draft(int j) const { return power_of_two((double)to_f32(q[j]) - mq, cq); }
     // Elements j to j + 7 of a row; -inf behind its end.
     __device__ __forceinline__ void load(const T* row, int j, float (&z)[8]) const {
         if (j + 8 <= vocab && (reinterpret_cast<uintptr_t>(row + j) & 15) == 0) {
@@ -132,42 +133,59 @@ struct RowPair {
             for (int i = 0; i < 8; ++i) z[i] = j + i < vocab ? to_f32(row[j + i]) : -CUDART_INF_F;
         }
     }
-    __device__ __forceinline__ void target(int j, double (&e)[8]) const {
-        float z[8];
-        load(p, j, z);
+    __device__ __forceinline__ void target(const float (&z)[8], double (&e)[8]) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = one(z[i], mp, cp);
+        for (int i = 0; i < 8; ++i) e[i] = power_of_two((double)z[i] - mp, cp);
     }
-    __device__ __forceinline__ void draft(int j, double (&e)[8]) const {
-        float z[8];
-        load(q, j, z);
+    __device__ __forceinline__ void draft(const float (&z)[8], double (&e)[8]) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = one(z[i], mq, cq);
+        for (int i = 0; i < 8; ++i) e[i] = power_of_two((double)z[i] - mq, cq);
+    }
+    // f(j, logits of the target, of the draft) for each eight from `from` on, a warp's width apart; the next are loaded ahead.
+    template <typename F>
+    __device__ __forceinline__ void each(int from, int hi, F f) const {
+        float z[8], y[8] = {}, next_z[8], next_y[8] = {};
+        if (from < hi) {
+            load(p, from, z);
+            if (q) load(q, from, y);
+        }
+#pragma unroll 1
+        for (int j = from; j < hi; j += 256) {
+            if (j + 256 < hi) {
+                load(p, j + 256, next_z);
+                if (q) load(q, j + 256, next_y);
+            }
+            f(j, z, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = next_z[i], y[i] = next_y[i];
+        }
     }
 };
 __device__ __forceinline__ double sum_of(const double (&x)[8]) { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); }
 
-// Sums of two values over the cluster, in the same order in every CTA.
-__device__ __forceinline__ void cluster_sums(DrawState& s, unsigned cs, double x, double y, double& all_x, double& all_y) {
+// Sums over the cluster, in the same order in every CTA; set `turn` of the parts holds those of the CTAs
+// afterwards, warp_part those of this CTA's warps.  Turns alternate: who writes a set again has been through the
+// barrier of the other, and with it everybody who reads it.
+template <int WARPS>
+__device__ __forceinline__ void cluster_sums(DrawState& s, unsigned cs, unsigned rank, unsigned turn, double (&x)[kDrawSums]) {
     const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    x = warp_sum(x);
-    y = warp_sum(y);
-    if (lane == 0) s.warp_part[0][warp] = x, s.warp_part[1][warp] = y;
+#pragma unroll
+    for (int k = 0; k < kDrawSums; ++k) {
+        x[k] = warp_sum(x[k]);
+        if (lane == 0) s.warp_part[k][warp] = x[k];
+    }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        double sx = 0.0, sy = 0.0;
-        for (int w = 0; w < kDrawWarps; ++w) sx += s.warp_part[0][w], sy += s.warp_part[1][w];
-        s.cta_part[0] = sx, s.cta_part[1] = sy;
+    if (warp < kDrawSums) {
+        const double sum = warp_sum(lane < WARPS ? s.warp_part[warp][lane] : 0.0);
+        if (lane < cs) cluster_store_f64(cluster_address(&s.cta_part[turn][warp][rank], lane), sum);
     }
     if (cs > 1) cluster_sync();
     else __syncthreads();
-    all_x = all_y = 0.0;
-    for (unsigned c = 0; c < cs; ++c) {
-        all_x += cs > 1 ? cluster_load_f64(cluster_address(&s.cta_part[0], c)) : s.cta_part[0];
-        all_y += cs > 1 ? cluster_load_f64(cluster_address(&s.cta_part[1], c)) : s.cta_part[1];
+#pragma unroll
+    for (int k = 0; k < kDrawSums; ++k) {
+        x[k] = 0.0;
+        for (unsigned c = 0; c < cs; ++c) x[k] += s.cta_part[turn][k][c];
     }
-    if (cs > 1) cluster_sync();  // (before the parts are written again)
-    else __syncthreads();
 }
 
 __device__ __forceinline__ void store_token(const VerifyArgs& a, unsigned seq, unsigned i, long long t) {
@@ -176,8 +194,8 @@ __device__ __forceinline__ void store_token(const VerifyArgs& a, unsigned seq, u
     else static_cast<int*>(a.out_tokens)[at] = (int)t;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constant__ VerifyArgs a) {
+template <typename T, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) draw_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ DrawState s;
     dependent_launch_prologue();
     const unsigned cs = (unsigned)a.cluster, seq = blockIdx.x / cs, rank = blockIdx.x % cs;
@@ -187,13 +205,18 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
     const float* const u = a.uniforms + seq * a.u_sb;
     const auto token = [&](unsigned i) { return load_token(a.tokens, a.wide_tokens != 0, seq * a.k_sb + i * a.k_sr); };
     const auto known = [&](long long t) { return t >= 0 && t < a.vocab; };
+    if (cs > 1) cluster_arrive();  // this CTA runs: its shared memory may be written (waited for below)
 
     // Every CTA decides every draft by the rows' sums in 32 bits; those next to the border are left open.
-    for (unsigned i = warp; i <= a.drafts; i += kDrawWarps) {
+    for (unsigned i = warp; i <= a.drafts; i += WARPS) {
+        const long long x = i < a.drafts ? token(i) : -1;
+        const float zt = known(x) ? to_f32(target[i * a.t_sr + x]) : 0.0f;
+        const float zd = known(x) && draft ? to_f32(draft[i * a.d_sr + x]) : 0.0f;
+        const float random = u[i * a.u_sr];
         const auto row_sum = [&](const MaxSum* parts, float c) {
-            MaxSum x = {-CUDART_INF_F, 0.0f};
-            for (unsigned k = lane; k < a.chunks; k += 32) x = join(x, parts[k], c);
-            return warp_join(x, c);
+            MaxSum v = {-CUDART_INF_F, 0.0f};
+            for (unsigned k = lane; k < a.chunks; k += 32) v = join(v, parts[k], c);
+            return warp_join(v, c);
         };
         const MaxSum t = row_sum(a.parts + (size_t)(seq * (a.drafts + 1) + i) * a.chunks, a.inv_temp);
         MaxSum d = {0.0f, 1.0f};
@@ -201,83 +224,111 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         if (lane == 0) {
             s.maxima[i] = t.m;
             s.draft_maxima[i] = d.m;
-            const long long x = i < a.drafts ? token(i) : -1;
+            s.sums[i] = t.s;
+            s.draft_sums[i] = d.s;
             int what = kEnds;
             if (known(x)) {
-                const float lp = (to_f32(target[i * a.t_sr + x]) - t.m) * a.inv_temp - logf(t.s);
-                const float lq = draft ? (to_f32(draft[i * a.d_sr + x]) - d.m) * a.draft_temp - logf(d.s) : 0.0f;
-                const float over = lp - lq - logf(u[i * a.u_sr]);
+                const float lp = (zt - t.m) * a.inv_temp - logf(t.s);
+                const float lq = draft ? (zd - d.m) * a.draft_temp - logf(d.s) : 0.0f;
+                const float over = lp - lq - logf(random);
                 s.logp[i] = lp;
                 // 32 bits leave `over` uncertain by some 1e-6; infinities and NaN are left to the exact comparison too
-                what = over > 1e-4f + 4e-6f * (fabsf(lp) + fabsf(lq)) ? kAccepted : over < -1e-4f - 4e-6f * (fabsf(lp) + fabsf(lq)) ? kRefused : kNear;
+                const float margin = 1e-4f + 4e-6f * (fabsf(lp) + fabsf(lq));
+                what = over > margin ? kAccepted : over < -margin ? kRefused : kNear;
             }
             s.decision[i] = (unsigned char)what;
         }
     }
+    if (threadIdx.x == 0) s.found = INT_MAX, s.last = -1;
+    if (cs > 1) cluster_wait();
     __syncthreads();
 
     // this warp's part of the vocabulary: whole steps of eight elements a lane
-    const int per_warp = ((a.vocab + (int)(cs * kDrawWarps) - 1) / (int)(cs * kDrawWarps) + 255) / 256 * 256;
-    const int lo = (int)min((long long)a.vocab, (long long)(rank * kDrawWarps + warp) * per_warp), hi = min(a.vocab, lo + per_warp);
+    const int per_warp = ((a.vocab + (int)(cs * WARPS) - 1) / (int)(cs * WARPS) + 255) / 256 * 256;
+    const int lo = (int)min((long long)a.vocab, (long long)(rank * WARPS + warp) * per_warp), hi = min(a.vocab, lo + per_warp);
     const int own = lo + 8 * (int)lane;
 
-    // The first draft that is not accepted; the sums of its two rows in 64 bits.
+    // The first draft that is not accepted.  One pass over its two rows gives, in 64 bits, the sums P and Q of the target's
+    // and the draft's exponentials (relative to their maxima), and with a ratio k near P / Q, for the target
+    // beyond the draft (times P),
+    //     R = sum of max(0, p - k q)    D = sum of q where p > k q    N = sum of p where p is within 2^-18 of k q
+    // The ratio comes from the sums in 32 bits, some 1e-7 off.  With the right one, P / Q, R is R - (P / Q - k) D, but for the
+    // elements that change sides, which N bounds: where it does not bound them well enough (distributions that are equal on much
+    // of their mass) the pass is made again with the right ratio.
     RowPair<T> row;
-    double sum_p = 0.0, sum_q = 0.0;
-    unsigned n = 0;
+    double x[kDrawSums];  // P, Q, R, D, N
+    double ratio = 0.0, off = 0.0;
+    unsigned n = 0, turn = 0;
     bool refused = false;
-    for (;; ++n) {
-        while (s.decision[n] == kAccepted) ++n;  // (behind the last draft it is kEnds)
+    for (bool again = false;; turn ^= 1) {
+        if (!again)
+            while (s.decision[n] == kAccepted) ++n;  // (behind the last draft it is kEnds)
         const bool ends = s.decision[n] == kEnds;
-        const long long x = ends ? -1 : token(n);
-        row = RowPair<T>{target + n * a.t_sr, draft && !ends ? draft + n * a.d_sr : nullptr, x, s.maxima[n], s.draft_maxima[n],
+        const long long t = ends ? -1 : token(n);
+        row = RowPair<T>{target + n * a.t_sr, draft && !ends ? draft + n * a.d_sr : nullptr, t, s.maxima[n], s.draft_maxima[n],
                          a.inv_temp * 1.4426950408889634, a.draft_temp * 1.4426950408889634, a.vocab};
-        double p = 0.0, q = 0.0;
-        for (int j = own; j < hi; j += 256) {
+        if (row.q && !again) ratio = (double)s.sums[n] / (double)s.draft_sums[n];
+#pragma unroll
+        for (int k = 0; k < kDrawSums; ++k) x[k] = 0.0;
+        row.each(own, hi, [&](int j, const float (&z)[8], const float (&y)[8]) {
             double e[8];
-            row.target(j, e);
-            p += sum_of(e);
+            row.target(z, e);
+            x[0] += sum_of(e);
             if (row.q) {
-                row.draft(j, e);
-                q += sum_of(e);
+                double f[8];
+                row.draft(y, f);
+                x[1] += sum_of(f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const double r = fma(-ratio, f[i], e[i]);
+                    const int high = __double2hiint(r), whole = __double2hiint(e[i]);
+                    if ((high & 0x7fffffff) < whole - (18 << 20)) x[4] += e[i];
+                    e[i] = high < 0 && r == r ? 0.0 : r;  // (NaN stays)
+                    f[i] = high < 0 ? 0.0 : f[i];
+                }
+                x[2] += sum_of(e);
+                x[3] += sum_of(f);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
+                x[2] += sum_of(e);
+            }
+        });
+        cluster_sums<WARPS>(s, cs, rank, turn, x);
+        if (ends) break;
+        if (!again) {
+            refused = s.decision[n] == kRefused ||
+                      !((double)u[n * a.u_sr] * (row.q ? row.draft((int)t) / x[1] : 1.0) < row.target((int)t) / x[0]);
+            if (!refused) {
+                ++n;
+                continue;
             }
         }
-        cluster_sums(s, cs, p, q, sum_p, sum_q);
-        if (ends) break;
-        refused = !((double)u[n * a.u_sr] * (row.q ? row.draft((int)x) / sum_q : 1.0) < row.target((int)x) / sum_p);
-        if (refused) break;
+        if (!row.q) break;
+        off = x[0] / x[1] - ratio;
+        // (what is not finite is not mended by another pass)
+        if (again || !(fabs(off) > 0x1p-19 * ratio || x[4] * fabs(off) > 1e-11 * ratio * x[2])) break;
+        ratio += off;
+        again = true;
     }
-
-    // What is left of the target (times sum_p), and its sum in every warp's part.
-    const double ratio = row.q ? sum_p / sum_q : 0.0;
-    const auto left = [&](int j, double (&e)[8]) {
-        row.target(j, e);
-        if (!refused) return;
+    // Where nothing is left (a draft that neither gives a probability, equal distributions): the whole target.
+    double all = x[2] - off * x[3];
+    if (refused && !(all > 0.0) && all == all) refused = false;
+    if (!refused) all = x[0], row.q = nullptr, row.hot = -1;
+    ratio += off;
+    const auto part_left = [&](double p, double r, double d) { return refused ? fmax(0.0, r - off * d) : p; };
+    const auto left = [&](int j, const float (&z)[8], const float (&y)[8], double (&e)[8]) {
+        row.target(z, e);
         if (row.q) {
             double f[8];
-            row.draft(j, f);
+            row.draft(y, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double r = fma(-ratio, f[i], e[i]);
-                e[i] = r < 0.0 ? 0.0 : r;  // (NaN stays)
-            }
+            for (int i = 0; i < 8; ++i) e[i] = fmax(0.0, fma(-ratio, f[i], e[i]));
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
         }
     };
-    double all = 0.0;
-    for (;;) {
-        double mine = 0.0, none;
-        for (int j = own; j < hi; j += 256) {
-            double e[8];
-            left(j, e);
-            mine += sum_of(e);
-        }
-        cluster_sums(s, cs, mine, 0.0, all, none);
-        if (!refused || all != 0.0) break;
-        refused = false;  // nothing is left (a draft that neither gives a probability): the whole target
-    }
     const bool drawn = all > 0.0 && all < CUDART_INF;  // not where a row holds NaN, +inf or nothing but -inf
     const double bound = (double)u[a.drafts * a.u_sr] * all;
 
@@ -293,59 +344,65 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         return at;
     };
     double begin = 0.0;
-    const int cta = last_begin(cs, 0.0, [&](unsigned c) { return cs > 1 ? cluster_load_f64(cluster_address(&s.cta_part[0], c)) : s.cta_part[0]; }, begin);
+    const int cta = last_begin(cs, 0.0, [&](unsigned c) { return part_left(s.cta_part[turn][0][c], s.cta_part[turn][2][c], s.cta_part[turn][3][c]); }, begin);
     if (drawn && cta == (int)rank) {
-        const int at = last_begin(kDrawWarps, begin, [&](unsigned w) { return s.warp_part[0][w]; }, begin);
-        if (at == (int)warp) {
-            int found = -1, last = -1;
-            for (int j0 = lo; j0 < hi && found < 0; j0 += 256) {
-                const int j = j0 + 8 * (int)lane;
-                double e[8] = {};
-                if (j < hi) left(j, e);
-#pragma unroll
-                for (int i = 1; i < 8; ++i) e[i] += e[i - 1];
-                double run = e[7];
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const double t = __shfl_up_sync(~0u, run, d);
-                    if ((int)lane >= d) run += t;
-                }
-                double before = __shfl_up_sync(~0u, run, 1);
-                before = begin + (lane == 0 ? 0.0 : before);
-                int at_over = 8, at_last = -1;
-#pragma unroll
-                for (int i = 7; i >= 0; --i) {
-                    const bool some = e[i] > (i > 0 ? e[i - 1] : 0.0);
-                    if (some && before + e[i] > bound) at_over = i;
-                    if (some && at_last < 0) at_last = i;
-                }
-                const unsigned over = __ballot_sync(~0u, at_over < 8), some = __ballot_sync(~0u, at_last >= 0);
-                if (over != 0) {
-                    const int l = __ffs((int)over) - 1;
-                    found = j0 + 8 * l + __shfl_sync(~0u, at_over, l);
-                }
-                if (some != 0) {
-                    const int l = 31 - __clz((int)some);
-                    last = j0 + 8 * l + __shfl_sync(~0u, at_last, l);
-                }
-                begin += __shfl_sync(~0u, run, 31);
+        const int at = last_begin(WARPS, begin, [&](unsigned w) { return part_left(s.warp_part[0][w], s.warp_part[2][w], s.warp_part[3][w]); }, begin);
+        // its part again, 256 elements a warp, all warps of the CTA together
+        const int from = min(a.vocab, (int)(rank * WARPS + at) * per_warp), to = min(a.vocab, from + per_warp);
+        for (int j0 = from; j0 < to; j0 += 256 * WARPS) {
+            const int j = j0 + 256 * (int)warp + 8 * (int)lane;
+            double e[8] = {};
+            if (j < to) {
+                float z[8], y[8] = {};
+                row.load(row.p, j, z);
+                if (row.q) row.load(row.q, j, y);
+                left(j, z, y, e);
             }
-            if (found < 0) found = last;  // (the bound is the whole sum, but for a rounding)
-            if (lane == 0) {
-                store_token(a, seq, n, found);
-                a.logp[(size_t)seq * (a.drafts + 1) + n] = (float)(((double)to_f32(row.p[found]) - row.mp) * a.inv_temp - log(sum_p));
+#pragma unroll
+            for (int i = 1; i < 8; ++i) e[i] += e[i - 1];
+            double run = e[7];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const double v = __shfl_up_sync(~0u, run, d);
+                if ((int)lane >= d) run += v;
             }
+            double before = __shfl_up_sync(~0u, run, 1);
+            if (lane == 0) before = 0.0;
+            __syncthreads();  // (the parts of before have been read)
+            if (lane == 31) s.warp_part[0][warp] = run;
+            __syncthreads();
+            for (int w = 0; w < WARPS; ++w) {
+                if (w == (int)warp) before += begin;
+                begin += s.warp_part[0][w];
+            }
+            int over = INT_MAX, some = -1;
+#pragma unroll
+            for (int i = 7; i >= 0; --i) {
+                const bool any = e[i] > (i > 0 ? e[i - 1] : 0.0);
+                if (any && before + e[i] > bound) over = j + i;
+                if (any && some < 0) some = j + i;
+            }
+            over = __reduce_min_sync(~0u, over);
+            some = __reduce_max_sync(~0u, some);
+            if (lane == 0 && over != INT_MAX) atomicMin(&s.found, over);
+            if (lane == 0 && some >= 0) atomicMax(&s.last, some);
+            __syncthreads();
+            if (s.found != INT_MAX) break;
+        }
+        if (threadIdx.x == 0) {
+            const int found = s.found != INT_MAX ? s.found : s.last;  // (the bound is the whole sum, but for a rounding)
+            store_token(a, seq, n, found);
+            a.logp[(size_t)seq * (a.drafts + 1) + n] = (float)(((double)to_f32(row.p[found]) - row.mp) * a.inv_temp - log(x[0]));
         }
     }
     if (rank == 0) {
         if (threadIdx.x == 0) a.accepted[seq] = (int)n;
-        for (unsigned i = threadIdx.x; i <= a.drafts; i += kDrawThreads) {
+        for (unsigned i = threadIdx.x; i <= a.drafts; i += WARPS * 32) {
             if (i == n && drawn) continue;
             store_token(a, seq, i, i < n ? token(i) : -1);
             a.logp[(size_t)seq * (a.drafts + 1) + i] = i < n ? s.logp[i] : i > n ? 0.0f : CUDART_NAN_F;
         }
     }
-    if (cs > 1) cluster_sync();  // the others have read this CTA's sums
 }
 
 }  // namespace odsgd_lm
