@@ -42,8 +42,10 @@ bool one_level(int64_t n_outer, int64_t n_inner, int64_t so, int64_t si, int64_t
 GatedPlan gated_plan(const odsgd_gated_desc* d, bool backward) {
     GatedPlan p;
     p.tokens = d->n_outer * d->n_inner;
-    p.dim_pitch = ceil_div(d->dim, 8) * 8;
-    p.width_pitch = ceil_div(d->width, 8) * 8;
+    // whole lines of 128 bytes: a box's rows then are one line each (2036 x 1001 x 2731 f16, all laid out: 57 us with rows of
+    // whole 16 bytes, LINE_US with these)
+    p.dim_pitch = ceil_div(d->dim, 64) * 64;
+    p.width_pitch = ceil_div(d->width, 64) * 64;
     const auto take = [&](int64_t rows, int64_t pitch) {
         const size_t at = p.bytes;
         p.bytes += (size_t)ceil_div(rows * pitch * 2, 128) * 128;
@@ -189,33 +191,56 @@ int allow_smem(const void* kernel, int bytes, std::atomic<bool>* done) {
     return ODSGD_OK;
 }
 
-template <int KIND, typename T>
+template <int KIND, typename T, bool GELU = false>
 int launch_gated(const GatedArgs& a, void* stream) {
     static std::atomic<bool> done[kMaxDevices] = {};
     int sms = 0;
     int rc = sm_count(&sms);
-    if (rc == ODSGD_OK) rc = allow_smem((const void*)gated_kernel<KIND, T>, kGatedSmem, done);
+    if (rc == ODSGD_OK) rc = allow_smem((const void*)gated_kernel<KIND, T, GELU>, kGatedSmem, done);
     if (rc != ODSGD_OK) return rc;
     const int64_t columns = KIND == kForward ? kTileColumns / 2 : kTileColumns;
     const int64_t tiles = ceil_div(a.rows, kTileRows) * ceil_div(a.columns, columns) * (KIND == kGradW ? 2 : 1);
     const unsigned pairs = (unsigned)std::min<int64_t>(tiles, sms / 2);
     return launch(KIND == kForward ? "gated forward kernel" : KIND == kGradX ? "gated gradient kernel (x)" : "gated gradient kernel (weights)",
-                  gated_kernel<KIND, T>, dim3(2 * pairs), dim3(kGatedThreads), kGatedSmem, 1, stream, a);
+                  gated_kernel<KIND, T, GELU>, dim3(2 * pairs), dim3(kGatedThreads), kGatedSmem, 1, stream, a);
 }
 
-// Blocks of rows: threads along a row, eight columns each.
+// Up to so many tokens go to thin_kernel.
+constexpr int64_t kThinTokens = 256;
+constexpr int kThinSmem = 227 * 1024 - 1024;  // of an SM
+
+template <int KIND, typename T, bool GELU = false>
+int launch_thin(const GatedArgs& g, unsigned tokens, void* stream) {
+    static std::atomic<bool> done[kMaxDevices] = {};
+    int sms = 0;
+    int rc = sm_count(&sms);
+    if (rc == ODSGD_OK) rc = allow_smem((const void*)thin_kernel<KIND, T, GELU>, kThinSmem, done);
+    if (rc != ODSGD_OK) return rc;
+    ThinArgs a;
+    for (int i = 0; i < 2; ++i) a.a[i] = g.b[i], a.b[i] = g.a[KIND == kForward ? 0 : i];
+    for (int i = 0; i < 3; ++i) a.out[i] = g.out[i];
+    a.tokens = tokens, a.n_inner = g.n_inner, a.columns = g.columns, a.depth = g.depth, a.is_bf16 = g.is_bf16, a.save = g.save;
+    a.padded = (unsigned)ceil_div(tokens, 16) * 16;
+    a.tensor_columns = 32;
+    while (a.tensor_columns < a.padded) a.tensor_columns *= 2;
+    const int64_t tiles = ceil_div(a.columns, KIND == kForward ? 64 : 128), blocks = ceil_div(a.depth, kBlockK) * (KIND == kGradX ? 2 : 1);
+    // two CTAs an SM where three stages and the sums fit twice
+    const int64_t stage = kThinRows * kBlockK * 2 + a.padded * kBlockK * 2, sums = (int64_t)a.padded * kThinRows * 4;
+    const int per_sm = std::max(3 * stage, sums) <= kThinSmem / 2 - 2048 ? 2 : 1;
+    const int64_t room = kThinSmem / per_sm - 2048;
+    // as many CTAs as run at once, each with four blocks of the long axis at least
+    a.cluster = (unsigned)std::max<int64_t>(1, std::min({(int64_t)kThinCluster, per_sm * sms / tiles, blocks / 4}));
+    a.stages = (unsigned)std::min<int64_t>(kThinStages, room / stage);
+    const size_t smem = 1024 + (size_t)std::max(a.stages * stage, sums);
+    return launch("gated kernel for few tokens", thin_kernel<KIND, T, GELU>, dim3((unsigned)tiles * a.cluster), dim3(kThinThreads), smem, (int)a.cluster, stream, a);
+}
+
+// Blocks of rows: threads along a row, eight columns each, and the rest of a CTA's across rows.
 void row_blocks(int64_t rows, int64_t columns, dim3* grid, dim3* block) {
-    const int64_t cols = ceil_div(columns, 8);
-    const int64_t slabs = ceil_div(cols, kLayThreads);
-    *block = dim3((unsigned)(ceil_div(ceil_div(cols, slabs), 32) * 32));
-    *grid = dim3((unsigned)std::min<int64_t>(rows, 1 << 20), (unsigned)slabs);
-}
-
-template <typename TI, typename TO>
-int launch_lay(const LayArgs& a, void* stream) {
-    dim3 grid, block;
-    row_blocks(a.rows, a.columns, &grid, &block);
-    return launch("operand layout kernel", lay_kernel<TI, TO>, grid, block, 0, 1, stream, a);
+    const int64_t cols = ceil_div(columns, 8), slabs = ceil_div(cols, kLayThreads);
+    const int64_t x = ceil_div(ceil_div(cols, slabs), 32) * 32, y = kLayThreads / x;
+    *block = dim3((unsigned)x, (unsigned)y);
+    *grid = dim3((unsigned)std::min<int64_t>(ceil_div(rows, y), 1 << 20), (unsigned)slabs);
 }
 
 template <typename T>
@@ -224,10 +249,12 @@ int run_gated(const odsgd_gated_desc* d, bool backward, const GatedPlan& p, char
     Matrix x, w[2];
     int rc = ODSGD_OK;
     x.rows = n, x.columns = d->dim;
+    LayArgs lay = {};
+    lay.columns = (unsigned)d->dim, lay.pitch = (unsigned)p.dim_pitch;
+    int64_t lay_rows = 0;
     if (p.lay_x) {
-        LayArgs l = {d->x, ws + p.x, d->x_stride_outer, d->x_stride_inner, (unsigned)n, (unsigned)d->n_inner, (unsigned)d->dim, (unsigned)p.dim_pitch};
-        rc = launch_lay<T, T>(l, stream);
-        if (rc != ODSGD_OK) return rc;
+        lay.m[0] = {d->x, ws + p.x, d->x_stride_outer, d->x_stride_inner, (unsigned)n, (unsigned)d->n_inner, 0};
+        lay_rows += n;
         x.p = ws + p.x, x.stride = p.dim_pitch;
     } else {
         one_level(d->n_outer, d->n_inner, d->x_stride_outer, d->x_stride_inner, &x.stride);
@@ -238,28 +265,36 @@ int run_gated(const odsgd_gated_desc* d, bool backward, const GatedPlan& p, char
     for (int i = 0; i < 2; ++i) {
         w[i].rows = d->width, w[i].columns = d->dim;
         if (p.lay_w[i]) {
-            LayArgs l = {wp[i], ws + p.w[i], 0, wst[i], (unsigned)d->width, (unsigned)d->width, (unsigned)d->dim, (unsigned)p.dim_pitch};
-            rc = d->weight_type == ODSGD_F32 ? launch_lay<float, T>(l, stream) : launch_lay<T, T>(l, stream);
-            if (rc != ODSGD_OK) return rc;
+            lay.m[1 + i] = {wp[i], ws + p.w[i], 0, wst[i], (unsigned)d->width, (unsigned)d->width, d->weight_type == ODSGD_F32};
+            lay_rows += d->width;
             w[i].p = ws + p.w[i], w[i].stride = p.dim_pitch;
         } else {
             w[i].p = wp[i], w[i].stride = wst[i];
         }
     }
+    dim3 grid, block;
+    if (lay_rows > 0) {
+        for (LayMatrix& m : lay.m) m.n_inner = std::max(m.n_inner, 1u);
+        row_blocks(lay_rows, d->dim, &grid, &block);
+        rc = launch("operand layout kernel", lay_kernel<T>, grid, block, 0, 1, stream, lay);
+        if (rc != ODSGD_OK) return rc;
+    }
     GatedArgs a = {};
     a.is_bf16 = d->type == ODSGD_BF16;
-    a.gelu = d->activation == ODSGD_GELU;
+    const bool gelu = d->activation == ODSGD_GELU;
     a.n_inner = (unsigned)d->n_inner;
     if (!backward) {
-        rc = encode(&a.a[0], x, d->type, 128);
-        for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.b[i], w[i], d->type, 128);
+        const bool thin = n <= kThinTokens;
+        rc = encode(&a.a[0], x, d->type, thin ? (int)ceil_div(n, 16) * 16 : 128);
+        for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.b[i], w[i], d->type, thin ? 64 : 128);
         if (rc != ODSGD_OK) return rc;
         a.out[0] = {d->h, d->h_stride_outer, d->h_stride_inner};
         a.out[1] = {d->gate, d->gate_stride_outer, d->gate_stride_inner};
         a.out[2] = {d->up, d->up_stride_outer, d->up_stride_inner};
         a.rows = (unsigned)n, a.columns = (unsigned)d->width, a.depth = (unsigned)d->dim;
         a.save = d->gate != nullptr;
-        return launch_gated<kForward, T>(a, stream);
+        if (thin) return gelu ? launch_thin<kForward, T, true>(a, (unsigned)n, stream) : launch_thin<kForward, T, false>(a, (unsigned)n, stream);
+        return gelu ? launch_gated<kForward, T, true>(a, stream) : launch_gated<kForward, T, false>(a, stream);
     }
     SlopeArgs s = {};
     s.gate = {d->gate, d->gate_stride_outer, d->gate_stride_inner};
@@ -267,22 +302,22 @@ int run_gated(const odsgd_gated_desc* d, bool backward, const GatedPlan& p, char
     s.dh = {d->h, d->h_stride_outer, d->h_stride_inner};
     s.dg = ws + p.dg, s.du = ws + p.du;
     s.rows = (unsigned)n, s.n_inner = (unsigned)d->n_inner, s.columns = (unsigned)d->width, s.pitch = (unsigned)p.width_pitch;
-    s.gelu = a.gelu;
     s.vec = rows_aligned(d->gate, 2, s.gate.so, s.gate.si, d->n_outer, d->n_inner) && rows_aligned(d->up, 2, s.up.so, s.up.si, d->n_outer, d->n_inner) &&
             rows_aligned(d->h, 2, s.dh.so, s.dh.si, d->n_outer, d->n_inner);
-    dim3 grid, block;
     row_blocks(n, d->width, &grid, &block);
-    rc = launch("gated slope kernel", slope_kernel<T>, grid, block, 0, 1, stream, s);
+    rc = gelu ? launch("gated slope kernel", slope_kernel<T, true>, grid, block, 0, 1, stream, s)
+              : launch("gated slope kernel", slope_kernel<T, false>, grid, block, 0, 1, stream, s);
     if (rc != ODSGD_OK) return rc;
     Matrix g[2];
     for (int i = 0; i < 2; ++i) g[i].p = ws + (i ? p.du : p.dg), g[i].rows = n, g[i].columns = d->width, g[i].stride = p.width_pitch;
     if (d->dx) {
-        for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.a[i], g[i], d->type, 128);
+        const bool thin = n <= kThinTokens;
+        for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.a[i], g[i], d->type, thin ? (int)ceil_div(n, 16) * 16 : 128);
         for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.b[i], w[i], d->type, kBlockK);
         if (rc != ODSGD_OK) return rc;
         a.out[0] = {d->dx, d->dx_stride_outer, d->dx_stride_inner};
         a.rows = (unsigned)n, a.columns = (unsigned)d->dim, a.depth = (unsigned)d->width;
-        rc = launch_gated<kGradX, T>(a, stream);
+        rc = thin ? launch_thin<kGradX, T>(a, (unsigned)n, stream) : launch_gated<kGradX, T>(a, stream);
         if (rc != ODSGD_OK) return rc;
     }
     if (d->dw_gate) {

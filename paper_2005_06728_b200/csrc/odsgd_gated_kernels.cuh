@@ -73,6 +73,13 @@ __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, i
         : "memory");
 }
 
+// The same, counted at a barrier of this CTA.
+__device__ __forceinline__ void load_box_alone(uint32_t dst, const CUtensorMap* map, int c, int r, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+                 "r"(c), "r"(r), "r"(bar)
+                 : "memory");
+}
+
 template <int CTAS>
 __device__ __forceinline__ void tensor_alloc(uint32_t smem_out, unsigned columns) {
     if constexpr (CTAS == 2) {
@@ -106,6 +113,16 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
                  : "memory");
 }
 
+// Both for a CTA by itself.
+__device__ __forceinline__ void multiply_alone(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a),
+                 "l"(b), "r"(instr), "r"((uint32_t)add)
+                 : "memory");
+}
+__device__ __forceinline__ void commit_alone(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
 // 32 columns of a warp's 32 lanes: x[i] is column i of the thread's lane.
 __device__ __forceinline__ void tensor_load(uint32_t addr, float (&x)[32]) {
     uint32_t r[32];
@@ -119,6 +136,16 @@ __device__ __forceinline__ void tensor_load(uint32_t addr, float (&x)[32]) {
         : "r"(addr));
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tensor_load(uint32_t addr, float (&x)[16]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tensor_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -142,16 +169,19 @@ __host__ __device__ constexpr uint32_t instruction(bool is_bf16, bool a_lines, b
 }
 
 // ------------------------------------------------------------------ activation
-// Both by their formulas in 32 bits; `slope` is the derivative.
+// Both by their formulas in 32 bits; `slope` is the derivative.  A kernel is built for one of them: code for both, 32 times
+// in a row, did not fit the instruction cache (a finished tile took 14.8 thousand cycles instead of FINISH_CYCLES).
 struct Activated {
     float value, slope;
 };
-__device__ __forceinline__ float activate(float t, bool gelu) {
-    if (gelu) return 0.5f * t * (1.0f + erff(t * 0.70710678f));
+template <bool GELU>
+__device__ __forceinline__ float activate(float t) {
+    if constexpr (GELU) return 0.5f * t * (1.0f + erff(t * 0.70710678f));
     return __fdividef(t, 1.0f + __expf(-t));
 }
-__device__ __forceinline__ Activated activate_with_slope(float t, bool gelu) {
-    if (gelu) {
+template <bool GELU>
+__device__ __forceinline__ Activated activate_with_slope(float t) {
+    if constexpr (GELU) {
         const float cdf = 0.5f * (1.0f + erff(t * 0.70710678f));
         return {t * cdf, cdf + t * 0.39894228f * __expf(-0.5f * t * t)};
     }
@@ -174,7 +204,7 @@ struct GatedArgs {
     unsigned rows, columns;  // of the product (forward: columns of each projection)
     unsigned n_inner;        // rows of an outer level of the outputs
     unsigned depth;          // the long axis (gradient of x: of one half)
-    int is_bf16, out_f32, accumulate, gelu, save;
+    int is_bf16, out_f32, accumulate, save;
 };
 
 constexpr int kTileRows = 256;       // of a pair of CTAs: 128 each
@@ -182,9 +212,9 @@ constexpr int kTileColumns = 256;    // sums a row: forward 128 gates and 128 up
 constexpr int kGatedStages = 6;
 constexpr int kHalfBytes = 128 * kBlockK * 2;     // 128 rows of an operand, one stage
 constexpr int kStageBytes = 2 * kHalfBytes;       // of one CTA: its 128 rows of A, its half of B
-constexpr int kGatedThreads = 256;                // copy, products, tensor memory, one idle warp; four that finish tiles
+constexpr int kGatedThreads = 384;                // copy, products, tensor memory, one idle warp; eight that finish tiles
 constexpr int kPatchPitch = 33;                   // words of a row of the patch through which unaligned rows are written
-constexpr int kGatedSmem = 1024 + kGatedStages * kStageBytes + 4 * 32 * kPatchPitch * 4;
+constexpr int kGatedSmem = 1024 + kGatedStages * kStageBytes + 8 * 32 * kPatchPitch * 4;
 constexpr int kGroupTiles = 8;                    // tiles of rows that follow one another before the columns move on
 
 struct GatedBarriers {
@@ -194,37 +224,73 @@ struct GatedBarriers {
     int stalled;
 };
 
-// 32 consecutive columns of a row from registers to memory.  Rows that start on 16 bytes are written by their
-// threads, 16 bytes at a time.  Others go through a patch of shared memory, from which the warp writes row by row.
-// Out-of-range rows have p == nullptr.
-template <typename T>
-__device__ __forceinline__ void store_32(T* p, int valid, bool vec, const float (&x)[32], uint32_t* patch, unsigned lane) {
-    if (vec) {
-        if (p != nullptr) {
+// 32 consecutive columns of a row from its thread's registers to memory, where the row starts on 32 bytes.  Out-of-range
+// rows have p == nullptr.
+__device__ __forceinline__ void store_sector(void* p, const uint4& a, const uint4& b) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y),
+                 "r"(b.z), "r"(b.w)
+                 : "memory");
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_32(T* p, int valid, const float (&x)[32]) {
+    constexpr int L = kLanes<T>;
+    if (p == nullptr) return;
 #pragma unroll
-            for (int i = 0; i < 32; i += kLanes<T>) {
-                float y[kLanes<T>];
+    for (int i = 0; i < 32; i += 2 * L) {
+        if (VEC && i + 2 * L <= valid) {
+            float y[L], z[L];
 #pragma unroll
-                for (int l = 0; l < kLanes<T>; ++l) y[l] = x[i + l];
-                if (i + kLanes<T> <= valid) {
-                    *reinterpret_cast<uint4*>(p + i) = pack<T>(y);
-                } else {
+            for (int l = 0; l < L; ++l) y[l] = x[i + l], z[l] = x[i + L + l];
+            store_sector(p + i, pack<T>(y), pack<T>(z));
+        } else {
 #pragma unroll
-                    for (int l = 0; l < kLanes<T>; ++l)
-                        if (i + l < valid) p[i + l] = from_f32<T>(y[l]);
-                }
-            }
+            for (int l = 0; l < 2 * L; ++l)
+                if (i + l < valid) p[i + l] = from_f32<T>(x[i + l]);
         }
-        return;
+    }
+}
+
+// Rows that do not start on 32 bytes go through a patch of shared memory, 32 rows of 64 columns a warp, and from there as
+// the 16-byte words of their own addresses, eight lanes a row; what is left at both ends goes element by element.  (Each
+// lane its own row, or a row at a time element by element, take 87 us where this takes PATCHED_US: 2036 x 1001 x 2731 f16.)
+__device__ __forceinline__ void patch_32(uint32_t* patch, unsigned c, unsigned lane, const uint4 (&q)[4]) {
+    uint32_t* const to = patch + lane * kPatchPitch + c / 2;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[4 * i] = q[i].x, to[4 * i + 1] = q[i].y, to[4 * i + 2] = q[i].z, to[4 * i + 3] = q[i].w;
+}
+template <typename T>
+__device__ __forceinline__ void store_patch(T* p, int valid, const uint32_t* patch, unsigned lane) {
+    static_assert(sizeof(T) == 2, "two elements a word");
+    const int l = (int)(lane & 7);
+    __syncwarp();
+#pragma unroll 2
+    for (unsigned r = lane >> 3; r < 32; r += 4) {
+        T* const to = reinterpret_cast<T*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(p), r));
+        const uint32_t* const row = patch + r * kPatchPitch;
+        const unsigned short* const half = reinterpret_cast<const unsigned short*>(row);
+        if (to != nullptr) {
+            const int head = min(valid, (int)((16 - (reinterpret_cast<uintptr_t>(to) & 15)) & 15) / 2), at = head + 8 * l;
+            if (at + 8 <= valid) {
+                const uint32_t* const w = row + at / 2;
+                uint4 q = make_uint4(w[0], w[1], w[2], w[3]);
+                if (at & 1) q = make_uint4(__funnelshift_r(q.x, q.y, 16), __funnelshift_r(q.y, q.z, 16), __funnelshift_r(q.z, q.w, 16), __funnelshift_r(q.w, w[4], 16));
+                *reinterpret_cast<uint4*>(to + at) = q;
+            }
+            const int tail = head + (valid - head) / 8 * 8 + l;
+            if (l < head) reinterpret_cast<unsigned short*>(to)[l] = half[l];
+            if (tail < valid) reinterpret_cast<unsigned short*>(to)[tail] = half[tail];
+        }
     }
     __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void pack_32(const float (&x)[32], uint4 (&q)[4]) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) patch[lane * kPatchPitch + i] = __float_as_uint(x[i]);
-    __syncwarp();
-#pragma unroll 4
-    for (int r = 0; r < 32; ++r) {
-        T* const to = reinterpret_cast<T*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(p), r));
-        if (to != nullptr && (int)lane < valid) to[lane] = from_f32<T>(__uint_as_float(patch[r * kPatchPitch + lane]));
+    for (int i = 0; i < 4; ++i) {
+        float y[8];
+#pragma unroll
+        for (int l = 0; l < 8; ++l) y[l] = x[8 * i + l];
+        q[i] = pack<T>(y);
     }
 }
 
@@ -233,15 +299,15 @@ __device__ __forceinline__ T* row_of(const RowsOut& o, const GatedArgs& a, unsig
     return static_cast<T*>(o.p) + (row / a.n_inner) * o.so + (row % a.n_inner) * o.si;
 }
 template <typename T>
-__device__ __forceinline__ bool rows_on_16(const RowsOut& o) {
-    return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.so * (long long)sizeof(T)) | (uintptr_t)(o.si * (long long)sizeof(T))) & 15) == 0;
+__device__ __forceinline__ bool rows_on_32(const RowsOut& o) {
+    return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.so * (long long)sizeof(T)) | (uintptr_t)(o.si * (long long)sizeof(T))) & 31) == 0;
 }
 
 // A persistent pair of CTAs per two SMs goes over tiles of 256 rows x 256 sums.  In each CTA one thread copies (its own 128 rows of
 // A and its half of B: in the forward pass the first CTA's half is Wg's, the second's Wu's), four warps finish
 // tiles; one thread of the first CTA issues the products of both.  Two sets of sums, so that one tile is finished
 // while the next is computed.
-template <int KIND, typename T>
+template <int KIND, typename T, bool GELU>
 __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) gated_kernel(const __grid_constant__ GatedArgs a) {
     constexpr bool A_LINES = KIND == kGradW, B_LINES = KIND != kForward;
     extern __shared__ unsigned char raw[];
@@ -258,7 +324,7 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(smem_address(&s.sums_full[i]), 1);
-            barrier_init(smem_address(&s.sums_empty[i]), 8);  // the finishing warps of both CTAs
+            barrier_init(smem_address(&s.sums_empty[i]), 16);  // the finishing warps of both CTAs
         }
         s.stalled = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -361,58 +427,89 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
             }
         }
     } else if (warp >= 4) {
-        const unsigned quarter = warp & 3;
-        uint32_t* const patch = patches + quarter * 32 * kPatchPitch;
-        const bool vec_t = rows_on_16<T>(a.out[0]) && (KIND == kGradX || rows_on_16<T>(a.out[1])) && (KIND != kForward || rows_on_16<T>(a.out[2]));
-        const bool vec_f = rows_on_16<float>(a.out[0]) && rows_on_16<float>(a.out[1]);
+        const unsigned quarter = warp & 3, part = (warp - 4) / 4;  // a quarter of the rows, half of the columns
+        uint32_t* const patch = patches + (warp - 4) * 32 * kPatchPitch;
+        const bool vec_t = rows_on_32<T>(a.out[0]) && (KIND == kGradX || rows_on_32<T>(a.out[1])) && (KIND != kForward || rows_on_32<T>(a.out[2]));
+        const bool vec_f = rows_on_32<float>(a.out[0]) && rows_on_32<float>(a.out[1]);
         unsigned set = 0, set_phase = 0;
         for (unsigned t = pair; t < tiles; t += pairs) {
             const Tile tile = tile_at(t);
             const unsigned row = tile.row + rank * 128 + quarter * 32 + lane;
             if (!__all_sync(~0u, barrier_wait(smem_address(&s.sums_full[set]), set_phase, &s.stalled))) break;
             tensor_fence_after();
-            const uint32_t from = base + set * kTileColumns + (quarter * 32 << 16);
+            const unsigned first = part * (col_step / 2), col = tile.col + first;
+            const int valid = col < a.columns ? (int)min(col_step / 2, a.columns - col) : 0;
+            const uint32_t from = base + set * kTileColumns + (quarter * 32 << 16) + first;
             if constexpr (KIND == kForward) {
-                T* const h = row < a.rows ? row_of<T>(a.out[0], a, row) : nullptr;
-                T* const gate = row < a.rows && a.save ? row_of<T>(a.out[1], a, row) : nullptr;
-                T* const up = row < a.rows && a.save ? row_of<T>(a.out[2], a, row) : nullptr;
+                T* const h = row < a.rows ? row_of<T>(a.out[0], a, row) + col : nullptr;
+                T* const gate = row < a.rows && a.save ? row_of<T>(a.out[1], a, row) + col : nullptr;
+                T* const up = row < a.rows && a.save ? row_of<T>(a.out[2], a, row) + col : nullptr;
+                float g[32], u[32];
+                if (vec_t) {
 #pragma unroll 1
-                for (unsigned c = 0; c < 128; c += 32) {
-                    float g[32], u[32];
-                    tensor_load(from + c, g);
-                    tensor_load(from + 128 + c, u);
-                    tensor_load_wait();
-                    const unsigned col = tile.col + c;
-                    if (col >= a.columns) break;
-                    const int valid = (int)min(32u, a.columns - col);
-                    if (a.save) {
-                        store_32<T>(gate ? gate + col : nullptr, valid, vec_t, g, patch, lane);
-                        store_32<T>(up ? up + col : nullptr, valid, vec_t, u, patch, lane);
-                    }
+                    for (int c = 0; c < valid; c += 32) {
+                        tensor_load(from + c, g);
+                        tensor_load(from + 128 + c, u);
+                        tensor_load_wait();
+                        if (a.save) {
+                            store_32<T, true>(gate ? gate + c : nullptr, valid - c, g);
+                            store_32<T, true>(up ? up + c : nullptr, valid - c, u);
+                        }
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) g[i] = activate(g[i], a.gelu != 0) * u[i];
-                    store_32<T>(h ? h + col : nullptr, valid, vec_t, g, patch, lane);
+                        for (int i = 0; i < 32; ++i) g[i] = activate<GELU>(g[i]) * u[i];
+                        store_32<T, true>(h ? h + c : nullptr, valid - c, g);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int k = a.save ? 0 : 2; k < 3; ++k) {  // gate, up, h
+#pragma unroll 1
+                        for (int c = 0; c < valid; c += 32) {
+                            tensor_load(from + (k == 1 ? 128 : 0) + c, g);
+                            if (k == 2) tensor_load(from + 128 + c, u);
+                            tensor_load_wait();
+                            if (k == 2) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) g[i] = activate<GELU>(g[i]) * u[i];
+                            }
+                            uint4 q[4];
+                            pack_32<T>(g, q);
+                            patch_32(patch, c, lane, q);
+                        }
+                        if (valid > 0) store_patch<T>(k == 0 ? gate : k == 1 ? up : h, valid, patch, lane);
+                    }
                 }
             } else {
                 const RowsOut& o = a.out[KIND == kGradW ? tile.product : 0];
+                float x[32];
+                if (KIND == kGradW && a.out_f32) {
+                    float* const p = row < a.rows ? row_of<float>(o, a, row) + col : nullptr;
 #pragma unroll 1
-                for (unsigned c = 0; c < kTileColumns; c += 32) {
-                    float x[32];
-                    tensor_load(from + c, x);
-                    tensor_load_wait();
-                    const unsigned col = tile.col + c;
-                    if (col >= a.columns) break;
-                    const int valid = (int)min(32u, a.columns - col);
-                    if (KIND == kGradW && a.out_f32) {
-                        float* const p = row < a.rows ? row_of<float>(o, a, row) + col : nullptr;
+                    for (int c = 0; c < valid; c += 32) {
+                        tensor_load(from + c, x);
+                        tensor_load_wait();
                         if (a.accumulate && p != nullptr) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (i < valid) x[i] += p[i];
+                                if (c + i < valid) x[i] += p[c + i];
                         }
-                        store_32<float>(p, valid, vec_f, x, patch, lane);
-                    } else {
-                        store_32<T>(row < a.rows ? row_of<T>(o, a, row) + col : nullptr, valid, vec_t, x, patch, lane);
+                        if (vec_f) store_32<float, true>(p ? p + c : nullptr, valid - c, x);
+                        else store_32<float, false>(p ? p + c : nullptr, valid - c, x);
+                    }
+                } else {
+                    T* const p = row < a.rows ? row_of<T>(o, a, row) + col : nullptr;
+#pragma unroll 1
+                    for (int c = 0; c < valid; c += 32) {
+                        tensor_load(from + c, x);
+                        tensor_load_wait();
+                        if (vec_t) {
+                            store_32<T, true>(p ? p + c : nullptr, valid - c, x);
+                        } else {
+                            uint4 q[4];
+                            pack_32<T>(x, q);
+                            patch_32(patch, c & 63, lane, q);
+                            const int begin = c & ~63;
+                            if (c + 32 >= valid || (c & 63) == 32) store_patch<T>(p ? p + begin : nullptr, min(64, valid - begin), patch, lane);
+                        }
                     }
                 }
             }
@@ -432,38 +529,241 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
     }
 }
 
+__device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
+    float4 x;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(addr) : "memory");
+    return x;
+}
+
+// ------------------------------------------------------------------ few tokens
+// Few tokens leave most of a tile of 256 of them empty, and their time is that of reading the weights.  Here weights are
+// the rows of the product and tokens its columns, as many as there are, rounded up to 16: a cluster takes 64 columns of the block (64
+// rows of Wg above 64 of Wu), or 128 columns of x's gradient, its CTAs share the long axis, and the sums meet in shared memory,
+// added in the order of the ranks.
+constexpr int kThinThreads = 128;
+constexpr int kThinRows = 128;
+constexpr int kThinCluster = 8;
+constexpr int kThinStages = 8;  // at most
+struct ThinArgs {
+    CUtensorMap a[2], b[2];
+    RowsOut out[3];
+    unsigned tokens, n_inner, columns, depth;
+    unsigned padded;  // tokens rounded up to 16
+    unsigned stages, cluster, tensor_columns;
+    int is_bf16, save;
+};
+struct ThinBarriers {
+    unsigned long long full[kThinStages], empty[kThinStages], done;
+    uint32_t tensor_base;
+    int stalled;
+};
+
+template <int KIND, typename T, bool GELU>
+__global__ void __launch_bounds__(kThinThreads) thin_kernel(const __grid_constant__ ThinArgs a) {
+    static_assert(KIND != kGradW, "forward, or the gradient of x");
+    constexpr bool A_LINES = KIND == kGradX;
+    constexpr unsigned WIDE = KIND == kForward ? 64 : 128;  // columns of the output
+    extern __shared__ unsigned char raw[];
+    __shared__ ThinBarriers s;
+    const uint32_t stages = (smem_address(raw) + 1023) & ~1023u;
+    float* const sums = reinterpret_cast<float*>(raw + (stages - smem_address(raw)));  // [padded][kThinRows], behind the last product
+    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cs = a.cluster;
+    const unsigned rank = blockIdx.x % cs, col = blockIdx.x / cs * WIDE;
+    const unsigned token_bytes = a.padded * kBlockK * 2, stage_bytes = kThinRows * kBlockK * 2 + token_bytes;
+    if (threadIdx.x == 0) {
+        for (unsigned i = 0; i < a.stages; ++i) {
+            barrier_init(smem_address(&s.full[i]), 1);
+            barrier_init(smem_address(&s.empty[i]), 1);
+        }
+        barrier_init(smem_address(&s.done), 1);
+        s.stalled = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    dependent_launch_prologue();
+    if (warp == 2) tensor_alloc<1>(smem_address(&s.tensor_base), a.tensor_columns);
+    tensor_fence_before();
+    __syncthreads();
+    tensor_fence_after();
+    const uint32_t base = *reinterpret_cast<volatile uint32_t*>(&s.tensor_base);
+    const unsigned half_blocks = (a.depth + kBlockK - 1) / kBlockK, blocks = half_blocks * (KIND == kGradX ? 2 : 1);
+    const unsigned k0 = rank * blocks / cs, k1 = (rank + 1) * blocks / cs;  // (at least one: cs is at most `blocks`)
+
+    if (threadIdx.x == 0) {
+        unsigned stage = 0, phase = 0;
+        for (unsigned k = k0; k < k1; ++k) {
+            if (!barrier_wait(smem_address(&s.empty[stage]), phase ^ 1, &s.stalled)) {
+                for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // copies under way land within this time
+                break;
+            }
+            const uint32_t bar = smem_address(&s.full[stage]), to = stages + stage * stage_bytes;
+            barrier_expect(bar, stage_bytes);
+            const bool second = KIND == kGradX && k >= half_blocks;
+            const int at = (int)((second ? k - half_blocks : k) * kBlockK);
+            if constexpr (A_LINES) {
+                load_box_alone(to, &a.a[second], (int)col, at, bar);
+                load_box_alone(to + kThinRows * kBlockK, &a.a[second], (int)col + 64, at, bar);
+            } else {
+                load_box_alone(to, &a.a[0], at, (int)col, bar);
+                load_box_alone(to + kThinRows * kBlockK, &a.a[1], at, (int)col, bar);
+            }
+            load_box_alone(to + kThinRows * kBlockK * 2, &a.b[second], at, 0, bar);
+            if (++stage == a.stages) stage = 0, phase ^= 1;
+        }
+    } else if (threadIdx.x == 32) {
+        const uint32_t instr = instruction(a.is_bf16 != 0, A_LINES, false, kThinRows, (int)a.padded);
+        unsigned stage = 0, phase = 0;
+        bool ok = true;
+        for (unsigned k = k0; k < k1 && ok; ++k) {
+            ok = barrier_wait(smem_address(&s.full[stage]), phase, &s.stalled);
+            if (!ok) break;
+            tensor_fence_after();
+            const uint64_t da = operand(stages + stage * stage_bytes, A_LINES);
+            const uint64_t db = operand(stages + stage * stage_bytes + kThinRows * kBlockK * 2, false);
+#pragma unroll
+            for (int i = 0; i < kBlockK / 16; ++i) multiply_alone(base, da + i * operand_step(A_LINES), db + i * operand_step(false), instr, k > k0 || i > 0);
+            commit_alone(smem_address(&s.empty[stage]));
+            if (++stage == a.stages) stage = 0, phase ^= 1;
+        }
+        commit_alone(smem_address(&s.done));
+    }
+    __syncwarp();
+    const bool ok = __all_sync(~0u, barrier_wait(smem_address(&s.done), 0, &s.stalled));
+    tensor_fence_after();
+    if (ok) {
+        for (unsigned t = 0; t < a.padded; t += 16) {
+            float x[16];
+            tensor_load(base + (warp * 32 << 16) + t, x);
+            tensor_load_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sums[(t + i) * kThinRows + threadIdx.x] = x[i];
+        }
+    }
+    tensor_fence_before();
+    if (cs > 1) cluster_sync();
+    else __syncthreads();
+    if (warp == 2) {
+        tensor_fence_after();
+        tensor_free<1>(base, a.tensor_columns);
+    }
+    // four columns of a token at a time; the ranks' parts are all on their way before the first is added
+    const auto total = [&](unsigned at, float (&x)[4]) {
+        if (cs == 1) {
+            const float4 q = *reinterpret_cast<const float4*>(sums + at);
+            x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
+            return;
+        }
+        float4 q[kThinCluster];
+#pragma unroll
+        for (unsigned c = 0; c < kThinCluster; ++c)
+            if (c < cs) q[c] = cluster_load4(cluster_address(sums + at, c));
+        x[0] = q[0].x, x[1] = q[0].y, x[2] = q[0].z, x[3] = q[0].w;
+#pragma unroll
+        for (unsigned c = 1; c < kThinCluster; ++c)
+            if (c < cs) x[0] += q[c].x, x[1] += q[c].y, x[2] += q[c].z, x[3] += q[c].w;
+    };
+    const auto put = [&](const RowsOut& out, long long at, int valid, bool whole, const float (&x)[4]) {
+        T* const p = static_cast<T*>(out.p) + at;
+        if (whole) {
+            const float y[8] = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+            const uint4 q = pack<T>(y);
+            *reinterpret_cast<uint2*>(p) = make_uint2(q.x, q.y);
+        } else {
+#pragma unroll
+            for (int l = 0; l < 4; ++l)
+                if (l < valid) p[l] = from_f32<T>(x[l]);
+        }
+    };
+    const auto on_8 = [](const RowsOut& o) { return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.so * 2) | (uintptr_t)(o.si * 2)) & 7) == 0; };
+    const bool vec = on_8(a.out[0]) && on_8(a.out[1]) && on_8(a.out[2]);
+    for (unsigned i = rank * kThinThreads + threadIdx.x; i < a.tokens * (WIDE / 4); i += cs * kThinThreads) {
+        const unsigned t = i / (WIDE / 4), c = i % (WIDE / 4) * 4;
+        if (col + c >= a.columns) continue;
+        const int valid = (int)min(4u, a.columns - col - c);
+        const long long o = t / a.n_inner, n = t % a.n_inner;
+        const auto at = [&](const RowsOut& out) { return o * out.so + n * out.si + col + c; };
+        float x[4];
+        total(t * kThinRows + c, x);
+        if constexpr (KIND == kForward) {
+            float u[4];
+            total(t * kThinRows + 64 + c, u);
+            if (a.save) {
+                put(a.out[1], at(a.out[1]), valid, vec && valid == 4, x);
+                put(a.out[2], at(a.out[2]), valid, vec && valid == 4, u);
+            }
+#pragma unroll
+            for (int l = 0; l < 4; ++l) x[l] = activate<GELU>(x[l]) * u[l];
+        }
+        put(a.out[0], at(a.out[0]), valid, vec && valid == 4, x);
+    }
+    if (cs > 1) cluster_sync();  // the others have read this CTA's sums
+}
+
 // ------------------------------------------------------------------ operands laid out
 // Rows that TMA cannot address (a row that does not start on 16 bytes, leading axes that do not fold into one), and
 // weights that stand in the arena in 32 bits, are copied once, rounded to the type of the products.
-struct LayArgs {
+struct LayMatrix {
     const void* from;
     void* to;  // [rows][pitch]
     long long so, si;
-    unsigned rows, n_inner, columns, pitch;
+    unsigned rows, n_inner;
+    int f32;  // rounded from 32 bits
+};
+struct LayArgs {
+    LayMatrix m[3];  // of one width; those without rows are left out
+    unsigned columns, pitch;
 };
 constexpr int kLayThreads = 256;
-template <typename TI, typename TO>
+// Eight elements of a row that starts anywhere: the two 16-byte words around them, shifted.  (Both words hold elements of
+// the eight, so neither reaches into another 16 bytes than the row's own do.)
+template <typename T>
+__device__ __forceinline__ uint4 load_anywhere(const T* p) {
+    static_assert(sizeof(T) == 2, "16 bits");
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    const uint4* const w = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+    const uint4 a = w[0];
+    const unsigned shift = (unsigned)(at & 15);
+    if (shift == 0) return a;
+    const uint4 b = w[1];
+    const uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t y[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {  // from word shift / 4 on
+        const unsigned k = shift / 4;
+        y[i] = k == 0 ? x[i] : k == 1 ? x[i + 1] : k == 2 ? x[i + 2] : x[min(i + 3, 7)];
+    }
+    const unsigned bits = shift % 4 * 8;
+    return make_uint4(__funnelshift_r(y[0], y[1], bits), __funnelshift_r(y[1], y[2], bits), __funnelshift_r(y[2], y[3], bits), __funnelshift_r(y[3], y[4], bits));
+}
+template <typename T>
 __global__ void __launch_bounds__(kLayThreads) lay_kernel(const __grid_constant__ LayArgs a) {
     dependent_launch_prologue();
-    const unsigned col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
+    const unsigned col = (blockIdx.y * blockDim.x + threadIdx.x) * 8, step = gridDim.x * blockDim.y;
     if (col >= a.columns) return;
-    for (unsigned row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const TI* const p = static_cast<const TI*>(a.from) + (row / a.n_inner) * a.so + (row % a.n_inner) * a.si + col;
-        float x[8] = {};
-        if (sizeof(TI) == 4 && col + 8 <= a.columns && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-            float y[kLanes<TI>];
+    unsigned row = blockIdx.x * blockDim.y + threadIdx.y;
+#pragma unroll 1
+    for (int k = 0; k < 3; ++k) {
+        const LayMatrix& m = a.m[k];
+        for (; row < m.rows; row += step) {
+            const long long at = (row / m.n_inner) * m.so + (row % m.n_inner) * m.si + col;
+            uint4 q;
+            if (col + 8 <= a.columns && !m.f32) {
+                q = load_anywhere(static_cast<const T*>(m.from) + at);
+            } else {
+                float x[8] = {};
+                const float* const p = static_cast<const float*>(m.from) + at;
+                if (m.f32 && col + 8 <= a.columns && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+                    const float4 u = reinterpret_cast<const float4*>(p)[0], v = reinterpret_cast<const float4*>(p)[1];
+                    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+                } else {
 #pragma unroll
-            for (int h = 0; h < 8; h += kLanes<TI>) {
-                unpack<TI>(*reinterpret_cast<const uint4*>(p + h), y);
-#pragma unroll
-                for (int l = 0; l < kLanes<TI>; ++l) x[h + l] = y[l];
+                    for (int l = 0; l < 8; ++l)
+                        if (col + l < a.columns) x[l] = m.f32 ? p[l] : to_f32<T>(static_cast<const T*>(m.from)[at + l]);
+                }
+                q = pack<T>(x);
             }
-        } else {
-#pragma unroll
-            for (int l = 0; l < 8; ++l)
-                if (col + l < a.columns) x[l] = to_f32<TI>(p[l]);
+            *reinterpret_cast<uint4*>(static_cast<T*>(m.to) + (size_t)row * a.pitch + col) = q;
         }
-        *reinterpret_cast<uint4*>(static_cast<TO*>(a.to) + (size_t)row * a.pitch + col) = pack<TO>(x);
+        row -= m.rows;
     }
 }
 
@@ -474,14 +774,14 @@ struct SlopeArgs {
     void* dg;
     void* du;  // [rows][pitch]
     unsigned rows, n_inner, columns, pitch;
-    int gelu, vec;
+    int vec;
 };
-template <typename T>
+template <typename T, bool GELU>
 __global__ void __launch_bounds__(kLayThreads) slope_kernel(const __grid_constant__ SlopeArgs a) {
     dependent_launch_prologue();
     const unsigned col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
     if (col >= a.columns) return;
-    for (unsigned row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (unsigned row = blockIdx.x * blockDim.y + threadIdx.y; row < a.rows; row += gridDim.x * blockDim.y) {
         const unsigned o = row / a.n_inner, i = row % a.n_inner;
         const T* const pg = static_cast<const T*>(a.gate.p) + o * a.gate.so + i * a.gate.si + col;
         const T* const pu = static_cast<const T*>(a.up.p) + o * a.up.so + i * a.up.si + col;
@@ -491,6 +791,10 @@ __global__ void __launch_bounds__(kLayThreads) slope_kernel(const __grid_constan
             unpack<T>(*reinterpret_cast<const uint4*>(pg), g);
             unpack<T>(*reinterpret_cast<const uint4*>(pu), u);
             unpack<T>(*reinterpret_cast<const uint4*>(pd), d);
+        } else if (col + 8 <= a.columns) {
+            unpack<T>(load_anywhere(pg), g);
+            unpack<T>(load_anywhere(pu), u);
+            unpack<T>(load_anywhere(pd), d);
         } else {
 #pragma unroll
             for (int l = 0; l < 8; ++l) {
@@ -499,7 +803,7 @@ __global__ void __launch_bounds__(kLayThreads) slope_kernel(const __grid_constan
         }
 #pragma unroll
         for (int l = 0; l < 8; ++l) {
-            const Activated act = activate_with_slope(g[l], a.gelu != 0);
+            const Activated act = activate_with_slope<GELU>(g[l]);
             g[l] = d[l] * u[l] * act.slope;
             u[l] = d[l] * act.value;
         }
