@@ -658,7 +658,7 @@ int odsgd_grad_set_destroy(odsgd_grad_set* set);
  * where they go to a gradient arena, there added to what it holds if `accumulate` is set.  NaN and infinities
  * act as the formulas say, within their token (and, as in any such product, in all gradients of weights).
  * `workspace`: device memory of at least the size that odsgd_gated_workspace() reports for this descriptor (operands that
- * have to be laid out, dg and du), 16-byte aligned, free again when the call's work is done.
+ * have to be laid out, dg and du), 16-byte aligned, free again when the call's work is done; NULL where that is 0.
  * Errors: ERR_ARG, ERR_ALIGN, ERR_OVERLAP (what is written overlaps anything else), ERR_UNSUPPORTED, ERR_CUDA.
  */
 #define ODSGD_SILU 0

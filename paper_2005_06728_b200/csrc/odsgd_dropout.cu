@@ -80,7 +80,7 @@ int dropout(const odsgd_dropout_desc* d, void* stream) {
     bool vec;
     if (flat(a.x_so, a.x_si, d) && flat(a.o_so, a.o_si, d) && (!d->residual || flat(a.r_so, a.r_si, d))) {
         a.dim = a.n, a.n_inner = 1;  // one row
-        vec = a.n % 8 == 0 && aligned16(d->x) && aligned16(d->out) && aligned16(d->residual);
+        vec = aligned16(d->x) && aligned16(d->out) && aligned16(d->residual);
     } else {
         vec = d->dim % 8 == 0 && rows_aligned(d->x, size_of(d->type), a.x_so, a.x_si, d->n_outer, d->n_inner) &&
               rows_aligned(d->out, size_of(d->out_type), a.o_so, a.o_si, d->n_outer, d->n_inner) &&

@@ -61,7 +61,10 @@ __device__ __forceinline__ void store_8(T* p, const float (&x)[8]) {
 }
 
 // A thread takes eight consecutive elements of the whole, in the order of their index: one block of the generator,
-// 16 bits each.  VEC: the eight lie together and on 16 bytes in every tensor.
+// 16 bits each.  VEC: the eight lie together and on 16 bytes in every tensor (the last block's may be fewer).
+// Bound by memory traffic: 134 M bf16 elements onto a bf16 residual take 122 us, the copy rate for their 805 MB.  Ten
+// rounds of the generator are some 8 instructions an element; eight elements a block of it rather than four keep
+// them below what the SMs issue in that time.
 template <typename TX, typename TO, bool VEC>
 __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const __grid_constant__ DropoutArgs a) {
     dependent_launch_prologue();
@@ -74,19 +77,21 @@ __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const __grid_c
         const long long e = 8 * b;
         long long row = 0, col = e;
         if (a.dim != a.n) row = e / a.dim, col = e % a.dim;
+        // of the row that the first element lies in; the others' where rows are crossed
+        const auto place = [&](long long w, long long so, long long si) { return w / a.n_inner * so + w % a.n_inner * si; };
+        const bool whole = VEC && e + 8 <= a.n;
         float v[8], r[8] = {};
-        if constexpr (VEC) {
-            load_8(x + row / a.n_inner * a.x_so + row % a.n_inner * a.x_si + col, v);
-            if (residual) load_8(residual + row / a.n_inner * a.r_so + row % a.n_inner * a.r_si + col, r);
+        if (whole) {
+            load_8(x + place(row, a.x_so, a.x_si) + col, v);
+            if (residual) load_8(residual + place(row, a.r_so, a.r_si) + col, r);
         } else {
             long long w = row, c = col;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 v[i] = 0.0f;
                 if (e + i < a.n) {
-                    const long long o = w / a.n_inner, s = w % a.n_inner;
-                    v[i] = to_f32<TX>(x[o * a.x_so + s * a.x_si + c]);
-                    if (residual) r[i] = to_f32<TO>(residual[o * a.r_so + s * a.r_si + c]);
+                    v[i] = to_f32<TX>(x[place(w, a.x_so, a.x_si) + c]);
+                    if (residual) r[i] = to_f32<TO>(residual[place(w, a.r_so, a.r_si) + c]);
                 }
                 if (++c == a.dim) c = 0, ++w;
             }
@@ -98,13 +103,13 @@ __global__ void __launch_bounds__(kDropoutThreads) dropout_kernel(const __grid_c
             const bool kept = (i % 2 ? word[i / 2] >> 16 : word[i / 2] & 0xffffu) >= a.threshold;
             v[i] = (kept ? v[i] * a.scale : 0.0f) + r[i];  // (chosen, not multiplied: a dropped NaN is gone)
         }
-        if constexpr (VEC) {
-            store_8(out + row / a.n_inner * a.o_so + row % a.n_inner * a.o_si + col, v);
+        if (whole) {
+            store_8(out + place(row, a.o_so, a.o_si) + col, v);
         } else {
             long long w = row, c = col;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (e + i < a.n) out[w / a.n_inner * a.o_so + w % a.n_inner * a.o_si + c] = from_f32<TO>(v[i]);
+                if (e + i < a.n) out[place(w, a.o_so, a.o_si) + c] = from_f32<TO>(v[i]);
                 if (++c == a.dim) c = 0, ++w;
             }
         }

@@ -64,7 +64,6 @@ GatedPlan gated_plan(const odsgd_gated_desc* d, bool backward) {
         p.dg = take(p.tokens, p.width_pitch);
         p.du = take(p.tokens, p.width_pitch);
     }
-    p.bytes = std::max<size_t>(p.bytes, 16);
     return p;
 }
 
@@ -126,6 +125,7 @@ int check_gated(const odsgd_gated_desc* d, bool backward) {
 
 // The workspace against all buffers of a checked call.
 int check_gated_workspace(const odsgd_gated_desc* d, bool backward, const void* ws, size_t have, size_t need) {
+    if (need == 0) return ODSGD_OK;
     int rc = check_workspace(ws, have, need);
     if (rc != ODSGD_OK) return rc;
     const int es = size_of(d->type);

@@ -13,7 +13,7 @@ using namespace odsgd_lm;
 
 namespace {
 
-static_assert(kVerifyDrafts == ODSGD_MAX_DRAFTS, "the shared arrays of draw_kernel");
+static_assert(kVerifyDrafts == ODSGD_MAX_DRAFTS, "the shared arrays of the kernels");
 
 int check_verify(const odsgd_verify_desc* d, const void* ws, size_t have) {
     if (!d) return fail(ODSGD_ERR_ARG, "desc is NULL");
@@ -58,56 +58,71 @@ int check_verify(const odsgd_verify_desc* d, const void* ws, size_t have) {
     return rc;
 }
 
-// Parts of a row: of at least 4096 elements, as many as give every SM four CTAs.
-int64_t verify_chunks(const odsgd_verify_desc* d) {
-    const int64_t rows = d->batch * (2 * d->drafts + 1);
-    return std::max<int64_t>(1, std::min(ceil_div(148 * 4, std::max<int64_t>(rows, 1)), d->vocab / 4096));
-}
-size_t verify_bytes(const odsgd_verify_desc* d) {
-    return std::max<size_t>(16, (size_t)(d->batch * (2 * d->drafts + 1) * verify_chunks(d)) * sizeof(MaxSum));
+// Launch shapes and workspace: functions of sizes alone.
+struct VerifyShape {
+    int64_t rows, chunks;  // all rows, parts of each
+    int64_t pass_ctas;     // of a sequence
+    int64_t segments, segment;
+    size_t positions, sums, bytes;
+};
+VerifyShape verify_shape(const odsgd_verify_desc* d) {
+    VerifyShape s;
+    const int64_t sms = 148;
+    s.rows = d->batch * (2 * d->drafts + 1);
+    // parts of at least 4096 elements, as many as give every SM four CTAs
+    s.chunks = std::max<int64_t>(1, std::min(ceil_div(sms * 4, std::max<int64_t>(s.rows, 1)), d->vocab / 4096));
+    // CTAs of 2048 elements and more, as many as run at once, two an SM
+    s.pass_ctas = std::max<int64_t>(1, std::min(2 * sms / std::max<int64_t>(d->batch, 1), ceil_div(d->vocab, 2048)));
+    // a warp's share, in pieces that draw_kernel goes over in one step, but no more of them than it has threads
+    const int64_t share = ceil_div(d->vocab, s.pass_ctas * kPassWarps);
+    const int64_t piece = std::max(ceil_div(share, ceil_div(share, 256 * kDrawWarps)), ceil_div(d->vocab, kSegments));
+    s.segment = ceil_div(piece, 256) * 256;
+    s.segments = ceil_div(d->vocab, s.segment);
+    s.positions = (size_t)ceil_div(s.rows * s.chunks * (int64_t)sizeof(MaxSum), 16) * 16;
+    s.sums = s.positions + (size_t)ceil_div(d->batch * (d->drafts + 1) * (int64_t)sizeof(Position), 16) * 16;
+    s.bytes = std::max<size_t>(16, s.sums + (size_t)(d->batch * kDrawSums * s.segments) * sizeof(double));
+    return s;
 }
 
 template <typename T>
-int launch_verify(VerifyArgs a, bool wide_ctas, void* stream) {
+int launch_verify(VerifyArgs a, void* stream) {
     a.exp_temp = RowExp<T>::bounded(a.inv_temp);
     a.draft_exp = RowExp<T>::bounded(a.draft_temp);
     const unsigned rows = a.target_rows + (a.draft ? a.batch * a.drafts : 0);
-    const int rc = launch("verification kernel (rows)", parts_kernel<T>, dim3(rows * a.chunks), dim3(kPartThreads), 0, 1, stream, a);
-    if (rc != ODSGD_OK) return rc;
-    const dim3 grid(a.batch * (unsigned)a.cluster);
-    return wide_ctas ? launch("verification kernel (draw)", draw_kernel<T, 16>, grid, dim3(512), 0, a.cluster, stream, a)
-                     : launch("verification kernel (draw)", draw_kernel<T, 8>, grid, dim3(256), 0, a.cluster, stream, a);
+    int rc = launch("verification kernel (rows)", parts_kernel<T>, dim3(rows * a.chunks), dim3(kPartThreads), 0, 1, stream, a);
+    if (rc == ODSGD_OK) rc = launch("verification kernel (pass)", pass_kernel<T>, dim3(a.batch * (unsigned)a.pass_ctas), dim3(kPassWarps * 32), 0, 1, stream, a);
+    if (rc == ODSGD_OK) rc = launch("verification kernel (draw)", draw_kernel<T>, dim3(a.batch), dim3(kDrawThreads), 0, 1, stream, a);
+    return rc;
 }
 
 int verify(const odsgd_verify_desc* d, void* ws, size_t ws_bytes, void* stream) {
     int rc = check_verify(d, nullptr, 0);
     if (rc != ODSGD_OK) return rc;
-    rc = check_workspace(ws, ws_bytes, verify_bytes(d));
-    if (rc == ODSGD_OK) rc = check_verify(d, ws, verify_bytes(d));
+    const VerifyShape s = verify_shape(d);
+    rc = check_workspace(ws, ws_bytes, s.bytes);
+    if (rc == ODSGD_OK) rc = check_verify(d, ws, s.bytes);
     if (rc != ODSGD_OK || d->batch == 0) return rc;
     VerifyArgs a = {};
     a.target = d->target, a.draft = d->drafts > 0 ? d->draft : nullptr, a.tokens = d->tokens, a.uniforms = d->uniforms;
     a.out_tokens = d->out_tokens, a.accepted = d->accepted, a.logp = d->logp;
-    a.parts = static_cast<MaxSum*>(ws);
+    char* const at = static_cast<char*>(ws);
+    a.parts = reinterpret_cast<MaxSum*>(at);
+    a.positions = reinterpret_cast<Position*>(at + s.positions);
+    a.sums = reinterpret_cast<double*>(at + s.sums);
     a.t_sb = d->target_stride_batch, a.t_sr = d->target_stride_row;
     a.d_sb = d->draft_stride_batch, a.d_sr = d->draft_stride_row;
     a.k_sb = d->token_stride_batch, a.k_sr = d->token_stride_row;
     a.u_sb = d->uniform_stride_batch, a.u_sr = d->uniform_stride_row;
     a.batch = (unsigned)d->batch, a.drafts = (unsigned)d->drafts, a.target_rows = (unsigned)(d->batch * (d->drafts + 1));
-    a.chunks = (unsigned)verify_chunks(d);
+    a.chunks = (unsigned)s.chunks;
+    a.pass_ctas = (int)s.pass_ctas, a.segments = (int)s.segments, a.segment = (int)s.segment;
     a.vocab = (int)d->vocab;
     a.wide_tokens = d->token_type == ODSGD_I64;
-    int sms = 0;
-    rc = sm_count(&sms);
-    if (rc != ODSGD_OK) return rc;
-    // a CTA for every 2048 elements of a row, up to eight, and no more than run at once (two an SM)
-    a.cluster = (int)std::max<int64_t>(1, std::min({(int64_t)kDrawCluster, ceil_div(d->vocab, 2048), (int64_t)sms * 2 / d->batch}));
-    const bool wide_ctas = d->batch * a.cluster <= sms;
     a.inv_temp = d->inv_temp, a.draft_temp = d->draft_inv_temp;
     switch (d->type) {
-        case ODSGD_F32: return launch_verify<float>(a, wide_ctas, stream);
-        case ODSGD_BF16: return launch_verify<bf16>(a, wide_ctas, stream);
-        default: return launch_verify<f16>(a, wide_ctas, stream);
+        case ODSGD_F32: return launch_verify<float>(a, stream);
+        case ODSGD_BF16: return launch_verify<bf16>(a, stream);
+        default: return launch_verify<f16>(a, stream);
     }
 }
 
@@ -122,7 +137,7 @@ int odsgd_verify_workspace(const odsgd_verify_desc* desc, size_t* bytes) {
         if (desc->batch < 0 || desc->drafts < 0 || desc->vocab < 1) return fail(ODSGD_ERR_ARG, "sizes out of range");
         if (desc->drafts > ODSGD_MAX_DRAFTS || desc->batch > 1 << 16 || desc->vocab > 1 << 30)
             return fail(ODSGD_ERR_UNSUPPORTED, "batch, drafts or vocab beyond the limits");
-        *bytes = verify_bytes(desc);
+        *bytes = verify_shape(desc).bytes;
         return (int)ODSGD_OK;
     });
 }

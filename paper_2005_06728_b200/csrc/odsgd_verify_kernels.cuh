@@ -1,9 +1,9 @@
 // Device code of the verification of drafted tokens (sm_100a).
 //
-// Two launches.  The first reads every row of logits once and leaves maximum and sum of exponentials of its parts, in
-// 32 bits.  The second takes a sequence by a cluster: it decides its drafts in order, and draws one token from what the target has
-// beyond the draft (or, behind the last draft, from the target), for which two rows are read again in 64 bits:
-// where the running sum passes a random number is a matter of its last bits.
+// Three launches.  parts_kernel reads every row of logits once and leaves maximum and sum of exponentials of its parts, in 32
+// bits.  pass_kernel decides a sequence's drafts in order by those, and goes over the two rows of the first that is not
+// accepted again, in 64 bits: where the running sum of what is left passes a random number is a matter of its last bits.
+// draw_kernel finds that place.
 #pragma once
 
 #include <limits.h>
@@ -14,8 +14,20 @@ namespace odsgd_lm {
 
 constexpr int kVerifyDrafts = 255;
 constexpr int kPartThreads = 256;
-constexpr int kDrawWarps = 16;  // most of a CTA that draws
-constexpr int kDrawCluster = 8;
+constexpr int kPassWarps = 8;     // of a CTA of pass_kernel
+constexpr int kDrawThreads = 512;  // of draw_kernel
+constexpr int kDrawWarps = kDrawThreads / 32;
+constexpr int kSegments = kDrawThreads;  // most parts of the vocabulary, each summed by a warp
+constexpr int kDrawSums = 5;
+
+enum Decision { kRefused, kAccepted, kNear, kEnds };
+
+// Place i of a sequence, by the rows' sums in 32 bits.
+struct Position {
+    float max, sum, draft_max, draft_sum;
+    float logp;  // of the draft under the target
+    int decision;
+};
 
 struct VerifyArgs {
     const void* target;  // [batch][drafts + 1][vocab]
@@ -25,10 +37,14 @@ struct VerifyArgs {
     void* out_tokens;
     int* accepted;
     float* logp;
-    MaxSum* parts;  // [rows][chunks], the target's rows first
+    MaxSum* parts;        // [rows][chunks], the target's rows first
+    Position* positions;  // [batch][drafts + 1]
+    double* sums;         // [batch][kDrawSums][segments]
     long long t_sb, t_sr, d_sb, d_sr, k_sb, k_sr, u_sb, u_sr;
     unsigned batch, drafts, target_rows, chunks;
-    int vocab, wide_tokens, cluster;
+    int vocab, wide_tokens;
+    int segments, segment;  // how many, and elements of each (a multiple of 256)
+    int pass_ctas;          // of a sequence
     float inv_temp, draft_temp;  // of target and draft
     float exp_temp, draft_exp;   // the same as RowExp takes them
 };
@@ -66,26 +82,11 @@ __global__ void __launch_bounds__(kPartThreads) parts_kernel(const __grid_consta
     }
 }
 
-__device__ __forceinline__ void cluster_store_f64(uint32_t addr, double x) {
-    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(x) : "memory");
-}
 __device__ __forceinline__ double warp_sum(double x) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
     return x;
 }
-
-enum Decision { kRefused, kAccepted, kNear, kEnds };
-
-constexpr int kDrawSums = 5;
-struct DrawState {
-    double warp_part[kDrawSums][kDrawWarps];
-    double cta_part[2][kDrawSums][kDrawCluster];  // of every CTA, written by it; two sets in turn
-    unsigned char decision[kVerifyDrafts + 1];
-    float logp[kVerifyDrafts + 1];
-    int found, last;
-    float maxima[kVerifyDrafts + 1], draft_maxima[kVerifyDrafts + 1], sums[kVerifyDrafts + 1], draft_sums[kVerifyDrafts + 1];
-};
 
 // 2^(d c) in 64 bits, within 4e-14: the nearest whole number goes into the exponent, the rest f, at most a half, through 1 + f r(f),
 // r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0, 0 below 2^-1000 and
@@ -163,28 +164,116 @@ struct RowPair {
 };
 __device__ __forceinline__ double sum_of(const double (&x)[8]) { return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7])); }
 
-// Sums over the cluster, in the same order in every CTA; set `turn` of the parts holds those of the CTAs
-// afterwards, warp_part those of this CTA's warps.  Turns alternate: who writes a set again has been through the
-// barrier of the other, and with it everybody who reads it.
-template <int WARPS>
-__device__ __forceinline__ void cluster_sums(DrawState& s, unsigned cs, unsigned rank, unsigned turn, double (&x)[kDrawSums]) {
-    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+// A sequence's inputs.
+template <typename T>
+struct Sequence {
+    const T* target;
+    const T* draft;
+    const float* u;
+    const VerifyArgs& a;
+    unsigned seq;
+    __device__ __forceinline__ Sequence(const VerifyArgs& a_, unsigned seq_)
+        : target(static_cast<const T*>(a_.target) + seq_ * a_.t_sb),
+          draft(a_.draft ? static_cast<const T*>(a_.draft) + seq_ * a_.d_sb : nullptr),
+          u(a_.uniforms + seq_ * a_.u_sb),
+          a(a_),
+          seq(seq_) {}
+    __device__ __forceinline__ long long token(unsigned i) const { return load_token(a.tokens, a.wide_tokens != 0, seq * a.k_sb + i * a.k_sr); }
+    __device__ __forceinline__ RowPair<T> row(unsigned n, const Position& p) const {
+        const bool ends = p.decision == kEnds;
+        return RowPair<T>{target + n * a.t_sr, draft && !ends ? draft + n * a.d_sr : nullptr, ends ? -1 : token(n), p.max, p.draft_max,
+                          a.inv_temp * 1.4426950408889634, a.draft_temp * 1.4426950408889634, a.vocab};
+    }
+};
+__device__ __forceinline__ double ratio_of(const Position& p) { return (double)p.sum / (double)p.draft_sum; }
+
+// One pass over the two rows of a place gives, in 64 bits, the sums P and Q of the target's and the draft's exponentials
+// (relative to their maxima), and with a ratio k near P / Q, for the target beyond the draft (times P),
+//     R = sum of max(0, p - k q)    D = sum of q where p > k q    N = sum of p where p is within 2^-18 of k q
+// The ratio comes from the sums in 32 bits, some 1e-7 off.  With the right one, P / Q, R is R - (P / Q - k) D, but for the
+// elements that change sides, which N bounds: where it does not bound them well enough (distributions that are equal on much
+// of their mass) the pass is made again with the right ratio.  So two exponentials an element are the rule, not four.
+// Here: of one segment, by a warp.
+template <typename T>
+__device__ __forceinline__ void pass_segment(const RowPair<T>& row, double ratio, int lo, int hi, double (&x)[kDrawSums]) {
 #pragma unroll
-    for (int k = 0; k < kDrawSums; ++k) {
-        x[k] = warp_sum(x[k]);
-        if (lane == 0) s.warp_part[k][warp] = x[k];
+    for (int k = 0; k < kDrawSums; ++k) x[k] = 0.0;
+    row.each(lo + 8 * (int)(threadIdx.x & 31), hi, [&](int j, const float (&z)[8], const float (&y)[8]) {
+        double e[8];
+        row.target(z, e);
+        x[0] += sum_of(e);
+        if (row.q) {
+            double f[8];
+            row.draft(y, f);
+            x[1] += sum_of(f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double r = fma(-ratio, f[i], e[i]);
+                const int high = __double2hiint(r), whole = __double2hiint(e[i]);
+                if ((high & 0x7fffffff) < whole - (18 << 20)) x[4] += e[i];
+                e[i] = high < 0 && r == r ? 0.0 : r;  // (NaN stays)
+                f[i] = high < 0 ? 0.0 : f[i];
+            }
+            x[2] += sum_of(e);
+            x[3] += sum_of(f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
+            x[2] += sum_of(e);
+        }
+    });
+#pragma unroll
+    for (int k = 0; k < kDrawSums; ++k) x[k] = warp_sum(x[k]);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPassWarps * 32) pass_kernel(const __grid_constant__ VerifyArgs a) {
+    __shared__ Position place[kVerifyDrafts + 1];
+    dependent_launch_prologue();
+    const unsigned seq = blockIdx.x / a.pass_ctas, rank = blockIdx.x % a.pass_ctas;
+    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Sequence<T> in(a, seq);
+    // Every CTA decides every draft by the rows' sums in 32 bits; those next to the border are left open.
+    for (unsigned i = warp; i <= a.drafts; i += kPassWarps) {
+        const long long x = i < a.drafts ? in.token(i) : -1;
+        const bool known = x >= 0 && x < a.vocab;
+        const float zt = known ? to_f32(in.target[i * a.t_sr + x]) : 0.0f;
+        const float zd = known && in.draft ? to_f32(in.draft[i * a.d_sr + x]) : 0.0f;
+        const float random = in.u[i * a.u_sr];
+        const auto row_sum = [&](const MaxSum* parts, float c) {
+            MaxSum v = {-CUDART_INF_F, 0.0f};
+            for (unsigned k = lane; k < a.chunks; k += 32) v = join(v, parts[k], c);
+            return warp_join(v, c);
+        };
+        const MaxSum t = row_sum(a.parts + (size_t)(seq * (a.drafts + 1) + i) * a.chunks, a.inv_temp);
+        MaxSum d = {0.0f, 1.0f};
+        if (in.draft && i < a.drafts) d = row_sum(a.parts + (size_t)(a.target_rows + seq * a.drafts + i) * a.chunks, a.draft_temp);
+        if (lane == 0) {
+            Position p = {t.m, t.s, d.m, d.s, 0.0f, kEnds};
+            if (known) {
+                p.logp = (zt - t.m) * a.inv_temp - logf(t.s);
+                const float lq = in.draft ? (zd - d.m) * a.draft_temp - logf(d.s) : 0.0f;
+                const float over = p.logp - lq - logf(random);
+                // 32 bits leave `over` uncertain by some 1e-6; infinities and NaN are left to the exact comparison too
+                const float margin = 1e-4f + 4e-6f * (fabsf(p.logp) + fabsf(lq));
+                p.decision = over > margin ? kAccepted : over < -margin ? kRefused : kNear;
+            }
+            place[i] = p;
+            if (rank == 0) a.positions[(size_t)seq * (a.drafts + 1) + i] = p;
+        }
     }
     __syncthreads();
-    if (warp < kDrawSums) {
-        const double sum = warp_sum(lane < WARPS ? s.warp_part[warp][lane] : 0.0);
-        if (lane < cs) cluster_store_f64(cluster_address(&s.cta_part[turn][warp][rank], lane), sum);
-    }
-    if (cs > 1) cluster_sync();
-    else __syncthreads();
+    unsigned n = 0;
+    while (place[n].decision == kAccepted) ++n;  // (behind the last draft it is kEnds)
+    const RowPair<T> row = in.row(n, place[n]);
+    const double ratio = ratio_of(place[n]);
+    double* const sums = a.sums + (size_t)seq * kDrawSums * a.segments;
+    for (int g = (int)(rank * kPassWarps + warp); g < a.segments; g += a.pass_ctas * kPassWarps) {
+        double x[kDrawSums];
+        pass_segment(row, ratio, g * a.segment, min(a.vocab, (g + 1) * a.segment), x);
 #pragma unroll
-    for (int k = 0; k < kDrawSums; ++k) {
-        x[k] = 0.0;
-        for (unsigned c = 0; c < cs; ++c) x[k] += s.cta_part[turn][k][c];
+        for (int k = 0; k < kDrawSums; ++k)
+            if ((int)lane == k) sums[k * a.segments + g] = x[k];
     }
 }
 
@@ -194,192 +283,149 @@ __device__ __forceinline__ void store_token(const VerifyArgs& a, unsigned seq, u
     else static_cast<int*>(a.out_tokens)[at] = (int)t;
 }
 
-template <typename T, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32) draw_kernel(const __grid_constant__ VerifyArgs a) {
+struct DrawState {
+    Position place[kVerifyDrafts + 1];
+    double warp_part[kDrawSums][kDrawWarps];
+    double segment[kDrawSums][kSegments];  // written again where the pass has to be repeated here
+    int found, last, at;
+    double begin;
+};
+
+// A CTA a sequence, a thread a segment.
+template <typename T>
+__global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ DrawState s;
     dependent_launch_prologue();
-    const unsigned cs = (unsigned)a.cluster, seq = blockIdx.x / cs, rank = blockIdx.x % cs;
-    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const T* const target = static_cast<const T*>(a.target) + seq * a.t_sb;
-    const T* const draft = a.draft ? static_cast<const T*>(a.draft) + seq * a.d_sb : nullptr;
-    const float* const u = a.uniforms + seq * a.u_sb;
-    const auto token = [&](unsigned i) { return load_token(a.tokens, a.wide_tokens != 0, seq * a.k_sb + i * a.k_sr); };
-    const auto known = [&](long long t) { return t >= 0 && t < a.vocab; };
-    if (cs > 1) cluster_arrive();  // this CTA runs: its shared memory may be written (waited for below)
-
-    // Every CTA decides every draft by the rows' sums in 32 bits; those next to the border are left open.
-    for (unsigned i = warp; i <= a.drafts; i += WARPS) {
-        const long long x = i < a.drafts ? token(i) : -1;
-        const float zt = known(x) ? to_f32(target[i * a.t_sr + x]) : 0.0f;
-        const float zd = known(x) && draft ? to_f32(draft[i * a.d_sr + x]) : 0.0f;
-        const float random = u[i * a.u_sr];
-        const auto row_sum = [&](const MaxSum* parts, float c) {
-            MaxSum v = {-CUDART_INF_F, 0.0f};
-            for (unsigned k = lane; k < a.chunks; k += 32) v = join(v, parts[k], c);
-            return warp_join(v, c);
-        };
-        const MaxSum t = row_sum(a.parts + (size_t)(seq * (a.drafts + 1) + i) * a.chunks, a.inv_temp);
-        MaxSum d = {0.0f, 1.0f};
-        if (draft && i < a.drafts) d = row_sum(a.parts + (size_t)(a.target_rows + seq * a.drafts + i) * a.chunks, a.draft_temp);
-        if (lane == 0) {
-            s.maxima[i] = t.m;
-            s.draft_maxima[i] = d.m;
-            s.sums[i] = t.s;
-            s.draft_sums[i] = d.s;
-            int what = kEnds;
-            if (known(x)) {
-                const float lp = (zt - t.m) * a.inv_temp - logf(t.s);
-                const float lq = draft ? (zd - d.m) * a.draft_temp - logf(d.s) : 0.0f;
-                const float over = lp - lq - logf(random);
-                s.logp[i] = lp;
-                // 32 bits leave `over` uncertain by some 1e-6; infinities and NaN are left to the exact comparison too
-                const float margin = 1e-4f + 4e-6f * (fabsf(lp) + fabsf(lq));
-                what = over > margin ? kAccepted : over < -margin ? kRefused : kNear;
-            }
-            s.decision[i] = (unsigned char)what;
-        }
-    }
-    if (threadIdx.x == 0) s.found = INT_MAX, s.last = -1;
-    if (cs > 1) cluster_wait();
+    const unsigned seq = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int mine = (int)threadIdx.x;
+    const Sequence<T> in(a, seq);
+    double x[kDrawSums];  // of the thread's segment, then P, Q, R, D, N
+#pragma unroll
+    for (int k = 0; k < kDrawSums; ++k) x[k] = mine < a.segments ? a.sums[((size_t)seq * kDrawSums + k) * a.segments + mine] : 0.0;
+    if (threadIdx.x <= a.drafts) s.place[threadIdx.x] = a.positions[(size_t)seq * (a.drafts + 1) + threadIdx.x];
+    if (threadIdx.x == 0) s.found = INT_MAX, s.last = -1, s.at = -1;
     __syncthreads();
-
-    // this warp's part of the vocabulary: whole steps of eight elements a lane
-    const int per_warp = ((a.vocab + (int)(cs * WARPS) - 1) / (int)(cs * WARPS) + 255) / 256 * 256;
-    const int lo = (int)min((long long)a.vocab, (long long)(rank * WARPS + warp) * per_warp), hi = min(a.vocab, lo + per_warp);
-    const int own = lo + 8 * (int)lane;
-
-    // The first draft that is not accepted.  One pass over its two rows gives, in 64 bits, the sums P and Q of the target's
-    // and the draft's exponentials (relative to their maxima), and with a ratio k near P / Q, for the target
-    // beyond the draft (times P),
-    //     R = sum of max(0, p - k q)    D = sum of q where p > k q    N = sum of p where p is within 2^-18 of k q
-    // The ratio comes from the sums in 32 bits, some 1e-7 off.  With the right one, P / Q, R is R - (P / Q - k) D, but for the
-    // elements that change sides, which N bounds: where it does not bound them well enough (distributions that are equal on much
-    // of their mass) the pass is made again with the right ratio.
-    RowPair<T> row;
-    double x[kDrawSums];  // P, Q, R, D, N
-    double ratio = 0.0, off = 0.0;
-    unsigned n = 0, turn = 0;
+    unsigned n = 0;
+    while (s.place[n].decision == kAccepted) ++n;
+    RowPair<T> row = in.row(n, s.place[n]);
+    double ratio = ratio_of(s.place[n]), off = 0.0, part_p, part_r, part_d;
     bool refused = false;
-    for (bool again = false;; turn ^= 1) {
-        if (!again)
-            while (s.decision[n] == kAccepted) ++n;  // (behind the last draft it is kEnds)
-        const bool ends = s.decision[n] == kEnds;
-        const long long t = ends ? -1 : token(n);
-        row = RowPair<T>{target + n * a.t_sr, draft && !ends ? draft + n * a.d_sr : nullptr, t, s.maxima[n], s.draft_maxima[n],
-                         a.inv_temp * 1.4426950408889634, a.draft_temp * 1.4426950408889634, a.vocab};
-        if (row.q && !again) ratio = (double)s.sums[n] / (double)s.draft_sums[n];
+    for (bool again = false;;) {
+        part_p = x[0], part_r = x[2], part_d = x[3];
 #pragma unroll
-        for (int k = 0; k < kDrawSums; ++k) x[k] = 0.0;
-        row.each(own, hi, [&](int j, const float (&z)[8], const float (&y)[8]) {
-            double e[8];
-            row.target(z, e);
-            x[0] += sum_of(e);
-            if (row.q) {
-                double f[8];
-                row.draft(y, f);
-                x[1] += sum_of(f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const double r = fma(-ratio, f[i], e[i]);
-                    const int high = __double2hiint(r), whole = __double2hiint(e[i]);
-                    if ((high & 0x7fffffff) < whole - (18 << 20)) x[4] += e[i];
-                    e[i] = high < 0 && r == r ? 0.0 : r;  // (NaN stays)
-                    f[i] = high < 0 ? 0.0 : f[i];
-                }
-                x[2] += sum_of(e);
-                x[3] += sum_of(f);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
-                x[2] += sum_of(e);
-            }
-        });
-        cluster_sums<WARPS>(s, cs, rank, turn, x);
-        if (ends) break;
-        if (!again) {
-            refused = s.decision[n] == kRefused ||
-                      !((double)u[n * a.u_sr] * (row.q ? row.draft((int)t) / x[1] : 1.0) < row.target((int)t) / x[0]);
-            if (!refused) {
-                ++n;
-                continue;
-            }
+        for (int k = 0; k < kDrawSums; ++k) {
+            x[k] = warp_sum(x[k]);
+            if (lane == 0) s.warp_part[k][warp] = x[k];
         }
-        if (!row.q) break;
-        off = x[0] / x[1] - ratio;
-        // (what is not finite is not mended by another pass)
-        if (again || !(fabs(off) > 0x1p-19 * ratio || x[4] * fabs(off) > 1e-11 * ratio * x[2])) break;
-        ratio += off;
-        again = true;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kDrawSums; ++k) x[k] = warp_sum(lane < kDrawWarps ? s.warp_part[k][lane] : 0.0);
+        if (s.place[n].decision == kEnds) break;
+        bool next = false;
+        if (!again) {
+            const int t = (int)row.hot;
+            refused = s.place[n].decision == kRefused || !((double)in.u[n * a.u_sr] * (row.q ? row.draft(t) / x[1] : 1.0) < row.target(t) / x[0]);
+            next = !refused;
+        }
+        if (!next) {
+            if (!row.q) break;
+            off = x[0] / x[1] - ratio;
+            // (what is not finite is not mended by another pass)
+            if (again || !(fabs(off) > 0x1p-19 * ratio || x[4] * fabs(off) > 1e-11 * ratio * x[2])) break;
+            ratio += off;
+            again = true;
+        } else {
+            do ++n;
+            while (s.place[n].decision == kAccepted);
+            row = in.row(n, s.place[n]);
+            ratio = ratio_of(s.place[n]);
+        }
+        // rare: the pass over this place, by this CTA alone
+        __syncthreads();
+        for (int g = (int)warp; g < a.segments; g += kDrawWarps) {
+            pass_segment(row, ratio, g * a.segment, min(a.vocab, (g + 1) * a.segment), x);
+#pragma unroll
+            for (int k = 0; k < kDrawSums; ++k)
+                if ((int)lane == k) s.segment[k][g] = x[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kDrawSums; ++k) x[k] = mine < a.segments ? s.segment[k][mine] : 0.0;
     }
     // Where nothing is left (a draft that neither gives a probability, equal distributions): the whole target.
     double all = x[2] - off * x[3];
     if (refused && !(all > 0.0) && all == all) refused = false;
     if (!refused) all = x[0], row.q = nullptr, row.hot = -1;
     ratio += off;
-    const auto part_left = [&](double p, double r, double d) { return refused ? fmax(0.0, r - off * d) : p; };
-    const auto left = [&](int j, const float (&z)[8], const float (&y)[8], double (&e)[8]) {
-        row.target(z, e);
-        if (row.q) {
-            double f[8];
-            row.draft(y, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = fmax(0.0, fma(-ratio, f[i], e[i]));
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
-        }
-    };
     const bool drawn = all > 0.0 && all < CUDART_INF;  // not where a row holds NaN, +inf or nothing but -inf
-    const double bound = (double)u[a.drafts * a.u_sr] * all;
+    const double bound = (double)in.u[a.drafts * a.u_sr] * all;
 
-    // The CTA, and in it the warp, in whose part the running sum passes the bound: the last that begins no higher, of
-    // those that have anything.
-    const auto last_begin = [&](unsigned many, double before, auto part, double& begin) {
-        int at = -1;
-        for (unsigned i = 0; i < many; ++i) {
-            const double x = part(i);
-            if (x > 0.0 && (at < 0 || before <= bound)) at = (int)i, begin = before;
-            before += x;
-        }
-        return at;
-    };
-    double begin = 0.0;
-    const int cta = last_begin(cs, 0.0, [&](unsigned c) { return part_left(s.cta_part[turn][0][c], s.cta_part[turn][2][c], s.cta_part[turn][3][c]); }, begin);
-    if (drawn && cta == (int)rank) {
-        const int at = last_begin(WARPS, begin, [&](unsigned w) { return part_left(s.warp_part[0][w], s.warp_part[2][w], s.warp_part[3][w]); }, begin);
-        // its part again, 256 elements a warp, all warps of the CTA together
-        const int from = min(a.vocab, (int)(rank * WARPS + at) * per_warp), to = min(a.vocab, from + per_warp);
-        for (int j0 = from; j0 < to; j0 += 256 * WARPS) {
+    // The segment in which the running sum passes the bound: the last that begins no higher, of those that have anything.
+    const double part = refused ? fmax(0.0, part_r - off * part_d) : part_p;
+    double run = part;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const double v = __shfl_up_sync(~0u, run, d);
+        if ((int)lane >= d) run += v;
+    }
+    __syncthreads();
+    if (lane == 31) s.warp_part[0][warp] = run;
+    __syncthreads();
+    double begin = warp_sum(lane < warp ? s.warp_part[0][lane] : 0.0);
+    const double before = __shfl_up_sync(~0u, run, 1);
+    if (lane > 0) begin += before;
+    // (a bound that is NaN or below 0 takes the first that has anything)
+    const int candidate = __reduce_max_sync(~0u, part > 0.0 && begin <= bound ? mine : -1);
+    const unsigned some_part = __ballot_sync(~0u, part > 0.0);
+    if (lane == 0 && candidate >= 0) atomicMax(&s.at, candidate);
+    if (lane == 0 && some_part != 0) atomicMin(&s.found, (int)warp * 32 + __ffs((int)some_part) - 1);
+    __syncthreads();
+    const int at = s.at >= 0 ? s.at : s.found;
+    if (mine == at) s.begin = begin;
+    __syncthreads();
+    begin = s.begin;
+    if (threadIdx.x == 0) s.found = INT_MAX;
+    if (drawn) {
+        // its elements again, 256 a warp
+        const int from = at * a.segment, to = min(a.vocab, from + a.segment);
+        for (int j0 = from; j0 < to; j0 += 256 * kDrawWarps) {
             const int j = j0 + 256 * (int)warp + 8 * (int)lane;
             double e[8] = {};
             if (j < to) {
-                float z[8], y[8] = {};
+                float z[8];
                 row.load(row.p, j, z);
-                if (row.q) row.load(row.q, j, y);
-                left(j, z, y, e);
+                row.target(z, e);
+                if (row.q) {
+                    double f[8];
+                    row.load(row.q, j, z);
+                    row.draft(z, f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[i] = fmax(0.0, fma(-ratio, f[i], e[i]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
+                }
             }
 #pragma unroll
             for (int i = 1; i < 8; ++i) e[i] += e[i - 1];
-            double run = e[7];
+            run = e[7];
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const double v = __shfl_up_sync(~0u, run, d);
                 if ((int)lane >= d) run += v;
             }
-            double before = __shfl_up_sync(~0u, run, 1);
-            if (lane == 0) before = 0.0;
-            __syncthreads();  // (the parts of before have been read)
+            __syncthreads();  // (the sums of before have been read)
             if (lane == 31) s.warp_part[0][warp] = run;
             __syncthreads();
-            for (int w = 0; w < WARPS; ++w) {
-                if (w == (int)warp) before += begin;
-                begin += s.warp_part[0][w];
-            }
+            double ahead = begin + warp_sum(lane < warp ? s.warp_part[0][lane] : 0.0);
+            begin += warp_sum(lane < kDrawWarps ? s.warp_part[0][lane] : 0.0);
+            const double lower = __shfl_up_sync(~0u, run, 1);
+            if (lane > 0) ahead += lower;
             int over = INT_MAX, some = -1;
 #pragma unroll
             for (int i = 7; i >= 0; --i) {
                 const bool any = e[i] > (i > 0 ? e[i - 1] : 0.0);
-                if (any && before + e[i] > bound) over = j + i;
+                if (any && ahead + e[i] > bound) over = j + i;
                 if (any && some < 0) some = j + i;
             }
             over = __reduce_min_sync(~0u, over);
@@ -395,13 +441,11 @@ __global__ void __launch_bounds__(WARPS * 32) draw_kernel(const __grid_constant_
             a.logp[(size_t)seq * (a.drafts + 1) + n] = (float)(((double)to_f32(row.p[found]) - row.mp) * a.inv_temp - log(x[0]));
         }
     }
-    if (rank == 0) {
-        if (threadIdx.x == 0) a.accepted[seq] = (int)n;
-        for (unsigned i = threadIdx.x; i <= a.drafts; i += WARPS * 32) {
-            if (i == n && drawn) continue;
-            store_token(a, seq, i, i < n ? token(i) : -1);
-            a.logp[(size_t)seq * (a.drafts + 1) + i] = i < n ? s.logp[i] : i > n ? 0.0f : CUDART_NAN_F;
-        }
+    if (threadIdx.x == 0) a.accepted[seq] = (int)n;
+    for (unsigned i = threadIdx.x; i <= a.drafts; i += kDrawThreads) {
+        if (i == n && drawn) continue;
+        store_token(a, seq, i, i < n ? in.token(i) : -1);
+        a.logp[(size_t)seq * (a.drafts + 1) + i] = i < n ? s.place[i].logp : i > n ? 0.0f : CUDART_NAN_F;
     }
 }
 

@@ -327,12 +327,15 @@ def _gated_inputs(x, w_gate, w_up, activation, dev):
     return kind, weight_type, width, dim, gate_stride, up_stride
 
 
-def _workspace(need: int, given: Optional[torch.Tensor], like: torch.Tensor, dev: int, stream) -> torch.Tensor:
+def _workspace(need: int, given: Optional[torch.Tensor], like: torch.Tensor, dev: int, stream):
+    """(tensor to keep, address, bytes) of a call's workspace; none where none is needed."""
     if given is None:
-        return _new(like, max(16, need), torch.uint8, stream)
-    if not given.is_contiguous() or given.get_device() != dev:
+        if need == 0:
+            return None, 0, 0
+        given = _new(like, need, torch.uint8, stream)
+    elif not given.is_contiguous() or given.get_device() != dev:
         raise ValueError("workspace: need a contiguous tensor on the current device")
-    return given
+    return given, given.data_ptr(), given.nbytes
 
 
 def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, *, activation: str = "silu", save: bool = False,
@@ -362,8 +365,8 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, *, acti
     lib = binding.load_library()
     need = ctypes.c_size_t()
     _check(lib.odsgd_gated_workspace(d, 0, ctypes.byref(need)))
-    workspace = _workspace(need.value, workspace, x, dev, stream)
-    _check(lib.odsgd_gated_forward(d, workspace.data_ptr(), workspace.nbytes, _handle(stream, dev)))
+    workspace, ws_at, ws_bytes = _workspace(need.value, workspace, x, dev, stream)
+    _check(lib.odsgd_gated_forward(d, ws_at, ws_bytes, _handle(stream, dev)))
     if given:
         increment_version(out)
     return GatedFfn(out, gate, up)
@@ -413,8 +416,8 @@ def gated_ffn_grad(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, ga
     lib = binding.load_library()
     need = ctypes.c_size_t()
     _check(lib.odsgd_gated_workspace(d, 1, ctypes.byref(need)))
-    workspace = _workspace(need.value, workspace, x, dev, stream)
-    _check(lib.odsgd_gated_backward(d, workspace.data_ptr(), workspace.nbytes, _handle(stream, dev)))
+    workspace, ws_at, ws_bytes = _workspace(need.value, workspace, x, dev, stream)
+    _check(lib.odsgd_gated_backward(d, ws_at, ws_bytes, _handle(stream, dev)))
     if written:
         increment_version(written)
     return GatedFfnGrad(dx, dw_gate, dw_up)
@@ -497,8 +500,8 @@ def verify_draft(target: torch.Tensor, draft_tokens: torch.Tensor, uniforms: tor
     lib = binding.load_library()
     need = ctypes.c_size_t()
     _check(lib.odsgd_verify_workspace(d, ctypes.byref(need)))
-    workspace = _workspace(need.value, workspace, target, dev, stream)
-    _check(lib.odsgd_verify_draft(d, workspace.data_ptr(), workspace.nbytes, _handle(stream, dev)))
+    workspace, ws_at, ws_bytes = _workspace(need.value, workspace, target, dev, stream)
+    _check(lib.odsgd_verify_draft(d, ws_at, ws_bytes, _handle(stream, dev)))
     return Verified(accepted, tokens, logp)
 
 

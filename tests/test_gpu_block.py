@@ -264,7 +264,9 @@ def test_gated_refusals():
     with pytest.raises(binding.OdsgdError):
         lm.gated_ffn_grad(x, wg, wu, r.gate, r.up, dh, dx=x)
     with pytest.raises(binding.OdsgdError):
-        lm.gated_ffn(x, wg, wu, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))
+        lm.gated_ffn_grad(x, wg, wu, r.gate, r.up, dh, workspace=torch.empty(8, dtype=torch.uint8, device=DEV))
+    with pytest.raises(binding.OdsgdError):
+        lm.gated_ffn(x, wg.float(), wu.float(), workspace=torch.empty(8, dtype=torch.uint8, device=DEV))
     with pytest.raises(ValueError):
         lm.gated_ffn(x, wg, wu, workspace=torch.empty(64, dtype=torch.uint8))
     out = torch.empty(4, 24, dtype=BF16, device=DEV)
