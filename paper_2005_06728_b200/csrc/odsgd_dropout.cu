@@ -45,11 +45,19 @@ bool flat(int64_t so, int64_t si, const odsgd_dropout_desc* d) {
 }
 
 template <typename TX, typename TO>
-int launch_dropout(const DropoutArgs& a, bool vec, int sms, void* stream) {
-    const int64_t ctas = ceil_div(ceil_div(a.n, 8), kDropoutThreads);
-    const dim3 grid((unsigned)std::min<int64_t>(ctas, (int64_t)sms * 64)), block(kDropoutThreads);
-    return vec ? launch("dropout kernel", dropout_kernel<TX, TO, true>, grid, block, 0, 1, stream, a)
-               : launch("dropout kernel", dropout_kernel<TX, TO, false>, grid, block, 0, 1, stream, a);
+int launch_dropout(DropoutArgs a, bool vec, int sms, void* stream) {
+    const int64_t most = (int64_t)sms * 64;
+    if (vec) {
+        const int64_t blocks = a.n / 8;
+        const dim3 grid((unsigned)std::min<int64_t>(ceil_div(blocks, kDropoutThreads), most));
+        const int rc = blocks > 0 ? launch("dropout kernel", dropout_kernel<TX, TO>, grid, dim3(kDropoutThreads), 0, 1, stream, a) : (int)ODSGD_OK;
+        if (rc != ODSGD_OK || a.n % 8 == 0) return rc;
+        a.first = blocks;  // fewer than eight elements are left
+    }
+    const int64_t rows = a.n / a.dim, blocks = a.first > 0 ? 1 : a.dim / 8 + 2;
+    const int64_t x = std::min<int64_t>(kDropoutThreads, ceil_div(blocks, 32) * 32), y = kDropoutThreads / x;
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows, y), most), (unsigned)std::min<int64_t>(ceil_div(blocks, x), 4096));
+    return launch("dropout kernel (rows)", row_dropout_kernel<TX, TO>, grid, dim3((unsigned)x, (unsigned)y), 0, 1, stream, a);
 }
 
 template <typename TX>

@@ -713,27 +713,6 @@ struct LayArgs {
     unsigned columns, pitch;
 };
 constexpr int kLayThreads = 256;
-// Eight elements of a row that starts anywhere: the two 16-byte words around them, shifted.  (Both words hold elements of
-// the eight, so neither reaches into another 16 bytes than the row's own do.)
-template <typename T>
-__device__ __forceinline__ uint4 load_anywhere(const T* p) {
-    static_assert(sizeof(T) == 2, "16 bits");
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    const uint4* const w = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
-    const uint4 a = w[0];
-    const unsigned shift = (unsigned)(at & 15);
-    if (shift == 0) return a;
-    const uint4 b = w[1];
-    const uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    uint32_t y[5];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {  // from word shift / 4 on
-        const unsigned k = shift / 4;
-        y[i] = k == 0 ? x[i] : k == 1 ? x[i + 1] : k == 2 ? x[i + 2] : x[min(i + 3, 7)];
-    }
-    const unsigned bits = shift % 4 * 8;
-    return make_uint4(__funnelshift_r(y[0], y[1], bits), __funnelshift_r(y[1], y[2], bits), __funnelshift_r(y[2], y[3], bits), __funnelshift_r(y[3], y[4], bits));
-}
 template <typename T>
 __global__ void __launch_bounds__(kLayThreads) lay_kernel(const __grid_constant__ LayArgs a) {
     dependent_launch_prologue();

@@ -69,8 +69,8 @@ VerifyShape verify_shape(const odsgd_verify_desc* d) {
     VerifyShape s;
     const int64_t sms = 148;
     s.rows = d->batch * (2 * d->drafts + 1);
-    // parts of at least 4096 elements, as many as give every SM four CTAs
-    s.chunks = std::max<int64_t>(1, std::min(ceil_div(sms * 4, std::max<int64_t>(s.rows, 1)), d->vocab / 4096));
+    // parts of at least 4096 elements, as many as fill every SM three times
+    s.chunks = std::max<int64_t>(1, std::min(ceil_div(sms * kPartCtas * 3, std::max<int64_t>(s.rows, 1)), d->vocab / 4096));
     // CTAs of 2048 elements and more, as many as run at once, two an SM
     s.pass_ctas = std::max<int64_t>(1, std::min(2 * sms / std::max<int64_t>(d->batch, 1), ceil_div(d->vocab, 2048)));
     // a warp's share, in pieces that draw_kernel goes over in one step, but no more of them than it has threads

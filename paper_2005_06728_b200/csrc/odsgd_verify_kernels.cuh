@@ -13,7 +13,8 @@
 namespace odsgd_lm {
 
 constexpr int kVerifyDrafts = 255;
-constexpr int kPartThreads = 256;
+constexpr int kPartThreads = 128;
+constexpr int kPartCtas = 12;  // an SM
 constexpr int kPassWarps = 8;     // of a CTA of pass_kernel
 constexpr int kDrawThreads = 512;  // of draw_kernel
 constexpr int kDrawWarps = kDrawThreads / 32;
@@ -49,9 +50,11 @@ struct VerifyArgs {
     float exp_temp, draft_exp;   // the same as RowExp takes them
 };
 
-// Part `chunk` of row `row`.
+// Part `chunk` of row `row`.  Bound by memory traffic, as the scores are: small CTAs, twelve an SM, and three times as many
+// parts as run at once (48 x 15 rows of 131072 bf16: 37 us in 256-thread CTAs of a row each, 30 so; the copy rate for
+// their bytes is 29).
 template <typename T>
-__global__ void __launch_bounds__(kPartThreads) parts_kernel(const __grid_constant__ VerifyArgs a) {
+__global__ void __launch_bounds__(kPartThreads, kPartCtas) parts_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ MaxSum warp_part[kPartThreads / 32];
     dependent_launch_prologue();
     const unsigned row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
@@ -119,21 +122,49 @@ struct RowPair {
     int vocab;
     __device__ __forceinline__ double target(int j) const { return power_of_two((double)to_f32(p[j]) - mp, cp); }
     __device__ __forceinline__ double draft(int j) const { return power_of_two((double)to_f32(q[j]) - mq, cq); }
-    // Elements j to j + 7 of a row; -inf behind its end.
-    __device__ __forceinline__ void load(const T* row, int j, float (&z)[8]) const {
-        if (j + 8 <= vocab && (reinterpret_cast<uintptr_t>(row + j) & 15) == 0) {
+    // Elements j to j + 7 of a row, as the 16-byte words that hold them: loaded ahead, taken apart when they are needed.  No word
+    // is read that has none of them.
+    static constexpr int kWords = 8 * (int)sizeof(T) / 16 + 1;
+    struct Raw {
+        uint4 w[kWords];
+    };
+    __device__ __forceinline__ Raw fetch(const T* row, int j) const {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(row + j), from = at & ~(uintptr_t)15, end = reinterpret_cast<uintptr_t>(row + min(j + 8, vocab));
+        Raw out;
 #pragma unroll
-            for (int h = 0; h < 8; h += kLanes<T>) {
-                float y[kLanes<T>];
-                unpack<T>(*reinterpret_cast<const uint4*>(row + j + h), y);
+        for (int k = 0; k < kWords; ++k) out.w[k] = from + 16 * k < end ? reinterpret_cast<const uint4*>(from)[k] : make_uint4(0, 0, 0, 0);
+        return out;
+    }
+    // -inf behind the row's end
+    __device__ __forceinline__ void take(const Raw& raw, const T* row, int j, float (&z)[8]) const {
+        uint32_t x[4 * kWords];
 #pragma unroll
-                for (int l = 0; l < kLanes<T>; ++l) z[h + l] = y[l];
+        for (int k = 0; k < kWords; ++k) x[4 * k] = raw.w[k].x, x[4 * k + 1] = raw.w[k].y, x[4 * k + 2] = raw.w[k].z, x[4 * k + 3] = raw.w[k].w;
+        const unsigned shift = (unsigned)(reinterpret_cast<uintptr_t>(row + j) & 15);  // the same for all of a row
+        if (shift != 0) {
+#pragma unroll
+            for (int i = 0; i + 2 < 4 * kWords; ++i) x[i] = shift & 8 ? x[i + 2] : x[i];
+#pragma unroll
+            for (int i = 0; i + 1 < 4 * kWords; ++i) x[i] = shift & 4 ? x[i + 1] : x[i];
+            if (sizeof(T) == 2) {
+#pragma unroll
+                for (int i = 0; i + 1 < 4 * kWords; ++i) x[i] = shift & 2 ? __funnelshift_r(x[i], x[i + 1], 16) : x[i];
             }
-        } else {
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = j + i < vocab ? to_f32(row[j + i]) : -CUDART_INF_F;
+        for (int h = 0; h < 8; h += kLanes<T>) {
+            float y[kLanes<T>];
+            const int k = h / kLanes<T> * 4;
+            unpack<T>(make_uint4(x[k], x[k + 1], x[k + 2], x[k + 3]), y);
+#pragma unroll
+            for (int l = 0; l < kLanes<T>; ++l) z[h + l] = y[l];
+        }
+        if (j + 8 > vocab) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = j + i < vocab ? z[i] : -CUDART_INF_F;
         }
     }
+    __device__ __forceinline__ void load(const T* row, int j, float (&z)[8]) const { take(fetch(row, j), row, j, z); }
     __device__ __forceinline__ void target(const float (&z)[8], double (&e)[8]) const {
 #pragma unroll
         for (int i = 0; i < 8; ++i) e[i] = power_of_two((double)z[i] - mp, cp);
@@ -145,20 +176,22 @@ struct RowPair {
     // f(j, logits of the target, of the draft) for each eight from `from` on, a warp's width apart; the next are loaded ahead.
     template <typename F>
     __device__ __forceinline__ void each(int from, int hi, F f) const {
-        float z[8], y[8] = {}, next_z[8], next_y[8] = {};
+        Raw next_p = {}, next_q = {};
         if (from < hi) {
-            load(p, from, z);
-            if (q) load(q, from, y);
+            next_p = fetch(p, from);
+            if (q) next_q = fetch(q, from);
         }
 #pragma unroll 1
         for (int j = from; j < hi; j += 256) {
+            const Raw now_p = next_p, now_q = next_q;
             if (j + 256 < hi) {
-                load(p, j + 256, next_z);
-                if (q) load(q, j + 256, next_y);
+                next_p = fetch(p, j + 256);
+                if (q) next_q = fetch(q, j + 256);
             }
+            float z[8], y[8] = {};
+            take(now_p, p, j, z);
+            if (q) take(now_q, q, j, y);
             f(j, z, y);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = next_z[i], y[i] = next_y[i];
         }
     }
 };
