@@ -568,3 +568,59 @@ def test_verify_beyond_32_bit_offsets():
     r = lm.verify_draft(target, tok, u)
     assert r.accepted.tolist() == [0] * 15 + [255] and r.tokens[15].tolist() == [7] * 255 + [v - 1]
     assert r.tokens[:15, 0].tolist() == [v // 2] * 15
+
+
+# --------------------------------------------------------------------------- together, in the token policy
+
+def test_policy_example_with_block_dropout_and_drafts():
+    from paper_2005_06728_b200 import policy_example
+
+    for kw in (dict(block=96), dict(block=50, drop=0.2), dict(drafts=3), dict(block=72, drop=0.1, drafts=4, vocab=53, dim=40)):
+        a, b = policy_example.train(steps=8, **kw), policy_example.train(steps=8, **kw)
+        assert all(math.isfinite(v) for v in a.losses) and bool(a.weights.isfinite().all())
+        assert a.rewards == b.rewards and torch.equal(a.weights, b.weights), "a run can be repeated"
+    with pytest.raises(ValueError):
+        policy_example.train(steps=1, drop=0.1)
+
+
+def test_policy_example_gradients():
+    """lookup, block, dropout, head: the gradients of all tensors against autograd in 64 bits."""
+    from paper_2005_06728_b200 import policy_example
+
+    vocab, dim, width, p = 61, 48, 72, 0.25
+    model = policy_example.GatedModel(vocab, dim, width, p)
+    w = model.views(model.init(5, torch.device(DEV)))
+    tokens = torch.randint(0, vocab, (6, 10), generator=gen(400), device=DEV)
+    tokens[2, 7:] = -1
+    z, kept = model.forward(w, tokens, 9, 4, training=True)
+    dz = randn(6, 10, vocab, seed=401, dtype=BF16)
+    dz[2, 7:] = 0
+    out = model.gradients(torch.device(DEV))
+    model.backward(w, tokens, kept, dz, out)
+    v = {k: t.double().requires_grad_() for k, t in w.items()}
+    x = torch.nn.functional.embedding(tokens.clamp(min=0), v["embedding"]) * math.sqrt(dim) * (tokens >= 0)[..., None]
+    t = x @ v["gate"].T
+    y = (t * torch.sigmoid(t) * (x @ v["up"].T)) @ v["down"].T
+    s = x + torch.where(R.kept((6, 10, dim), p, 9, 4).to(DEV), y / 0.75, torch.zeros((), dtype=torch.float64, device=DEV))
+    zz = s @ v["head"].T
+    zz.backward(dz.double())
+    # along the longest way (embedding) some twelve roundings to 8 bits, each of at most 2^-8 and of either sign
+    assert float((z.double() - zz.detach()).norm() / zz.detach().norm()) < 6 * 2.0 ** -8
+    for (name, _), got in zip(model.shapes, out):
+        want = v[name].grad
+        assert float((got.double() - want).norm() / want.norm()) < 12 * 2.0 ** -8, name
+
+
+def test_drafted_answers_carry_their_scores():
+    from paper_2005_06728_b200 import policy_example
+
+    z = randn(9, 14, 37, seed=410, sigma=1.5)
+    draft = z + randn(9, 14, 37, seed=411, sigma=0.7)
+    counts = torch.arange(14, device=DEV)[None, :] < torch.tensor([14, 1, 7, 13, 2, 14, 5, 9, 3], device=DEV)[:, None]
+    for drafts in (1, 3, 20):
+        answers, acting = policy_example.drafted_answers(z, draft, counts, drafts, gen(412 + drafts))
+        assert bool((answers >= 0).all()) and bool((answers < 37).all())
+        want = lm.token_logprob(z, answers).logp
+        # both are sums of 37 exponentials in 32 bits
+        assert float((acting - want)[counts].abs().max()) < 40 * 2.0 ** -22
+        assert not bool(acting[~counts].any())
