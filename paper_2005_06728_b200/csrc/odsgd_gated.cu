@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "odsgd.h"
 #include "odsgd_lm_host.h"
@@ -205,34 +206,97 @@ int launch_gated(const GatedArgs& a, void* stream) {
                   gated_kernel<KIND, T, GELU>, dim3(2 * pairs), dim3(kGatedThreads), kGatedSmem, 1, stream, a);
 }
 
-// Up to so many tokens go to thin_kernel.
-constexpr int64_t kThinTokens = 256;
-constexpr int kThinSmem = 227 * 1024 - 1024;  // of an SM
+// dynamic shared memory of a CTA of thin_kernel, one and two an SM
+constexpr int kThinSmem[2] = {226 * 1024, 110 * 1024};
+
+// How many clusters of `cluster` CTAs of thin_kernel run at once, one or two CTAs an SM: what the GPU's clusters of SMs leave
+// room for, asked once a device.  The question is put for a kernel without tensor memory: for one that has some the answer
+// is one CTA an SM, though two of thin_kernel do run (their times and SMs were recorded).
+int thin_clusters(int per_sm, int cluster, int* out) {
+    static std::atomic<int> known[kMaxDevices][2][kThinCluster + 1] = {};
+    static std::atomic<bool> done[kMaxDevices] = {};
+    int dev = 0;
+    int rc = current_device(&dev);
+    if (rc != ODSGD_OK) return rc;
+    int n = dev < kMaxDevices ? known[dev][per_sm - 1][cluster].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+        rc = allow_smem((const void*)thin_room_kernel, kThinSmem[0], done);
+        if (rc != ODSGD_OK) return rc;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)cluster);
+        cfg.blockDim = dim3(kThinThreads);
+        cfg.dynamicSmemBytes = (size_t)kThinSmem[per_sm - 1];
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)cluster;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, thin_room_kernel, &cfg);
+        if (e != cudaSuccess) return cuda_fail("cudaOccupancyMaxActiveClusters", e);
+        n = std::max(n, 1);
+        if (dev < kMaxDevices) known[dev][per_sm - 1][cluster].store(n, std::memory_order_relaxed);
+    }
+    *out = n;
+    return ODSGD_OK;
+}
+
+// Whether a product of `tokens` goes to thin_kernel, and how: its tokens in chunks of up to 256, each CTA of a cluster with four
+// blocks of the long axis at least, as many CTAs to a cluster as leave all clusters running at once.
+struct ThinShape {
+    int64_t chunk = 0;  // 0: gated_kernel
+    int cluster = 1, per_sm = 1;
+};
+// Both kernels' cycles, from runs of (dim, width) (256, 700) to (4096, 11000) with 1 to 3000 tokens, burst, forward and gradient
+// of x: a block of the long axis takes gated_kernel some 520 where tiles are few and operands come from memory; thin_kernel
+// takes it at 60 bytes a cycle and SM, and finishes at 65 cycles a token; 12500 and 7600 pass beside that.  For example
+// (2048, 5440), forward: 64 tokens 11.0 us thin and 16.2 not, 128 14.1 and 16.7, 200 18.8 and 16.7; gradient of x: 256 tokens
+// 22 and 58, 1024 58 and 66, 1536 79 and 71; (512, 1400), forward, 768 tokens 8.9 and 9.6, 1024 10.4 and 10.1.
+template <int KIND>
+int thin_shape(int64_t tokens, int64_t columns, int64_t depth, int sms, ThinShape* out) {
+    const int64_t blocks = ceil_div(depth, kBlockK) * (KIND == kGradX ? 2 : 1), tiles = ceil_div(columns, KIND == kForward ? 64 : 128);
+    const int64_t wide = ceil_div(tokens, kTileRows) * ceil_div(columns, KIND == kForward ? kTileColumns / 2 : kTileColumns);
+    double least = 12500.0 + 520.0 * (double)ceil_div(wide, sms / 2) * (double)blocks;
+    *out = ThinShape{};
+    if (tokens > 8192) return ODSGD_OK;
+    for (int64_t most : {64, 96, 128, 192, 256}) {
+        const int64_t chunks = ceil_div(tokens, most), chunk = ceil_div(ceil_div(tokens, chunks), 16) * 16;
+        const int64_t stage = kThinRows * kBlockK * 2 + chunk * kBlockK * 2, sums = chunk * kThinRows * 4;
+        const int per_sm = std::max(3 * stage, sums) <= kThinSmem[1] - 1024 ? 2 : 1;
+        int cluster = 1;
+        for (int c = 2; c <= kThinCluster && blocks >= 4 * c; ++c) {
+            int room = 0;
+            const int rc = thin_clusters(per_sm, c, &room);
+            if (rc != ODSGD_OK) return rc;
+            if (tiles * chunks <= room) cluster = c;
+        }
+        const double ctas = (double)(tiles * chunks * cluster), waves = std::ceil(ctas / (per_sm * sms));
+        const double an_sm = std::max(1.0, std::min((double)per_sm, ctas / sms));
+        const double cycles = 7600.0 + waves * ((double)ceil_div(blocks, cluster) * an_sm * (double)stage / 60.0 + 65.0 * (double)chunk);
+        if (cycles < least) least = cycles, *out = ThinShape{chunk, cluster, per_sm};
+        if (chunks == 1) break;  // (the wider ones are the same)
+    }
+    return ODSGD_OK;
+}
 
 template <int KIND, typename T, bool GELU = false>
-int launch_thin(const GatedArgs& g, unsigned tokens, void* stream) {
+int launch_thin(const GatedArgs& g, unsigned tokens, const ThinShape& s, void* stream) {
     static std::atomic<bool> done[kMaxDevices] = {};
-    int sms = 0;
-    int rc = sm_count(&sms);
-    if (rc == ODSGD_OK) rc = allow_smem((const void*)thin_kernel<KIND, T, GELU>, kThinSmem, done);
+    const int rc = allow_smem((const void*)thin_kernel<KIND, T, GELU>, kThinSmem[0], done);
     if (rc != ODSGD_OK) return rc;
     ThinArgs a;
     for (int i = 0; i < 2; ++i) a.a[i] = g.b[i], a.b[i] = g.a[KIND == kForward ? 0 : i];
     for (int i = 0; i < 3; ++i) a.out[i] = g.out[i];
     a.tokens = tokens, a.n_inner = g.n_inner, a.columns = g.columns, a.depth = g.depth, a.is_bf16 = g.is_bf16, a.save = g.save;
-    a.padded = (unsigned)ceil_div(tokens, 16) * 16;
+    a.chunk = (unsigned)s.chunk, a.cluster = (unsigned)s.cluster;
     a.tensor_columns = 32;
-    while (a.tensor_columns < a.padded) a.tensor_columns *= 2;
-    const int64_t tiles = ceil_div(a.columns, KIND == kForward ? 64 : 128), blocks = ceil_div(a.depth, kBlockK) * (KIND == kGradX ? 2 : 1);
-    // two CTAs an SM where three stages and the sums fit twice
-    const int64_t stage = kThinRows * kBlockK * 2 + a.padded * kBlockK * 2, sums = (int64_t)a.padded * kThinRows * 4;
-    const int per_sm = std::max(3 * stage, sums) <= kThinSmem / 2 - 2048 ? 2 : 1;
-    const int64_t room = kThinSmem / per_sm - 2048;
-    // as many CTAs as run at once, each with four blocks of the long axis at least
-    a.cluster = (unsigned)std::max<int64_t>(1, std::min({(int64_t)kThinCluster, per_sm * sms / tiles, blocks / 4}));
-    a.stages = (unsigned)std::min<int64_t>(kThinStages, room / stage);
+    while (a.tensor_columns < a.chunk) a.tensor_columns *= 2;
+    const int64_t stage = kThinRows * kBlockK * 2 + s.chunk * kBlockK * 2, sums = s.chunk * kThinRows * 4;
+    a.stages = (unsigned)std::min<int64_t>(kThinStages, (kThinSmem[s.per_sm - 1] - 1024) / stage);
     const size_t smem = 1024 + (size_t)std::max(a.stages * stage, sums);
-    return launch("gated kernel for few tokens", thin_kernel<KIND, T, GELU>, dim3((unsigned)tiles * a.cluster), dim3(kThinThreads), smem, (int)a.cluster, stream, a);
+    const int64_t tiles = ceil_div(a.columns, KIND == kForward ? 64 : 128);
+    return launch("gated kernel for few tokens", thin_kernel<KIND, T, GELU>, dim3((unsigned)tiles * a.cluster, (unsigned)ceil_div(tokens, s.chunk)),
+                  dim3(kThinThreads), smem, s.cluster, stream, a);
 }
 
 // Blocks of rows: threads along a row, eight columns each, and the rest of a CTA's across rows.
@@ -279,13 +343,19 @@ int run_gated(const odsgd_gated_desc* d, bool backward, const GatedPlan& p, char
         rc = launch("operand layout kernel", lay_kernel<T>, grid, block, 0, 1, stream, lay);
         if (rc != ODSGD_OK) return rc;
     }
+    int sms = 0;
+    rc = sm_count(&sms);
+    if (rc != ODSGD_OK) return rc;
+    ThinShape shape;
     GatedArgs a = {};
     a.is_bf16 = d->type == ODSGD_BF16;
     const bool gelu = d->activation == ODSGD_GELU;
     a.n_inner = (unsigned)d->n_inner;
     if (!backward) {
-        const bool thin = n <= kThinTokens;
-        rc = encode(&a.a[0], x, d->type, thin ? (int)ceil_div(n, 16) * 16 : 128);
+        rc = thin_shape<kForward>(n, d->width, d->dim, sms, &shape);
+        if (rc != ODSGD_OK) return rc;
+        const bool thin = shape.chunk > 0;
+        rc = encode(&a.a[0], x, d->type, thin ? (int)shape.chunk : 128);
         for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.b[i], w[i], d->type, thin ? 64 : 128);
         if (rc != ODSGD_OK) return rc;
         a.out[0] = {d->h, d->h_stride_outer, d->h_stride_inner};
@@ -293,7 +363,7 @@ int run_gated(const odsgd_gated_desc* d, bool backward, const GatedPlan& p, char
         a.out[2] = {d->up, d->up_stride_outer, d->up_stride_inner};
         a.rows = (unsigned)n, a.columns = (unsigned)d->width, a.depth = (unsigned)d->dim;
         a.save = d->gate != nullptr;
-        if (thin) return gelu ? launch_thin<kForward, T, true>(a, (unsigned)n, stream) : launch_thin<kForward, T, false>(a, (unsigned)n, stream);
+        if (thin) return gelu ? launch_thin<kForward, T, true>(a, (unsigned)n, shape, stream) : launch_thin<kForward, T, false>(a, (unsigned)n, shape, stream);
         return gelu ? launch_gated<kForward, T, true>(a, stream) : launch_gated<kForward, T, false>(a, stream);
     }
     SlopeArgs s = {};
@@ -311,13 +381,14 @@ int run_gated(const odsgd_gated_desc* d, bool backward, const GatedPlan& p, char
     Matrix g[2];
     for (int i = 0; i < 2; ++i) g[i].p = ws + (i ? p.du : p.dg), g[i].rows = n, g[i].columns = d->width, g[i].stride = p.width_pitch;
     if (d->dx) {
-        const bool thin = n <= kThinTokens;
-        for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.a[i], g[i], d->type, thin ? (int)ceil_div(n, 16) * 16 : 128);
+        rc = thin_shape<kGradX>(n, d->dim, d->width, sms, &shape);
+        const bool thin = shape.chunk > 0;
+        for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.a[i], g[i], d->type, thin ? (int)shape.chunk : 128);
         for (int i = 0; i < 2 && rc == ODSGD_OK; ++i) rc = encode(&a.b[i], w[i], d->type, kBlockK);
         if (rc != ODSGD_OK) return rc;
         a.out[0] = {d->dx, d->dx_stride_outer, d->dx_stride_inner};
         a.rows = (unsigned)n, a.columns = (unsigned)d->dim, a.depth = (unsigned)d->width;
-        rc = thin ? launch_thin<kGradX, T>(a, (unsigned)n, stream) : launch_gated<kGradX, T>(a, stream);
+        rc = thin ? launch_thin<kGradX, T>(a, (unsigned)n, shape, stream) : launch_gated<kGradX, T>(a, stream);
         if (rc != ODSGD_OK) return rc;
     }
     if (d->dw_gate) {

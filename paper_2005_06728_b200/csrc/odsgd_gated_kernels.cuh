@@ -548,7 +548,7 @@ struct ThinArgs {
     CUtensorMap a[2], b[2];
     RowsOut out[3];
     unsigned tokens, n_inner, columns, depth;
-    unsigned padded;  // tokens rounded up to 16
+    unsigned chunk;  // tokens of a cluster, a multiple of 16
     unsigned stages, cluster, tensor_columns;
     int is_bf16, save;
 };
@@ -566,10 +566,10 @@ __global__ void __launch_bounds__(kThinThreads) thin_kernel(const __grid_constan
     extern __shared__ unsigned char raw[];
     __shared__ ThinBarriers s;
     const uint32_t stages = (smem_address(raw) + 1023) & ~1023u;
-    float* const sums = reinterpret_cast<float*>(raw + (stages - smem_address(raw)));  // [padded][kThinRows], behind the last product
-    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cs = a.cluster;
-    const unsigned rank = blockIdx.x % cs, col = blockIdx.x / cs * WIDE;
-    const unsigned token_bytes = a.padded * kBlockK * 2, stage_bytes = kThinRows * kBlockK * 2 + token_bytes;
+    float* const sums = reinterpret_cast<float*>(raw + (stages - smem_address(raw)));  // [chunk][kThinRows], behind the last product
+    const unsigned warp = threadIdx.x >> 5, cs = a.cluster;
+    const unsigned rank = blockIdx.x % cs, col = blockIdx.x / cs * WIDE, first = blockIdx.y * a.chunk, many = min(a.chunk, a.tokens - first);
+    const unsigned token_bytes = a.chunk * kBlockK * 2, stage_bytes = kThinRows * kBlockK * 2 + token_bytes;
     if (threadIdx.x == 0) {
         for (unsigned i = 0; i < a.stages; ++i) {
             barrier_init(smem_address(&s.full[i]), 1);
@@ -606,11 +606,11 @@ __global__ void __launch_bounds__(kThinThreads) thin_kernel(const __grid_constan
                 load_box_alone(to, &a.a[0], at, (int)col, bar);
                 load_box_alone(to + kThinRows * kBlockK, &a.a[1], at, (int)col, bar);
             }
-            load_box_alone(to + kThinRows * kBlockK * 2, &a.b[second], at, 0, bar);
+            load_box_alone(to + kThinRows * kBlockK * 2, &a.b[second], at, (int)first, bar);
             if (++stage == a.stages) stage = 0, phase ^= 1;
         }
     } else if (threadIdx.x == 32) {
-        const uint32_t instr = instruction(a.is_bf16 != 0, A_LINES, false, kThinRows, (int)a.padded);
+        const uint32_t instr = instruction(a.is_bf16 != 0, A_LINES, false, kThinRows, (int)a.chunk);
         unsigned stage = 0, phase = 0;
         bool ok = true;
         for (unsigned k = k0; k < k1 && ok; ++k) {
@@ -630,7 +630,7 @@ __global__ void __launch_bounds__(kThinThreads) thin_kernel(const __grid_constan
     const bool ok = __all_sync(~0u, barrier_wait(smem_address(&s.done), 0, &s.stalled));
     tensor_fence_after();
     if (ok) {
-        for (unsigned t = 0; t < a.padded; t += 16) {
+        for (unsigned t = 0; t < many; t += 16) {
             float x[16];
             tensor_load(base + (warp * 32 << 16) + t, x);
             tensor_load_wait();
@@ -675,11 +675,11 @@ __global__ void __launch_bounds__(kThinThreads) thin_kernel(const __grid_constan
     };
     const auto on_8 = [](const RowsOut& o) { return ((reinterpret_cast<uintptr_t>(o.p) | (uintptr_t)(o.so * 2) | (uintptr_t)(o.si * 2)) & 7) == 0; };
     const bool vec = on_8(a.out[0]) && on_8(a.out[1]) && on_8(a.out[2]);
-    for (unsigned i = rank * kThinThreads + threadIdx.x; i < a.tokens * (WIDE / 4); i += cs * kThinThreads) {
+    for (unsigned i = rank * kThinThreads + threadIdx.x; i < many * (WIDE / 4); i += cs * kThinThreads) {
         const unsigned t = i / (WIDE / 4), c = i % (WIDE / 4) * 4;
         if (col + c >= a.columns) continue;
         const int valid = (int)min(4u, a.columns - col - c);
-        const long long o = t / a.n_inner, n = t % a.n_inner;
+        const long long o = (first + t) / a.n_inner, n = (first + t) % a.n_inner;
         const auto at = [&](const RowsOut& out) { return o * out.so + n * out.si + col + c; };
         float x[4];
         total(t * kThinRows + c, x);
@@ -696,6 +696,13 @@ __global__ void __launch_bounds__(kThinThreads) thin_kernel(const __grid_constan
         put(a.out[0], at(a.out[0]), valid, vec && valid == 4, x);
     }
     if (cs > 1) cluster_sync();  // the others have read this CTA's sums
+}
+
+// Of thin_kernel's size but for tensor memory; never launched (thin_clusters).
+static __global__ void __launch_bounds__(kThinThreads) thin_room_kernel() {
+    extern __shared__ unsigned char raw[];
+    if (blockDim.x > kThinThreads) raw[threadIdx.x] = 0;
+    dependent_launch_prologue();
 }
 
 // ------------------------------------------------------------------ operands laid out
