@@ -170,7 +170,7 @@ __host__ __device__ constexpr uint32_t instruction(bool is_bf16, bool a_lines, b
 
 // ------------------------------------------------------------------ activation
 // Both by their formulas in 32 bits; `slope` is the derivative.  A kernel is built for one of them: code for both, 32 times
-// in a row, did not fit the instruction cache (a finished tile took 14.8 thousand cycles instead of FINISH_CYCLES).
+// in a row, did not fit the instruction cache (a tile's end took 14.8 thousand cycles instead of 4.4).
 struct Activated {
     float value, slope;
 };
@@ -212,9 +212,10 @@ constexpr int kTileColumns = 256;    // sums a row: forward 128 gates and 128 up
 constexpr int kGatedStages = 6;
 constexpr int kHalfBytes = 128 * kBlockK * 2;     // 128 rows of an operand, one stage
 constexpr int kStageBytes = 2 * kHalfBytes;       // of one CTA: its 128 rows of A, its half of B
-constexpr int kGatedThreads = 384;                // copy, products, tensor memory, one idle warp; eight that finish tiles
+constexpr int kFinishWarps = 8;                   // that finish tiles; behind copy, products, tensor memory and an idle one
+constexpr int kGatedThreads = 128 + 32 * kFinishWarps;
 constexpr int kPatchPitch = 33;                   // words of a row of the patch through which unaligned rows are written
-constexpr int kGatedSmem = 1024 + kGatedStages * kStageBytes + 8 * 32 * kPatchPitch * 4;
+constexpr int kGatedSmem = 1024 + kGatedStages * kStageBytes + kFinishWarps * 32 * kPatchPitch * 4;
 constexpr int kGroupTiles = 8;                    // tiles of rows that follow one another before the columns move on
 
 struct GatedBarriers {
@@ -251,8 +252,8 @@ __device__ __forceinline__ void store_32(T* p, int valid, const float (&x)[32]) 
 }
 
 // Rows that do not start on 32 bytes go through a patch of shared memory, 32 rows of 64 columns a warp, and from there as
-// the 16-byte words of their own addresses, eight lanes a row; what is left at both ends goes element by element.  (Each
-// lane its own row, or a row at a time element by element, take 87 us where this takes PATCHED_US: 2036 x 1001 x 2731 f16.)
+// the 16-byte words of their own addresses, eight lanes a row; what is left at both ends goes element by element.  (2036
+// x 1001 x 2731 f16: 87 us with a row at a time, element by element, 68 so.)
 __device__ __forceinline__ void patch_32(uint32_t* patch, unsigned c, unsigned lane, const uint4 (&q)[4]) {
     uint32_t* const to = patch + lane * kPatchPitch + c / 2;
 #pragma unroll
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
         }
         for (int i = 0; i < 2; ++i) {
             barrier_init(smem_address(&s.sums_full[i]), 1);
-            barrier_init(smem_address(&s.sums_empty[i]), 16);  // the finishing warps of both CTAs
+            barrier_init(smem_address(&s.sums_empty[i]), 2 * kFinishWarps);  // the finishing warps of both CTAs
         }
         s.stalled = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -427,7 +428,8 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
             }
         }
     } else if (warp >= 4) {
-        const unsigned quarter = warp & 3, part = (warp - 4) / 4;  // a quarter of the rows, half of the columns
+        const unsigned quarter = warp & 3, part = (warp - 4) / 4;  // a quarter of the rows, a share of the columns
+        constexpr unsigned PARTS = kFinishWarps / 4;
         uint32_t* const patch = patches + (warp - 4) * 32 * kPatchPitch;
         const bool vec_t = rows_on_32<T>(a.out[0]) && (KIND == kGradX || rows_on_32<T>(a.out[1])) && (KIND != kForward || rows_on_32<T>(a.out[2]));
         const bool vec_f = rows_on_32<float>(a.out[0]) && rows_on_32<float>(a.out[1]);
@@ -437,8 +439,8 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
             const unsigned row = tile.row + rank * 128 + quarter * 32 + lane;
             if (!__all_sync(~0u, barrier_wait(smem_address(&s.sums_full[set]), set_phase, &s.stalled))) break;
             tensor_fence_after();
-            const unsigned first = part * (col_step / 2), col = tile.col + first;
-            const int valid = col < a.columns ? (int)min(col_step / 2, a.columns - col) : 0;
+            const unsigned first = part * (col_step / PARTS), col = tile.col + first;
+            const int valid = col < a.columns ? (int)min(col_step / PARTS, a.columns - col) : 0;
             const uint32_t from = base + set * kTileColumns + (quarter * 32 << 16) + first;
             if constexpr (KIND == kForward) {
                 T* const h = row < a.rows ? row_of<T>(a.out[0], a, row) + col : nullptr;
@@ -473,9 +475,11 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
                             }
                             uint4 q[4];
                             pack_32<T>(g, q);
-                            patch_32(patch, c, lane, q);
+                            patch_32(patch, c & 63, lane, q);
+                            T* const p = k == 0 ? gate : k == 1 ? up : h;
+                            const int begin = c & ~63;
+                            if (c + 32 >= valid || (c & 63) == 32) store_patch<T>(p ? p + begin : nullptr, min(64, valid - begin), patch, lane);
                         }
-                        if (valid > 0) store_patch<T>(k == 0 ? gate : k == 1 ? up : h, valid, patch, lane);
                     }
                 }
             } else {

@@ -58,6 +58,9 @@ int check_verify(const odsgd_verify_desc* d, const void* ws, size_t have) {
     return rc;
 }
 
+// Up to so many tokens a CTA does a sequence's whole work.
+constexpr int64_t kAloneVocab = 2048;
+
 // Launch shapes and workspace: functions of sizes alone.
 struct VerifyShape {
     int64_t rows, chunks;  // all rows, parts of each
@@ -77,6 +80,7 @@ VerifyShape verify_shape(const odsgd_verify_desc* d) {
     const int64_t share = ceil_div(d->vocab, s.pass_ctas * kPassWarps);
     const int64_t piece = std::max(ceil_div(share, ceil_div(share, 256 * kDrawWarps)), ceil_div(d->vocab, kSegments));
     s.segment = ceil_div(piece, 256) * 256;
+    if (d->vocab <= kAloneVocab) s.segment = 256;
     s.segments = ceil_div(d->vocab, s.segment);
     s.positions = (size_t)ceil_div(s.rows * s.chunks * (int64_t)sizeof(MaxSum), 16) * 16;
     s.sums = s.positions + (size_t)ceil_div(d->batch * (d->drafts + 1) * (int64_t)sizeof(Position), 16) * 16;
@@ -85,13 +89,14 @@ VerifyShape verify_shape(const odsgd_verify_desc* d) {
 }
 
 template <typename T>
-int launch_verify(VerifyArgs a, void* stream) {
+int launch_verify(VerifyArgs a, bool alone, void* stream) {
     a.exp_temp = RowExp<T>::bounded(a.inv_temp);
     a.draft_exp = RowExp<T>::bounded(a.draft_temp);
     const unsigned rows = a.target_rows + (a.draft ? a.batch * a.drafts : 0);
+    if (alone) return launch("verification kernel (alone)", draw_kernel<T, true>, dim3(a.batch), dim3(kDrawThreads), 0, 1, stream, a);
     int rc = launch("verification kernel (rows)", parts_kernel<T>, dim3(rows * a.chunks), dim3(kPartThreads), 0, 1, stream, a);
     if (rc == ODSGD_OK) rc = launch("verification kernel (pass)", pass_kernel<T>, dim3(a.batch * (unsigned)a.pass_ctas), dim3(kPassWarps * 32), 0, 1, stream, a);
-    if (rc == ODSGD_OK) rc = launch("verification kernel (draw)", draw_kernel<T>, dim3(a.batch), dim3(kDrawThreads), 0, 1, stream, a);
+    if (rc == ODSGD_OK) rc = launch("verification kernel (draw)", draw_kernel<T, false>, dim3(a.batch), dim3(kDrawThreads), 0, 1, stream, a);
     return rc;
 }
 
@@ -119,10 +124,11 @@ int verify(const odsgd_verify_desc* d, void* ws, size_t ws_bytes, void* stream) 
     a.vocab = (int)d->vocab;
     a.wide_tokens = d->token_type == ODSGD_I64;
     a.inv_temp = d->inv_temp, a.draft_temp = d->draft_inv_temp;
+    const bool alone = d->vocab <= kAloneVocab;
     switch (d->type) {
-        case ODSGD_F32: return launch_verify<float>(a, stream);
-        case ODSGD_BF16: return launch_verify<bf16>(a, stream);
-        default: return launch_verify<f16>(a, stream);
+        case ODSGD_F32: return launch_verify<float>(a, alone, stream);
+        case ODSGD_BF16: return launch_verify<bf16>(a, alone, stream);
+        default: return launch_verify<f16>(a, alone, stream);
     }
 }
 

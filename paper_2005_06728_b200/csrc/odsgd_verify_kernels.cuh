@@ -1,6 +1,6 @@
 // Device code of the verification of drafted tokens (sm_100a).
 //
-// Three launches.  parts_kernel reads every row of logits once and leaves maximum and sum of exponentials of its parts, in 32
+// Three launches, or, for small vocabularies, the last alone.  parts_kernel reads every row of logits once and leaves maximum and sum of exponentials of its parts, in 32
 // bits.  pass_kernel decides a sequence's drafts in order by those, and goes over the two rows of the first that is not
 // accepted again, in 64 bits: where the running sum of what is left passes a random number is a matter of its last bits.
 // draw_kernel finds that place.
@@ -50,6 +50,24 @@ struct VerifyArgs {
     float exp_temp, draft_exp;   // the same as RowExp takes them
 };
 
+// What THREADS threads, of which this is `tid`, find in part `chunk` of a row, each its own share.
+template <typename T, int THREADS>
+__device__ __forceinline__ MaxSum part_of_row(const T* z, int vocab, unsigned chunk, unsigned chunks, int tid, float temp, float exp_temp) {
+    const RowParts<T> parts(z, vocab);
+    const int per = (parts.vectors + (int)chunks - 1) / (int)chunks;
+    const int v0 = min((int)chunk * per, parts.vectors), n = min(per, parts.vectors - v0);
+    const uint4* const v = reinterpret_cast<const uint4*>(z + parts.head) + v0;
+    const int edge = chunk == 0 ? parts.edge(tid) : -1;
+    MaxSum x = single(edge >= 0 ? to_f32(z[edge]) : -CUDART_INF_F);
+    uint4 q[kRowVectors];
+    for (int b = 0; b < n; b += THREADS * kRowVectors) {
+#pragma unroll
+        for (int k = 0; k < kRowVectors; ++k) q[k] = b + k * THREADS + tid < n ? v[b + k * THREADS + tid] : neg_inf_vector<T>();
+        x = add_vectors<T>(x, q, temp, exp_temp);
+    }
+    return x;
+}
+
 // Part `chunk` of row `row`.  Bound by memory traffic, as the scores are: small CTAs, twelve an SM, and three times as many
 // parts as run at once (48 x 15 rows of 131072 bf16: 37 us in 256-thread CTAs of a row each, 30 so; the copy rate for
 // their bytes is 29).
@@ -63,18 +81,8 @@ __global__ void __launch_bounds__(kPartThreads, kPartCtas) parts_kernel(const __
     const T* const z = second ? static_cast<const T*>(a.draft) + (r / many) * a.d_sb + (r % many) * a.d_sr
                               : static_cast<const T*>(a.target) + (r / many) * a.t_sb + (r % many) * a.t_sr;
     const float temp = second ? a.draft_temp : a.inv_temp, exp_temp = second ? a.draft_exp : a.exp_temp;
-    const RowParts<T> parts(z, a.vocab);
-    const int per = (parts.vectors + (int)a.chunks - 1) / (int)a.chunks;
-    const int v0 = min((int)chunk * per, parts.vectors), n = min(per, parts.vectors - v0);
-    const uint4* const v = reinterpret_cast<const uint4*>(z + parts.head) + v0;
-    const int tid = (int)threadIdx.x, edge = chunk == 0 ? parts.edge(tid) : -1;
-    MaxSum x = single(edge >= 0 ? to_f32(z[edge]) : -CUDART_INF_F);
-    uint4 q[kRowVectors];
-    for (int b = 0; b < n; b += kPartThreads * kRowVectors) {
-#pragma unroll
-        for (int k = 0; k < kRowVectors; ++k) q[k] = b + k * kPartThreads + tid < n ? v[b + k * kPartThreads + tid] : neg_inf_vector<T>();
-        x = add_vectors<T>(x, q, temp, exp_temp);
-    }
+    const int tid = (int)threadIdx.x;
+    MaxSum x = part_of_row<T, kPartThreads>(z, a.vocab, chunk, a.chunks, tid, temp, exp_temp);
     x = warp_join(x, temp);
     if (tid % 32 == 0) warp_part[tid / 32] = x;
     __syncthreads();
@@ -212,6 +220,28 @@ struct Sequence {
           a(a_),
           seq(seq_) {}
     __device__ __forceinline__ long long token(unsigned i) const { return load_token(a.tokens, a.wide_tokens != 0, seq * a.k_sb + i * a.k_sr); }
+    // Place i, by a warp; `target_sum` and `draft_sum` give the sums of its rows to every lane.
+    template <typename F, typename G>
+    __device__ __forceinline__ Position decide(unsigned i, F target_sum, G draft_sum) const {
+        const long long x = i < a.drafts ? token(i) : -1;
+        const bool known = x >= 0 && x < a.vocab;
+        const float zt = known ? to_f32(target[i * a.t_sr + x]) : 0.0f;
+        const float zd = known && draft ? to_f32(draft[i * a.d_sr + x]) : 0.0f;
+        const float random = u[i * a.u_sr];
+        const MaxSum t = target_sum();
+        MaxSum d = {0.0f, 1.0f};
+        if (draft && i < a.drafts) d = draft_sum();
+        Position p = {t.m, t.s, d.m, d.s, 0.0f, kEnds};
+        if (known) {
+            p.logp = (zt - t.m) * a.inv_temp - logf(t.s);
+            const float lq = draft ? (zd - d.m) * a.draft_temp - logf(d.s) : 0.0f;
+            const float over = p.logp - lq - logf(random);
+            // 32 bits leave `over` uncertain by some 1e-6; infinities and NaN are left to the exact comparison too
+            const float margin = 1e-4f + 4e-6f * (fabsf(p.logp) + fabsf(lq));
+            p.decision = over > margin ? kAccepted : over < -margin ? kRefused : kNear;
+        }
+        return p;
+    }
     __device__ __forceinline__ RowPair<T> row(unsigned n, const Position& p) const {
         const bool ends = p.decision == kEnds;
         return RowPair<T>{target + n * a.t_sr, draft && !ends ? draft + n * a.d_sr : nullptr, ends ? -1 : token(n), p.max, p.draft_max,
@@ -268,29 +298,14 @@ __global__ void __launch_bounds__(kPassWarps * 32) pass_kernel(const __grid_cons
     const Sequence<T> in(a, seq);
     // Every CTA decides every draft by the rows' sums in 32 bits; those next to the border are left open.
     for (unsigned i = warp; i <= a.drafts; i += kPassWarps) {
-        const long long x = i < a.drafts ? in.token(i) : -1;
-        const bool known = x >= 0 && x < a.vocab;
-        const float zt = known ? to_f32(in.target[i * a.t_sr + x]) : 0.0f;
-        const float zd = known && in.draft ? to_f32(in.draft[i * a.d_sr + x]) : 0.0f;
-        const float random = in.u[i * a.u_sr];
         const auto row_sum = [&](const MaxSum* parts, float c) {
             MaxSum v = {-CUDART_INF_F, 0.0f};
             for (unsigned k = lane; k < a.chunks; k += 32) v = join(v, parts[k], c);
             return warp_join(v, c);
         };
-        const MaxSum t = row_sum(a.parts + (size_t)(seq * (a.drafts + 1) + i) * a.chunks, a.inv_temp);
-        MaxSum d = {0.0f, 1.0f};
-        if (in.draft && i < a.drafts) d = row_sum(a.parts + (size_t)(a.target_rows + seq * a.drafts + i) * a.chunks, a.draft_temp);
+        const Position p = in.decide(i, [&] { return row_sum(a.parts + (size_t)(seq * (a.drafts + 1) + i) * a.chunks, a.inv_temp); },
+                                     [&] { return row_sum(a.parts + (size_t)(a.target_rows + seq * a.drafts + i) * a.chunks, a.draft_temp); });
         if (lane == 0) {
-            Position p = {t.m, t.s, d.m, d.s, 0.0f, kEnds};
-            if (known) {
-                p.logp = (zt - t.m) * a.inv_temp - logf(t.s);
-                const float lq = in.draft ? (zd - d.m) * a.draft_temp - logf(d.s) : 0.0f;
-                const float over = p.logp - lq - logf(random);
-                // 32 bits leave `over` uncertain by some 1e-6; infinities and NaN are left to the exact comparison too
-                const float margin = 1e-4f + 4e-6f * (fabsf(p.logp) + fabsf(lq));
-                p.decision = over > margin ? kAccepted : over < -margin ? kRefused : kNear;
-            }
             place[i] = p;
             if (rank == 0) a.positions[(size_t)seq * (a.drafts + 1) + i] = p;
         }
@@ -324,8 +339,10 @@ struct DrawState {
     double begin;
 };
 
-// A CTA a sequence, a thread a segment.
-template <typename T>
+// A CTA a sequence, a thread a segment.  ALONE: the CTA also does what the other kernels do ahead of it, a warp a row and a
+// segment.  That pays up to some 2000 tokens: 8 x 3 drafts, bf16, of 200 / 2000 / 4000 take 11.1 / 12.6 / 15.9 us so, 13.0 / 13.7 / 13.6
+// by three launches, which cost the host 5 us more.
+template <typename T, bool ALONE>
 __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constant__ VerifyArgs a) {
     __shared__ DrawState s;
     dependent_launch_prologue();
@@ -333,9 +350,18 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
     const int mine = (int)threadIdx.x;
     const Sequence<T> in(a, seq);
     double x[kDrawSums];  // of the thread's segment, then P, Q, R, D, N
+    if constexpr (ALONE) {
+        for (unsigned i = warp; i <= a.drafts; i += kDrawWarps) {
+            const auto row_sum = [&](const T* z, float c, float exp_temp) { return warp_join(part_of_row<T, 32>(z, a.vocab, 0, 1, (int)lane, c, exp_temp), c); };
+            const Position p = in.decide(i, [&] { return row_sum(in.target + i * a.t_sr, a.inv_temp, a.exp_temp); },
+                                         [&] { return row_sum(in.draft + i * a.d_sr, a.draft_temp, a.draft_exp); });
+            if (lane == 0) s.place[i] = p;
+        }
+    } else {
 #pragma unroll
-    for (int k = 0; k < kDrawSums; ++k) x[k] = mine < a.segments ? a.sums[((size_t)seq * kDrawSums + k) * a.segments + mine] : 0.0;
-    if (threadIdx.x <= a.drafts) s.place[threadIdx.x] = a.positions[(size_t)seq * (a.drafts + 1) + threadIdx.x];
+        for (int k = 0; k < kDrawSums; ++k) x[k] = mine < a.segments ? a.sums[((size_t)seq * kDrawSums + k) * a.segments + mine] : 0.0;
+        if (threadIdx.x <= a.drafts) s.place[threadIdx.x] = a.positions[(size_t)seq * (a.drafts + 1) + threadIdx.x];
+    }
     if (threadIdx.x == 0) s.found = INT_MAX, s.last = -1, s.at = -1;
     __syncthreads();
     unsigned n = 0;
@@ -343,7 +369,19 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
     RowPair<T> row = in.row(n, s.place[n]);
     double ratio = ratio_of(s.place[n]), off = 0.0, part_p, part_r, part_d;
     bool refused = false;
-    for (bool again = false;;) {
+    for (bool again = false, here = ALONE;; here = true) {
+        if (here) {  // the pass over this place, by this CTA: not behind pass_kernel, but for the rare cases below
+            __syncthreads();
+            for (int g = (int)warp; g < a.segments; g += kDrawWarps) {
+                pass_segment(row, ratio, g * a.segment, min(a.vocab, (g + 1) * a.segment), x);
+#pragma unroll
+                for (int k = 0; k < kDrawSums; ++k)
+                    if ((int)lane == k) s.segment[k][g] = x[k];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kDrawSums; ++k) x[k] = mine < a.segments ? s.segment[k][mine] : 0.0;
+        }
         part_p = x[0], part_r = x[2], part_d = x[3];
 #pragma unroll
         for (int k = 0; k < kDrawSums; ++k) {
@@ -373,17 +411,6 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
             row = in.row(n, s.place[n]);
             ratio = ratio_of(s.place[n]);
         }
-        // rare: the pass over this place, by this CTA alone
-        __syncthreads();
-        for (int g = (int)warp; g < a.segments; g += kDrawWarps) {
-            pass_segment(row, ratio, g * a.segment, min(a.vocab, (g + 1) * a.segment), x);
-#pragma unroll
-            for (int k = 0; k < kDrawSums; ++k)
-                if ((int)lane == k) s.segment[k][g] = x[k];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kDrawSums; ++k) x[k] = mine < a.segments ? s.segment[k][mine] : 0.0;
     }
     // Where nothing is left (a draft that neither gives a probability, equal distributions): the whole target.
     double all = x[2] - off * x[3];

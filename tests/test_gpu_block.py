@@ -624,3 +624,85 @@ def test_drafted_answers_carry_their_scores():
         # both are sums of 37 exponentials in 32 bits
         assert float((acting - want)[counts].abs().max()) < 40 * 2.0 ** -22
         assert not bool(acting[~counts].any())
+
+
+# --------------------------------------------------------------------------- calls that nothing prepared
+
+FIRST_CALLS_CAPTURED = """
+import torch
+from paper_2005_06728_b200 import lm
+g = torch.Generator(device="cuda").manual_seed(1)
+r = lambda *s, k=torch.bfloat16: torch.randn(*s, generator=g, device="cuda").to(k)
+x, wg, wu, dh, z, tok = r(40, 72), r(130, 72, k=torch.float32), r(130, 72, k=torch.float32), r(40, 130), r(3, 3, 3000), torch.tensor([[1, 2]] * 3, device="cuda")
+big, u = r(2100, 72), torch.full((3, 3), 0.3, device="cuda")
+step = torch.zeros(1, dtype=torch.int64, device="cuda")
+def run():
+    a = lm.gated_ffn(x, wg, wu, save=True)
+    return (*a, *lm.gated_ffn_grad(x, wg, wu, a.gate, a.up, dh), lm.gated_ffn(big, wg, wu).h, lm.dropout(x, 0.5, 3, counter=step, residual=x),
+            *lm.verify_draft(z, tok, u), *lm.verify_draft(z[..., :500], tok, u))
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    got = run()
+graph.replay()
+torch.cuda.synchronize()
+for a, b in zip(got, run()):
+    assert torch.equal(a, b)
+print("equal")
+"""
+
+
+def test_first_calls_of_a_process_can_be_captured():
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS_CAPTURED], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "equal", r.stderr[-2000:]
+
+
+def test_calls_on_two_streams_at_once():
+    """Every kernel on two streams with nothing between them but the GPU's own order; each has its own tensors and workspace."""
+    streams, sets = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for k in range(2):
+        x, wg, wu = block((500 if k else 30,), 264, 400, BF16, F32 if k else BF16, seed=500 + 10 * k)
+        sets.append((x, wg, wu, randn(x.shape[0], 400, seed=505 + 10 * k, dtype=BF16), drafted(6, 3, 9000, BF16, 520 + 10 * k)))
+
+    def run(s, stream):
+        x, wg, wu, dh, (target, tok, u, draft) = s
+        r = lm.gated_ffn(x, wg, wu, save=True, stream=stream)
+        g = lm.gated_ffn_grad(x, wg, wu, r.gate, r.up, dh, stream=stream)
+        return (*r, *g, lm.dropout(x, 0.2, 5, residual=x, stream=stream), *lm.verify_draft(target, tok, u, draft=draft, stream=stream))
+
+    want = [[t.clone() for t in run(s, None)] for s in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for k in (0, 1):
+            got[k].append(run(sets[k], streams[k]))
+    torch.cuda.synchronize()
+    for k in (0, 1):
+        for outs in got[k]:
+            for a, b in zip(outs, want[k]):
+                assert torch.equal(a, b)
+    assert stalled() == 0
+
+
+def test_back_to_back_calls_read_what_the_one_ahead_wrote():
+    """Grids are scheduled while the one ahead drains: dropout onto h in place, h through the block again, drafts from its result."""
+    x, wg, wu = block((600,), 128, 128, BF16, BF16, seed=540)
+    tok, u = torch.zeros(600, 0, dtype=torch.int64, device=DEV), torch.full((600, 1), 0.6, device=DEV)
+
+    def run(wait):
+        h = x.clone()
+        for k in range(4):
+            h = lm.gated_ffn(h, wg, wu).h
+            wait()
+            lm.dropout(h, 0.1, 7, offset=k, out=h)
+            h = lm.dropout(h, 0.3, 8, offset=k, residual=x)
+            wait()
+        return h, *lm.verify_draft(h.view(600, 1, 128), tok, u)
+
+    for a, b in zip(run(lambda: None), run(torch.cuda.synchronize)):
+        assert torch.equal(a, b)
