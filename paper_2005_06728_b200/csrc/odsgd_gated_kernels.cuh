@@ -169,21 +169,39 @@ __host__ __device__ constexpr uint32_t instruction(bool is_bf16, bool a_lines, b
 }
 
 // ------------------------------------------------------------------ activation
-// Both by their formulas in 32 bits; `slope` is the derivative.  A kernel is built for one of them: code for both, 32 times
-// in a row, did not fit the instruction cache (a tile's end took 14.8 thousand cycles instead of 4.4).
+// Both in 32 bits; `slope` is the derivative.  A kernel is built for one of them: code for both, 32 times in a row, did not fit
+// the instruction cache (a tile's end took 14.8 thousand cycles instead of 4.4).
 struct Activated {
     float value, slope;
 };
+// The normal distribution function by Abramowitz and Stegun 7.1.26, 2^-23 off at most: for t < 0
+//     cdf(t) = exp(-t^2 / 2) (a1 k + ... + a5 k^5) / 2,  k = 1 / (1 + p |t| / sqrt 2)
+// and 1 - cdf(-t) above; `bell` is exp(-t^2 / 2), which the slope needs too.  (A third of the instructions of 1 + erf, and
+// nothing cancels below 0.)
+__device__ __forceinline__ float normal_cdf(float t, float& bell) {
+    bell = __expf(-0.5f * t * t);
+    const float k = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(t), 1.0f));
+    float r = fmaf(k, 1.061405429f, -1.453152027f);
+    r = fmaf(k, r, 1.421413741f);
+    r = fmaf(k, r, -0.284496736f);
+    r = fmaf(k, r, 0.254829592f);
+    const float tail = 0.5f * k * r * bell;
+    return t < 0.0f ? tail : 1.0f - tail;
+}
 template <bool GELU>
 __device__ __forceinline__ float activate(float t) {
-    if constexpr (GELU) return 0.5f * t * (1.0f + erff(t * 0.70710678f));
+    if constexpr (GELU) {
+        float bell;
+        return t * normal_cdf(t, bell);
+    }
     return __fdividef(t, 1.0f + __expf(-t));
 }
 template <bool GELU>
 __device__ __forceinline__ Activated activate_with_slope(float t) {
     if constexpr (GELU) {
-        const float cdf = 0.5f * (1.0f + erff(t * 0.70710678f));
-        return {t * cdf, cdf + t * 0.39894228f * __expf(-0.5f * t * t)};
+        float bell;
+        const float cdf = normal_cdf(t, bell);
+        return {t * cdf, cdf + t * 0.39894228f * bell};
     }
     const float s = __fdividef(1.0f, 1.0f + __expf(-t));
     return {t * s, s * (1.0f + t * (1.0f - s))};
@@ -264,7 +282,7 @@ __device__ __forceinline__ void store_patch(T* p, int valid, const uint32_t* pat
     static_assert(sizeof(T) == 2, "two elements a word");
     const int l = (int)(lane & 7);
     __syncwarp();
-#pragma unroll 2
+#pragma unroll 4
     for (unsigned r = lane >> 3; r < 32; r += 4) {
         T* const to = reinterpret_cast<T*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(p), r));
         const uint32_t* const row = patch + r * kPatchPitch;
@@ -273,13 +291,20 @@ __device__ __forceinline__ void store_patch(T* p, int valid, const uint32_t* pat
             const int head = min(valid, (int)((16 - (reinterpret_cast<uintptr_t>(to) & 15)) & 15) / 2), at = head + 8 * l;
             if (at + 8 <= valid) {
                 const uint32_t* const w = row + at / 2;
-                uint4 q = make_uint4(w[0], w[1], w[2], w[3]);
-                if (at & 1) q = make_uint4(__funnelshift_r(q.x, q.y, 16), __funnelshift_r(q.y, q.z, 16), __funnelshift_r(q.z, q.w, 16), __funnelshift_r(q.w, w[4], 16));
-                *reinterpret_cast<uint4*>(to + at) = q;
+                const unsigned shift = at & 1 ? 16 : 0;
+                const uint32_t x[5] = {w[0], w[1], w[2], w[3], w[4]};  // (the last is not used where `shift` is 0; the row has a spare word)
+                *reinterpret_cast<uint4*>(to + at) = make_uint4(__funnelshift_r(x[0], x[1], shift), __funnelshift_r(x[1], x[2], shift),
+                                                                __funnelshift_r(x[2], x[3], shift), __funnelshift_r(x[3], x[4], shift));
             }
-            const int tail = head + (valid - head) / 8 * 8 + l;
-            if (l < head) reinterpret_cast<unsigned short*>(to)[l] = half[l];
-            if (tail < valid) reinterpret_cast<unsigned short*>(to)[tail] = half[tail];
+            // fewer than eight elements at each end; of whole eights, eight in all (or none)
+            const int tail = valid % 8 == 0 ? valid - 8 + l : head + (valid - head) / 8 * 8 + l;
+            if (valid % 8 == 0) {
+                const int e = l < head ? l : tail;
+                if (head != 0) reinterpret_cast<unsigned short*>(to)[e] = half[e];
+            } else {
+                if (l < head) reinterpret_cast<unsigned short*>(to)[l] = half[l];
+                if (tail < valid) reinterpret_cast<unsigned short*>(to)[tail] = half[tail];
+            }
         }
     }
     __syncwarp();
