@@ -38,6 +38,8 @@ _FLOATS = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _FLOAT32 = {torch.float32: F32}
 _INTS = {torch.int32: I32, torch.int64: I64}
 _HALVES = {torch.bfloat16: BF16, torch.float16: F16}
+_SAME = {t: {t: c} for t, c in _FLOATS.items()}                             # a tensor of the same type
+_OR_FLOAT32 = {t: {t: c, torch.float32: F32} for t, c in _HALVES.items()}  # or of 32 bits
 _ACTIVATIONS = {"silu": 0, "gelu": 1}
 
 # odsgd_embed_desc, odsgd_policy_desc and odsgd_grad_tensor of include/odsgd.h, packed by struct: a call is
@@ -145,6 +147,14 @@ def _rows(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int]:
     if t.stride(-1) != 1 and t.shape[-1] != 1:
         raise ValueError(f"{name}: the last axis must be contiguous")
     return _levels(t, lead, name)
+
+
+def _dense(shape) -> Tuple[int, int]:
+    """Strides of the rows of new memory of this shape."""
+    n = len(shape)
+    if n < 2:
+        return 0, 0
+    return (0 if n == 2 else shape[-2] * shape[-1]), shape[-1]
 
 
 def _new(like: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
@@ -312,13 +322,12 @@ def policy_loss(logits: torch.Tensor, labels: torch.Tensor, old_logp: torch.Tens
 
 def _gated_inputs(x, w_gate, w_up, activation, dev):
     kind = _need(x, "x", _HALVES, dev)
-    codes = {x.dtype: kind, torch.float32: F32}
-    weight_type = _need(w_gate, "w_gate", codes, dev)
-    _need(w_up, "w_up", {w_gate.dtype: weight_type}, dev)
+    weight_type = _need(w_gate, "w_gate", _OR_FLOAT32[x.dtype], dev)
+    _need(w_up, "w_up", _SAME[w_gate.dtype], dev)
     if x.dim() < 1:
         raise ValueError("x: need [..., dim]")
     width, dim, gate_stride = _table(w_gate, "w_gate")
-    _shape(w_up, (width, dim), "w_up")
+    _shape(w_up, w_gate.shape, "w_up")
     up_stride = _table(w_up, "w_up")[2]
     if x.shape[-1] != dim:
         raise ValueError(f"x: last axis {x.shape[-1]}, expected {dim}")
@@ -352,21 +361,23 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, *, acti
     if not given:
         out = _new(x, shape, x.dtype, stream)
     else:
-        _need(out, "out", {x.dtype: kind}, dev)
+        _need(out, "out", _SAME[x.dtype], dev)
         _shape(out, shape, "out")
     gate = up = None
-    kept, at, up_at = (0, 0), 0, 0
+    dense, at, up_at = _dense(shape), 0, 0
     if save:
         gate, up = _new(x, shape, x.dtype, stream), _new(x, shape, x.dtype, stream)
-        kept, at, up_at = _levels(gate, lead, "gate"), gate.data_ptr(), up.data_ptr()
+        at, up_at = gate.data_ptr(), up.data_ptr()
     d = _GATED.pack(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), out.data_ptr(), at, up_at, 0, 0, 0, kind, weight_type, kind,
-                    _ACTIVATIONS[activation], 0, *_sizes(x.shape[:-1]), dim, width, *_rows(x, lead, "x"), *_rows(out, lead, "out"),
-                    *kept, *kept, 0, 0, gate_stride, up_stride, 0, 0)
-    lib = binding.load_library()
-    need = ctypes.c_size_t()
-    _check(lib.odsgd_gated_workspace(d, 0, ctypes.byref(need)))
-    workspace, ws_at, ws_bytes = _workspace(need.value, workspace, x, dev, stream)
-    _check(lib.odsgd_gated_forward(d, ws_at, ws_bytes, _handle(stream, dev)))
+                    _ACTIVATIONS[activation], 0, *_sizes(shape[:-1]), dim, width, *_rows(x, lead, "x"),
+                    *(_rows(out, lead, "out") if given else dense), *dense, *dense, 0, 0, gate_stride, up_stride, 0, 0)
+    lib, handle = binding.load_library(), _handle(stream, dev)
+    # most calls need no workspace and are done here; one that does has been refused, with nothing written
+    if workspace is not None or lib.odsgd_gated_forward(d, 0, 0, handle) != OK:
+        need = ctypes.c_size_t()
+        _check(lib.odsgd_gated_workspace(d, 0, ctypes.byref(need)))
+        workspace, ws_at, ws_bytes = _workspace(need.value, workspace, x, dev, stream)
+        _check(lib.odsgd_gated_forward(d, ws_at, ws_bytes, handle))
     if given:
         increment_version(out)
     return GatedFfn(out, gate, up)
@@ -382,9 +393,11 @@ def gated_ffn_grad(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, ga
     kind, weight_type, width, dim, gate_stride, up_stride = _gated_inputs(x, w_gate, w_up, activation, dev)
     lead = x.dim() - 1
     shape = (*x.shape[:-1], width)
+    same = _SAME[x.dtype]
     for t, name in ((gate, "gate"), (up, "up"), (dh, "dh")):
-        _need(t, name, {x.dtype: kind}, dev)
-        _shape(t, shape, name)
+        _need(t, name, same, dev)
+        if t.shape != shape:
+            _shape(t, shape, name)
     want_dx, want_dw = want_dx or dx is not None, want_dw or dw_gate is not None or dw_up is not None
     if (dw_gate is None) != (dw_up is None):
         raise ValueError("dw_gate and dw_up go together")
@@ -394,20 +407,24 @@ def gated_ffn_grad(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, ga
     dx_strides, dx_at = (0, 0), 0
     if want_dx:
         if dx is None:
-            dx = _new(x, tuple(x.shape), x.dtype, stream)
+            dx = _new(x, x.shape, x.dtype, stream)
+            dx_strides = _dense(x.shape)
         else:
-            _need(dx, "dx", {x.dtype: kind}, dev)
+            _need(dx, "dx", same, dev)
             _shape(dx, x.shape, "dx")
-        dx_strides, dx_at = _rows(dx, lead, "dx"), dx.data_ptr()
+            dx_strides = _rows(dx, lead, "dx")
+        dx_at = dx.data_ptr()
     dw_type, dg_stride, du_stride, dg_at, du_at = kind, 0, 0, 0, 0
     if want_dw:
         if dw_gate is None:
             dw_gate, dw_up = _new(x, (width, dim), x.dtype, stream), _new(x, (width, dim), x.dtype, stream)
-        dw_type = _need(dw_gate, "dw_gate", {x.dtype: kind, torch.float32: F32}, dev)
-        _need(dw_up, "dw_up", {dw_gate.dtype: dw_type}, dev)
-        _shape(dw_gate, (width, dim), "dw_gate")
-        _shape(dw_up, (width, dim), "dw_up")
-        dg_stride, du_stride = _table(dw_gate, "dw_gate")[2], _table(dw_up, "dw_up")[2]
+            dg_stride = du_stride = dim
+        else:
+            dw_type = _need(dw_gate, "dw_gate", _OR_FLOAT32[x.dtype], dev)
+            _need(dw_up, "dw_up", _SAME[dw_gate.dtype], dev)
+            _shape(dw_gate, (width, dim), "dw_gate")
+            _shape(dw_up, (width, dim), "dw_up")
+            dg_stride, du_stride = _table(dw_gate, "dw_gate")[2], _table(dw_up, "dw_up")[2]
         dg_at, du_at = dw_gate.data_ptr(), dw_up.data_ptr()
     d = _GATED.pack(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), dh.data_ptr(), gate.data_ptr(), up.data_ptr(), dx_at, dg_at, du_at,
                     kind, weight_type, dw_type, _ACTIVATIONS[activation], 1 if accumulate else 0, *_sizes(x.shape[:-1]), dim, width,
