@@ -761,7 +761,7 @@ typedef struct odsgd_verify_desc {
     int64_t draft_stride_batch, draft_stride_row;
     int64_t token_stride_batch, token_stride_row;
     int64_t uniform_stride_batch, uniform_stride_row;
-    float inv_temp, draft_inv_temp; /* > 0 */
+    float inv_temp, draft_inv_temp; /* 1e-30 .. 1e30 */
 } odsgd_verify_desc;
 
 int odsgd_verify_workspace(const odsgd_verify_desc* desc, size_t* bytes);

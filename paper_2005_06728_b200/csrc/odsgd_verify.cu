@@ -23,8 +23,8 @@ int check_verify(const odsgd_verify_desc* d, const void* ws, size_t have) {
     if (d->vocab < 1) return fail(ODSGD_ERR_ARG, "vocab must be at least 1");
     if (d->drafts > ODSGD_MAX_DRAFTS || d->batch > 1 << 16 || d->vocab > 1 << 30)
         return fail(ODSGD_ERR_UNSUPPORTED, "batch, drafts or vocab beyond the limits");
-    if (!(d->inv_temp > 0.0f) || !(d->draft_inv_temp > 0.0f) || std::isinf(d->inv_temp) || std::isinf(d->draft_inv_temp))
-        return fail(ODSGD_ERR_ARG, "inv_temp and draft_inv_temp must be positive and finite");
+    if (!(d->inv_temp >= 1e-30f && d->inv_temp <= 1e30f && d->draft_inv_temp >= 1e-30f && d->draft_inv_temp <= 1e30f))
+        return fail(ODSGD_ERR_ARG, "inv_temp and draft_inv_temp must be in [1e-30, 1e30]");
     const int es = size_of(d->type), ts = size_of(d->token_type);
     const int64_t many = d->drafts + 1;
     const Buf rows[6] = {{"target", d->target, es, d->target_stride_batch, d->target_stride_row, d->vocab, false},

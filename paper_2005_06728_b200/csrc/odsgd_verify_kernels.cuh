@@ -20,6 +20,7 @@ constexpr int kDrawThreads = 512;  // of draw_kernel
 constexpr int kDrawWarps = kDrawThreads / 32;
 constexpr int kSegments = kDrawThreads;  // most parts of the vocabulary, each summed by a warp
 constexpr int kDrawSums = 5;
+constexpr double kNothing = 0x1p-900;  // relative to a row's largest element: sums up to this hold masked elements alone
 
 enum Decision { kRefused, kAccepted, kNear, kEnds };
 
@@ -101,7 +102,8 @@ __device__ __forceinline__ double warp_sum(double x) {
 
 // 2^(d c) in 64 bits, within 4e-14: the nearest whole number goes into the exponent, the rest f, at most a half, through 1 + f r(f),
 // r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0, 0 below 2^-1000 and
-// at -inf; for d c <= 1 or NaN.
+// at -inf; for d c <= 1 or NaN.  OPEN: for -1000 <= d c, or NaN, alone.
+template <bool OPEN = false>
 __device__ __forceinline__ double power_of_two(double d, double c) {
     const double w = fma(d, c, 6755399441055744.0);  // 1.5 * 2^52: the lower half is the whole number
     const double f = fma(d, c, 6755399441055744.0 - w);
@@ -115,6 +117,7 @@ __device__ __forceinline__ double power_of_two(double d, double c) {
     r = fma(r, f, 0.2402265069581299);
     r = fma(r, f, 0.6931471805599453);
     r = fma(r, f, 1.0);
+    if constexpr (OPEN) return __hiloint2double(__double2hiint(r) + (__double2loint(w) << 20), __double2loint(r));
     // (a number below -2^31 leaves another upper half)
     const bool none = __double2hiint(w) < 0x4337ffff || __double2loint(w) < -1000;
     return __hiloint2double(none ? 0 : __double2hiint(r) + (__double2loint(w) << 20), none ? 0 : __double2loint(r));
@@ -180,6 +183,22 @@ struct RowPair {
     __device__ __forceinline__ void draft(const float (&z)[8], double (&e)[8]) const {
 #pragma unroll
         for (int i = 0; i < 8; ++i) e[i] = power_of_two((double)z[i] - mq, cq);
+    }
+    // The same for sums, which kNothing does not change: what is lower (a mask) counts as 2^-980, one instruction instead of five.
+    __device__ __forceinline__ static float no_lower(float z, float low) {
+        float x;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(z), "f"(low));
+        return x;
+    }
+    __device__ __forceinline__ void target_sums(const float (&z)[8], double (&e)[8]) const {
+        const float low = (float)(mp - 980.0 / cp);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = power_of_two<true>((double)no_lower(z[i], low) - mp, cp);
+    }
+    __device__ __forceinline__ void draft_sums(const float (&z)[8], double (&e)[8]) const {
+        const float low = (float)(mq - 980.0 / cq);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = power_of_two<true>((double)no_lower(z[i], low) - mq, cq);
     }
     // f(j, logits of the target, of the draft) for each eight from `from` on, a warp's width apart; the next are loaded ahead.
     template <typename F>
@@ -263,19 +282,28 @@ __device__ __forceinline__ void pass_segment(const RowPair<T>& row, double ratio
     for (int k = 0; k < kDrawSums; ++k) x[k] = 0.0;
     row.each(lo + 8 * (int)(threadIdx.x & 31), hi, [&](int j, const float (&z)[8], const float (&y)[8]) {
         double e[8];
-        row.target(z, e);
+        row.target_sums(z, e);
         x[0] += sum_of(e);
         if (row.q) {
-            double f[8];
-            row.draft(y, f);
+            double f[8], r[8];
+            row.draft_sums(y, f);
             x[1] += sum_of(f);
+            int near = 0;  // the least of the exponents of |p - k q| less those of p
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double r = fma(-ratio, f[i], e[i]);
-                const int high = __double2hiint(r), whole = __double2hiint(e[i]);
-                if ((high & 0x7fffffff) < whole - (18 << 20)) x[4] += e[i];
-                e[i] = high < 0 && r == r ? 0.0 : r;  // (NaN stays)
-                f[i] = high < 0 ? 0.0 : f[i];
+                r[i] = fma(-ratio, f[i], e[i]);
+                near = min(near, (__double2hiint(r[i]) & 0x7fffffff) - __double2hiint(e[i]));
+            }
+            if (near < -(18 << 20)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if ((__double2hiint(r[i]) & 0x7fffffff) < __double2hiint(e[i]) - (18 << 20)) x[4] += e[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {  // (NaN comes out of P and Q)
+                const bool less = __double2hiint(r[i]) < 0;
+                e[i] = less ? 0.0 : r[i];
+                f[i] = less ? 0.0 : f[i];
             }
             x[2] += sum_of(e);
             x[3] += sum_of(f);
@@ -414,10 +442,10 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
     }
     // Where nothing is left (a draft that neither gives a probability, equal distributions): the whole target.
     double all = x[2] - off * x[3];
-    if (refused && !(all > 0.0) && all == all) refused = false;
+    if (refused && all <= kNothing) refused = false;
     if (!refused) all = x[0], row.q = nullptr, row.hot = -1;
     ratio += off;
-    const bool drawn = all > 0.0 && all < CUDART_INF;  // not where a row holds NaN, +inf or nothing but -inf
+    const bool drawn = all > kNothing && all < CUDART_INF;  // not where a row holds NaN, +inf or nothing but -inf
     const double bound = (double)in.u[a.drafts * a.u_sr] * all;
 
     // The segment in which the running sum passes the bound: the last that begins no higher, of those that have anything.
@@ -435,8 +463,8 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
     const double before = __shfl_up_sync(~0u, run, 1);
     if (lane > 0) begin += before;
     // (a bound that is NaN or below 0 takes the first that has anything)
-    const int candidate = __reduce_max_sync(~0u, part > 0.0 && begin <= bound ? mine : -1);
-    const unsigned some_part = __ballot_sync(~0u, part > 0.0);
+    const int candidate = __reduce_max_sync(~0u, part > kNothing && begin <= bound ? mine : -1);
+    const unsigned some_part = __ballot_sync(~0u, part > kNothing);
     if (lane == 0 && candidate >= 0) atomicMax(&s.at, candidate);
     if (lane == 0 && some_part != 0) atomicMin(&s.found, (int)warp * 32 + __ffs((int)some_part) - 1);
     __syncthreads();

@@ -504,6 +504,27 @@ def test_verify_masked_and_void_rows():
             assert torch.equal(a[keep], b[keep])
 
 
+def test_verify_masks_at_the_ends():
+    """Random numbers of 0 and next to 1 pass over masked tokens at both ends, whatever the mask's value and the temperature."""
+    for kind in (F32, BF16, F16):
+        for v in (40, 700, 20000):
+            for mask in (float("-inf"), torch.finfo(kind).min, -6e4):
+                z = torch.full((4, 2, v), mask, dtype=kind, device=DEV)
+                lo, hi = v // 3, 2 * v // 3
+                z[..., lo:hi] = randn(4, 2, hi - lo, seed=345, dtype=kind)
+                q = z[:, :1].clone()
+                q[..., lo] += 3  # what is left does not hold the first
+                tok = torch.full((4, 1), lo, device=DEV)
+                u = torch.tensor([[1 - 2.0 ** -24, 0.0], [1 - 2.0 ** -24, 1 - 2.0 ** -24], [0.0, 0.0], [0.0, 1 - 2.0 ** -24]], device=DEV)
+                for c in (1.0, 0.05, 30.0):
+                    r = lm.verify_draft(z, tok, u, draft=q, inv_temp=c)
+                    t = r.tokens.tolist()
+                    # (at 30 the draft's share of token lo may be below what 64 bits hold beside the rest: equal distributions then)
+                    first = lo if c == 30.0 else lo + 1
+                    assert r.accepted.tolist() == [0, 0, 1, 1] and first <= t[0][0] < hi and first <= t[1][0] < hi, (kind, v, mask, c)
+                    assert t[2][1] == lo and lo <= t[3][1] < hi and t[2][0] == t[3][0] == lo
+
+
 def test_verify_draws_as_the_target_does():
     """Drafts of another distribution, verified: what comes out first is distributed as the target (5 tokens, 200000 sequences)."""
     n, v = 65536, 5
@@ -548,7 +569,7 @@ def test_verify_streams_graphs_and_refusals():
         lm.verify_draft(target, tok, u[:, :2])
     with pytest.raises(ValueError):
         lm.verify_draft(target, tok, u, draft=draft[..., :100])
-    for t in (0.0, -1.0, float("nan"), float("inf")):
+    for t in (0.0, -1.0, float("nan"), float("inf"), 1e-31, 1e31):
         with pytest.raises(binding.OdsgdError):
             lm.verify_draft(target, tok, u, inv_temp=t)
     with pytest.raises(binding.OdsgdError):
