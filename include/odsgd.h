@@ -479,7 +479,9 @@ int odsgd_get_launch_count(odsgd_ctx* ctx, uint64_t* launches);
  * token rows out of the weight arena (odsgd_embed_lookup) and their gradient into the gradient
  * arena (odsgd_embed_grad), the score of a taken token (odsgd_token_logprob), the clipped policy
  * loss with its gradient (odsgd_policy_loss), and the norm, clipping and lay-out of a list of
- * gradient tensors into the arena the server reads (odsgd_grad_set_*).
+ * gradient tensors into the arena the server reads (odsgd_grad_set_*).  Inside the model: a gated feed-forward
+ * block and its gradient (odsgd_gated_*) and dropout (odsgd_dropout); for acting, the verification of drafted tokens
+ * (odsgd_verify_draft).
  *
  * These calls take no context.  They run on the current CUDA device, on `stream`, and allocate
  * nothing (odsgd_grad_set_create alone allocates a table); outputs and workspaces are the

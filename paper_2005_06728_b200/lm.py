@@ -1,14 +1,17 @@
-"""Language-model operators around the update: argument marshalling for the odsgd_embed_*,
-odsgd_token_logprob, odsgd_policy_loss and odsgd_grad_set_* calls of libodsgd.so.
+"""Language-model operators around the update: argument marshalling for the odsgd_embed_*, odsgd_token_logprob,
+odsgd_policy_loss, odsgd_grad_set_*, odsgd_gated_*, odsgd_dropout and odsgd_verify_* calls of libodsgd.so.
 
-What a worker runs on either side of its model when the parameter set is a language model's:
+What a worker runs on either side of its model, and in it, when the parameter set is a language model's:
 
 * `embed_lookup` / `embed_grad`: token rows out of the weight arena, and their gradient into the
   gradient arena (`arena[a:b].view(vocab, dim)` is a table);
 * `token_logprob`: the score of each taken token (acting policy, reference policy, evaluation);
 * `policy_loss`: the clipped policy loss with a KL term, and its gradient, in one pass;
 * `GradSet`: norm and clipping of a list of gradient tensors, laid out into the arenas the server
-  reads.
+  reads;
+* `gated_ffn` / `gated_ffn_grad`: the gated feed-forward block, on 16-bit activations, and its gradients;
+* `dropout`: onto a residual, by a mask that is a function of a seed; its own gradient;
+* `verify_draft`: drafted tokens accepted under the current policy, one more drawn, and their scores.
 
 include/odsgd.h has the formulas and the treatment of padding, masks and special values.  Every
 call is asynchronous on `stream` (default: the current stream), on the current device; results are
