@@ -330,9 +330,11 @@ __device__ __forceinline__ bool rows_on_32(const RowsOut& o) {
 }
 
 // A persistent pair of CTAs per two SMs goes over tiles of 256 rows x 256 sums.  In each CTA one thread copies (its own 128 rows of
-// A and its half of B: in the forward pass the first CTA's half is Wg's, the second's Wu's), four warps finish
+// A and its half of B: in the forward pass the first CTA's half is Wg's, the second's Wu's) and eight warps finish
 // tiles; one thread of the first CTA issues the products of both.  Two sets of sums, so that one tile is finished
-// while the next is computed.
+// while the next is computed.  Bound by the tensor cores where products are large: 8192 x 4096 x 11008 bf16 forward 930 us
+// in a burst, 1.59 PFLOP/s, 0.99 of the library's rate there, 1157 under the power cap (0.92); gradient of x 913, of weights 950.
+// A block of 64 of the long axis takes 320 cycles then; 530 to 600 where the long axis is 1024 and tiles are few.
 template <int KIND, typename T, bool GELU>
 __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) gated_kernel(const __grid_constant__ GatedArgs a) {
     constexpr bool A_LINES = KIND == kGradW, B_LINES = KIND != kForward;
@@ -568,7 +570,8 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t addr) {
 // Few tokens leave most of a tile of 256 of them empty, and their time is that of reading the weights.  Here weights are
 // the rows of the product and tokens its columns, as many as there are, rounded up to 16: a cluster takes 64 columns of the block (64
 // rows of Wg above 64 of Wu), or 128 columns of x's gradient, its CTAs share the long axis, and the sums meet in shared memory,
-// added in the order of the ranks.
+// added in the order of the ranks.  Bound by the read of the weights: 48 tokens x 4096 x 11000 36 us, 0.77 of the copy rate
+// (57 us by gated_kernel), one token x 2048 x 5440 9.3 us (27.5).
 constexpr int kThinThreads = 128;
 constexpr int kThinRows = 128;
 constexpr int kThinCluster = 8;

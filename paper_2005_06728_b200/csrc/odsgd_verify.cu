@@ -72,8 +72,11 @@ VerifyShape verify_shape(const odsgd_verify_desc* d) {
     VerifyShape s;
     const int64_t sms = 148;
     s.rows = d->batch * (2 * d->drafts + 1);
-    // parts of at least 4096 elements, as many as fill every SM three times
-    s.chunks = std::max<int64_t>(1, std::min(ceil_div(sms * kPartCtas * 3, std::max<int64_t>(s.rows, 1)), d->vocab / 4096));
+    // parts of at least 4096 elements, as many as fill every SM three times; each of whole steps of its CTA, so that none goes round
+    // again for a few elements (16 x 11 rows of 50021 bf16: 7.3 us in 12 parts a row, 6.1 in 13)
+    const int64_t step = (int64_t)kPartThreads * kRowVectors * 16 / size_of(d->type);
+    const int64_t wanted = std::max<int64_t>(1, std::min(ceil_div(sms * kPartCtas * 3, std::max<int64_t>(s.rows, 1)), d->vocab / 4096));
+    s.chunks = ceil_div(d->vocab, step * std::max<int64_t>(1, d->vocab / (step * wanted)));
     // CTAs of 2048 elements and more, as many as run at once, two an SM
     s.pass_ctas = std::max<int64_t>(1, std::min(2 * sms / std::max<int64_t>(d->batch, 1), ceil_div(d->vocab, 2048)));
     // a warp's share, in pieces that draw_kernel goes over in one step, but no more of them than it has threads
@@ -140,6 +143,7 @@ int odsgd_verify_workspace(const odsgd_verify_desc* desc, size_t* bytes) {
     return guarded([&] {
         if (!desc || !bytes) return fail(ODSGD_ERR_ARG, "desc / bytes is NULL");
         *bytes = 0;
+        if (!is_float_type(desc->type)) return fail(ODSGD_ERR_ARG, "type must be ODSGD_F32, ODSGD_BF16 or ODSGD_F16");
         if (desc->batch < 0 || desc->drafts < 0 || desc->vocab < 1) return fail(ODSGD_ERR_ARG, "sizes out of range");
         if (desc->drafts > ODSGD_MAX_DRAFTS || desc->batch > 1 << 16 || desc->vocab > 1 << 30)
             return fail(ODSGD_ERR_UNSUPPORTED, "batch, drafts or vocab beyond the limits");

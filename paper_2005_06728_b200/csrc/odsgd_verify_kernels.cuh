@@ -29,6 +29,7 @@ struct Position {
     float max, sum, draft_max, draft_sum;
     float logp;  // of the draft under the target
     int decision;
+    int token;   // the draft; -1 where decision is kEnds
 };
 
 struct VerifyArgs {
@@ -250,8 +251,9 @@ struct Sequence {
         const MaxSum t = target_sum();
         MaxSum d = {0.0f, 1.0f};
         if (draft && i < a.drafts) d = draft_sum();
-        Position p = {t.m, t.s, d.m, d.s, 0.0f, kEnds};
+        Position p = {t.m, t.s, d.m, d.s, 0.0f, kEnds, -1};
         if (known) {
+            p.token = (int)x;
             p.logp = (zt - t.m) * a.inv_temp - logf(t.s);
             const float lq = draft ? (zd - d.m) * a.draft_temp - logf(d.s) : 0.0f;
             const float over = p.logp - lq - logf(random);
@@ -262,8 +264,7 @@ struct Sequence {
         return p;
     }
     __device__ __forceinline__ RowPair<T> row(unsigned n, const Position& p) const {
-        const bool ends = p.decision == kEnds;
-        return RowPair<T>{target + n * a.t_sr, draft && !ends ? draft + n * a.d_sr : nullptr, ends ? -1 : token(n), p.max, p.draft_max,
+        return RowPair<T>{target + n * a.t_sr, draft && p.token >= 0 ? draft + n * a.d_sr : nullptr, p.token, p.max, p.draft_max,
                           a.inv_temp * 1.4426950408889634, a.draft_temp * 1.4426950408889634, a.vocab};
     }
 };
@@ -377,6 +378,7 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
     const unsigned seq = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int mine = (int)threadIdx.x;
     const Sequence<T> in(a, seq);
+    const double last_random = (double)in.u[a.drafts * a.u_sr];
     double x[kDrawSums];  // of the thread's segment, then P, Q, R, D, N
     if constexpr (ALONE) {
         for (unsigned i = warp; i <= a.drafts; i += kDrawWarps) {
@@ -446,7 +448,14 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
     if (!refused) all = x[0], row.q = nullptr, row.hot = -1;
     ratio += off;
     const bool drawn = all > kNothing && all < CUDART_INF;  // not where a row holds NaN, +inf or nothing but -inf
-    const double bound = (double)in.u[a.drafts * a.u_sr] * all;
+    const double bound = last_random * all;
+
+    if (threadIdx.x == 0) a.accepted[seq] = (int)n;
+    for (unsigned i = threadIdx.x; i <= a.drafts; i += kDrawThreads) {
+        if (i == n && drawn) continue;
+        store_token(a, seq, i, i < n ? s.place[i].token : -1);
+        a.logp[(size_t)seq * (a.drafts + 1) + i] = i < n ? s.place[i].logp : i > n ? 0.0f : CUDART_NAN_F;
+    }
 
     // The segment in which the running sum passes the bound: the last that begins no higher, of those that have anything.
     const double part = refused ? fmax(0.0, part_r - off * part_d) : part_p;
@@ -528,12 +537,6 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
             store_token(a, seq, n, found);
             a.logp[(size_t)seq * (a.drafts + 1) + n] = (float)(((double)to_f32(row.p[found]) - row.mp) * a.inv_temp - log(x[0]));
         }
-    }
-    if (threadIdx.x == 0) a.accepted[seq] = (int)n;
-    for (unsigned i = threadIdx.x; i <= a.drafts; i += kDrawThreads) {
-        if (i == n && drawn) continue;
-        store_token(a, seq, i, i < n ? in.token(i) : -1);
-        a.logp[(size_t)seq * (a.drafts + 1) + i] = i < n ? s.place[i].logp : i > n ? 0.0f : CUDART_NAN_F;
     }
 }
 

@@ -255,6 +255,7 @@ def test_verify_workspace(lib):
     assert lib.odsgd_verify_draft(verify(), ctypes.c_void_p(0x2000000), 1 << 30, None) == binding.ERR_OVERLAP
     assert lib.odsgd_verify_workspace(None, ctypes.byref(need)) == binding.ERR_ARG
     assert lib.odsgd_verify_workspace(verify(vocab=0), ctypes.byref(need)) == binding.ERR_ARG
+    assert lib.odsgd_verify_workspace(verify(type=7), ctypes.byref(need)) == binding.ERR_ARG
     assert lib.odsgd_verify_workspace(verify(drafts=300), ctypes.byref(need)) == binding.ERR_UNSUPPORTED
     # a workspace as large as all shapes allow does not overflow
     assert lib.odsgd_verify_workspace(verify(batch=1 << 16, drafts=255, vocab=1 << 30), ctypes.byref(need)) == binding.OK
