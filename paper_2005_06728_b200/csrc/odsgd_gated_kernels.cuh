@@ -271,40 +271,48 @@ __device__ __forceinline__ void store_32(T* p, int valid, const float (&x)[32]) 
 
 // Rows that do not start on 32 bytes go through a patch of shared memory, 32 rows of 64 columns a warp, and from there as
 // the 16-byte words of their own addresses, eight lanes a row; what is left at both ends goes element by element.  (2036
-// x 1001 x 2731 f16: 87 us with a row at a time, element by element, 68 so.)
+// x 1001 x 2731 f16, kept: 87 us with a row at a time, element by element, 44 so.)
 __device__ __forceinline__ void patch_32(uint32_t* patch, unsigned c, unsigned lane, const uint4 (&q)[4]) {
     uint32_t* const to = patch + lane * kPatchPitch + c / 2;
 #pragma unroll
     for (int i = 0; i < 4; ++i) to[4 * i] = q[i].x, to[4 * i + 1] = q[i].y, to[4 * i + 2] = q[i].z, to[4 * i + 3] = q[i].w;
+}
+// Stores behind a predicate rather than a branch, which the loads of the next rows may pass (nothing reads what they write, and the
+// patch is written again behind a barrier): 64 columns of 32 rows took a warp 3.5 thousand cycles with branches and take 2.8 so.
+// (Rows turned in the patch so that no two lanes meet in a bank took longer by their addresses.)
+__device__ __forceinline__ void store_if(void* p, const uint4& q, bool yes) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %5, 0;\n @p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n}\n" ::"l"(p), "r"(q.x), "r"(q.y), "r"(q.z),
+                 "r"(q.w), "r"((uint32_t)yes));
+}
+__device__ __forceinline__ void store_if(void* p, unsigned short x, bool yes) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %2, 0;\n @p st.global.b16 [%0], %1;\n}\n" ::"l"(p), "h"(x), "r"((uint32_t)yes));
 }
 template <typename T>
 __device__ __forceinline__ void store_patch(T* p, int valid, const uint32_t* patch, unsigned lane) {
     static_assert(sizeof(T) == 2, "two elements a word");
     const int l = (int)(lane & 7);
     __syncwarp();
-#pragma unroll 4
-    for (unsigned r = lane >> 3; r < 32; r += 4) {
-        T* const to = reinterpret_cast<T*>(__shfl_sync(~0u, reinterpret_cast<unsigned long long>(p), r));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned r = (lane >> 3) + 4 * i;
+        const unsigned long long to = __shfl_sync(~0u, reinterpret_cast<unsigned long long>(p), r);
         const uint32_t* const row = patch + r * kPatchPitch;
         const unsigned short* const half = reinterpret_cast<const unsigned short*>(row);
-        if (to != nullptr) {
-            const int head = min(valid, (int)((16 - (reinterpret_cast<uintptr_t>(to) & 15)) & 15) / 2), at = head + 8 * l;
-            if (at + 8 <= valid) {
-                const uint32_t* const w = row + at / 2;
-                const unsigned shift = at & 1 ? 16 : 0;
-                const uint32_t x[5] = {w[0], w[1], w[2], w[3], w[4]};  // (the last is not used where `shift` is 0; the row has a spare word)
-                *reinterpret_cast<uint4*>(to + at) = make_uint4(__funnelshift_r(x[0], x[1], shift), __funnelshift_r(x[1], x[2], shift),
-                                                                __funnelshift_r(x[2], x[3], shift), __funnelshift_r(x[3], x[4], shift));
-            }
-            // fewer than eight elements at each end; of whole eights, eight in all (or none)
-            const int tail = valid % 8 == 0 ? valid - 8 + l : head + (valid - head) / 8 * 8 + l;
-            if (valid % 8 == 0) {
-                const int e = l < head ? l : tail;
-                if (head != 0) reinterpret_cast<unsigned short*>(to)[e] = half[e];
-            } else {
-                if (l < head) reinterpret_cast<unsigned short*>(to)[l] = half[l];
-                if (tail < valid) reinterpret_cast<unsigned short*>(to)[tail] = half[tail];
-            }
+        const int head = min(valid, (int)(-(unsigned)to & 15) / 2), at = head + 8 * l;
+        const uint32_t* const w = row + min(at, 56) / 2;  // (what begins later is not stored)
+        const unsigned shift = at & 1 ? 16 : 0;
+        const uint32_t x[5] = {w[0], w[1], w[2], w[3], w[4]};  // (the last is not used where `shift` is 0; the row has a spare word)
+        const uint4 q = make_uint4(__funnelshift_r(x[0], x[1], shift), __funnelshift_r(x[1], x[2], shift), __funnelshift_r(x[2], x[3], shift),
+                                   __funnelshift_r(x[3], x[4], shift));
+        store_if(reinterpret_cast<void*>(to + 2 * at), q, to != 0 && at + 8 <= valid);
+        // fewer than eight elements at each end; of whole eights, eight in all (or none)
+        if (valid % 8 == 0) {
+            const int e = l < head ? l : valid - 8 + l;
+            store_if(reinterpret_cast<void*>(to + 2 * e), half[e], to != 0 && head != 0);
+        } else {
+            const int tail = head + (valid - head) / 8 * 8 + l;
+            store_if(reinterpret_cast<void*>(to + 2 * l), half[l], to != 0 && l < head);
+            store_if(reinterpret_cast<void*>(to + 2 * tail), half[min(tail, 63)], to != 0 && tail < valid);
         }
     }
     __syncwarp();
@@ -502,9 +510,9 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
                             }
                             uint4 q[4];
                             pack_32<T>(g, q);
-                            patch_32(patch, c & 63, lane, q);
                             T* const p = k == 0 ? gate : k == 1 ? up : h;
                             const int begin = c & ~63;
+                            patch_32(patch, c & 63, lane, q);
                             if (c + 32 >= valid || (c & 63) == 32) store_patch<T>(p ? p + begin : nullptr, min(64, valid - begin), patch, lane);
                         }
                     }
@@ -537,8 +545,8 @@ __global__ void __launch_bounds__(kGatedThreads, 1) __cluster_dims__(2, 1, 1) ga
                         } else {
                             uint4 q[4];
                             pack_32<T>(x, q);
-                            patch_32(patch, c & 63, lane, q);
                             const int begin = c & ~63;
+                            patch_32(patch, c & 63, lane, q);
                             if (c + 32 >= valid || (c & 63) == 32) store_patch<T>(p ? p + begin : nullptr, min(64, valid - begin), patch, lane);
                         }
                     }
