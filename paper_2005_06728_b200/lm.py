@@ -160,11 +160,25 @@ def _dense(shape) -> Tuple[int, int]:
     return (0 if n == 2 else shape[-2] * shape[-1]), shape[-1]
 
 
+# Memory of the current device and stream without what a factory function looks at besides (0.7 us instead of 1.9).
+_empty_strided = getattr(getattr(getattr(torch._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
+
+
 def _new(like: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """Contiguous memory of the stream that the work runs on; `shape` None: like's."""
+    """Contiguous memory of the stream that the work runs on (`like` is on the current device); `shape` None: like's."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return _new(like, shape, dtype, None)
+    if _empty_strided is not None:
+        if shape is None:
+            shape = like.shape
+        elif type(shape) is int:
+            return _empty_strided((shape,), (1,), dtype or like.dtype)
+        strides, step = (), 1
+        for n in reversed(shape):
+            strides = (step, *strides)
+            step *= n or 1
+        return _empty_strided(tuple(shape), strides, dtype or like.dtype)
     if shape is None:
         return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
     return like.new_empty(shape, dtype=dtype)
