@@ -219,15 +219,12 @@ constexpr int kThinSmem[2] = {226 * 1024, 110 * 1024};
 // How many clusters of `cluster` CTAs of thin_kernel run at once, one or two CTAs an SM: what the GPU's clusters of SMs leave
 // room for, asked once a device.  The question is put for a kernel without tensor memory: for one that has some the answer
 // is one CTA an SM, though two of thin_kernel do run (their times and SMs were recorded).
-int thin_clusters(int per_sm, int cluster, int* out) {
+int thin_clusters(int dev, int per_sm, int cluster, int* out) {
     static std::atomic<int> known[kMaxDevices][2][kThinCluster + 1] = {};
     static std::atomic<bool> done[kMaxDevices] = {};
-    int dev = 0;
-    int rc = current_device(&dev);
-    if (rc != ODSGD_OK) return rc;
     int n = dev < kMaxDevices ? known[dev][per_sm - 1][cluster].load(std::memory_order_relaxed) : 0;
     if (n == 0) {
-        rc = allow_smem((const void*)thin_room_kernel, kThinSmem[0], done);
+        const int rc = allow_smem((const void*)thin_room_kernel, kThinSmem[0], done);
         if (rc != ODSGD_OK) return rc;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)cluster);
@@ -266,6 +263,9 @@ int thin_shape(int64_t tokens, int64_t columns, int64_t depth, int sms, ThinShap
     double least = 12500.0 + 520.0 * (double)ceil_div(wide, sms / 2) * (double)blocks;
     *out = ThinShape{};
     if (tokens > 8192) return ODSGD_OK;
+    int dev = 0;
+    const int rc = current_device(&dev);
+    if (rc != ODSGD_OK) return rc;
     for (int64_t most : {64, 96, 128, 192, 256}) {
         const int64_t chunks = ceil_div(tokens, most), chunk = ceil_div(ceil_div(tokens, chunks), 16) * 16;
         const int64_t stage = kThinRows * kBlockK * 2 + chunk * kBlockK * 2, sums = chunk * kThinRows * 4;
@@ -273,8 +273,8 @@ int thin_shape(int64_t tokens, int64_t columns, int64_t depth, int sms, ThinShap
         int cluster = 1;
         for (int c = 2; c <= kThinCluster && blocks >= 4 * c; ++c) {
             int room = 0;
-            const int rc = thin_clusters(per_sm, c, &room);
-            if (rc != ODSGD_OK) return rc;
+            const int asked = thin_clusters(dev, per_sm, c, &room);
+            if (asked != ODSGD_OK) return asked;
             if (tiles * chunks <= room) cluster = c;
         }
         const double ctas = (double)(tiles * chunks * cluster), waves = std::ceil(ctas / (per_sm * sms));
