@@ -147,8 +147,13 @@ def _levels(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int]:
 
 def _rows(t: torch.Tensor, lead: int, name: str) -> Tuple[int, int]:
     """The same of a tensor with one more axis, which has to be contiguous."""
-    if t.stride(-1) != 1 and t.shape[-1] != 1:
+    stride = t.stride()
+    if stride[-1] != 1 and t.shape[-1] != 1:
         raise ValueError(f"{name}: the last axis must be contiguous")
+    if lead == 2:
+        return stride[:2]
+    if lead == 1:
+        return 0, stride[0]
     return _levels(t, lead, name)
 
 
