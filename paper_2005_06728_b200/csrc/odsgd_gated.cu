@@ -307,11 +307,11 @@ int launch_thin(const GatedArgs& g, unsigned tokens, const ThinShape& s, void* s
 }
 
 // Blocks of rows: threads along a row, eight columns each, and the rest of a CTA's across rows.
-void row_blocks(int64_t rows, int64_t columns, dim3* grid, dim3* block) {
+void row_blocks(int64_t rows, int64_t columns, int rows_a_thread, dim3* grid, dim3* block) {
     const int64_t cols = ceil_div(columns, 8), slabs = ceil_div(cols, kLayThreads);
     const int64_t x = ceil_div(ceil_div(cols, slabs), 32) * 32, y = kLayThreads / x;
     *block = dim3((unsigned)x, (unsigned)y);
-    *grid = dim3((unsigned)std::min<int64_t>(ceil_div(rows, y), 1 << 20), (unsigned)slabs);
+    *grid = dim3((unsigned)std::min<int64_t>(ceil_div(rows, y * rows_a_thread), 1 << 20), (unsigned)slabs);
 }
 
 template <typename T>
@@ -346,7 +346,7 @@ int run_gated(const odsgd_gated_desc* d, bool backward, const GatedPlan& p, char
     dim3 grid, block;
     if (lay_rows > 0) {
         for (LayMatrix& m : lay.m) m.n_inner = std::max(m.n_inner, 1u);
-        row_blocks(lay_rows, d->dim, &grid, &block);
+        row_blocks(lay_rows, d->dim, kLayRows, &grid, &block);
         rc = launch("operand layout kernel", lay_kernel<T>, grid, block, 0, 1, stream, lay);
         if (rc != ODSGD_OK) return rc;
     }
@@ -381,7 +381,7 @@ int run_gated(const odsgd_gated_desc* d, bool backward, const GatedPlan& p, char
     s.rows = (unsigned)n, s.n_inner = (unsigned)d->n_inner, s.columns = (unsigned)d->width, s.pitch = (unsigned)p.width_pitch;
     s.vec = rows_aligned(d->gate, 2, s.gate.so, s.gate.si, d->n_outer, d->n_inner) && rows_aligned(d->up, 2, s.up.so, s.up.si, d->n_outer, d->n_inner) &&
             rows_aligned(d->h, 2, s.dh.so, s.dh.si, d->n_outer, d->n_inner);
-    row_blocks(n, d->width, &grid, &block);
+    row_blocks(n, d->width, 1, &grid, &block);
     rc = gelu ? launch("gated slope kernel", slope_kernel<T, true>, grid, block, 0, 1, stream, s)
               : launch("gated slope kernel", slope_kernel<T, false>, grid, block, 0, 1, stream, s);
     if (rc != ODSGD_OK) return rc;

@@ -102,6 +102,16 @@ __device__ __forceinline__ uint4 pack<f16>(const float (&x)[8]) {
     return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
+// Eight elements of 16 bits that start `shift` bytes into two 16-byte words.
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, unsigned shift) {
+    uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) x[i] = shift & 8 ? x[i + 2] : x[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) x[i] = shift & 4 ? x[i + 1] : x[i];
+    const unsigned bits = shift & 2 ? 16 : 0;
+    return make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits), __funnelshift_r(x[3], x[4], bits));
+}
 // Eight elements of 16 bits that start anywhere: the two 16-byte words around them, shifted.  (Both words hold elements of
 // the eight, so neither reaches into another 16 bytes than the row's own do.)
 template <typename T>
@@ -112,17 +122,9 @@ __device__ __forceinline__ uint4 load_anywhere(const T* p) {
     const uint4 a = w[0];
     const unsigned shift = (unsigned)(at & 15);
     if (shift == 0) return a;
-    const uint4 b = w[1];
-    const uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    uint32_t y[5];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {  // from word shift / 4 on
-        const unsigned k = shift / 4;
-        y[i] = k == 0 ? x[i] : k == 1 ? x[i + 1] : k == 2 ? x[i + 2] : x[min(i + 3, 7)];
-    }
-    const unsigned bits = shift % 4 * 8;
-    return make_uint4(__funnelshift_r(y[0], y[1], bits), __funnelshift_r(y[1], y[2], bits), __funnelshift_r(y[2], y[3], bits), __funnelshift_r(y[3], y[4], bits));
+    return shifted(a, w[1], shift);
 }
+
 // Eight floats in one store, 32-byte aligned (two of 16 bytes leave every sector half written at a time).
 __device__ __forceinline__ void store_eight(float* p, const float* x) {
     asm volatile("st.global.cs.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]),
