@@ -368,6 +368,96 @@ struct DrawState {
     double begin;
 };
 
+// The token at which the running sum of what is left passes `bound`, to every thread: first the segment, by the sums `part` of
+// its thread's, then the element.  Sums and elements come out of different roundings, so that a segment that is next to nothing
+// can turn out to hold none; the whole row is then gone over.  -1 where that has nothing either.
+template <typename T>
+__device__ __forceinline__ int find_place(const RowPair<T>& row, double ratio, double part, double bound, int segment, DrawState& s) {
+    const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int mine = (int)threadIdx.x;
+    // The segment in which the running sum passes the bound: the last that begins no higher, of those that have anything.
+    double run = part;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const double v = __shfl_up_sync(~0u, run, d);
+        if ((int)lane >= d) run += v;
+    }
+    __syncthreads();
+    if (lane == 31) s.warp_part[0][warp] = run;
+    if (threadIdx.x == 0) s.found = INT_MAX, s.last = -1, s.at = -1;
+    __syncthreads();
+    double begin = warp_sum(lane < warp ? s.warp_part[0][lane] : 0.0);
+    const double before = __shfl_up_sync(~0u, run, 1);
+    if (lane > 0) begin += before;
+    // (a bound that is NaN or below 0 takes the first that has anything)
+    const int candidate = __reduce_max_sync(~0u, part > kNothing && begin <= bound ? mine : -1);
+    const unsigned some_part = __ballot_sync(~0u, part > kNothing);
+    if (lane == 0 && candidate >= 0) atomicMax(&s.at, candidate);
+    if (lane == 0 && some_part != 0) atomicMin(&s.found, (int)warp * 32 + __ffs((int)some_part) - 1);
+    __syncthreads();
+    const int at = s.at >= 0 ? s.at : s.found;
+    if (mine == at) s.begin = begin;
+    __syncthreads();
+    begin = s.begin;
+    if (threadIdx.x == 0) s.found = INT_MAX;
+    int from = 0, to = row.vocab;
+    if (at != INT_MAX) from = at * segment, to = min(row.vocab, from + segment);
+    else begin = 0.0;
+    for (;;) {  // twice at most
+        // its elements again, 256 a warp
+        for (int j0 = from; j0 < to; j0 += 256 * kDrawWarps) {
+            const int j = j0 + 256 * (int)warp + 8 * (int)lane;
+            double e[8] = {};
+            if (j < to) {
+                float z[8];
+                row.load(row.p, j, z);
+                row.target(z, e);
+                if (row.q) {
+                    double f[8];
+                    row.load(row.q, j, z);
+                    row.draft(z, f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[i] = fmax(0.0, fma(-ratio, f[i], e[i]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
+                }
+            }
+#pragma unroll
+            for (int i = 1; i < 8; ++i) e[i] += e[i - 1];
+            run = e[7];
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const double v = __shfl_up_sync(~0u, run, d);
+                if ((int)lane >= d) run += v;
+            }
+            __syncthreads();  // (the sums of before have been read)
+            if (lane == 31) s.warp_part[0][warp] = run;
+            __syncthreads();
+            double ahead = begin + warp_sum(lane < warp ? s.warp_part[0][lane] : 0.0);
+            begin += warp_sum(lane < kDrawWarps ? s.warp_part[0][lane] : 0.0);
+            const double lower = __shfl_up_sync(~0u, run, 1);
+            if (lane > 0) ahead += lower;
+            int over = INT_MAX, some = -1;
+#pragma unroll
+            for (int i = 7; i >= 0; --i) {
+                const bool any = e[i] > (i > 0 ? e[i - 1] : 0.0);
+                if (any && ahead + e[i] > bound) over = j + i;
+                if (any && some < 0) some = j + i;
+            }
+            over = __reduce_min_sync(~0u, over);
+            some = __reduce_max_sync(~0u, some);
+            if (lane == 0 && over != INT_MAX) atomicMin(&s.found, over);
+            if (lane == 0 && some >= 0) atomicMax(&s.last, some);
+            __syncthreads();
+            if (s.found != INT_MAX) break;
+        }
+        if (s.last >= 0 || (from == 0 && to == row.vocab)) break;
+        from = 0, to = row.vocab, begin = 0.0;
+    }
+    return s.found != INT_MAX ? s.found : s.last;  // (the bound is the whole sum, but for a rounding)
+}
+
 // A CTA a sequence, a thread a segment.  ALONE: the CTA also does what the other kernels do ahead of it, a warp a row and a
 // segment.  That pays up to some 2000 tokens: 8 x 3 drafts, bf16, of 200 / 2000 / 4000 take 11.1 / 12.6 / 15.9 us so, 13.0 / 13.7 / 13.6
 // by three launches, which cost the host 5 us more.
@@ -392,7 +482,6 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         for (int k = 0; k < kDrawSums; ++k) x[k] = mine < a.segments ? a.sums[((size_t)seq * kDrawSums + k) * a.segments + mine] : 0.0;
         if (threadIdx.x <= a.drafts) s.place[threadIdx.x] = a.positions[(size_t)seq * (a.drafts + 1) + threadIdx.x];
     }
-    if (threadIdx.x == 0) s.found = INT_MAX, s.last = -1, s.at = -1;
     __syncthreads();
     unsigned n = 0;
     while (s.place[n].decision == kAccepted) ++n;
@@ -442,101 +531,29 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
             ratio = ratio_of(s.place[n]);
         }
     }
-    // Where nothing is left (a draft that neither gives a probability, equal distributions): the whole target.
-    double all = x[2] - off * x[3];
-    if (refused && all <= kNothing) refused = false;
-    if (!refused) all = x[0], row.q = nullptr, row.hot = -1;
+    // Where nothing is left (a draft that neither gives a probability, equal distributions, by the sums or by the elements): the
+    // whole target.  Nothing is drawn where a row holds NaN, +inf or nothing but -inf.
     ratio += off;
-    const bool drawn = all > kNothing && all < CUDART_INF;  // not where a row holds NaN, +inf or nothing but -inf
-    const double bound = last_random * all;
-
+    if (refused && x[2] - off * x[3] <= kNothing) refused = false;
     if (threadIdx.x == 0) a.accepted[seq] = (int)n;
     for (unsigned i = threadIdx.x; i <= a.drafts; i += kDrawThreads) {
-        if (i == n && drawn) continue;
+        if (i == n) continue;
         store_token(a, seq, i, i < n ? s.place[i].token : -1);
-        a.logp[(size_t)seq * (a.drafts + 1) + i] = i < n ? s.place[i].logp : i > n ? 0.0f : CUDART_NAN_F;
+        a.logp[(size_t)seq * (a.drafts + 1) + i] = i < n ? s.place[i].logp : 0.0f;
     }
-
-    // The segment in which the running sum passes the bound: the last that begins no higher, of those that have anything.
-    const double part = refused ? fmax(0.0, part_r - off * part_d) : part_p;
-    double run = part;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const double v = __shfl_up_sync(~0u, run, d);
-        if ((int)lane >= d) run += v;
+    int found = -1;
+    for (;;) {  // twice at most
+        if (!refused) row.q = nullptr, row.hot = -1;
+        const double all = refused ? x[2] - off * x[3] : x[0];
+        if (!(all > kNothing && all < CUDART_INF)) break;
+        found = find_place(row, ratio, refused ? fmax(0.0, part_r - off * part_d) : part_p, last_random * all, a.segment, s);
+        if (found >= 0 || !refused) break;
+        refused = false;
     }
-    __syncthreads();
-    if (lane == 31) s.warp_part[0][warp] = run;
-    __syncthreads();
-    double begin = warp_sum(lane < warp ? s.warp_part[0][lane] : 0.0);
-    const double before = __shfl_up_sync(~0u, run, 1);
-    if (lane > 0) begin += before;
-    // (a bound that is NaN or below 0 takes the first that has anything)
-    const int candidate = __reduce_max_sync(~0u, part > kNothing && begin <= bound ? mine : -1);
-    const unsigned some_part = __ballot_sync(~0u, part > kNothing);
-    if (lane == 0 && candidate >= 0) atomicMax(&s.at, candidate);
-    if (lane == 0 && some_part != 0) atomicMin(&s.found, (int)warp * 32 + __ffs((int)some_part) - 1);
-    __syncthreads();
-    const int at = s.at >= 0 ? s.at : s.found;
-    if (mine == at) s.begin = begin;
-    __syncthreads();
-    begin = s.begin;
-    if (threadIdx.x == 0) s.found = INT_MAX;
-    if (drawn) {
-        // its elements again, 256 a warp
-        const int from = at * a.segment, to = min(a.vocab, from + a.segment);
-        for (int j0 = from; j0 < to; j0 += 256 * kDrawWarps) {
-            const int j = j0 + 256 * (int)warp + 8 * (int)lane;
-            double e[8] = {};
-            if (j < to) {
-                float z[8];
-                row.load(row.p, j, z);
-                row.target(z, e);
-                if (row.q) {
-                    double f[8];
-                    row.load(row.q, j, z);
-                    row.draft(z, f);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) e[i] = fmax(0.0, fma(-ratio, f[i], e[i]));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) e[i] = j + i == row.hot ? 0.0 : e[i];
-                }
-            }
-#pragma unroll
-            for (int i = 1; i < 8; ++i) e[i] += e[i - 1];
-            run = e[7];
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const double v = __shfl_up_sync(~0u, run, d);
-                if ((int)lane >= d) run += v;
-            }
-            __syncthreads();  // (the sums of before have been read)
-            if (lane == 31) s.warp_part[0][warp] = run;
-            __syncthreads();
-            double ahead = begin + warp_sum(lane < warp ? s.warp_part[0][lane] : 0.0);
-            begin += warp_sum(lane < kDrawWarps ? s.warp_part[0][lane] : 0.0);
-            const double lower = __shfl_up_sync(~0u, run, 1);
-            if (lane > 0) ahead += lower;
-            int over = INT_MAX, some = -1;
-#pragma unroll
-            for (int i = 7; i >= 0; --i) {
-                const bool any = e[i] > (i > 0 ? e[i - 1] : 0.0);
-                if (any && ahead + e[i] > bound) over = j + i;
-                if (any && some < 0) some = j + i;
-            }
-            over = __reduce_min_sync(~0u, over);
-            some = __reduce_max_sync(~0u, some);
-            if (lane == 0 && over != INT_MAX) atomicMin(&s.found, over);
-            if (lane == 0 && some >= 0) atomicMax(&s.last, some);
-            __syncthreads();
-            if (s.found != INT_MAX) break;
-        }
-        if (threadIdx.x == 0) {
-            const int found = s.found != INT_MAX ? s.found : s.last;  // (the bound is the whole sum, but for a rounding)
-            store_token(a, seq, n, found);
-            a.logp[(size_t)seq * (a.drafts + 1) + n] = (float)(((double)to_f32(row.p[found]) - row.mp) * a.inv_temp - log(x[0]));
-        }
+    if (threadIdx.x == 0) {
+        store_token(a, seq, n, found);
+        a.logp[(size_t)seq * (a.drafts + 1) + n] =
+            found >= 0 ? (float)(((double)to_f32(row.p[found]) - row.mp) * a.inv_temp - log(x[0])) : CUDART_NAN_F;
     }
 }
 

@@ -1,0 +1,81 @@
+"""Verification of drafted tokens where its arithmetic is at its ends: what 64 bits hardly hold, far masks, high and low temperatures.
+
+Expected values are block_reference's 64-bit form on rows that were shifted by their maximum beforehand (in 64 bits, where the
+difference of two elements is exact); logp is bounded as in test_gpu_block."""
+import math
+
+import pytest
+import torch
+
+import block_reference as R
+from paper_2005_06728_b200 import lm
+from test_gpu_block import drafted
+from test_gpu_lm import BF16, DEV, F16, F32, gen, randn
+
+pytestmark = pytest.mark.gpu
+NEXT_TO_ONE = 1 - 2.0 ** -24
+
+
+def shifted(z):
+    z = z.double()
+    top = z.amax(-1, keepdim=True)
+    return z - top.masked_fill(top == float("-inf"), 0.0)
+
+
+def check(target, tok, u, draft, c=1.0, e=None):
+    """Equal decisions, draws and scores, where nothing is nearer to a border than 64-bit sums are off: 1e-11, some 2^53 / 90000, is more
+    than any sum of a row here added one by one, and far more than the tree sums of the kernel."""
+    e = c if e is None else e
+    r = lm.verify_draft(target, tok, u, draft=draft, inv_temp=c, draft_inv_temp=e)
+    accepted, tokens, logp, near = R.verify(shifted(target), tok, u, None if draft is None else shifted(draft), c, e)
+    assert near > 1e-11, "on the border: choose another seed"
+    assert torch.equal(r.accepted.cpu().long(), accepted)
+    assert torch.equal(r.tokens.cpu().long(), tokens)
+    # the difference to the maximum, its product with the temperature and the sum's logarithm: a few roundings of 2^-24 of logp, and
+    # the error of the sum as in test_gpu_block
+    R.within(r.logp.cpu(), logp, 2.0 ** -19 + logp.abs().nan_to_num() * 2.0 ** -21, "logp")
+    return r
+
+
+# --------------------------------------------------------------------------- next to nothing left
+
+@pytest.mark.parametrize("vocab", [700, 20000, 70001])
+def test_what_is_left_is_small_everywhere(vocab):
+    """All of the target's mass is taken off, what is left are elements of 2^-909: no part of the vocabulary reaches 2^-900, their sum
+    does."""
+    z = torch.full((3, 2, vocab), -909 * math.log(2.0), device=DEV)
+    z[..., 100] = 0.0
+    q = torch.full((3, 1, vocab), float("-inf"), device=DEV)
+    q[..., 100], q[..., 300] = 0.0, -100 * math.log(2.0)
+    tok = torch.full((3, 1), 300, device=DEV)
+    u = torch.tensor([[0.5, 0.37], [0.25, 0.9], [0.75, 0.0123]], device=DEV)
+    r = check(z, tok, u, q)
+    assert r.accepted.tolist() == [0, 0, 0]
+
+
+@pytest.mark.parametrize("vocab", [40, 700, 5000, 70001])
+@pytest.mark.parametrize("way", ["same", "permuted", "shifted"])
+def test_differences_that_64_bits_hardly_hold(vocab, way):
+    """Two rows that differ in a token of 1e-20 of their mass, and in the order of their elements or by a constant: what is drawn is a
+    token all the same, not the refused one, with its score."""
+    n = 48
+    base = randn(n, 1, vocab, seed=600 + vocab, sigma=2.0)
+    x = torch.randint(0, vocab, (n, 1), generator=gen(601), device=DEV)
+    base.scatter_(2, x[..., None], base.amax(-1, keepdim=True) - 46.0)
+    q = base.clone()
+    if way == "permuted":
+        half = vocab // 2
+        q[..., half:] = q[..., half:][..., torch.randperm(vocab - half, generator=gen(602), device=DEV)]
+    elif way == "shifted":
+        q = (q + 0.1) - 0.1
+    q.scatter_(2, x[..., None], base.gather(2, x[..., None]) + 1.0)
+    u = torch.rand(n, 2, generator=gen(603), device=DEV)
+    u[:, 0] = 0.9
+    u[:n // 4, 1], u[n // 4:n // 2, 1] = 0.0, NEXT_TO_ONE
+    z = torch.cat((base, base), 1)
+    r = lm.verify_draft(z, x, u, draft=q)
+    assert not bool(r.accepted.any())
+    t = r.tokens[:, :1]
+    assert bool(((t >= 0) & (t < vocab) & (t != x)).all()) and bool((r.tokens[:, 1] == -1).all())
+    want = torch.log_softmax(base[:, 0].double(), -1).gather(1, t)[:, 0]
+    R.within(r.logp[:, 0].cpu(), want.cpu(), (2.0 ** -19 + want.abs() * 2.0 ** -21).cpu(), "logp")
