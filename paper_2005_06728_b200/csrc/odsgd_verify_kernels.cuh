@@ -22,6 +22,8 @@ constexpr int kSegments = kDrawThreads;  // most parts of the vocabulary, each s
 constexpr int kDrawSums = 5;
 constexpr double kNothing = 0x1p-900;  // relative to a row's largest element: sums up to this hold masked elements alone
 
+constexpr float kHeld = -600.0f;           // log-probabilities above this are no matter of the range of 64 bits
+
 enum Decision { kRefused, kAccepted, kNear, kEnds };
 
 // Place i of a sequence, by the rows' sums in 32 bits.
@@ -257,9 +259,10 @@ struct Sequence {
             p.logp = (zt - t.m) * a.inv_temp - logf(t.s);
             const float lq = draft ? (zd - d.m) * a.draft_temp - logf(d.s) : 0.0f;
             const float over = p.logp - lq - logf(random);
-            // 32 bits leave `over` uncertain by some 1e-6; infinities and NaN are left to the exact comparison too
+            // 32 bits leave `over` uncertain by some 1e-6; infinities and NaN are left to the exact comparison too, and so is a draft to
+            // which the target may give nothing that 64 bits hold (a masked token at u = 0, or masked in both rows)
             const float margin = 1e-4f + 4e-6f * (fabsf(p.logp) + fabsf(lq));
-            p.decision = over > margin ? kAccepted : over < -margin ? kRefused : kNear;
+            p.decision = over > margin && p.logp > kHeld ? kAccepted : over < -margin ? kRefused : kNear;
         }
         return p;
     }

@@ -22,13 +22,14 @@ def shifted(z):
     return z - top.masked_fill(top == float("-inf"), 0.0)
 
 
-def check(target, tok, u, draft, c=1.0, e=None):
+def check(target, tok, u, draft, c=1.0, e=None, exact=False):
     """Equal decisions, draws and scores, where nothing is nearer to a border than 64-bit sums are off: 1e-11, some 2^53 / 90000, is more
-    than any sum of a row here added one by one, and far more than the tree sums of the kernel."""
+    than any sum of a row here added one by one, and far more than the tree sums of the kernel.  `exact`: some decisions are made on
+    zeros, which are borders by themselves, without any rounding."""
     e = c if e is None else e
     r = lm.verify_draft(target, tok, u, draft=draft, inv_temp=c, draft_inv_temp=e)
     accepted, tokens, logp, near = R.verify(shifted(target), tok, u, None if draft is None else shifted(draft), c, e)
-    assert near > 1e-11, "on the border: choose another seed"
+    assert exact or near > 1e-11, "on the border: choose another seed"
     assert torch.equal(r.accepted.cpu().long(), accepted)
     assert torch.equal(r.tokens.cpu().long(), tokens)
     # the difference to the maximum, its product with the temperature and the sum's logarithm: a few roundings of 2^-24 of logp, and
@@ -79,3 +80,21 @@ def test_differences_that_64_bits_hardly_hold(vocab, way):
     assert bool(((t >= 0) & (t < vocab) & (t != x)).all()) and bool((r.tokens[:, 1] == -1).all())
     want = torch.log_softmax(base[:, 0].double(), -1).gather(1, t)[:, 0]
     R.within(r.logp[:, 0].cpu(), want.cpu(), (2.0 ** -19 + want.abs() * 2.0 ** -21).cpu(), "logp")
+
+
+# --------------------------------------------------------------------------- masks
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("vocab", [40, 700, 20000])
+def test_masked_drafts_are_refused(kind, vocab):
+    """A draft that the target's mask leaves nothing is refused, whatever the mask's value, the random number and the draft's own mask and
+    temperature."""
+    for mask in (float("-inf"), torch.finfo(kind).min, -6e4):
+        target, tok, u, draft = drafted(8, 2, vocab, kind, 610)
+        target[..., ::3] = mask
+        draft[:4, ..., ::3] = mask
+        tok = tok // 3 * 3
+        u[::2, 0] = 0.0
+        for q, c, e in ((draft, 1.0, 1.0), (draft, 0.5, 1.0), (draft, 1.0, 0.25), (None, 1.0, 1.0)):
+            r = check(target, tok, u, q, c, e, exact=True)
+            assert not bool(r.accepted.any()) and bool((r.tokens[:, 0] % 3 != 0).all())
