@@ -121,8 +121,7 @@ __device__ __forceinline__ double power_of_two(double d, double c) {
     r = fma(r, f, 0.6931471805599453);
     r = fma(r, f, 1.0);
     if constexpr (OPEN) return __hiloint2double(__double2hiint(r) + (__double2loint(w) << 20), __double2loint(r));
-    // (a number below -2^31 leaves another upper half)
-    const bool none = __double2hiint(w) < 0x4337ffff || __double2loint(w) < -1000;
+    const bool none = d * c < -1000.0;  // (asked of the product: w's lower half says nothing beyond 32 bits)
     return __hiloint2double(none ? 0 : __double2hiint(r) + (__double2loint(w) << 20), none ? 0 : __double2loint(r));
 }
 

@@ -98,3 +98,20 @@ def test_masked_drafts_are_refused(kind, vocab):
         for q, c, e in ((draft, 1.0, 1.0), (draft, 0.5, 1.0), (draft, 1.0, 0.25), (None, 1.0, 1.0)):
             r = check(target, tok, u, q, c, e, exact=True)
             assert not bool(r.accepted.any()) and bool((r.tokens[:, 0] % 3 != 0).all())
+
+
+@pytest.mark.parametrize("kind,mask,c", [(F32, -1e9, 2.0), (F32, -1e9, 1.5), (F32, -1e9, 2.97), (BF16, -1e9, 2.0), (F32, -2e9, 1.0), (F32, -1.5e9, 1.0),
+                                         (BF16, -2.5e9, 1.0), (F32, -1e4, 2e5), (F16, -6e4, 4e4), (F32, -1e9, 1.0), (F32, -3.5e9, 1.0), (BF16, -1e12, 1.0)])
+@pytest.mark.parametrize("vocab", [40, 700, 20000])
+def test_masks_far_below(kind, mask, c, vocab):
+    """Masks whose exponent is about 2^31 to 2^32: nothing of them counts, drafts of masked tokens are refused, and none is drawn."""
+    target, tok, u, draft = drafted(12, 2, vocab, kind, 620, sigma=2.5 / max(c, 1.0), int_kind=torch.int64)
+    keep = torch.arange(vocab, device=DEV) % 7 == 3
+    target, draft = target.masked_fill(~keep, mask), draft.masked_fill(~keep, mask)
+    tok = tok // 7 * 7 + 3
+    tok[tok >= vocab] = 3
+    tok[::4] -= 1  # a masked token
+    for q in (draft, None):
+        r = check(target, tok, u, q, c)
+        drawn = r.tokens.gather(1, r.accepted.long()[:, None])
+        assert bool((drawn % 7 == 3).all())
