@@ -104,8 +104,8 @@ __device__ __forceinline__ double warp_sum(double x) {
 }
 
 // 2^(d c) in 64 bits, within 4e-14: the nearest whole number goes into the exponent, the rest f, at most a half, through 1 + f r(f),
-// r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0, 0 below 2^-1000 and
-// at -inf; for d c <= 1 or NaN.  OPEN: for -1000 <= d c, or NaN, alone.
+// r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0, 0 below 2^-1021 and
+// at -inf; for d c <= 1 or NaN.  OPEN: for -1021 <= d c, or NaN, alone.
 template <bool OPEN = false>
 __device__ __forceinline__ double power_of_two(double d, double c) {
     const double w = fma(d, c, 6755399441055744.0);  // 1.5 * 2^52: the lower half is the whole number
@@ -121,7 +121,7 @@ __device__ __forceinline__ double power_of_two(double d, double c) {
     r = fma(r, f, 0.6931471805599453);
     r = fma(r, f, 1.0);
     if constexpr (OPEN) return __hiloint2double(__double2hiint(r) + (__double2loint(w) << 20), __double2loint(r));
-    const bool none = d * c < -1000.0;  // (asked of the product: w's lower half says nothing beyond 32 bits)
+    const bool none = d * c < -1021.0;  // (asked of the product: w's lower half says nothing beyond 32 bits)
     return __hiloint2double(none ? 0 : __double2hiint(r) + (__double2loint(w) << 20), none ? 0 : __double2loint(r));
 }
 

@@ -82,6 +82,20 @@ def test_differences_that_64_bits_hardly_hold(vocab, way):
     R.within(r.logp[:, 0].cpu(), want.cpu(), (2.0 ** -19 + want.abs() * 2.0 ** -21).cpu(), "logp")
 
 
+@pytest.mark.parametrize("vocab", [40, 700, 20000])
+def test_probabilities_at_the_end_of_64_bits(vocab):
+    """Drafts of e^-704 of a row's largest element are still compared by their probabilities."""
+    z = torch.full((5, 2, vocab), -5.0, device=DEV)
+    z[..., 7] = 0.0
+    z[..., 11] = -704.0
+    q = z[:, :1].clone()
+    q[3:, :, 11] = -700.0
+    tok = torch.full((5, 1), 11, device=DEV)
+    u = torch.tensor([[0.5, 0.3], [0.0, 0.6], [NEXT_TO_ONE, 0.2], [0.01, 0.9], [0.03, 0.4]], device=DEV)
+    r = check(z, tok, u, q, exact=True)  # (u = 0: a border by itself)
+    assert r.accepted.tolist() == [1, 1, 1, 1, 0]
+
+
 # --------------------------------------------------------------------------- masks
 
 @pytest.mark.parametrize("kind", [F32, BF16, F16])
