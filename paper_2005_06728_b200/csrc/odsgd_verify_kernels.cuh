@@ -20,8 +20,6 @@ constexpr int kDrawThreads = 512;  // of draw_kernel
 constexpr int kDrawWarps = kDrawThreads / 32;
 constexpr int kSegments = kDrawThreads;  // most parts of the vocabulary, each summed by a warp
 constexpr int kDrawSums = 5;
-constexpr double kNothing = 0x1p-900;  // relative to a row's largest element: sums up to this hold masked elements alone
-
 constexpr float kHeld = -600.0f;           // log-probabilities above this are no matter of the range of 64 bits
 
 enum Decision { kRefused, kAccepted, kNear, kEnds };
@@ -104,9 +102,10 @@ __device__ __forceinline__ double warp_sum(double x) {
 }
 
 // 2^(d c) in 64 bits, within 4e-14: the nearest whole number goes into the exponent, the rest f, at most a half, through 1 + f r(f),
-// r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0, 0 below 2^-1021 and
-// at -inf; for d c <= 1 or NaN.  OPEN: for -1021 <= d c, or NaN, alone.
-template <bool OPEN = false>
+// r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0; for kLeast <= d c <= 0.
+// What is lower counts as nothing (is_nothing): a mask, or at that size no matter to any sum.
+constexpr double kLeast = -1020.0;
+__device__ __forceinline__ bool is_nothing(double d, double c) { return d * c < kLeast; }
 __device__ __forceinline__ double power_of_two(double d, double c) {
     const double w = fma(d, c, 6755399441055744.0);  // 1.5 * 2^52: the lower half is the whole number
     const double f = fma(d, c, 6755399441055744.0 - w);
@@ -120,9 +119,7 @@ __device__ __forceinline__ double power_of_two(double d, double c) {
     r = fma(r, f, 0.2402265069581299);
     r = fma(r, f, 0.6931471805599453);
     r = fma(r, f, 1.0);
-    if constexpr (OPEN) return __hiloint2double(__double2hiint(r) + (__double2loint(w) << 20), __double2loint(r));
-    const bool none = d * c < -1021.0;  // (asked of the product: w's lower half says nothing beyond 32 bits)
-    return __hiloint2double(none ? 0 : __double2hiint(r) + (__double2loint(w) << 20), none ? 0 : __double2loint(r));
+    return __hiloint2double(__double2hiint(r) + (__double2loint(w) << 20), __double2loint(r));
 }
 
 // One of the target's rows and the draft's beside it, element by element in 64 bits.
@@ -133,8 +130,13 @@ struct RowPair {
     long long hot;  // -1: no draft to take off
     double mp, mq, cp, cq;  // maxima, temperatures times log2 e
     int vocab;
-    __device__ __forceinline__ double target(int j) const { return power_of_two((double)to_f32(p[j]) - mp, cp); }
-    __device__ __forceinline__ double draft(int j) const { return power_of_two((double)to_f32(q[j]) - mq, cq); }
+    float low_p, low_q;     // no element above these is nothing
+    __device__ __forceinline__ static double one(float z, double m, double c) {
+        const double d = (double)z - m;
+        return is_nothing(d, c) ? 0.0 : power_of_two(d, c);
+    }
+    __device__ __forceinline__ double target(int j) const { return one(to_f32(p[j]), mp, cp); }
+    __device__ __forceinline__ double draft(int j) const { return one(to_f32(q[j]), mq, cq); }
     // Elements j to j + 7 of a row, as the 16-byte words that hold them: loaded ahead, taken apart when they are needed.  No word
     // is read that has none of them.
     static constexpr int kWords = 8 * (int)sizeof(T) / 16 + 1;
@@ -178,30 +180,21 @@ struct RowPair {
         }
     }
     __device__ __forceinline__ void load(const T* row, int j, float (&z)[8]) const { take(fetch(row, j), row, j, z); }
-    __device__ __forceinline__ void target(const float (&z)[8], double (&e)[8]) const {
+    // Eight at a time; only where one may be nothing they are looked at one by one (asked of each it takes three instructions more,
+    // 48 x 7 drafts at 131072: 73 us in all, 68 so).
+    __device__ __forceinline__ static void eight(const float (&z)[8], double m, double c, float low, double (&e)[8]) {
+        float least = z[0];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = power_of_two((double)z[i] - mp, cp);
-    }
-    __device__ __forceinline__ void draft(const float (&z)[8], double (&e)[8]) const {
+        for (int i = 1; i < 8; ++i) least = fminf(least, z[i]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = power_of_two((double)z[i] - mq, cq);
-    }
-    // The same for sums, which kNothing does not change: what is lower (a mask) counts as 2^-980, one instruction instead of five.
-    __device__ __forceinline__ static float no_lower(float z, float low) {
-        float x;
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(z), "f"(low));
-        return x;
-    }
-    __device__ __forceinline__ void target_sums(const float (&z)[8], double (&e)[8]) const {
-        const float low = (float)(mp - 980.0 / cp);
+        for (int i = 0; i < 8; ++i) e[i] = power_of_two((double)z[i] - m, c);
+        if (least <= low) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = power_of_two<true>((double)no_lower(z[i], low) - mp, cp);
+            for (int i = 0; i < 8; ++i) e[i] = is_nothing((double)z[i] - m, c) ? 0.0 : e[i];
+        }
     }
-    __device__ __forceinline__ void draft_sums(const float (&z)[8], double (&e)[8]) const {
-        const float low = (float)(mq - 980.0 / cq);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = power_of_two<true>((double)no_lower(z[i], low) - mq, cq);
-    }
+    __device__ __forceinline__ void target(const float (&z)[8], double (&e)[8]) const { eight(z, mp, cp, low_p, e); }
+    __device__ __forceinline__ void draft(const float (&z)[8], double (&e)[8]) const { eight(z, mq, cq, low_q, e); }
     // f(j, logits of the target, of the draft) for each eight from `from` on, a warp's width apart; the next are loaded ahead.
     template <typename F>
     __device__ __forceinline__ void each(int from, int hi, F f) const {
@@ -265,11 +258,16 @@ struct Sequence {
         }
         return p;
     }
+    // (rounded up, so that all above is above kLeast, however large the logits and the temperature are)
+    __device__ __forceinline__ static float low(double m, double c) { return __double2float_ru(m + kLeast / c); }
     __device__ __forceinline__ RowPair<T> row(unsigned n, const Position& p) const {
-        return RowPair<T>{target + n * a.t_sr, draft && p.token >= 0 ? draft + n * a.d_sr : nullptr, p.token, p.max, p.draft_max,
-                          a.inv_temp * 1.4426950408889634, a.draft_temp * 1.4426950408889634, a.vocab};
+        const double cp = a.inv_temp * 1.4426950408889634, cq = a.draft_temp * 1.4426950408889634;
+        return RowPair<T>{target + n * a.t_sr, draft && p.token >= 0 ? draft + n * a.d_sr : nullptr, p.token, p.max, p.draft_max, cp, cq, a.vocab,
+                          low(p.max, cp), low(p.draft_max, cq)};
     }
 };
+// A row that holds NaN or +inf has a sum that is NaN, one of nothing but -inf a sum of 0.
+__device__ __forceinline__ bool is_void(const Position& p) { return !(p.sum > 0.0f && p.draft_sum > 0.0f); }
 __device__ __forceinline__ double ratio_of(const Position& p) { return (double)p.sum / (double)p.draft_sum; }
 
 // One pass over the two rows of a place gives, in 64 bits, the sums P and Q of the target's and the draft's exponentials
@@ -285,11 +283,11 @@ __device__ __forceinline__ void pass_segment(const RowPair<T>& row, double ratio
     for (int k = 0; k < kDrawSums; ++k) x[k] = 0.0;
     row.each(lo + 8 * (int)(threadIdx.x & 31), hi, [&](int j, const float (&z)[8], const float (&y)[8]) {
         double e[8];
-        row.target_sums(z, e);
+        row.target(z, e);
         x[0] += sum_of(e);
         if (row.q) {
             double f[8], r[8];
-            row.draft_sums(y, f);
+            row.draft(y, f);
             x[1] += sum_of(f);
             int near = 0;  // the least of the exponents of |p - k q| less those of p
 #pragma unroll
@@ -303,7 +301,7 @@ __device__ __forceinline__ void pass_segment(const RowPair<T>& row, double ratio
                     if ((__double2hiint(r[i]) & 0x7fffffff) < __double2hiint(e[i]) - (18 << 20)) x[4] += e[i];
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {  // (NaN comes out of P and Q)
+            for (int i = 0; i < 8; ++i) {  // (rows with NaN do not count: is_void)
                 const bool less = __double2hiint(r[i]) < 0;
                 e[i] = less ? 0.0 : r[i];
                 f[i] = less ? 0.0 : f[i];
@@ -392,8 +390,8 @@ __device__ __forceinline__ int find_place(const RowPair<T>& row, double ratio, d
     const double before = __shfl_up_sync(~0u, run, 1);
     if (lane > 0) begin += before;
     // (a bound that is NaN or below 0 takes the first that has anything)
-    const int candidate = __reduce_max_sync(~0u, part > kNothing && begin <= bound ? mine : -1);
-    const unsigned some_part = __ballot_sync(~0u, part > kNothing);
+    const int candidate = __reduce_max_sync(~0u, part > 0.0 && begin <= bound ? mine : -1);
+    const unsigned some_part = __ballot_sync(~0u, part > 0.0);
     if (lane == 0 && candidate >= 0) atomicMax(&s.at, candidate);
     if (lane == 0 && some_part != 0) atomicMin(&s.found, (int)warp * 32 + __ffs((int)some_part) - 1);
     __syncthreads();
@@ -512,7 +510,7 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kDrawSums; ++k) x[k] = warp_sum(lane < kDrawWarps ? s.warp_part[k][lane] : 0.0);
-        if (s.place[n].decision == kEnds) break;
+        if (s.place[n].decision == kEnds || is_void(s.place[n])) break;
         bool next = false;
         if (!again) {
             const int t = (int)row.hot;
@@ -534,9 +532,9 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         }
     }
     // Where nothing is left (a draft that neither gives a probability, equal distributions, by the sums or by the elements): the
-    // whole target.  Nothing is drawn where a row holds NaN, +inf or nothing but -inf.
+    // whole target.
     ratio += off;
-    if (refused && x[2] - off * x[3] <= kNothing) refused = false;
+    if (refused && x[2] - off * x[3] <= 0.0) refused = false;
     if (threadIdx.x == 0) a.accepted[seq] = (int)n;
     for (unsigned i = threadIdx.x; i <= a.drafts; i += kDrawThreads) {
         if (i == n) continue;
@@ -544,10 +542,9 @@ __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constan
         a.logp[(size_t)seq * (a.drafts + 1) + i] = i < n ? s.place[i].logp : 0.0f;
     }
     int found = -1;
-    for (;;) {  // twice at most
+    while (!is_void(s.place[n])) {  // twice at most
         if (!refused) row.q = nullptr, row.hot = -1;
         const double all = refused ? x[2] - off * x[3] : x[0];
-        if (!(all > kNothing && all < CUDART_INF)) break;
         found = find_place(row, ratio, refused ? fmax(0.0, part_r - off * part_d) : part_p, last_random * all, a.segment, s);
         if (found >= 0 || !refused) break;
         refused = false;

@@ -129,3 +129,104 @@ def test_masks_far_below(kind, mask, c, vocab):
         r = check(target, tok, u, q, c)
         drawn = r.tokens.gather(1, r.accepted.long()[:, None])
         assert bool((drawn % 7 == 3).all())
+
+
+# --------------------------------------------------------------------------- temperatures
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("vocab", [40, 700, 20000])
+@pytest.mark.parametrize("c", [1e-30, 1e-3, 30.0, 1e3, 1e6, 1e8, 1e9, 1e10, 1e12, 1e30])
+def test_temperatures(kind, vocab, c):
+    """From flat rows to rows that are nothing but their largest elements, the target's, the draft's or both; drafts are the most likely
+    tokens of either row, or any."""
+    target, tok, u, draft = drafted(24, 3, vocab, kind, 630 + vocab)
+    target[::5, :, ::3] = float("-inf")
+    top, near = target[:, :3].argmax(-1), draft.argmax(-1)
+    pick = torch.randint(0, 4, tok.shape, generator=gen(631), device=DEV)
+    tok = torch.where(pick == 0, tok, torch.where(pick == 1, top, near))
+    for q, e in ((draft, c), (draft, 1.0), (None, c)):
+        check(target, tok, u, q, c, e)
+    check(target, tok, u, draft, 1.0, c)
+    if c >= 1e6:  # one element is all of the row (or a few equal ones): whatever the random number
+        u = u.clone()
+        u[:12, 3], u[12:, 3] = 0.0, NEXT_TO_ONE
+        r = lm.verify_draft(target, tok, u, draft=draft, inv_temp=c)
+        t = r.tokens.gather(1, r.accepted.long()[:, None])
+        row = target.gather(1, r.accepted.long()[:, None, None].expand(-1, -1, vocab))[:, 0]
+        assert torch.equal(row.gather(1, t)[:, 0], row.amax(-1))
+        score = r.logp.gather(1, r.accepted.long()[:, None])[:, 0]
+        many = (row == row.amax(-1, keepdim=True)).sum(-1)
+        assert float((score + many.double().log()).abs().max()) <= 2.0 ** -23 * math.log(vocab) + 2.0 ** -30
+
+
+@pytest.mark.parametrize("offset,c", [(1e9, 1.0), (-1e9, 0.01), (1e9, 0.001), (1e12, 1e-5), (1e9, 1e9), (-3e38, 1e-30)])
+@pytest.mark.parametrize("vocab", [40, 700, 20000])
+def test_rows_far_from_zero(offset, c, vocab):
+    """32-bit logits whose size is far above their differences."""
+    step = float(torch.tensor(abs(offset)) - torch.nextafter(torch.tensor(abs(offset)), torch.tensor(0.0)))
+    whole = lambda *s, seed: (randn(*s, seed=seed, sigma=4.0).round().double() * step + offset).to(F32)  # noqa: E731
+    target, draft = whole(12, 3, vocab, seed=640), whole(12, 2, vocab, seed=641)
+    target[::3, :, ::4] = float("-inf")
+    tok = torch.randint(0, vocab, (12, 2), generator=gen(642), device=DEV)
+    tok[::2] = draft.argmax(-1)[::2]
+    u = torch.rand(12, 3, generator=gen(643), device=DEV)
+    for q in (draft, None):
+        check(target, tok, u, q, c)
+
+
+def test_the_lowest_value_beside_infinities():
+    """The type's lowest value is an element like others where it is the largest."""
+    for kind in (F32, BF16, F16):
+        for v in (40, 700, 20000):
+            z = torch.full((3, 1, v), float("-inf"), dtype=kind, device=DEV)
+            z[..., v // 2], z[..., v - 1] = torch.finfo(kind).min, torch.finfo(kind).min
+            u = torch.tensor([[0.0], [0.49], [0.51]], device=DEV)
+            r = lm.verify_draft(z, torch.zeros(3, 0, dtype=torch.int64, device=DEV), u)
+            assert r.tokens.tolist() == [[v // 2], [v // 2], [v - 1]]
+            assert float((r.logp + math.log(2.0)).abs().max()) <= 2.0 ** -24
+
+
+def test_what_is_left_leaves_the_refused_token_out():
+    """As test_gpu_block's masks at both ends, at a temperature where the draft's share is still well above rounding."""
+    for kind in (F32, BF16, F16):
+        for v in (40, 700, 20000):
+            z = torch.full((4, 2, v), float("-inf"), dtype=kind, device=DEV)
+            lo, hi = v // 3, 2 * v // 3
+            z[..., lo:hi] = randn(4, 2, hi - lo, seed=650, dtype=kind, sigma=0.01)
+            q = z[:, :1].clone()
+            q[..., lo] += 0.25  # e^7.5 times its share at 30
+            tok = torch.full((4, 1), lo, device=DEV)
+            u = torch.tensor([[NEXT_TO_ONE, 0.0], [NEXT_TO_ONE, NEXT_TO_ONE], [0.0, 0.0], [0.0, NEXT_TO_ONE]], device=DEV)
+            r = lm.verify_draft(z, tok, u, draft=q, inv_temp=30.0)
+            t = r.tokens.tolist()
+            assert r.accepted.tolist() == [0, 0, 1, 1] and lo < t[0][0] < hi and lo < t[1][0] < hi
+            assert t[2] == [lo, lo] and t[3][0] == lo and lo <= t[3][1] < hi
+
+
+@pytest.mark.parametrize("kind", [F32, BF16, F16])
+@pytest.mark.parametrize("vocab", [40, 700, 20000])
+def test_void_rows(kind, vocab):
+    """NaN of either sign, +inf and rows of nothing but -inf, in the target's or the draft's row of a place that counts: nothing is drawn
+    there.  In rows that do not count they change nothing."""
+    target, tok, u, draft = drafted(6, 2, vocab, kind, 660)
+    u[:, :2] = 0.999
+    target.scatter_(2, tok[:, :1, None].expand(-1, 1, 1), -4.0)  # the first draft is refused
+    draft.scatter_(2, tok[:, :1, None], draft.amax(-1)[:, :1, None])
+    want = check(target, tok, u, draft)
+    assert not bool(want.accepted.any())
+    negative = torch.full((1,), float("nan"), dtype=kind, device=DEV)
+    negative = torch.copysign(negative, torch.tensor([-1.0], dtype=kind, device=DEV))
+    for bad in (float("nan"), negative, float("inf"), None):
+        for rows, place in ((target, 0), (draft, 0), (target, 1), (draft, 1), (target, 2)):
+            t, q = target.clone(), draft.clone()
+            spoiled = t if rows is target else q
+            if bad is None:
+                spoiled[3, place] = float("-inf")
+            else:
+                spoiled[3, place, vocab // 2] = bad if isinstance(bad, float) else bad[0]
+            r = lm.verify_draft(t, tok, u, draft=q)
+            if place == 0:
+                assert r.accepted[3] == 0 and r.tokens[3].tolist() == [-1] * 3 and math.isnan(float(r.logp[3, 0])) and not bool(r.logp[3, 1:].any())
+            keep = [k for k in range(6) if k != 3 or place > 0]
+            for a, b in zip(r, want):
+                assert torch.equal(a[keep], b[keep])
