@@ -174,18 +174,24 @@ __host__ __device__ constexpr uint32_t instruction(bool is_bf16, bool a_lines, b
 struct Activated {
     float value, slope;
 };
-// The normal distribution function by Abramowitz and Stegun 7.1.26, 2^-23 off at most: for t < 0
-//     cdf(t) = exp(-t^2 / 2) (a1 k + ... + a5 k^5) / 2,  k = 1 / (1 + p |t| / sqrt 2)
-// and 1 - cdf(-t) above; `bell` is exp(-t^2 / 2), which the slope needs too.  (A third of the instructions of 1 + erf, and
-// nothing cancels below 0.)
+// The normal distribution function: for t < 0
+//     cdf(t) = exp(-t^2 / 2) k r(k),  k = 1 / (1 + 0.37 |t|)
+// and 1 - cdf(-t) above; `bell` is exp(-t^2 / 2), which the slope needs too.  r, of degree 8, is the polynomial whose largest relative
+// error over all t <= 0 is least (a linear program on 1500 Chebyshev points of k): 1.8e-7.  In 32 bits the whole is off by 6e-7
+// relative at -1, 1e-6 at -4 and 8e-6 at -13, where exp(-t^2 / 2) carries the rounding of its argument; h is rounded to 2^-12 at
+// best.  (Half the instructions of 1 + erf, and nothing cancels below 0.)
 __device__ __forceinline__ float normal_cdf(float t, float& bell) {
     bell = __expf(-0.5f * t * t);
-    const float k = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(t), 1.0f));
-    float r = fmaf(k, 1.061405429f, -1.453152027f);
-    r = fmaf(k, r, 1.421413741f);
-    r = fmaf(k, r, -0.284496736f);
-    r = fmaf(k, r, 0.254829592f);
-    const float tail = 0.5f * k * r * bell;
+    const float k = __fdividef(1.0f, fmaf(0.37f, fabsf(t), 1.0f));
+    float r = fmaf(k, -0.0313809665f, 0.135318485f);
+    r = fmaf(k, r, -0.194549723f);
+    r = fmaf(k, r, 0.0646818255f);
+    r = fmaf(k, r, 0.0133536168f);
+    r = fmaf(k, r, 0.0901881908f);
+    r = fmaf(k, r, 0.127164879f);
+    r = fmaf(k, r, 0.147615132f);
+    r = fmaf(k, r, 0.147608617f);
+    const float tail = k * r * bell;
     return t < 0.0f ? tail : 1.0f - tail;
 }
 template <bool GELU>
