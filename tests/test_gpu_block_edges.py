@@ -1,0 +1,44 @@
+"""Calls of the operators inside a worker's step that their documentation allows and test_gpu_block does not make."""
+import pytest
+import torch
+from torch.utils._python_dispatch import TorchDispatchMode
+
+from paper_2005_06728_b200 import lm
+from test_gpu_block import block, drafted
+from test_gpu_lm import BF16, DEV, F32, randn
+
+pytestmark = pytest.mark.gpu
+
+
+def all_calls():
+    x, wg, wu = block((2, 20), 72, 130, BF16, F32, seed=700)
+    r = lm.gated_ffn(x, wg, wu, save=True)
+    g = lm.gated_ffn_grad(x, wg, wu, r.gate, r.up, randn(2, 20, 130, seed=703, dtype=BF16))
+    target, tok, u, draft = drafted(3, 2, 3000, BF16, 710)
+    return (*r, *g, lm.dropout(x, 0.3, 5, residual=x), *lm.verify_draft(target, tok, u, draft=draft), *lm.token_logprob(target, u.long()))
+
+
+class Dispatched(TorchDispatchMode):
+    def __init__(self):
+        super().__init__()
+        self.calls = []
+
+    def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+        self.calls.append(str(func))
+        return func(*args, **(kwargs or {}))
+
+
+def test_new_memory_under_modes():
+    want = all_calls()
+    with Dispatched() as m:
+        got = all_calls()
+    assert any("empty" in c for c in m.calls)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    try:
+        torch.use_deterministic_algorithms(True)
+        x = randn(4, 8)
+        got = lm.dropout(x, 0.3, 5), lm.dropout(x, 0.3, 5, out=torch.zeros_like(x))
+        assert torch.equal(*got) and bool(lm._new(x, (3, 5), F32, None).isnan().all())
+    finally:
+        torch.use_deterministic_algorithms(False)
