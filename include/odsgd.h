@@ -697,7 +697,9 @@ int odsgd_gated_backward(const odsgd_gated_desc* desc, void* workspace, size_t w
 
 /*
  * How many waits inside the kernels of the gated block have given up on the current device since the library was loaded.  They wait for
- * their own copies and products alone and give up after seconds: not 0 means that a result is void.  Waits for the GPU.
+ * their own copies and products alone and give up after seconds, with the call long returned: a count that has grown since means that
+ * a result is void.  Waits for all work of the device, on whatever stream; not while a stream is being captured (that would end the
+ * capture).  Errors: ERR_ARG, ERR_CUDA.
  */
 int odsgd_stalled_waits(unsigned int* count);
 

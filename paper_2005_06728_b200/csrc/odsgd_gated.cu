@@ -1,5 +1,5 @@
 // Host side of the gated feed-forward block: checks of arguments, operands that have to be laid out, tensor maps,
-// launches.  No allocation, no synchronisation, nothing thrown across the boundary.
+// launches.  No allocation, no synchronisation (but in odsgd_stalled_waits), nothing thrown across the boundary.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -461,7 +461,9 @@ int odsgd_gated_backward(const odsgd_gated_desc* desc, void* workspace, size_t w
 int odsgd_stalled_waits(unsigned int* count) {
     return guarded([&] {
         if (!count) return fail(ODSGD_ERR_ARG, "count is NULL");
-        const cudaError_t e = cudaMemcpyFromSymbol(count, stalled_waits, sizeof(*count));
+        cudaError_t e = cudaDeviceSynchronize();  // (the copy by itself waits for no stream that was made non-blocking)
+        if (e != cudaSuccess) return cuda_fail("cudaDeviceSynchronize", e);
+        e = cudaMemcpyFromSymbol(count, stalled_waits, sizeof(*count));
         return e == cudaSuccess ? (int)ODSGD_OK : cuda_fail("cudaMemcpyFromSymbol", e);
     });
 }

@@ -9,7 +9,8 @@ What a worker runs on either side of its model, and in it, when the parameter se
 * `policy_loss`: the clipped policy loss with a KL term, and its gradient, in one pass;
 * `GradSet`: norm and clipping of a list of gradient tensors, laid out into the arenas the server
   reads;
-* `gated_ffn` / `gated_ffn_grad`: the gated feed-forward block, on 16-bit activations, and its gradients;
+* `gated_ffn` / `gated_ffn_grad`: the gated feed-forward block up to its gated product h, on 16-bit activations, and its
+  gradients (the product that leads back to the model's width is the caller's); `stalled_waits`: whether any was cut short;
 * `dropout`: onto a residual, by a mask that is a function of a seed; its own gradient;
 * `verify_draft`: drafted tokens accepted under the current policy, one more drawn, and their scores.
 
@@ -465,6 +466,17 @@ def gated_ffn_grad(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, ga
     if written:
         increment_version(written)
     return GatedFfnGrad(dx, dw_gate, dw_up)
+
+
+def stalled_waits() -> int:
+    """How many waits inside the kernels of the gated block have given up on the current device since the library was loaded: what a
+    program looks at where it waits for the GPU anyway (a checkpoint, a report).  Always 0, unless the GPU was kept from running a
+    kernel for seconds: results since the last look are void then.  Waits for the device; not while a stream is being captured."""
+    if torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("stalled_waits: the current stream is being captured")
+    count = ctypes.c_uint()
+    _check(binding.load_library().odsgd_stalled_waits(ctypes.byref(count)))
+    return count.value
 
 
 # --------------------------------------------------------------------------- dropout

@@ -163,6 +163,7 @@ def train(steps: int = 60, workers: int = 3, vocab: int = 61, dim: int = 32, bat
     weights = counts.float() / counts.sum()
     batches = [None] * workers
     rewards, losses, norms = [], [], []
+    stalled = lm.stalled_waits()
     for step in range(steps):
         reward_sum, loss_sum = torch.zeros((), device=dev), torch.zeros((), device=dev)
         for m in range(workers):
@@ -204,6 +205,8 @@ def train(steps: int = 60, workers: int = 3, vocab: int = 61, dim: int = 32, bat
         rewards.append(float(reward_sum) / workers)
         losses.append(float(loss_sum) / workers)
         norms.append(norm.tolist())
+    if lm.stalled_waits() != stalled:
+        raise RuntimeError("a product of the gated block was cut short: the run is void")
     out = Report(rewards, losses, norms, ctx.weights().clone())
     clipper.close()
     bound.unbind()

@@ -42,3 +42,35 @@ def test_new_memory_under_modes():
         assert torch.equal(*got) and bool(lm._new(x, (3, 5), F32, None).isnan().all())
     finally:
         torch.use_deterministic_algorithms(False)
+
+
+def test_stalled_waits_waits_for_every_stream():
+    x, wg, wu = block((300,), 264, 400, BF16, F32, seed=720)
+    side, done = torch.cuda.Stream(), torch.cuda.Event()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)  # some tenth of a second
+        lm.gated_ffn(x, wg, wu)
+        done.record()
+    assert not done.query()
+    assert lm.stalled_waits() == 0
+    assert done.query()
+    y = torch.zeros(4, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(RuntimeError):
+            lm.stalled_waits()
+        y += 1
+    graph.replay()
+    torch.cuda.synchronize()
+    assert y.tolist() == [1.0] * 4, "the capture went on"
+
+
+def test_a_run_whose_products_were_cut_short_is_void(monkeypatch):
+    from paper_2005_06728_b200 import policy_example
+
+    counts = iter((0, 1))
+    monkeypatch.setattr(lm, "stalled_waits", lambda: next(counts))
+    with pytest.raises(RuntimeError, match="void"):
+        policy_example.train(steps=1, block=40)
