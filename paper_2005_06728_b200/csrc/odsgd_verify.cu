@@ -60,6 +60,9 @@ int check_verify(const odsgd_verify_desc* d, const void* ws, size_t have) {
 
 // Up to so many tokens a CTA does a sequence's whole work.
 constexpr int64_t kAloneVocab = 2048;
+// SMs that the shapes are made for: a B200's.  Not asked of the device, so that the workspace stays a function of sizes alone; on
+// another number the same results would come out in more or fewer waves.
+constexpr int64_t kVerifySms = 148;
 
 // Launch shapes and workspace: functions of sizes alone.
 struct VerifyShape {
@@ -70,15 +73,14 @@ struct VerifyShape {
 };
 VerifyShape verify_shape(const odsgd_verify_desc* d) {
     VerifyShape s;
-    const int64_t sms = 148;
     s.rows = d->batch * (2 * d->drafts + 1);
     // parts of at least 4096 elements, as many as fill every SM three times; each of whole steps of its CTA, so that none goes round
     // again for a few elements (16 x 11 rows of 50021 bf16: 7.3 us in 12 parts a row, 6.1 in 13)
     const int64_t step = (int64_t)kPartThreads * kRowVectors * 16 / size_of(d->type);
-    const int64_t wanted = std::max<int64_t>(1, std::min(ceil_div(sms * kPartCtas * 3, std::max<int64_t>(s.rows, 1)), d->vocab / 4096));
+    const int64_t wanted = std::max<int64_t>(1, std::min(ceil_div(kVerifySms * kPartCtas * 3, std::max<int64_t>(s.rows, 1)), d->vocab / 4096));
     s.chunks = ceil_div(d->vocab, step * std::max<int64_t>(1, d->vocab / (step * wanted)));
     // CTAs of 2048 elements and more, as many as run at once, two an SM
-    s.pass_ctas = std::max<int64_t>(1, std::min(2 * sms / std::max<int64_t>(d->batch, 1), ceil_div(d->vocab, 2048)));
+    s.pass_ctas = std::max<int64_t>(1, std::min(2 * kVerifySms / std::max<int64_t>(d->batch, 1), ceil_div(d->vocab, 2048)));
     // a warp's share, in pieces that draw_kernel goes over in one step, but no more of them than it has threads
     const int64_t share = ceil_div(d->vocab, s.pass_ctas * kPassWarps);
     const int64_t piece = std::max(ceil_div(share, ceil_div(share, 256 * kDrawWarps)), ceil_div(d->vocab, kSegments));
@@ -127,6 +129,7 @@ int verify(const odsgd_verify_desc* d, void* ws, size_t ws_bytes, void* stream) 
     a.vocab = (int)d->vocab;
     a.wide_tokens = d->token_type == ODSGD_I64;
     a.inv_temp = d->inv_temp, a.draft_temp = d->draft_inv_temp;
+    a.least = kLeast / (d->inv_temp * 1.4426950408889634), a.draft_least = kLeast / (d->draft_inv_temp * 1.4426950408889634);
     const bool alone = d->vocab <= kAloneVocab;
     switch (d->type) {
         case ODSGD_F32: return launch_verify<float>(a, alone, stream);

@@ -22,6 +22,8 @@ constexpr int kSegments = kDrawThreads;  // most parts of the vocabulary, each s
 constexpr int kDrawSums = 5;
 constexpr float kHeld = -600.0f;           // log-probabilities above this are no matter of the range of 64 bits
 
+constexpr double kLeast = -1020.0;         // the exponent below which an element is nothing
+
 enum Decision { kRefused, kAccepted, kNear, kEnds };
 
 // Place i of a sequence, by the rows' sums in 32 bits.
@@ -50,6 +52,7 @@ struct VerifyArgs {
     int pass_ctas;          // of a sequence
     float inv_temp, draft_temp;  // of target and draft
     float exp_temp, draft_exp;   // the same as RowExp takes them
+    double least, draft_least;   // kLeast in logits: kLeast / (temperature times log2 e)
 };
 
 // What THREADS threads, of which this is `tid`, find in part `chunk` of a row, each its own share.
@@ -104,7 +107,6 @@ __device__ __forceinline__ double warp_sum(double x) {
 // 2^(d c) in 64 bits, within 4e-14: the nearest whole number goes into the exponent, the rest f, at most a half, through 1 + f r(f),
 // r being the polynomial that meets (2^f - 1) / f at the nine Chebyshev points of [-1/2, 1/2].  1 at 0; for kLeast <= d c <= 0.
 // What is lower counts as nothing (is_nothing): a mask, or at that size no matter to any sum.
-constexpr double kLeast = -1020.0;
 __device__ __forceinline__ bool is_nothing(double d, double c) { return d * c < kLeast; }
 __device__ __forceinline__ double power_of_two(double d, double c) {
     const double w = fma(d, c, 6755399441055744.0);  // 1.5 * 2^52: the lower half is the whole number
@@ -259,11 +261,11 @@ struct Sequence {
         return p;
     }
     // (rounded up, so that all above is above kLeast, however large the logits and the temperature are)
-    __device__ __forceinline__ static float low(double m, double c) { return __double2float_ru(m + kLeast / c); }
+    __device__ __forceinline__ static float low(double m, double least) { return __double2float_ru(m + least); }
     __device__ __forceinline__ RowPair<T> row(unsigned n, const Position& p) const {
         const double cp = a.inv_temp * 1.4426950408889634, cq = a.draft_temp * 1.4426950408889634;
         return RowPair<T>{target + n * a.t_sr, draft && p.token >= 0 ? draft + n * a.d_sr : nullptr, p.token, p.max, p.draft_max, cp, cq, a.vocab,
-                          low(p.max, cp), low(p.draft_max, cq)};
+                          low(p.max, a.least), low(p.draft_max, a.draft_least)};
     }
 };
 // A row that holds NaN or +inf has a sum that is NaN, one of nothing but -inf a sum of 0.
