@@ -648,7 +648,8 @@ int odsgd_grad_set_clip(odsgd_grad_set* set, float max_norm, float* norms, void*
 int odsgd_grad_set_destroy(odsgd_grad_set* set);
 
 /*
- * Gated feed-forward block over rows of tokens x, with weights [width][dim]:
+ * Gated feed-forward block over rows of tokens x up to its gated product h (the product that leads back to dim is the
+ * caller's), with weights [width][dim]:
  *     gate = x Wg^T    up = x Wu^T    h = act(gate) * up
  *     act  = SILU: t / (1 + exp(-t))    GELU: t (1 + erf(t / sqrt 2)) / 2
  * and its gradient from dh and the kept gate and up:
@@ -656,7 +657,8 @@ int odsgd_grad_set_destroy(odsgd_grad_set* set);
  *     dx = dg Wg + du Wu    dWg (+)= dg^T x    dWu (+)= du^T x
  * x, h, gate, up, dh and dx are of `type`, 16 bits.  Weights are of `type`, or stand in an arena in 32 bits and are
  * rounded to `type` by the call (they are operands of products of that type, as are dg and du, which are rounded to it
- * too).  Sums and activation are held in 32 bits and rounded once.  Gradients of weights come in `type`, or in 32 bits
+ * too: in ODSGD_F16 what of them is below 6e-8 is lost, as in any backward pass of that type, and dh has to be scaled up with the
+ * loss).  Sums and activation are held in 32 bits and rounded once.  Gradients of weights come in `type`, or in 32 bits
  * where they go to a gradient arena, there added to what it holds if `accumulate` is set.  NaN and infinities
  * act as the formulas say, within their token (and, as in any such product, in all gradients of weights).
  * `workspace`: device memory of at least the size that odsgd_gated_workspace() reports for this descriptor (operands that
@@ -745,8 +747,10 @@ int odsgd_dropout(const odsgd_dropout_desc* desc, void* stream);
  * logp is what odsgd_policy_loss takes as old_logp.  A token outside [0, vocab) ends the sequence's drafts (shorter
  * drafts are padded with -1); `drafts` 0 draws a token alone.  -inf has probability 0.  Where a row that counts is
  * nothing but -inf, or holds NaN or +inf, nothing is drawn: the token is -1 and its logp NaN.
- * Rows are read once for their sums in 32 bits; the two rows of place n, and of any draft that comes within 1e-4 of the border,
- * again in 64 bits, in which all decisions stand.  `workspace` as for odsgd_embed_grad.
+ * Rows are read once for their sums in 32 bits.  These decide a draft where |log(u q / p)| is above 1e-4 + 4e-6 (|log p| + |log q|)
+ * (they are off by some 1e-6) and, to accept it, log p above -600.  Any other draft is decided, and the two rows of place n are
+ * drawn from, in 64 bits: an element below 2^-1020 of its row's largest has probability 0 there (a mask, whatever its value), and
+ * p_n - q_n is what differs by more than their rounding.  `workspace` as for odsgd_embed_grad.
  * Errors: ERR_ARG, ERR_ALIGN, ERR_OVERLAP, ERR_UNSUPPORTED, ERR_CUDA.
  */
 #define ODSGD_MAX_DRAFTS 255

@@ -55,7 +55,8 @@ GatedPlan gated_plan(const odsgd_gated_desc* d, bool backward) {
     };
     // A box of rows that start on 16 bytes but not on 64 crosses twice the lines: the forward pass then takes a quarter longer, which
     // pays for laying operands out where the product is large against them (8192 tokens of 4088 x 11008 1178 us as they are,
-    // of 4095 1031, laid out; 2044 of 2040 x 5440 75, of 2047 88).  The backward products lose less by it.
+    // of 4095 1031, laid out; 2044 of 2040 x 5440 75, of 2047 88).  The backward products lose less by it.  The rule: a quarter of the
+    // products' time at 1.6 PFLOP/s against the launch and the bytes of the layout at 5 TB/s.
     const double n = (double)p.tokens, dim = (double)d->dim, width = (double)d->width;
     const bool large = !backward && 0.25 * 4.0 * n * dim * width / 1.6e15 > 4e-6 + 4.0 * dim * (n + 2.0 * width) / 5e12;
     const int64_t line = large ? 64 : 16;

@@ -21,7 +21,9 @@ torch's.
 With --block the model is a gated feed-forward block of that width on a residual stream, in bfloat16 from the float32 arena
 (`gated_ffn`, `gated_ffn_grad`), what it adds dropped out with probability --drop (`dropout`, whose gradient is the
 same call).  With --drafts a worker's answers are drafted by the reference policy, so many at a time, and verified under the
-weights it acts with (`verify_draft`), which gives the scores that the loss takes as the acting policy's.
+weights it acts with (`verify_draft`), which gives the scores that the loss takes as the acting policy's.  Answers do not depend on one
+another here, so the acting policy's logits are known for all positions beforehand and no time is saved: the option shows the call in its
+place (rounds of drafts, ragged sequences, scores into the loss), not what drafting is for.
 """
 from __future__ import annotations
 

@@ -74,3 +74,25 @@ def test_a_run_whose_products_were_cut_short_is_void(monkeypatch):
     monkeypatch.setattr(lm, "stalled_waits", lambda: next(counts))
     with pytest.raises(RuntimeError, match="void"):
         policy_example.train(steps=1, block=40)
+
+
+@pytest.mark.parametrize("shape,dim,width", [((1,), 1, 1), ((2, 9), 33, 65), ((70,), 200, 129), ((300,), 1001, 257), ((9000,), 40, 24)])
+def test_what_a_workspace_held_before_has_no_effect(shape, dim, width):
+    """Workspaces of NaN (every byte 0xff), larger than needed, against those that a call makes."""
+    for weight_kind in (BF16, F32):
+        x, wg, wu = block(shape, dim, width, BF16, weight_kind, seed=730)
+        dh = randn(*shape, width, seed=733, dtype=BF16)
+        ws = torch.full((1 << 26,), 255, dtype=torch.uint8, device=DEV)
+        want = lm.gated_ffn(x, wg, wu, save=True)
+        grads = lm.gated_ffn_grad(x, wg, wu, want.gate, want.up, dh)
+        got = lm.gated_ffn(x, wg, wu, save=True, workspace=ws)
+        ws.fill_(255)
+        got_grads = lm.gated_ffn_grad(x, wg, wu, want.gate, want.up, dh, workspace=ws)
+        for a, b in zip((*want, *grads), (*got, *got_grads)):
+            assert torch.equal(a, b)
+    for vocab in (40, 5000):
+        target, tok, u, draft = drafted(3, 2, vocab, BF16, 740)
+        ws = torch.full((1 << 20,), 255, dtype=torch.uint8, device=DEV)
+        for q in (draft, None):
+            for a, b in zip(lm.verify_draft(target, tok, u, draft=q), lm.verify_draft(target, tok, u, draft=q, workspace=ws)):
+                assert torch.equal(a, b)
