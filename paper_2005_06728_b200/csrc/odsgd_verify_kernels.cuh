@@ -461,7 +461,7 @@ __device__ __forceinline__ int find_place(const RowPair<T>& row, double ratio, d
 }
 
 // A CTA a sequence, a thread a segment.  ALONE: the CTA also does what the other kernels do ahead of it, a warp a row and a
-// segment.  That pays up to some 2000 tokens: 8 x 3 drafts, bf16, of 200 / 2000 / 4000 take 11.1 / 12.6 / 15.9 us so, 13.0 / 13.7 / 13.6
+// segment.  That pays up to some 2000 tokens: 8 x 3 drafts, bf16, of 200 / 2000 / 4000 take 11.3 / 12.3 / 15.4 us so, 13.8 / 14.3 / 14.3
 // by three launches, which cost the host 5 us more.
 template <typename T, bool ALONE>
 __global__ void __launch_bounds__(kDrawThreads) draw_kernel(const __grid_constant__ VerifyArgs a) {
