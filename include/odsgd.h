@@ -750,7 +750,8 @@ int odsgd_dropout(const odsgd_dropout_desc* desc, void* stream);
  * Rows are read once for their sums in 32 bits.  These decide a draft where |log(u q / p)| is above 1e-4 + 4e-6 (|log p| + |log q|)
  * (they are off by some 1e-6) and, to accept it, log p above -600.  Any other draft is decided, and the two rows of place n are
  * drawn from, in 64 bits: an element below 2^-1020 of its row's largest has probability 0 there (a mask, whatever its value), and
- * p_n - q_n is what differs by more than their rounding.  `workspace` as for odsgd_embed_grad.
+ * p_n - q_n is what differs by more than their rounding.  Logits of a row are less than 3.4e38 apart (or -inf).  `workspace` as for
+ * odsgd_embed_grad.
  * Errors: ERR_ARG, ERR_ALIGN, ERR_OVERLAP, ERR_UNSUPPORTED, ERR_CUDA.
  */
 #define ODSGD_MAX_DRAFTS 255

@@ -23,9 +23,9 @@ def shifted(z):
 
 
 def check(target, tok, u, draft, c=1.0, e=None, exact=False):
-    """Equal decisions, draws and scores, where nothing is nearer to a border than 64-bit sums are off: 1e-11, some 2^53 / 90000, is more
-    than any sum of a row here added one by one, and far more than the tree sums of the kernel.  `exact`: some decisions are made on
-    zeros, which are borders by themselves, without any rounding."""
+    """Equal decisions, draws and scores, where nothing is nearer to a border than 64-bit sums are off: 70001 elements, the most here, added
+    one by one 7.8e-12 of the whole, the kernel's sums far less.  `exact`: some decisions are made on zeros, which are borders by
+    themselves, without any rounding."""
     e = c if e is None else e
     r = lm.verify_draft(target, tok, u, draft=draft, inv_temp=c, draft_inv_temp=e)
     accepted, tokens, logp, near = R.verify(shifted(target), tok, u, None if draft is None else shifted(draft), c, e)
